@@ -1,0 +1,433 @@
+"""What is measured of the operators of a recurrent language model's training and serving step.
+
+Three operators: the gated linear recurrence (forward, forward + backward, one token a sequence), the
+selection of a teacher's top logits, and the distillation loss over them with its gradient.  Each case
+runs in a plain form (elementary torch operations in 32 bits) or, where `own` is true, through the
+library's calls.
+"""
+from __future__ import annotations
+
+import math
+import random
+
+import torch
+
+own = False
+
+DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+SIZE = {"f32": 4, "bf16": 2, "f16": 2}
+
+
+# --------------------------------------------------------------------------- cases
+
+def listed():
+    return [
+        # serving: 64 sequences, one token each, the hidden size of the 2-layer LSTM language model;
+        # the states sit in a cache of 96 slots
+        dict(name="step_64x1500_bf16", op="scan_step", seqs=64, slots=96, channels=1500, dtype="bf16"),
+        # serving at a large batch, odd sizes, full precision
+        dict(name="step_1023x2048_f32", op="scan_step", seqs=1023, slots=2047, channels=2048, dtype="f32"),
+        # training, the LSTM language model's truncated batch: 20 sequences of 35 tokens, hidden 1500
+        dict(name="train_20x35x1500_f32", op="scan_train", tokens=700, seqs=20, channels=1500, dtype="f32",
+             ragged=False, reverse=False, joint=False),
+        # scoring of documents of all lengths packed back to back; gate and input are the two halves of one product
+        dict(name="forward_packed_40007x1024_bf16", op="scan_forward", tokens=40007, seqs=37, channels=1024,
+             dtype="bf16", ragged=True, reverse=False, joint=True),
+        # training of the backward direction of a bidirectional speech layer: utterances of uneven length
+        dict(name="train_reverse_25013x1024_f16", op="scan_train", tokens=25013, seqs=32, channels=1024,
+             dtype="f16", ragged=True, reverse=True, joint=True),
+        # training on one very long document
+        dict(name="train_long_65536x2048_bf16", op="scan_train", tokens=65536, seqs=1, channels=2048,
+             dtype="bf16", ragged=False, reverse=False, joint=False),
+        # a teacher's lists for one small batch over the LSTM language model's vocabulary
+        dict(name="top16_32x10000_f32", op="top", rows=32, vocab=10000, k=16, dtype="f32"),
+        # a teacher's lists for a training batch, vocabulary of odd size (rows start at any 2-byte address)
+        dict(name="top64_4096x50021_bf16", op="top", rows=4096, vocab=50021, k=64, dtype="bf16"),
+        # the last tokens of a few prompts over a very large vocabulary
+        dict(name="top128_3x250007_f32", op="top", rows=3, vocab=250007, k=128, dtype="f32"),
+        # evaluation: the loss of one truncated batch, with labels and a temperature
+        dict(name="loss_700x10000_f32", op="distill_loss", rows=700, vocab=10000, k=16, dtype="f32",
+             temperature=2.0, labels=True),
+        # training: loss and gradient in one call
+        dict(name="loss_grad_4096x50021_bf16", op="distill_loss_grad", rows=4096, vocab=50021, k=64, dtype="bf16",
+             temperature=1.0, labels=True),
+        # training under an autograd engine: the loss first, the gradient later
+        dict(name="loss_then_grad_1024x131072_f16", op="distill_two_calls", rows=1024, vocab=131072, k=32,
+             dtype="f16", temperature=2.0, labels=False),
+    ]
+
+
+def _log_int(rng, lo, hi):
+    return max(lo, min(hi, int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))))
+
+
+def draw(rng: random.Random):
+    op = rng.choice(["scan_step", "scan_forward", "scan_train", "scan_train", "top", "top", "distill_loss",
+                     "distill_loss_grad", "distill_loss_grad", "distill_two_calls"])
+    dtype = rng.choice(["f32", "bf16", "bf16", "f16"])
+    if op == "scan_step":
+        seqs = _log_int(rng, 1, 4000)
+        return dict(op=op, seqs=seqs, slots=seqs + rng.randrange(0, seqs + 3), channels=_log_int(rng, 64, 4096),
+                    dtype=dtype)
+    if op.startswith("scan"):
+        channels = _log_int(rng, 65, 4096)
+        tokens = _log_int(rng, 1, min(70000, 2 ** 26 // channels))
+        ragged = rng.random() < 0.5
+        seqs = _log_int(rng, 1, max(1, min(300, tokens)))
+        if not ragged:
+            tokens = seqs * max(1, tokens // seqs)
+        return dict(op=op, tokens=tokens, seqs=seqs, channels=channels, dtype=dtype, ragged=ragged,
+                    reverse=rng.random() < 0.4, joint=rng.random() < 0.5)
+    vocab = _log_int(rng, 1000, 260000)
+    rows = _log_int(rng, 1, min(8000, 2 ** 27 // vocab))
+    k = min(_log_int(rng, 1, 256), vocab)
+    if op == "top":
+        return dict(op=op, rows=rows, vocab=vocab, k=k, dtype=dtype)
+    return dict(op=op, rows=rows, vocab=vocab, k=k, dtype=dtype, temperature=rng.choice([1.0, 1.0, 2.0, 3.5]),
+                labels=rng.random() < 0.5)
+
+
+def work(case):
+    op, sz = case["op"], SIZE[case["dtype"]]
+    if op == "scan_step":
+        n = case["seqs"] * case["channels"]
+        return {"bytes": n * (3 * sz + 8) + 4 * case["seqs"], "flops": 8 * n}
+    if op.startswith("scan"):
+        n, states = case["tokens"] * case["channels"], case["seqs"] * case["channels"] * 4
+        if op == "scan_forward":
+            return {"bytes": 3 * n * sz + 2 * states, "flops": 8 * n}
+        return {"bytes": 6 * n * sz + 4 * states, "flops": 24 * n}   # z, x, dh in; h, dz, dx out
+    n, pairs = case["rows"] * case["vocab"], case["rows"] * case["k"] * 8
+    if op == "top":
+        return {"bytes": n * sz + pairs, "flops": n}
+    per_row = case["rows"] * (16 if case["labels"] else 8)
+    exps = 2 if case["labels"] and case["temperature"] != 1.0 else 1
+    if op == "distill_loss":
+        return {"bytes": n * sz + pairs + per_row, "flops": 3 * exps * n}
+    return {"bytes": 2 * n * sz + pairs + per_row, "flops": 6 * exps * n}
+
+
+# --------------------------------------------------------------------------- inputs
+
+def _lengths(case, seed):
+    """Lengths of a pack: most of them uneven, one of one token and one of none where there is room."""
+    seqs, tokens = case["seqs"], case["tokens"]
+    if not case["ragged"]:
+        return [tokens // seqs] * seqs
+    rng = random.Random(seed * 7919 + tokens)
+    weight = [rng.expovariate(1.0) + 0.05 for _ in range(seqs)]
+    if seqs >= 4:
+        weight[rng.randrange(seqs)] = 0.0
+    total = sum(weight)
+    cuts, acc = [0], 0.0
+    for w in weight[:-1]:
+        acc += w
+        cuts.append(min(tokens, int(round(tokens * acc / total))))
+    cuts.append(tokens)
+    return [b - a for a, b in zip(cuts, cuts[1:])]
+
+
+def prepare(case, seed):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    dt, op = DTYPES[case["dtype"]], case["op"]
+
+    def normal(*shape, mean=0.0, std=1.0):
+        return torch.randn(*shape, generator=gen, device="cuda", dtype=torch.float32).mul_(std).add_(mean)
+
+    st = {"case": case}
+    if op.startswith("scan"):
+        C = case["channels"]
+        if op == "scan_step":
+            S = case["seqs"]
+            st["gate"], st["x"] = normal(S, C, mean=1.5, std=2.0).to(dt), normal(S, C).to(dt)
+            st["state"] = normal(case["slots"], C, std=0.5)
+            st["slots"] = torch.randperm(case["slots"], generator=gen, device="cuda")[:S].to(torch.int32)
+            st["out"] = torch.empty(S, C, dtype=dt, device="cuda")
+            return st
+        N, S = case["tokens"], case["seqs"]
+        if case["joint"]:        # one product's output, the gate's half first
+            both = torch.empty(N, 2 * C, dtype=dt, device="cuda")
+            both[:, :C] = normal(N, C, mean=1.5, std=2.0)
+            both[:, C:] = normal(N, C)
+            st["gate"], st["x"] = both[:, :C], both[:, C:]
+        else:
+            st["gate"], st["x"] = normal(N, C, mean=1.5, std=2.0).to(dt), normal(N, C).to(dt)
+        lens = _lengths(case, seed)
+        starts = [0]
+        for n in lens:
+            starts.append(starts[-1] + n)
+        st["seqs"], st["longest"] = S, max(lens)
+        st["seq_start"] = torch.tensor(starts, dtype=torch.int32, device="cuda")
+        st["packed"] = st["seq_start"] if case["ragged"] else None
+        st["h0"] = normal(S, C, std=0.5)
+        st["h"] = torch.empty(N, C, dtype=dt, device="cuda")
+        st["h_last"] = torch.empty(S, C, dtype=torch.float32, device="cuda")
+        if op == "scan_train":
+            st["dh"], st["dh_last"] = normal(N, C, std=1e-2).to(dt), normal(S, C, std=1e-2)
+            if case["joint"]:
+                grads = torch.empty(N, 2 * C, dtype=dt, device="cuda")
+                st["dgate"], st["dx"] = grads[:, :C], grads[:, C:]
+            else:
+                st["dgate"], st["dx"] = (torch.empty(N, C, dtype=dt, device="cuda") for _ in range(2))
+            st["dh0"] = torch.empty(S, C, dtype=torch.float32, device="cuda")
+        return st
+
+    R, V, K = case["rows"], case["vocab"], case["k"]
+    logits = normal(R, V, std=2.5)
+    logits += normal(1, V, std=1.5)                    # some words are likelier everywhere
+    pad = V - max(1, V // 200)
+    logits[:, pad:] = -math.inf                        # the vocabulary is padded: never chosen
+    if op == "top":
+        if R >= 8:                                     # a constrained row: only a few words allowed
+            logits[R // 3, max(1, K // 2):] = -math.inf
+        st["logits"] = logits.to(dt)
+        st["idx"] = torch.empty(R, K, dtype=torch.int32, device="cuda")
+        st["val"] = torch.empty(R, K, dtype=torch.float32, device="cuda")
+        return st
+    st["logits"] = logits.to(dt)
+    teacher = logits.add_(normal(R, V))                # a teacher that half agrees
+    val, idx = torch.topk(teacher, K, dim=1)
+    del teacher, logits
+    idx = torch.where(val > -math.inf, idx, -torch.ones_like(idx))
+    if R >= 4:                                         # padding tokens: nothing to learn from
+        idx[R // 2] = -1
+    if K >= 4 and R >= 2:
+        idx[1, K // 2:] = -1                           # a shorter list
+    st["idx"], st["val"] = idx.to(torch.int32), val.contiguous()
+    st["temperature"] = case["temperature"]
+    st["labels"], st["hard"] = None, 0.0
+    if case["labels"]:
+        lab = torch.randint(0, pad, (R,), generator=gen, device="cuda", dtype=torch.int32)
+        if R >= 4:
+            lab[R // 2] = -1
+        st["labels"], st["hard"] = lab, 0.25
+    st["soft"] = 1.0 - st["hard"]
+    st["loss"] = torch.empty(R, dtype=torch.float32, device="cuda")
+    st["lse"] = torch.empty(R, 2, dtype=torch.float32, device="cuda")
+    if op != "distill_loss":
+        # token weights over the count; 16-bit floats of a narrow range come with a loss scale, as such training does
+        scale = 4096.0 if case["dtype"] == "f16" else 1.0
+        st["dloss"] = torch.rand(R, generator=gen, device="cuda").add_(0.5).mul_(scale / R)
+        st["dlogits"] = torch.empty_like(st["logits"])
+    return st
+
+
+# --------------------------------------------------------------------------- plain forms
+
+def _ends(starts, n, reverse):
+    """Per non-empty sequence: its number, and its first and last token in the scan's order."""
+    a, b = starts[:-1].long(), starts[1:].long()
+    live = torch.nonzero(b > a).flatten()
+    first, last = a[live], b[live] - 1
+    return (live, last, first) if reverse else (live, first, last)
+
+
+def _doubling(a, b, longest, down):
+    """y_t = a_t y_{t-1} + b_t over the token axis (y_{t+1} for `down`), by doubling: log2 of the longest sequence."""
+    d = 1
+    while d < longest:
+        if down:
+            lo, hi = slice(0, a.shape[0] - d), slice(d, None)
+        else:
+            lo, hi = slice(d, None), slice(0, a.shape[0] - d)
+        b2, a2 = b.clone(), a.clone()
+        b2[lo] += a[lo] * b[hi]
+        a2[lo] *= a[hi]
+        a, b, d = a2, b2, 2 * d
+    return b
+
+
+def _scan_plain(st):
+    rev, dt = st["case"]["reverse"], st["gate"].dtype
+    z, x = st["gate"].float(), st["x"].float()
+    f, omf = 1 / (1 + torch.exp(-z)), 1 / (1 + torch.exp(z))
+    live, first, last = _ends(st["seq_start"], z.shape[0], rev)
+    a, b = f.clone(), omf * x
+    b[first] += a[first] * st["h0"][live]
+    a[first] = 0
+    h = _doubling(a, b, st["longest"], rev)
+    h_last = st["h0"].clone()
+    h_last[live] = h[last]
+    if st["case"]["op"] == "scan_forward":
+        return h.to(dt), h_last
+    before = torch.roll(h, -1 if rev else 1, 0)
+    before[first] = st["h0"][live]
+    c, g = torch.roll(f, 1 if rev else -1, 0), st["dh"].float()
+    c[last] = 0
+    g[last] += st["dh_last"][live]
+    g = _doubling(c, g, st["longest"], not rev)
+    dh0 = st["dh_last"].clone()
+    dh0[live] = f[first] * g[first]
+    return h.to(dt), h_last, (f * omf * g * (before - x)).to(dt), (omf * g).to(dt), dh0
+
+
+def _step_plain(st):
+    z, x, at = st["gate"].float(), st["x"].float(), st["slots"].long()
+    h = st["state"][at] / (1 + torch.exp(-z)) + x / (1 + torch.exp(z))
+    st["state"][at] = h
+    return h.to(st["gate"].dtype), st["state"]
+
+
+def _top_plain(st):
+    v = st["logits"].float() + 0.0
+    bits = v.view(torch.int32)
+    order = torch.where(bits < 0, bits ^ 0x7FFFFFFF, bits).long() << 32
+    order |= 0xFFFFFFFF - torch.arange(v.shape[1], device=v.device)
+    best = torch.topk(order, st["case"]["k"], dim=1).values
+    idx = 0xFFFFFFFF - (best & 0xFFFFFFFF)
+    val = torch.gather(v, 1, idx)
+    return torch.where(val > -math.inf, idx, -1).to(torch.int32), val
+
+
+def _distill_plain(st):
+    op, T, dt = st["case"]["op"], st["temperature"], st["logits"].dtype
+    s = st["logits"].float()
+    V = s.shape[1]
+    there = (st["idx"] >= 0) & (st["idx"] < V) & (st["val"] > -math.inf)
+    at = torch.where(there, st["idx"], 0).long()
+    t = torch.where(there, st["val"] / T, -math.inf)
+    taught = there.any(1)
+    t = t - torch.where(taught, t.amax(1), 0.0)[:, None]
+    q = torch.exp(t)
+    z = torch.where(taught, q.sum(1), 1.0)[:, None]
+    q = q / z
+    logq = t - torch.log(z)
+    m = s.amax(1, keepdim=True)
+    p = torch.exp((s - m) / T)
+    sum_t = p.sum(1, keepdim=True)
+    lse_t = m / T + torch.log(sum_t)
+    picked = torch.gather(s, 1, at) / T - lse_t
+    loss = st["soft"] * T * T * torch.where(there & (q > 0), q * (logq - picked), 0.0).sum(1)
+    labelled = None
+    if st["labels"] is not None:
+        labelled = (st["labels"] >= 0) & (st["labels"] < V)
+        y = torch.where(labelled, st["labels"], 0).long()[:, None]
+        p1 = p if T == 1.0 else torch.exp(s - m)
+        sum_1 = p1.sum(1, keepdim=True)
+        ce = (m + torch.log(sum_1) - torch.gather(s, 1, y))[:, 0]
+        loss = loss + st["hard"] * torch.where(labelled, ce, 0.0)
+    if op == "distill_loss":
+        return loss
+    w = st["dloss"][:, None]
+    soft = st["soft"] * T * w * taught[:, None]
+    grad = p * (soft / sum_t)
+    grad.scatter_add_(1, at, -soft * torch.where(there, q, 0.0))
+    if labelled is not None:
+        hard = st["hard"] * w * labelled[:, None]
+        grad += p1 * (hard / sum_1)
+        grad.scatter_add_(1, y, -hard)
+    return loss, grad.to(dt)
+
+
+# --------------------------------------------------------------------------- one pass
+
+def run(st):
+    case = st["case"]
+    op = case["op"]
+    if not own:
+        if op == "scan_step":
+            return _step_plain(st)
+        if op.startswith("scan"):
+            return _scan_plain(st)
+        return _top_plain(st) if op == "top" else _distill_plain(st)
+    from paper_1712_01887_b200 import binding as B
+    if op == "scan_step":
+        B.gated_scan_step(st["gate"], st["x"], st["state"], st["out"], slots=st["slots"])
+        return st["out"], st["state"]
+    if op.startswith("scan"):
+        how = dict(seq_start=st["packed"], num_seqs=st["seqs"], h0=st["h0"], reverse=case["reverse"])
+        B.gated_scan_forward(st["gate"], st["x"], st["h"], h_last=st["h_last"], **how)
+        if op == "scan_forward":
+            return st["h"], st["h_last"]
+        B.gated_scan_backward(st["gate"], st["x"], st["h"], st["dh"], st["dgate"], st["dx"], dh_last=st["dh_last"],
+                              dh0=st["dh0"], **how)
+        return st["h"], st["h_last"], st["dgate"], st["dx"], st["dh0"]
+    if op == "top":
+        B.top_logits(st["logits"], st["idx"], st["val"])
+        return st["idx"], st["val"]
+    how = dict(temperature=st["temperature"], soft_weight=st["soft"], hard_weight=st["hard"], labels=st["labels"])
+    if op == "distill_loss":
+        B.distill_forward(st["logits"], st["idx"], st["val"], st["loss"], st["lse"], **how)
+        return st["loss"]
+    if op == "distill_loss_grad":
+        B.distill_loss_grad(st["logits"], st["idx"], st["val"], st["dloss"], st["loss"], st["dlogits"], **how)
+    else:
+        B.distill_forward(st["logits"], st["idx"], st["val"], st["loss"], st["lse"], **how)
+        B.distill_backward(st["logits"], st["idx"], st["val"], st["lse"], st["dloss"], st["dlogits"], **how)
+    return st["loss"], st["dlogits"]
+
+
+# --------------------------------------------------------------------------- the definition in 64 bits
+
+def _exact_scan(st):
+    rev = st["case"]["reverse"]
+    starts = st["seq_start"].tolist()
+    f = torch.sigmoid(st["gate"].double())
+    x, h0 = st["x"].double(), st["h0"].double()
+    N = f.shape[0]
+    b = torch.sigmoid(-st["gate"].double()) * x
+    h, h_last, before = torch.empty_like(x), h0.clone(), torch.empty_like(x)
+    for s in range(st["seqs"]):
+        order = range(starts[s], starts[s + 1])
+        cur = h0[s]
+        for t in (reversed(order) if rev else order):
+            before[t] = cur
+            cur = torch.addcmul(b[t], f[t], cur, out=h[t])
+        h_last[s] = cur
+    if st["case"]["op"] == "scan_forward":
+        return h, h_last
+    dh, e0 = st["dh"].double(), st["dh_last"].double()
+    dh0, g = e0.clone(), dh
+    for s in range(st["seqs"]):
+        order = range(starts[s], starts[s + 1])
+        e = e0[s]
+        for t in (order if rev else reversed(order)):
+            e = (g[t].add_(e)) * f[t]
+        dh0[s] = e
+    return h, h_last, f * (1 - f) * g * (before - x), (1 - f) * g, dh0
+
+
+def _exact_distill(st):
+    T, op = st["temperature"], st["case"]["op"]
+    R, V = st["logits"].shape
+    loss = torch.zeros(R, dtype=torch.float64, device="cuda")
+    grad = torch.zeros(R, V, dtype=torch.float64, device="cuda") if op != "distill_loss" else None
+    idx, val = st["idx"].tolist(), st["val"].double().cpu()
+    for r in range(R):
+        s = st["logits"][r].double()
+        on = [j for j, i in enumerate(idx[r]) if 0 <= i < V and float(val[r, j]) > -math.inf]
+        w = float(st["dloss"][r]) if grad is not None else 0.0
+        if on:
+            at = torch.tensor([idx[r][j] for j in on], device="cuda")
+            logq = torch.log_softmax(val[r, on].cuda() / T, 0)
+            logp = torch.log_softmax(s / T, 0)
+            loss[r] += st["soft"] * T * T * (logq.exp() * (logq - logp[at])).sum()
+            if grad is not None:
+                grad[r] += w * st["soft"] * T * logp.exp()
+                grad[r].index_add_(0, at, -w * st["soft"] * T * logq.exp())
+        y = int(st["labels"][r]) if st["labels"] is not None else -1
+        if 0 <= y < V:
+            logp = torch.log_softmax(s, 0)
+            loss[r] -= st["hard"] * logp[y]
+            if grad is not None:
+                grad[r] += w * st["hard"] * logp.exp()
+                grad[r, y] -= w * st["hard"]
+    return loss if grad is None else (loss, grad)
+
+
+def exact(case, seed):
+    st = prepare(case, seed)
+    op = case["op"]
+    if op == "scan_step":
+        f, at = torch.sigmoid(st["gate"].double()), st["slots"].long()
+        state = st["state"].double()
+        state[at] = f * state[at] + (1 - f) * st["x"].double()
+        return state[at], state
+    if op.startswith("scan"):
+        return _exact_scan(st)
+    if op == "top":
+        K, vals = case["k"], []
+        for rows in torch.split(st["logits"], 256):
+            vals.append(torch.sort(rows.double(), dim=1, descending=True).values[:, :K].clone())
+        return None, torch.cat(vals)
+    return _exact_distill(st)
