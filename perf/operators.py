@@ -252,7 +252,7 @@ def _scan_plain(st):
         return h.to(dt), h_last
     before = torch.roll(h, -1 if rev else 1, 0)
     before[first] = st["h0"][live]
-    c, g = torch.roll(f, 1 if rev else -1, 0), st["dh"].float()
+    c, g = torch.roll(f, 1 if rev else -1, 0), st["dh"].float().clone()
     c[last] = 0
     g[last] += st["dh_last"][live]
     g = _doubling(c, g, st["longest"], not rev)
