@@ -54,6 +54,11 @@ extern "C" {
                                      /* zeros, few distinct magnitudes) complete    */
                                      /* the list, lowest indices first; not slow    */
 
+/* element types of the calls that take `dtype` */
+#define DGC_F32   0
+#define DGC_BF16  1
+#define DGC_F16   2
+
 typedef struct dgc_state dgc_state;   /* opaque */
 
 typedef struct dgc_config {
@@ -382,6 +387,60 @@ int32_t dgc_profile_read(dgc_state* st, float* ms_out, int32_t capacity, int32_t
  * DGC_EINVAL from dgc_timeline_read if not enabled. */
 int32_t dgc_timeline_enable(dgc_state* st, int32_t on);
 int32_t dgc_timeline_read(dgc_state* st, void* stream, uint64_t* ns_out);
+
+/* ---------------------------------------------------------------- a recurrent model's step
+ * The calls below are what a language model trained with this library computes beside its
+ * matrix products: a gated recurrent layer (whose gradients the arena takes) and the
+ * distillation loss that its gradients start from.  They are stateless, take matrices as a
+ * base pointer and a row stride `ld_*` in elements (>= the row's length; columns are
+ * adjacent), so that a slice of a wider product's output can be passed as it is, and accept
+ * DGC_F32, DGC_BF16 and DGC_F16.  All arithmetic is in 32 bits; results are rounded once.
+ * Outputs must not overlap inputs unless stated.  Base pointers are aligned to their element;
+ * 16-bit matrices whose bases are 4-byte aligned and whose strides and row lengths are even
+ * run about twice as fast as others. */
+
+/* Gated linear recurrence over packed sequences, per channel:
+ *   f_t = 1 / (1 + exp(-z_t)) ;  h_t = f_t h_{t-1} + (1 - f_t) x_t
+ * with z the gate's logits.  Sequence s is rows seq_start[s] .. seq_start[s+1] of the
+ * [tokens, channels] matrices; a sequence may be empty.
+ *   seq_start  device int32 [num_seqs + 1], ascending from 0 to tokens; offsets outside
+ *              [0, tokens] are clamped (nothing outside the matrices is touched whatever the
+ *              table holds).  NULL: num_seqs sequences of tokens / num_seqs rows each
+ *   reverse    non-zero: every sequence is walked from its last row to its first
+ *   h0         fp32 [num_seqs, channels], the states before the first step; NULL: 0
+ *   h_last     fp32 [num_seqs, channels], the states after the last step (those of empty
+ *              sequences are h0's); may be NULL
+ * Results do not vary from run to run, and no value of one sequence (an infinity, a NaN)
+ * reaches another.  Rows outside every sequence are not written.  tokens < 2^31.  No
+ * workspace.  Errors: DGC_EINVAL (sizes < 1, tokens no multiple of num_seqs where seq_start
+ * is NULL, a stride below channels, a NULL or misaligned matrix), DGC_ECUDA.  Asynchronous. */
+int32_t dgc_gated_scan_forward(int32_t dtype, int64_t tokens, int32_t num_seqs, int32_t channels,
+                               const int32_t* seq_start, int32_t reverse, const void* gate_logits,
+                               int64_t ld_gate, const void* x, int64_t ld_x, const float* h0, void* h,
+                               int64_t ld_h, float* h_last, void* stream);
+
+/* The gradients of dgc_gated_scan_forward, with g_t the gradient that reaches h_t in all:
+ *   g_t = dh_t + f_{t+1} g_{t+1}  (+ dh_last at the last step)
+ *   dx_t = (1 - f_t) g_t ;  dgate_t = f_t (1 - f_t) g_t (h_{t-1} - x_t) ;  dh0 = f_first g_first
+ * First arguments as in the forward call; h is its output.
+ *   dh         gradient of h;   dh_last  fp32 [num_seqs, channels], of h_last; NULL: 0
+ *   dh0        fp32 [num_seqs, channels] output (dh_last's row for an empty sequence); may be NULL */
+int32_t dgc_gated_scan_backward(int32_t dtype, int64_t tokens, int32_t num_seqs, int32_t channels,
+                                const int32_t* seq_start, int32_t reverse, const void* gate_logits,
+                                int64_t ld_gate, const void* x, int64_t ld_x, const float* h0,
+                                const void* h, int64_t ld_h, const void* dh, int64_t ld_dh,
+                                const float* dh_last, void* dgate, int64_t ld_dgate, void* dx,
+                                int64_t ld_dx, float* dh0, void* stream);
+
+/* One step of the recurrence for `rows` sequences at once (one token each), their states kept
+ * in a cache: row r's state is row slots[r] of `state` (fp32 [num_slots, channels]; slots
+ * NULL: row r), which is advanced in place; out's row r is the new state.  A slot outside
+ * [0, num_slots) marks an idle row: no state changes and out's row is 0.  Two rows must not
+ * name one slot. */
+int32_t dgc_gated_scan_step(int32_t dtype, int32_t rows, int32_t channels, const void* gate_logits,
+                            int64_t ld_gate, const void* x, int64_t ld_x, float* state,
+                            const int32_t* slots, int32_t num_slots, void* out, int64_t ld_out,
+                            void* stream);
 
 /* Number of kernels this library has launched in this process (all states). */
 uint64_t dgc_launch_count(void);

@@ -98,6 +98,18 @@ _sigs = {
     "dgc_profile_enable": (ctypes.c_int32, [_vp, ctypes.c_int32]),
     "dgc_profile_read": (ctypes.c_int32, [_vp, _vp, ctypes.c_int32,
                                           ctypes.POINTER(ctypes.c_int32)]),
+    "dgc_gated_scan_forward": (ctypes.c_int32, [ctypes.c_int32, ctypes.c_int64, ctypes.c_int32,
+                                                ctypes.c_int32, _vp, ctypes.c_int32, _vp,
+                                                ctypes.c_int64, _vp, ctypes.c_int64, _vp, _vp,
+                                                ctypes.c_int64, _vp, _vp]),
+    "dgc_gated_scan_backward": (ctypes.c_int32, [ctypes.c_int32, ctypes.c_int64, ctypes.c_int32,
+                                                 ctypes.c_int32, _vp, ctypes.c_int32, _vp,
+                                                 ctypes.c_int64, _vp, ctypes.c_int64, _vp, _vp,
+                                                 ctypes.c_int64, _vp, ctypes.c_int64, _vp, _vp,
+                                                 ctypes.c_int64, _vp, ctypes.c_int64, _vp, _vp]),
+    "dgc_gated_scan_step": (ctypes.c_int32, [ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, _vp,
+                                             ctypes.c_int64, _vp, ctypes.c_int64, _vp, _vp,
+                                             ctypes.c_int32, _vp, ctypes.c_int64, _vp]),
     "dgc_launch_count": (ctypes.c_uint64, []),
     "dgc_error_string": (ctypes.c_char_p, [ctypes.c_int32]),
 }
@@ -444,3 +456,93 @@ def apply_sgd(w: torch.Tensor, dense_grad: torch.Tensor, lr: float, stream=None)
         raise ValueError("length mismatch")
     _check(_lib.dgc_apply_sgd(_dev(w, torch.float32), _dev(dense_grad, torch.float32), w.numel(),
                               float(lr), _stream(stream)), "dgc_apply_sgd")
+
+
+# ----------------------------------------------------------------- a recurrent model's step
+
+DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}   # DGC_F32, DGC_BF16, DGC_F16
+
+
+def _rows(t: torch.Tensor, dtype, rows: int, cols: int, what: str):
+    """(pointer, row stride) of a CUDA matrix whose columns are adjacent."""
+    if t.dtype != dtype or not t.is_cuda or t.dim() != 2:
+        raise ValueError(f"{what}: expected a CUDA {dtype} matrix")
+    if t.shape[0] != rows or t.shape[1] != cols:
+        raise ValueError(f"{what}: expected shape ({rows}, {cols}), got {tuple(t.shape)}")
+    if t.stride(1) != 1 and cols > 1:
+        raise ValueError(f"{what}: columns must be adjacent in memory")
+    return t.data_ptr(), (t.stride(0) if rows > 1 else max(cols, t.stride(0)))
+
+
+def _vec(t: Optional[torch.Tensor], dtype, numel: int, what: str):
+    """Pointer of a contiguous CUDA tensor of `numel` elements, or None."""
+    if t is None:
+        return None
+    if t.dtype != dtype or not t.is_cuda or not t.is_contiguous() or t.numel() != numel:
+        raise ValueError(f"{what}: expected a contiguous CUDA {dtype} tensor of {numel} elements")
+    return t.data_ptr()
+
+
+def _dtype(t: torch.Tensor, what: str) -> int:
+    code = DTYPES.get(t.dtype)
+    if code is None or t.dim() != 2:
+        raise ValueError(f"{what}: expected a float32, bfloat16 or float16 matrix")
+    return code
+
+
+def gated_scan_forward(gate: torch.Tensor, x: torch.Tensor, h: torch.Tensor,
+                       seq_start: Optional[torch.Tensor] = None, num_seqs: int = 1,
+                       h0: Optional[torch.Tensor] = None, h_last: Optional[torch.Tensor] = None,
+                       reverse: bool = False, stream=None) -> None:
+    """h_t = f_t h_{t-1} + (1 - f_t) x_t, f = sigmoid(gate), over packed sequences: rows
+    seq_start[s] .. seq_start[s+1] of the [tokens, channels] matrices (seq_start None: num_seqs
+    sequences of equal length).  Writes h, and the last states to h_last."""
+    code = _dtype(gate, "gate")
+    n, c = gate.shape
+    zp, zl = _rows(gate, gate.dtype, n, c, "gate")
+    xp, xl = _rows(x, gate.dtype, n, c, "x")
+    hp, hl = _rows(h, gate.dtype, n, c, "h")
+    _check(_lib.dgc_gated_scan_forward(
+        code, n, num_seqs, c, _vec(seq_start, torch.int32, num_seqs + 1, "seq_start"), bool(reverse),
+        zp, zl, xp, xl, _vec(h0, torch.float32, num_seqs * c, "h0"), hp, hl,
+        _vec(h_last, torch.float32, num_seqs * c, "h_last"), _stream(stream)),
+        "dgc_gated_scan_forward")
+
+
+def gated_scan_backward(gate: torch.Tensor, x: torch.Tensor, h: torch.Tensor, dh: torch.Tensor,
+                        dgate: torch.Tensor, dx: torch.Tensor,
+                        seq_start: Optional[torch.Tensor] = None, num_seqs: int = 1,
+                        h0: Optional[torch.Tensor] = None, dh_last: Optional[torch.Tensor] = None,
+                        dh0: Optional[torch.Tensor] = None, reverse: bool = False,
+                        stream=None) -> None:
+    """Gradients of gated_scan_forward: writes dgate, dx and dh0 from dh (of h) and dh_last."""
+    code = _dtype(gate, "gate")
+    n, c = gate.shape
+    zp, zl = _rows(gate, gate.dtype, n, c, "gate")
+    xp, xl = _rows(x, gate.dtype, n, c, "x")
+    hp, hl = _rows(h, gate.dtype, n, c, "h")
+    dp, dl = _rows(dh, gate.dtype, n, c, "dh")
+    gp, gl = _rows(dgate, gate.dtype, n, c, "dgate")
+    yp, yl = _rows(dx, gate.dtype, n, c, "dx")
+    _check(_lib.dgc_gated_scan_backward(
+        code, n, num_seqs, c, _vec(seq_start, torch.int32, num_seqs + 1, "seq_start"), bool(reverse),
+        zp, zl, xp, xl, _vec(h0, torch.float32, num_seqs * c, "h0"), hp, hl, dp, dl,
+        _vec(dh_last, torch.float32, num_seqs * c, "dh_last"), gp, gl, yp, yl,
+        _vec(dh0, torch.float32, num_seqs * c, "dh0"), _stream(stream)), "dgc_gated_scan_backward")
+
+
+def gated_scan_step(gate: torch.Tensor, x: torch.Tensor, state: torch.Tensor, out: torch.Tensor,
+                    slots: Optional[torch.Tensor] = None, stream=None) -> None:
+    """One token for each row: row slots[r] of `state` (fp32 [slots, channels]) is advanced in
+    place and written to out[r]; a slot outside the cache marks an idle row."""
+    code = _dtype(gate, "gate")
+    n, c = gate.shape
+    zp, zl = _rows(gate, gate.dtype, n, c, "gate")
+    xp, xl = _rows(x, gate.dtype, n, c, "x")
+    op, ol = _rows(out, gate.dtype, n, c, "out")
+    if state.dim() != 2 or state.shape[1] != c:
+        raise ValueError("state: expected [slots, channels]")
+    _check(_lib.dgc_gated_scan_step(
+        code, n, c, zp, zl, xp, xl, _vec(state, torch.float32, state.numel(), "state"),
+        _vec(slots, torch.int32, n, "slots"), state.shape[0], op, ol, _stream(stream)),
+        "dgc_gated_scan_step")

@@ -7,12 +7,13 @@ import subprocess
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(_HERE)
-SRC = os.path.join(_HERE, "csrc", "dgc.cu")
+SRC = [os.path.join(_HERE, "csrc", f) for f in ("dgc.cu", "scan.cu")]
+HEADERS = [os.path.join(_HERE, "csrc", f) for f in ("common.cuh", "dgc_kernels.cuh")]
 LIB = os.path.join(_HERE, "libdgc.so")
 INCLUDE = os.path.join(ROOT, "include")
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-              "-Xcompiler", "-fPIC", "-shared"]
+              "-Xcompiler", "-fPIC", "-shared", "--threads", "0"]
 
 
 def _fresh(deps) -> bool:
@@ -20,7 +21,7 @@ def _fresh(deps) -> bool:
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
-    deps = [SRC, os.path.join(_HERE, "csrc", "dgc_kernels.cuh"), os.path.join(INCLUDE, "dgc.h")]
+    deps = SRC + HEADERS + [os.path.join(INCLUDE, "dgc.h")]
     if not force and _fresh(deps):
         return LIB
     # several ranks of one job may get here at once: one of them compiles (into a file of its
@@ -34,7 +35,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
             extra = os.environ.get("NVCC_EXTRA_FLAGS", "").split()   # e.g. -D switches of variants
             tmp = f"{LIB}.{os.getpid()}.tmp"
             cmd = [nvcc] + NVCC_FLAGS + extra + (["-Xptxas", "-v"] if verbose else []) + \
-                  ["-I", INCLUDE, "-o", tmp, SRC]
+                  ["-I", INCLUDE, "-o", tmp] + SRC
             try:
                 subprocess.run(cmd, check=True)
                 os.replace(tmp, LIB)

@@ -14,6 +14,7 @@
 #include <new>
 #include <vector>
 
+#include "common.cuh"
 #include "dgc.h"
 #include "dgc_kernels.cuh"
 
@@ -21,7 +22,6 @@ using namespace dgc;
 
 namespace {
 
-std::atomic<uint64_t> g_launches{0};
 constexpr int kClusterLaunchMinParts = 16;   // k_select_cluster when a tensor has this many parts
 
 // ------------------------------------------------------------------ host side
@@ -101,15 +101,6 @@ struct dgc_state {
 };
 
 namespace {
-
-#define DGC_CUDA(call)                         \
-  do {                                         \
-    cudaError_t e__ = (call);                  \
-    if (e__ != cudaSuccess) {                  \
-      (void)cudaGetLastError();                \
-      return e__ == cudaErrorMemoryAllocation ? DGC_ENOMEM : DGC_ECUDA; \
-    }                                          \
-  } while (0)
 
 // Makes `dev` the current device and puts the caller's device back on scope exit.
 struct DeviceGuard {
@@ -403,52 +394,6 @@ int32_t upload_plan(dgc_state* st, bool first) {
                                 cudaFuncAttributeMaxDynamicSharedMemorySize,
                                 (kSelectMaxSmemKeys + kHistWords(kClusterThreads)) * 4));
   return DGC_OK;
-}
-
-inline cudaStream_t as_stream(void* s) { return reinterpret_cast<cudaStream_t>(s); }
-
-// Launch with the programmatic-dependent-launch attribute (see pdl_enter in the kernels).
-template <class... KArgs, class... Args>
-inline void launch(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t s,
-                   Args... args) {
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = grid;
-  cfg.blockDim = block;
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = s;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  (void)cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);   // error: check_launch()
-}
-
-// The same with a thread-block cluster of `cluster` blocks along x.
-template <class... KArgs, class... Args>
-inline void launch_cluster(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem,
-                           cudaStream_t s, unsigned cluster, Args... args) {
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = grid;
-  cfg.blockDim = block;
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = s;
-  cudaLaunchAttribute attr[2];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = cluster;
-  attr[1].val.clusterDim.y = 1;
-  attr[1].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 2;
-  (void)cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);   // error: check_launch()
-}
-
-int32_t check_launch() {
-  g_launches.fetch_add(1, std::memory_order_relaxed);
-  cudaError_t e = cudaGetLastError();
-  return e == cudaSuccess ? DGC_OK : DGC_ECUDA;
 }
 
 int32_t flush_pending_mask(dgc_state* st, cudaStream_t s) {

@@ -36,6 +36,7 @@
 
 #include <cstdint>
 
+#include "common.cuh"
 #include "dgc.h"
 
 namespace dgc {
@@ -179,7 +180,7 @@ __device__ __forceinline__ T load_record(const T* ptr) {
 
 // ------------------------------------------------------------------ device helpers
 // Programmatic dependent launch: every kernel of the library is launched with the
-// programmatic-serialization attribute and starts with pdl_enter().  The wait returns once
+// programmatic-serialization attribute and starts with pdl_enter() (common.cuh).  It returns once
 // the preceding kernel in the stream has completed and its writes are visible, so the order
 // of the stream is kept; what is gained is that this kernel's launch was processed while the
 // predecessor still ran, which hides the launch latency between the short kernels.  No kernel
@@ -187,7 +188,6 @@ __device__ __forceinline__ T load_record(const T* ptr) {
 // long predecessor would take the slots that another stream's streaming kernel needs (measured:
 // 10 % slower steps with early signalling).  The wait is executed by every block, so that
 // "grid N has completed" still implies "grid N-1 has completed".
-__device__ __forceinline__ void pdl_enter() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
 // Timeline aid: every block of the four kernels of a compress call notes when it started.
 __device__ __forceinline__ void timeline_mark(unsigned long long* tl, int kernel) {

@@ -1,0 +1,317 @@
+"""The gated linear recurrence (dgc_gated_scan_*) against a plain recurrence in 64 bits.
+
+Tolerances.  f and 1 - f come from one exponential and one division in 32 bits: at most 4 ulp,
+2.4e-7.  A relative error d of every f moves a state by at most d / (1 - f_max); with the gates'
+logits inside [-6, 6] that is d * 404 < 1e-4 of the largest state, and the same holds for the
+gradients (their recurrence has the same coefficients).  Rounding to a 16-bit type adds half a
+unit in the last place: at most eps / 2 = 2^-8 (bf16) or 2^-11 (f16) of the value; where the backward pass starts a
+run from a stored state, that state's rounding enters dgate once more, times f (1 - f) |g|."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+UNIT = {torch.float32: 0.0, **{d: torch.finfo(d).eps / 2 for d in (torch.bfloat16, torch.float16)}}   # half an ulp
+TINY = {torch.float32: 0.0, torch.bfloat16: 0.0, torch.float16: 2.0 ** -25}   # f16 subnormals
+DT = [torch.float32, torch.bfloat16, torch.float16]
+F32_TOL = 1e-4
+
+
+def plain(z, x, h0, starts, reverse):
+    """float64, one step after the other."""
+    h, before = torch.zeros_like(x), torch.zeros_like(x)
+    last = h0.clone()
+    f = torch.sigmoid(z)
+    for s in range(len(starts) - 1):
+        order = list(range(starts[s], starts[s + 1]))
+        cur = h0[s]
+        for t in (order[::-1] if reverse else order):
+            before[t] = cur
+            cur = f[t] * cur + torch.sigmoid(-z[t]) * x[t]
+            h[t] = cur
+        last[s] = cur
+    return h, last, before
+
+
+def plain_backward(z, x, h0, starts, reverse, dh, dlast):
+    _, _, before = plain(z, x, h0, starts, reverse)
+    f, omf = torch.sigmoid(z), torch.sigmoid(-z)
+    g, dh0 = torch.zeros_like(x), dlast.clone()
+    for s in range(len(starts) - 1):
+        order = list(range(starts[s], starts[s + 1]))
+        e = dlast[s]
+        for t in (order if reverse else order[::-1]):
+            g[t] = dh[t] + e
+            e = f[t] * g[t]
+        dh0[s] = e
+    return f * omf * g * (before - x), omf * g, dh0, g
+
+
+def test_plain_backward_agrees_with_differences():
+    """The formulas the kernels are tested against, against the forward recurrence itself."""
+    gen = torch.Generator().manual_seed(5)
+    starts, C = [0, 7, 7, 8, 20], 3
+    z, x, dh = (torch.randn(20, C, generator=gen, dtype=torch.float64) for _ in range(3))
+    h0, dl = (torch.randn(4, C, generator=gen, dtype=torch.float64) for _ in range(2))
+    for reverse in (False, True):
+        gz, gx, g0, _ = plain_backward(z, x, h0, starts, reverse, dh, dl)
+        vz, vx = torch.randn(20, C, generator=gen, dtype=torch.float64), torch.randn(20, C, generator=gen, dtype=torch.float64)
+        v0 = torch.randn(4, C, generator=gen, dtype=torch.float64)
+
+        def value(e):
+            h, last, _ = plain(z + e * vz, x + e * vx, h0 + e * v0, starts, reverse)
+            return (h * dh).sum() + (last * dl).sum()
+        eps = 1e-5
+        num = (value(eps) - value(-eps)) / (2 * eps)
+        ana = (gz * vz).sum() + (gx * vx).sum() + (g0 * v0).sum()
+        assert abs(num - ana) <= 1e-8 * (1 + abs(ana))
+
+
+def _bind():
+    if not torch.cuda.is_available():
+        pytest.fail("no CUDA device: the gpu tests need a B200")
+    from paper_1712_01887_b200 import binding as B
+    return B
+
+
+def _near(got, want, dt, what, extra=0.0):
+    got = got.double().cpu()
+    tol = UNIT[dt] * want.abs() + TINY[dt] + F32_TOL * max(1e-30, float(want.abs().max()) if want.numel() else 0) + extra
+    bad = (got - want).abs() > tol
+    assert not bad.any(), (what, int(bad.sum()), float(((got - want).abs() / tol).max()))
+    assert torch.isfinite(got).all(), what
+
+
+def _case(lens, C, dt, joint, seed, gate_mean=1.5):
+    gen = torch.Generator().manual_seed(seed)
+    N, S = sum(lens), len(lens)
+    starts = np.concatenate([[0], np.cumsum(lens)]).astype(int).tolist()
+    z = (torch.randn(N, C, generator=gen) * 2 + gate_mean).clamp(-6, 6).to(dt)
+    x = torch.randn(N, C, generator=gen).to(dt)
+    dh = torch.randn(N, C, generator=gen).to(dt)
+    h0, dl = torch.randn(S, C, generator=gen), torch.randn(S, C, generator=gen)
+
+    def dev(t):
+        if not joint:
+            return t.cuda()
+        wide = torch.full((N, 2 * C + joint), 7.0, dtype=dt, device="cuda")   # joint: extra columns of the row
+        wide[:, joint:joint + C] = t.cuda()
+        return wide[:, joint:joint + C]
+    return starts, z, x, dh, h0, dl, dev
+
+
+def _check(B, lens, C, dt, joint=0, reverse=False, packed=True, seed=0, with_h0=True, gate_mean=1.5):
+    starts, z, x, dh, h0, dl, dev = _case(lens, C, dt, joint, seed, gate_mean)
+    N, S = sum(lens), len(lens)
+    how = dict(num_seqs=S, reverse=reverse, h0=h0.cuda() if with_h0 else None,
+               seq_start=torch.tensor(starts, dtype=torch.int32, device="cuda") if packed else None)
+    zd, xd, gd = dev(z), dev(x), dev(dh)
+    whole = torch.full((N + 2, C + 3), -5.0, dtype=dt, device="cuda")
+    h = whole[1:N + 1, 1:C + 1] if joint else torch.empty(N, C, dtype=dt, device="cuda")
+    last = torch.full((S, C), float("nan"), device="cuda")
+    B.gated_scan_forward(zd, xd, h, h_last=last, **how)
+    start = h0.double() if with_h0 else torch.zeros(S, C, dtype=torch.float64)
+    rh, rl, _ = plain(z.double(), x.double(), start, starts, reverse)
+    _near(h, rh, dt, "h")
+    _near(last, rl, torch.float32, "h_last")
+    if joint:   # nothing outside the matrix was written
+        assert (whole[0] == -5).all() and (whole[-1] == -5).all()
+        assert (whole[:, 0] == -5).all() and (whole[:, C + 1:] == -5).all()
+    pair = torch.full((N, 2 * C + 1), -5.0, dtype=dt, device="cuda")
+    dgate, dx = (pair[:, :C], pair[:, C + 1:]) if joint else (torch.empty(N, C, dtype=dt, device="cuda") for _ in range(2))
+    dh0 = torch.full((S, C), float("nan"), device="cuda")
+    B.gated_scan_backward(zd, xd, h, gd, dgate, dx, dh_last=dl.cuda(), dh0=dh0, **how)
+    rz, rx, r0, g = plain_backward(z.double(), x.double(), start, starts, reverse, dh.double(), dl.double())
+    f = torch.sigmoid(z.double())
+    hmax = float(rh.abs().max()) if N else 0.0
+    _near(dgate, rz, dt, "dgate", UNIT[dt] * hmax * (f * (1 - f) * g).abs())
+    _near(dx, rx, dt, "dx")
+    _near(dh0, r0, torch.float32, "dh0")
+    if joint:
+        assert (pair[:, C] == -5).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dt", DT, ids=str)
+@pytest.mark.parametrize("reverse", [False, True])
+@pytest.mark.parametrize("lens,C,joint", [
+    ([1], 1, 0), ([1], 64, 0), ([2, 0, 1], 65, 1), ([0, 0, 5, 0], 66, 2), ([15, 16, 17], 128, 0), ([127, 128, 129], 33, 0),
+    ([255, 1, 513], 70, 2), ([1025], 64, 0), ([3001], 10, 1), ([40, 0, 2500, 3], 96, 4), ([7] * 50, 130, 0)])
+def test_scan_and_gradients(lens, C, joint, reverse, dt):
+    _check(_bind(), lens, C, dt, joint, reverse, seed=len(lens) * 100 + C)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dt", DT, ids=str)
+def test_scan_of_equal_lengths_without_a_table(dt):
+    _check(_bind(), [35] * 20, 150, dt, packed=False)
+    _check(_bind(), [300] * 3, 1500, dt, packed=False, with_h0=False, reverse=True)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("mean", [-4.0, 5.0])
+def test_scan_with_gates_that_forget_or_keep(mean):
+    _check(_bind(), [2000, 90], 64, torch.float32, gate_mean=mean)
+    _check(_bind(), [2000, 90], 64, torch.bfloat16, gate_mean=mean)
+
+
+@pytest.mark.gpu
+def test_scan_of_many_sequences_and_long_ones():
+    _check(_bind(), [i % 5 for i in range(700)], 40, torch.bfloat16)
+    _check(_bind(), [9000], 32, torch.float32, reverse=True)
+
+
+@pytest.mark.gpu
+def test_extreme_gates_and_neighbours_that_are_not_finite():
+    """Gates of +-inf and of the type's lowest value are exactly 1 and 0; a sequence full of NaN
+    and infinities leaves its neighbours in the pack untouched, bit for bit."""
+    B = _bind()
+    for dt in DT:
+        lens, C = [70, 200, 33], 64
+        starts, z, x, dh, h0, dl, _ = _case(lens, C, dt, 0, 3)
+        z[5], z[6], z[7] = float("inf"), -float("inf"), torch.finfo(dt).min
+        clean = None
+        for poison in (False, True):
+            zz, xx, gg = z.clone(), x.clone(), dh.clone()
+            if poison:
+                zz[80:90], xx[100:150], gg[70:270] = float("nan"), float("inf"), float("nan")
+            tab = torch.tensor(starts, dtype=torch.int32, device="cuda")
+            zd, xd, gd = zz.cuda(), xx.cuda(), gg.cuda()
+            h, gz, gx = (torch.empty(303, C, dtype=dt, device="cuda") for _ in range(3))
+            last, d0 = (torch.empty(3, C, device="cuda") for _ in range(2))
+            how = dict(seq_start=tab, num_seqs=3, h0=h0.cuda())
+            B.gated_scan_forward(zd, xd, h, h_last=last, **how)
+            B.gated_scan_backward(zd, xd, h, gd, gz, gx, dh_last=dl.cuda(), dh0=d0, **how)
+            keep = [t[i].clone() for t in (h, gz, gx) for i in (slice(0, 70), slice(270, 303))] + [last[::2].clone(), d0[::2].clone()]
+            assert all(torch.isfinite(k).all() for k in keep)
+            if clean is None:
+                clean = keep
+            else:
+                assert all(torch.equal(a, b) for a, b in zip(clean, keep))
+        # gate = 1: the state passes unchanged; gate = 0: the state is the input
+        assert torch.equal(h[5], h[4]) and torch.equal(h[6], x[6].cuda()) and torch.equal(h[7], x[7].cuda())
+
+
+@pytest.mark.gpu
+def test_scan_is_the_same_from_run_to_run_and_on_another_stream():
+    B = _bind()
+    starts, z, x, *_ = _case([5000, 3], 64, torch.bfloat16, 0, 9)
+    zd, xd = z.cuda(), x.cuda()
+    tab = torch.tensor(starts, dtype=torch.int32, device="cuda")
+    a, b = torch.empty_like(xd), torch.empty_like(xd)
+    B.gated_scan_forward(zd, xd, a, seq_start=tab, num_seqs=2)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    B.gated_scan_forward(zd, xd, b, seq_start=tab, num_seqs=2, stream=side)
+    side.synchronize()
+    assert torch.equal(a, b)
+
+
+@pytest.mark.gpu
+def test_damaged_offsets_stay_inside():
+    """Offsets beyond the pack and descending ones are clamped; guard rows keep their bits."""
+    B = _bind()
+    N, C = 100, 32
+    z, x = torch.randn(N, C, device="cuda"), torch.randn(N, C, device="cuda")
+    whole = torch.full((N + 64, C), -5.0, device="cuda")
+    tab = torch.tensor([-30, 40, 20, 130], dtype=torch.int32, device="cuda")
+    B.gated_scan_forward(z, x, whole[32:32 + N], seq_start=tab, num_seqs=3)
+    torch.cuda.synchronize()
+    assert (whole[:32] == -5).all() and (whole[32 + N:] == -5).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dt", DT, ids=str)
+@pytest.mark.parametrize("S,C,slots", [(1, 1, 1), (3, 7, 5), (64, 1500, 96), (130, 66, 130)])
+def test_step(S, C, slots, dt):
+    B = _bind()
+    gen = torch.Generator().manual_seed(S)
+    z, x = (torch.randn(S, C, generator=gen) * 2).to(dt), torch.randn(S, C, generator=gen).to(dt)
+    state = torch.randn(slots, C, generator=gen)
+    at = torch.randperm(slots, generator=gen)[:S].to(torch.int32)
+    if S > 2:
+        at[1], at[2] = -1, slots          # idle rows
+    sd, out = state.cuda(), torch.full((S, C), -5.0, dtype=dt, device="cuda")
+    B.gated_scan_step(z.cuda(), x.cuda(), sd, out, slots=at.cuda())
+    want, ro = state.double(), torch.zeros(S, C, dtype=torch.float64)
+    for r in range(S):
+        i = int(at[r])
+        if 0 <= i < slots:
+            want[i] = torch.sigmoid(z[r].double()) * want[i] + torch.sigmoid(-z[r].double()) * x[r].double()
+            ro[r] = want[i]
+    _near(sd, want, torch.float32, "state")
+    _near(out, ro, dt, "out")
+
+
+@pytest.mark.gpu
+def test_steps_continue_a_scan():
+    """The prompt by the scan, the next tokens one by one: the same states as one scan of all."""
+    B = _bind()
+    S, L, C = 4, 50, 96
+    z, x = torch.randn(S, L, C, device="cuda"), torch.randn(S, L, C, device="cuda")
+    h, last = torch.empty(S * L, C, device="cuda"), torch.empty(S, C, device="cuda")
+    B.gated_scan_forward(z.view(-1, C), x.view(-1, C), h, num_seqs=S, h_last=last)
+    h1, st = torch.empty(S * 40, C, device="cuda"), torch.empty(S, C, device="cuda")
+    B.gated_scan_forward(z[:, :40].reshape(-1, C), x[:, :40].reshape(-1, C), h1, num_seqs=S, h_last=st)
+    out = torch.empty(S, C, device="cuda")
+    for t in range(40, L):
+        B.gated_scan_step(z[:, t], x[:, t], st, out)
+        assert float((out - h.view(S, L, C)[:, t]).abs().max()) <= F32_TOL * float(h.abs().max())
+    assert float((st - last).abs().max()) <= F32_TOL * float(last.abs().max())
+
+
+@pytest.mark.gpu
+def test_scan_in_a_graph():
+    B = _bind()
+    starts, z, x, *_ = _case([300, 20], 64, torch.float16, 0, 2)
+    zd, xd = z.cuda(), x.cuda()
+    tab = torch.tensor(starts, dtype=torch.int32, device="cuda")
+    a, b = torch.empty_like(xd), torch.empty_like(xd)
+    B.gated_scan_forward(zd, xd, a, seq_start=tab, num_seqs=2)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        B.gated_scan_forward(zd, xd, b, seq_start=tab, num_seqs=2)
+    b.zero_()
+    g.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(a, b)
+
+
+def test_refusals_of_the_c_calls():
+    """Bad arguments come back as DGC_EINVAL before anything is enqueued (no GPU needed)."""
+    from paper_1712_01887_b200 import binding as B
+    lib, p = B._lib, ctypes.c_void_p(4096)
+    null = ctypes.c_void_p(0)
+
+    def fwd(dtype=0, tokens=8, seqs=2, ch=4, ld=4, z=p, x=p, h=p):
+        return lib.dgc_gated_scan_forward(dtype, tokens, seqs, ch, null, 0, z, ld, x, ld, null, h, ld, null, null)
+    for bad in (dict(dtype=3), dict(dtype=-1), dict(tokens=-1), dict(tokens=7), dict(tokens=1 << 31), dict(seqs=0), dict(ch=0),
+                dict(ld=3), dict(z=null), dict(x=null), dict(h=null), dict(x=ctypes.c_void_p(4098)), dict(dtype=1, h=ctypes.c_void_p(4097))):
+        assert fwd(**bad) == B.EINVAL, bad
+
+    def bwd(dtype=0, tokens=8, seqs=2, ch=4, ld=4, dh=p, dx=p):
+        return lib.dgc_gated_scan_backward(dtype, tokens, seqs, ch, null, 0, p, 4, p, 4, null, p, 4, dh, ld, null, p, 4, dx, 4, null, null)
+    for bad in (dict(dtype=9), dict(tokens=9), dict(seqs=-1), dict(ch=-4), dict(ld=2), dict(dh=null), dict(dx=null), dict(dh=ctypes.c_void_p(4097))):
+        assert bwd(**bad) == B.EINVAL, bad
+
+    def step(dtype=0, rows=2, ch=4, ld=4, state=p, slots=null, n=2):
+        return lib.dgc_gated_scan_step(dtype, rows, ch, p, ld, p, 4, state, slots, n, p, 4, null)
+    for bad in (dict(dtype=5), dict(rows=-1), dict(ch=0), dict(ld=1), dict(state=null), dict(n=1), dict(n=-1), dict(slots=ctypes.c_void_p(4097))):
+        assert step(**bad) == B.EINVAL, bad
+    assert step(rows=0) == B.OK and fwd(tokens=0) == B.OK
+
+
+@pytest.mark.gpu
+def test_refusals_of_the_binding():
+    B = _bind()
+    z = torch.zeros(8, 4, device="cuda")
+    for gate, x, h in ((z.double(), z, z), (z, z[:, :3], z), (z, z.half(), z), (z, z, z.t().contiguous().t()), (z, z.cpu(), z), (z[0], z, z)):
+        with pytest.raises(ValueError):
+            B.gated_scan_forward(gate, x, h)
+    with pytest.raises(ValueError):
+        B.gated_scan_forward(z, z.clone(), z.clone(), seq_start=torch.zeros(3, dtype=torch.int64, device="cuda"), num_seqs=2)
+    with pytest.raises(ValueError):
+        B.gated_scan_forward(z, z.clone(), z.clone(), h0=torch.zeros(3, 4, device="cuda"))
+    with pytest.raises(B.DgcError):
+        B.gated_scan_forward(z, z.clone(), z.clone(), num_seqs=3)
