@@ -59,6 +59,8 @@ extern "C" {
 #define DGC_BF16  1
 #define DGC_F16   2
 
+#define DGC_MAX_TOP  256   /* longest list of dgc_top_logits and the dgc_distill_* calls */
+
 typedef struct dgc_state dgc_state;   /* opaque */
 
 typedef struct dgc_config {
@@ -441,6 +443,50 @@ int32_t dgc_gated_scan_step(int32_t dtype, int32_t rows, int32_t channels, const
                             int64_t ld_gate, const void* x, int64_t ld_x, float* state,
                             const int32_t* slots, int32_t num_slots, void* out, int64_t ld_out,
                             void* stream);
+
+/* The k largest entries of every row of `logits` [rows, vocab], the form in which a teacher's
+ * distribution is kept for dgc_distill_*: largest first, the lowest index first among equals
+ * (-0 equals +0, NaN counts as larger than every number).  Entries of -infinity (words masked
+ * out) are never listed; a row with fewer than k others is filled up with (-1, -infinity).
+ *   idx, val   int32 and fp32 [rows, k] outputs;   1 <= k <= DGC_MAX_TOP
+ * Errors: DGC_EINVAL, DGC_ECUDA.  Asynchronous. */
+int32_t dgc_top_logits(int32_t dtype, int64_t rows, int32_t vocab, int32_t k, const void* logits,
+                       int64_t ld_logits, int32_t* idx, float* val, void* stream);
+
+/* Distillation from a teacher's top logits, one loss a row.  With T the temperature,
+ *   q = softmax of the row's listed teacher logits / T ;  p = softmax(s / T) ;  p1 = softmax(s)
+ *   loss = soft_weight T^2 sum_k q_k (log q_k - log p[idx_k]) + hard_weight (-log p1[label])
+ *   logits     [rows, vocab], the student's;  words masked out are -infinity (their p is 0)
+ *   idx, val   int32 and fp32 [rows, k], the teacher's list (dgc_top_logits); an entry whose
+ *              index is outside [0, vocab) or whose value is -infinity or NaN is absent; an
+ *              index listed twice counts twice.  A row with no entry has no soft term
+ *   labels     int32 [rows] or NULL; a label outside [0, vocab) (a padding token) has no hard term
+ *   loss       fp32 [rows] output; +infinity where a listed entry or the label has p = 0
+ *   lse        fp32 [rows, 2] output for dgc_distill_backward: log sum exp of s / T, and of s
+ *              (only where labels and a non-zero hard_weight need it); may be NULL
+ * temperature > 0; weights finite.  Asynchronous. */
+int32_t dgc_distill_forward(int32_t dtype, int64_t rows, int32_t vocab, int32_t k, const void* logits,
+                            int64_t ld_logits, const int32_t* idx, const float* val, const int32_t* labels,
+                            float temperature, float soft_weight, float hard_weight, float* loss, float* lse,
+                            void* stream);
+
+/* Its gradient: dlogits[r][j] = dloss[r] (soft_weight T (p_j - sum of q listed at j)
+ * + hard_weight (p1_j - [j = label])), with lse the forward call's and dloss fp32 [rows] the
+ * gradient that reaches the row's loss.  Every element of dlogits [rows, vocab] is written; a row
+ * with neither term, or with dloss 0, gets zeros.  dlogits may be the logits themselves (same
+ * base and stride); rows at the same distance from a 16-byte boundary as the logits' are
+ * written in 16-byte words, others element by element.  Asynchronous. */
+int32_t dgc_distill_backward(int32_t dtype, int64_t rows, int32_t vocab, int32_t k, const void* logits,
+                             int64_t ld_logits, const int32_t* idx, const float* val, const int32_t* labels,
+                             float temperature, float soft_weight, float hard_weight, const float* lse,
+                             const float* dloss, void* dlogits, int64_t ld_dlogits, void* stream);
+
+/* Loss and gradient in one call (dloss known beforehand: a token's weight over the number of
+ * tokens): the same results, the logits read from memory once. */
+int32_t dgc_distill_loss_grad(int32_t dtype, int64_t rows, int32_t vocab, int32_t k, const void* logits,
+                              int64_t ld_logits, const int32_t* idx, const float* val, const int32_t* labels,
+                              float temperature, float soft_weight, float hard_weight, const float* dloss,
+                              float* loss, void* dlogits, int64_t ld_dlogits, void* stream);
 
 /* Number of kernels this library has launched in this process (all states). */
 uint64_t dgc_launch_count(void);

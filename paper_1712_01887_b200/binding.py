@@ -110,6 +110,20 @@ _sigs = {
     "dgc_gated_scan_step": (ctypes.c_int32, [ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, _vp,
                                              ctypes.c_int64, _vp, ctypes.c_int64, _vp, _vp,
                                              ctypes.c_int32, _vp, ctypes.c_int64, _vp]),
+    "dgc_top_logits": (ctypes.c_int32, [ctypes.c_int32, ctypes.c_int64, ctypes.c_int32,
+                                        ctypes.c_int32, _vp, ctypes.c_int64, _vp, _vp, _vp]),
+    "dgc_distill_forward": (ctypes.c_int32, [ctypes.c_int32, ctypes.c_int64, ctypes.c_int32,
+                                             ctypes.c_int32, _vp, ctypes.c_int64, _vp, _vp, _vp,
+                                             ctypes.c_float, ctypes.c_float, ctypes.c_float, _vp,
+                                             _vp, _vp]),
+    "dgc_distill_backward": (ctypes.c_int32, [ctypes.c_int32, ctypes.c_int64, ctypes.c_int32,
+                                              ctypes.c_int32, _vp, ctypes.c_int64, _vp, _vp, _vp,
+                                              ctypes.c_float, ctypes.c_float, ctypes.c_float, _vp,
+                                              _vp, _vp, ctypes.c_int64, _vp]),
+    "dgc_distill_loss_grad": (ctypes.c_int32, [ctypes.c_int32, ctypes.c_int64, ctypes.c_int32,
+                                               ctypes.c_int32, _vp, ctypes.c_int64, _vp, _vp, _vp,
+                                               ctypes.c_float, ctypes.c_float, ctypes.c_float, _vp,
+                                               _vp, _vp, ctypes.c_int64, _vp]),
     "dgc_launch_count": (ctypes.c_uint64, []),
     "dgc_error_string": (ctypes.c_char_p, [ctypes.c_int32]),
 }
@@ -460,6 +474,7 @@ def apply_sgd(w: torch.Tensor, dense_grad: torch.Tensor, lr: float, stream=None)
 
 # ----------------------------------------------------------------- a recurrent model's step
 
+MAX_TOP = 256
 DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}   # DGC_F32, DGC_BF16, DGC_F16
 
 
@@ -546,3 +561,62 @@ def gated_scan_step(gate: torch.Tensor, x: torch.Tensor, state: torch.Tensor, ou
         code, n, c, zp, zl, xp, xl, _vec(state, torch.float32, state.numel(), "state"),
         _vec(slots, torch.int32, n, "slots"), state.shape[0], op, ol, _stream(stream)),
         "dgc_gated_scan_step")
+
+
+def top_logits(logits: torch.Tensor, idx: torch.Tensor, val: torch.Tensor, stream=None) -> None:
+    """The k largest entries of every row, largest first (idx, val: [rows, k]; the lowest index
+    first among equals; -inf is never listed, missing entries are (-1, -inf))."""
+    code = _dtype(logits, "logits")
+    n, v = logits.shape
+    lp, ll = _rows(logits, logits.dtype, n, v, "logits")
+    k = idx.shape[-1]
+    _check(_lib.dgc_top_logits(code, n, v, k, lp, ll, _vec(idx, torch.int32, n * k, "idx"),
+                               _vec(val, torch.float32, n * k, "val"), _stream(stream)),
+           "dgc_top_logits")
+
+
+def _distill(logits, idx, val, labels, temperature, soft_weight, hard_weight):
+    code = _dtype(logits, "logits")
+    n, v = logits.shape
+    lp, ll = _rows(logits, logits.dtype, n, v, "logits")
+    k = idx.shape[-1]
+    return n, v, (code, n, v, k, lp, ll, _vec(idx, torch.int32, n * k, "idx"),
+                  _vec(val, torch.float32, n * k, "val"), _vec(labels, torch.int32, n, "labels"),
+                  temperature, soft_weight, hard_weight)
+
+
+def distill_forward(logits: torch.Tensor, idx: torch.Tensor, val: torch.Tensor, loss: torch.Tensor,
+                    lse: Optional[torch.Tensor] = None, temperature: float = 1.0,
+                    soft_weight: float = 1.0, hard_weight: float = 0.0,
+                    labels: Optional[torch.Tensor] = None, stream=None) -> None:
+    """loss[r] = soft_weight T^2 KL(teacher's listed distribution || student's) + hard_weight
+    cross entropy with labels[r]; lse [rows, 2] is kept for distill_backward."""
+    n, _, head = _distill(logits, idx, val, labels, temperature, soft_weight, hard_weight)
+    _check(_lib.dgc_distill_forward(*head, _vec(loss, torch.float32, n, "loss"),
+                                    _vec(lse, torch.float32, 2 * n, "lse"), _stream(stream)),
+           "dgc_distill_forward")
+
+
+def distill_backward(logits: torch.Tensor, idx: torch.Tensor, val: torch.Tensor, lse: torch.Tensor,
+                     dloss: torch.Tensor, dlogits: torch.Tensor, temperature: float = 1.0,
+                     soft_weight: float = 1.0, hard_weight: float = 0.0,
+                     labels: Optional[torch.Tensor] = None, stream=None) -> None:
+    """The gradient of distill_forward's losses, dloss[r] being that of row r's; dlogits may be
+    the logits themselves."""
+    n, v, head = _distill(logits, idx, val, labels, temperature, soft_weight, hard_weight)
+    dp, dl = _rows(dlogits, logits.dtype, n, v, "dlogits")
+    _check(_lib.dgc_distill_backward(*head, _vec(lse, torch.float32, 2 * n, "lse"),
+                                     _vec(dloss, torch.float32, n, "dloss"), dp, dl,
+                                     _stream(stream)), "dgc_distill_backward")
+
+
+def distill_loss_grad(logits: torch.Tensor, idx: torch.Tensor, val: torch.Tensor,
+                      dloss: torch.Tensor, loss: torch.Tensor, dlogits: torch.Tensor,
+                      temperature: float = 1.0, soft_weight: float = 1.0, hard_weight: float = 0.0,
+                      labels: Optional[torch.Tensor] = None, stream=None) -> None:
+    """distill_forward and distill_backward in one call, the logits read from memory once."""
+    n, v, head = _distill(logits, idx, val, labels, temperature, soft_weight, hard_weight)
+    dp, dl = _rows(dlogits, logits.dtype, n, v, "dlogits")
+    _check(_lib.dgc_distill_loss_grad(*head, _vec(dloss, torch.float32, n, "dloss"),
+                                      _vec(loss, torch.float32, n, "loss"), dp, dl,
+                                      _stream(stream)), "dgc_distill_loss_grad")

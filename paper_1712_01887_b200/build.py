@@ -7,8 +7,8 @@ import subprocess
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(_HERE)
-SRC = [os.path.join(_HERE, "csrc", f) for f in ("dgc.cu", "scan.cu")]
-HEADERS = [os.path.join(_HERE, "csrc", f) for f in ("common.cuh", "dgc_kernels.cuh")]
+SRC = [os.path.join(_HERE, "csrc", f) for f in ("dgc.cu", "scan.cu", "top_logits.cu", "distill.cu")]
+HEADERS = [os.path.join(_HERE, "csrc", f) for f in ("common.cuh", "dgc_kernels.cuh", "rows.cuh")]
 LIB = os.path.join(_HERE, "libdgc.so")
 INCLUDE = os.path.join(ROOT, "include")
 

@@ -1,0 +1,266 @@
+// The k largest entries of every row of a matrix (sm_100a): kernel and C ABI.
+//
+// The list is in the library's form, (int32 index, fp32 value), largest value first and the
+// lowest index first among equals.  A row is read once from memory:
+//
+//   1. every thread takes the maximum of the elements it is dealt;
+//   2. the k-th largest of these maxima is a bound that at least k elements reach, and that
+//      few others do (about k + k^2 / 2 threads of them when the row is in no special order);
+//   3. the threads whose maximum reaches it, and only those, look at their elements again
+//      (k of the block's threads, out of L2) and list the ones that reach it;
+//   4. a listed entry's place is the number of listed entries that come before it.
+//
+// Where more entries reach the bound than the list holds (a row of equal values, an order that
+// deals all large values to a few threads), the k-th value is found by bisection over the row,
+// then its equals are taken in index order: slow, and always right.
+
+#include <cooperative_groups.h>
+
+#include <algorithm>
+
+#include "rows.cuh"
+
+namespace cg = cooperative_groups;
+using namespace dgc;
+
+namespace {
+
+constexpr int kTopThreads = 512;
+constexpr int kTopList = 4096;            // candidates a block can hold
+constexpr int kTopRank = 512;             // up to this many are ranked directly
+constexpr uint32_t kLowest = 0x00800000u; // order key of the lowest finite value; -infinity is below
+
+// Order key: larger float, larger key; -0 and +0 alike; NaN above everything.
+__device__ __forceinline__ uint32_t order_key(float v) {
+  v += 0.0f;
+  const uint32_t b = __float_as_uint(v);
+  if (v != v) return 0xFFFFFFFFu;
+  return b ^ ((b >> 31) ? 0xFFFFFFFFu : 0x80000000u);
+}
+__device__ __forceinline__ float key_value(uint32_t k) {
+  if (k == 0xFFFFFFFFu) return __uint_as_float(0x7FFFFFFFu);
+  return __uint_as_float(k ^ ((k >> 31) ? 0x80000000u : 0xFFFFFFFFu));
+}
+__device__ __forceinline__ unsigned long long entry(uint32_t key, int index) {
+  return ((unsigned long long)key << 32) | (0xFFFFFFFFu - (uint32_t)index);
+}
+
+struct TopShared {
+  unsigned long long list[kTopList];
+  unsigned long long best[DGC_MAX_TOP];
+  int count, total[2];
+};
+
+// Sum over the block of a per-thread count.
+template <int NT>
+__device__ __forceinline__ int block_sum(int v, TopShared& sm, int par) {
+  v = __reduce_add_sync(0xFFFFFFFFu, v);
+  if (threadIdx.x == 0) sm.total[par] = 0;
+  __syncthreads();
+  if ((threadIdx.x & 31) == 0) atomicAdd(&sm.total[par], v);
+  __syncthreads();
+  return sm.total[par];
+}
+
+// The k largest of the n listed entries (all different), in order, to sm.best.  Ends with a barrier.
+template <int NT>
+__device__ void rank_list(TopShared& sm, int n, int k) {
+  const int tid = threadIdx.x;
+  unsigned long long floor = 0;   // entries below it are out
+  if (n > kTopRank && n > k) {
+    for (int bit = 63; bit >= 0; --bit) {
+      const unsigned long long c = floor | (1ull << bit);
+      int mine = 0;
+      for (int i = tid; i < n; i += NT) mine += sm.list[i] >= c;
+      if (block_sum<NT>(mine, sm, bit & 1) >= k) floor = c;
+    }
+  }
+  for (int i = tid; i < n; i += NT) {
+    const unsigned long long e = sm.list[i];
+    if (e < floor) continue;
+    int before = 0;
+    for (int j = 0; j < n; ++j) before += sm.list[j] > e;
+    if (before < k) sm.best[before] = e;
+  }
+  __syncthreads();
+}
+
+// The row's part [lo, hi) in chunks: its k largest entries above -infinity, in order, to
+// sm.best; returns how many there are.
+template <class T, int NT>
+__device__ int top_of_part(const Row<T>& row, int lo, int hi, int k, TopShared& sm) {
+  const int tid = threadIdx.x;
+  float top = -INFINITY;
+  bool nan = false;
+  each_chunk<T, NT, 4>(row, lo, hi, [&](const float (&v)[Row<T>::E], int, bool) {
+#pragma unroll
+    for (int i = 0; i < Row<T>::E; ++i) {
+      nan |= v[i] != v[i];
+      top = fmaxf(top, v[i]);
+    }
+  });
+  const uint32_t key = nan ? 0xFFFFFFFFu : order_key(top);
+  // k-th largest maximum, from the top bit down; what a type's rounding leaves in the low bits
+  // (or, for f32, a closer bound than 2^-15 of the value) is not worth a barrier a bit
+  constexpr int low = sizeof(T) == 4 ? 8 : std::is_same_v<T, __nv_bfloat16> ? 16 : 13;
+  uint32_t bound = 0;
+#pragma unroll 1
+  for (int bit = 31; bit >= low; --bit) {
+    const uint32_t c = bound | (1u << bit);
+    if (__syncthreads_count(key >= c) >= k) bound = c;
+  }
+  bound = max(bound, kLowest);
+  if (tid == 0) sm.count = 0;
+  __syncthreads();
+  auto list_above = [&](uint32_t from) {
+    each_chunk<T, NT, 2>(row, lo, hi, [&](const float (&v)[Row<T>::E], int e0, bool) {
+#pragma unroll
+      for (int i = 0; i < Row<T>::E; ++i) {
+        const uint32_t q = order_key(v[i]);
+        if (q >= from) {
+          const int at = atomicAdd(&sm.count, 1);
+          if (at < kTopList) sm.list[at] = entry(q, e0 + i);
+        }
+      }
+    });
+  };
+  if (key >= bound) list_above(bound);
+  __syncthreads();
+  int n = sm.count;
+  __syncthreads();
+  if (n > kTopList) {
+    // bisection for the k-th value: `good` is reached by k entries or more, `bad` by fewer
+    uint32_t good = bound, bad = 0xFFFFFFFFu;
+    int par = 0;
+    auto reach = [&](uint32_t from) {
+      int mine = 0;
+      each_chunk<T, NT, 2>(row, lo, hi, [&](const float (&v)[Row<T>::E], int, bool) {
+#pragma unroll
+        for (int i = 0; i < Row<T>::E; ++i) mine += order_key(v[i]) >= from;
+      });
+      return block_sum<NT>(mine, sm, par ^= 1);
+    };
+    if (reach(bad) >= k) good = bad;   // k NaN
+    while (bad - good > 1) {
+      const uint32_t mid = good + (bad - good) / 2;
+      if (reach(mid) >= k) good = mid;
+      else bad = mid;
+    }
+    if (tid == 0) sm.count = 0;
+    __syncthreads();
+    if (good != 0xFFFFFFFFu) list_above(good + 1);   // fewer than k
+    __syncthreads();
+    n = sm.count;
+    // the k-th value's equals in index order, until the list is full
+    for (int j0 = lo; j0 < hi && n < k; j0 += NT) {
+      const int j = j0 + tid;
+      uint32_t hit = 0;
+      const int e0 = row.first(j);
+      if (j < hi) {
+#pragma unroll
+        for (int i = 0; i < Row<T>::E; ++i) {
+          const int e = e0 + i;
+          if (e >= 0 && e < row.n && order_key(to_float<T>(row.p[e])) == good) hit |= 1u << i;
+        }
+      }
+      // places in order: hits of the warps before, then of the lanes before
+      const int lane = tid & 31, warp = tid >> 5;
+      int before = __popc(hit);
+#pragma unroll
+      for (int d = 1; d < 32; d *= 2) {
+        const int o = __shfl_up_sync(0xFFFFFFFFu, before, d);
+        if (lane >= d) before += o;
+      }
+      __shared__ int warps[NT / 32];
+      if (lane == 31) warps[warp] = before;
+      __syncthreads();
+      int base = n, all = 0;
+      for (int w = 0; w < NT / 32; ++w) {
+        if (w < warp) base += warps[w];
+        all += warps[w];
+      }
+      base += before - __popc(hit);
+#pragma unroll
+      for (int i = 0; i < Row<T>::E; ++i) {
+        if (hit >> i & 1) {
+          if (base < k) sm.list[base] = entry(good, e0 + i);
+          ++base;
+        }
+      }
+      n = min(k, n + all);
+      __syncthreads();
+    }
+  }
+  rank_list<NT>(sm, n, k);
+  return min(n, k);
+}
+
+// One cluster a row: its blocks take parts of the row, the first block joins their lists.
+template <class T, int NT>
+__global__ void __launch_bounds__(NT)
+k_top_logits(const T* logits, int64_t ld, int32_t rows, int32_t vocab, int32_t k, int32_t ncl,
+             int32_t* idx, float* val) {
+  pdl_enter();
+  __shared__ TopShared sm;
+  const int rank = ncl > 1 ? (int)(blockIdx.x % ncl) : 0;
+  const int64_t r = blockIdx.x / ncl;
+  const Row<T> row(logits + r * ld, vocab);
+  const int lo = (int)((int64_t)row.chunks * rank / ncl), hi = (int)((int64_t)row.chunks * (rank + 1) / ncl);
+  int n = top_of_part<T, NT>(row, lo, hi, k, sm);
+  if (ncl > 1) {
+    cg::cluster_group cl = cg::this_cluster();
+    if (threadIdx.x == 0) sm.total[0] = n;
+    cl.sync();
+    if (rank == 0) {
+      int at = 0;
+      for (int q = 0; q < ncl; ++q) {
+        TopShared* peer = cl.map_shared_rank(&sm, q);
+        const int m = peer->total[0];
+        for (int i = threadIdx.x; i < m; i += NT) sm.list[at + i] = peer->best[i];
+        at += m;
+      }
+      __syncthreads();
+      n = at;
+    }
+    cl.sync();   // the peers' lists have been read
+    if (rank != 0) return;
+    rank_list<NT>(sm, n, k);
+    n = min(n, k);
+  }
+  for (int i = threadIdx.x; i < k; i += NT) {
+    const unsigned long long e = i < n ? sm.best[i] : 0;
+    idx[r * k + i] = i < n ? (int32_t)(0xFFFFFFFFu - (uint32_t)e) : -1;
+    val[r * k + i] = i < n ? key_value((uint32_t)(e >> 32)) : -INFINITY;
+  }
+}
+
+template <class T>
+int32_t enqueue(const void* logits, int64_t ld, int64_t rows, int32_t vocab, int32_t k, int32_t* idx,
+                float* val, cudaStream_t s) {
+  int ncl = 1;
+  while (ncl < 8 && rows * ncl < 148 && vocab / ncl > 16384) ncl *= 2;
+  const int64_t grid = rows * ncl;
+  if (grid > INT32_MAX) return DGC_EINVAL;
+  launch_cluster(k_top_logits<T, kTopThreads>, dim3((unsigned)grid), kTopThreads, 0, s, (unsigned)ncl,
+                 static_cast<const T*>(logits), ld, (int32_t)rows, vocab, k, ncl, idx, val);
+  return check_launch();
+}
+
+}  // namespace
+
+extern "C" int32_t dgc_top_logits(int32_t dtype, int64_t rows, int32_t vocab, int32_t k,
+                                  const void* logits, int64_t ld_logits, int32_t* idx, float* val,
+                                  void* stream) {
+  if (dtype < DGC_F32 || dtype > DGC_F16 || rows < 0 || rows > INT32_MAX || vocab < 1 || vocab > INT32_MAX - 64 ||
+      k < 1 || k > DGC_MAX_TOP || ld_logits < vocab)
+    return DGC_EINVAL;
+  if (rows == 0) return DGC_OK;
+  const uintptr_t es = dtype == DGC_F32 ? 4 : 2;
+  if (!logits || !idx || !val || (reinterpret_cast<uintptr_t>(logits) & (es - 1)) ||
+      ((reinterpret_cast<uintptr_t>(idx) | reinterpret_cast<uintptr_t>(val)) & 3))
+    return DGC_EINVAL;
+  cudaStream_t s = as_stream(stream);
+  if (dtype == DGC_F32) return enqueue<float>(logits, ld_logits, rows, vocab, k, idx, val, s);
+  if (dtype == DGC_BF16) return enqueue<__nv_bfloat16>(logits, ld_logits, rows, vocab, k, idx, val, s);
+  return enqueue<__half>(logits, ld_logits, rows, vocab, k, idx, val, s);
+}
