@@ -10,12 +10,13 @@
 //   backward   e_t = f_t g_t,   g_t = dh_t + e_{t+1}:  the same map, walked from the end
 //
 // A lane owns one 32-bit word of a row (two 16-bit channels, or one of 32 bits) and a warp L
-// consecutive steps of 32 such words, kept in registers.  A block of NW warps holds NW*L steps;
-// a cluster of blocks holds consecutive ones.  Every thread reduces its run to (P, S), the runs
-// are joined in order through shared memory (the blocks' through the cluster's), and the second
-// walk over the registers starts from the true state.  The words of the next steps are loaded
-// before the join, so memory stays busy while the blocks talk.  One pass over the data, no
-// workspace, and a fixed order of the additions: results do not vary from run to run.
+// consecutive steps of 32 such words.  A block of NW warps holds NW*L steps; a cluster of blocks
+// holds consecutive ones.  Every warp fetches its own rows into shared memory with 16-byte
+// asynchronous copies, a stage ahead, whatever the alignment of the rows (see copy_rows).  Every
+// thread walks its run once to reduce it to (P, S), the runs are joined in order through shared
+// memory (the blocks' through the cluster's), and a second walk over the coefficients kept in
+// registers starts from the true state.  One pass over the data, no workspace, and a fixed
+// order of the additions: results do not vary from run to run.
 //
 // A sequence is one cluster's work, so nothing (no infinity, no NaN) can cross from one
 // sequence into its neighbour in the pack.
@@ -23,6 +24,7 @@
 #include <cooperative_groups.h>
 
 #include <algorithm>
+#include <initializer_list>
 
 #include "common.cuh"
 
@@ -43,14 +45,16 @@ struct ScanArgs {
   int32_t tokens, seqs, seq_len, channels, ctiles, cluster, reverse;
 };
 
-// sigma(z) and 1 - sigma(z), each to full relative precision (1 - f is not formed by
-// subtraction: for gates near 1 it is the weight of the input).
+// f = sigma(z) and 1 - f, each to full relative precision (1 - f is not formed by subtraction:
+// for gates near 1 it is the weight of the input).  The exponent is held below 2^126, so that
+// e f cannot become inf * 0; a NaN passes through.
 __device__ __forceinline__ void gate(float z, float& f, float& omf) {
-  const float e = __expf(-fabsf(z));
-  const float big = __fdividef(1.0f, 1.0f + e);
-  const float small = e * big;
-  f = z >= 0.0f ? big : small;
-  omf = z >= 0.0f ? small : big;
+  float x = z * -1.4426950408889634f, e;
+  asm("min.NaN.f32 %0, %0, 0f42FC0000;" : "+f"(x));   // 126
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(x));
+  const float t = 1.0f + e;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(f) : "f"(t));
+  omf = e * f;
 }
 
 __device__ __forceinline__ void sequence_range(const ScanArgs& a, int s, int& first, int& len) {
@@ -138,212 +142,345 @@ __device__ __forceinline__ void join_runs(Join<VEC, NW>& sm, int par, int ncl, i
   }
 }
 
-template <class T, int VEC, int L, int NW>
-__global__ void __launch_bounds__(NW * 32) k_scan_forward(const ScanArgs a) {
-  pdl_enter();
-  __shared__ Join<VEC, NW> sm;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int ncl = a.cluster, rank = ncl > 1 ? (int)(blockIdx.x % ncl) : 0;
-  const int unit = blockIdx.x / ncl;
-  const int c = ((unit % a.ctiles) * 32 + lane) * VEC;
-  const int s = unit / a.ctiles;
-  const bool on = c < a.channels;
-  int first, len;
-  sequence_range(a, s, first, len);
-  const int64_t at0 = a.reverse ? (int64_t)first + len - 1 : first;   // the scan's first token
-  const int64_t dir = a.reverse ? -1 : 1;
-  const T* z = static_cast<const T*>(a.z) + at0 * a.ld_z + c;
-  const T* x = static_cast<const T*>(a.x) + at0 * a.ld_x + c;
-  T* h = static_cast<T*>(a.h) + at0 * a.ld_h + c;
-  const int64_t dz = dir * a.ld_z, dx = dir * a.ld_x, dh = dir * a.ld_h;
+// ------------------------------------------------------------------ rows into shared memory
+// How the rows lie against 16-byte boundaries, over all matrices of a call.
+enum Lie { kAligned, kWords, kHalves };   // every row on a boundary; on 4 bytes; on 2 bytes
 
+constexpr int kRowBytes = 128;            // a warp's part of a row: 32 words
+template <Lie LIE> constexpr int kGranules = LIE == kAligned ? kRowBytes / 16 : kRowBytes / 16 + 1;
+template <Lie LIE> constexpr int kPitch = kGranules<LIE> * 16;
+
+struct Rows {              // a matrix as the copies see it, at this thread's channels' block
+  const char* row;         // the scan's first row, the tile's first channel
+  int64_t stride;          // bytes from one step to the next (negative: from the end)
+  const char *begin, *end; // the matrix
+};
+
+template <class T>
+__device__ __forceinline__ Rows rows_of(const void* base, int64_t ld, int64_t at0, int64_t dir, int c0,
+                                        const ScanArgs& a) {
+  Rows r;
+  r.begin = static_cast<const char*>(base);
+  r.end = r.begin + ((int64_t)(a.tokens - 1) * ld + a.channels) * sizeof(T);
+  r.row = r.begin + (at0 * ld + c0) * (int64_t)sizeof(T);
+  r.stride = dir * ld * (int64_t)sizeof(T);
+  return r;
+}
+
+// Copies the warp's part of the steps [t0, t0 + n) (steps outside [0, len) are left out) in
+// aligned 16-byte granules; `width` is the part's bytes inside the matrix's columns.  Where
+// rows do not start on a boundary the granules at a part's ends also hold neighbouring
+// elements, which nobody uses; a granule that reaches outside the matrix itself is fetched by
+// elements.
+template <class T, Lie LIE, int L>
+__device__ __forceinline__ void copy_rows(char* to, const Rows& m, int64_t t0, int len, int width, int lane) {
+  constexpr int G = kGranules<LIE>;
+  const uint32_t dst = (uint32_t)__cvta_generic_to_shared(to);
+#pragma unroll
+  for (int k = 0; k < (L * G + 31) / 32; ++k) {
+    const int i = lane + 32 * k, r = i / G, g = i % G;
+    const int64_t t = t0 + r;
+    if (r < L && t >= 0 && t < len) {
+      const char* p = m.row + t * m.stride;
+      if (LIE == kAligned) {
+        if (g * 16 < width)
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + r * kPitch<LIE> + g * 16),
+                       "l"(p + g * 16) : "memory");
+      } else {
+        const char* q = reinterpret_cast<const char*>(reinterpret_cast<uintptr_t>(p) & ~(uintptr_t)15) + g * 16;
+        if (q < p + width) {
+          if (q >= m.begin && q + 16 <= m.end) {
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + r * kPitch<LIE> + g * 16), "l"(q)
+                         : "memory");
+          } else {
+            for (int b = 0; b < 16; b += sizeof(T))
+              if (q + b >= p && q + b < p + width)
+                *reinterpret_cast<T*>(to + r * kPitch<LIE> + g * 16 + b) = *reinterpret_cast<const T*>(q + b);
+          }
+        }
+      }
+    }
+  }
+}
+
+// Word of this lane in row r of a copied part; `first` is the low half of the address of the
+// part's first row, `stride` the low half of the stride.
+template <class T, Lie LIE>
+__device__ __forceinline__ void row_word(const char* from, uint32_t first, uint32_t stride, int r, int lane,
+                                         float (&v)[4 / sizeof(T)]) {
+  const char* p = from + r * kPitch<LIE> + lane * 4;
+  if (LIE != kAligned) p += (first + r * stride) & 15u;
+  if constexpr (LIE == kHalves) {
+    static_assert(sizeof(T) == 2, "");
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      float one[1];
+      unpack<T, 1>(*reinterpret_cast<const unsigned short*>(p + 2 * i), one);
+      v[i] = one[0];
+    }
+  } else {
+    unpack<T, 4 / sizeof(T)>(*reinterpret_cast<const uint32_t*>(p), v);
+  }
+}
+
+template <class T, Lie LIE>
+__device__ __forceinline__ void put_word(char* p, const float (&v)[4 / sizeof(T)], bool on0, bool on1) {
+  if constexpr (LIE == kHalves) {
+    const float a[1] = {v[0]}, b[1] = {v[1]};
+    if (on0) store_word<T, 1>(reinterpret_cast<T*>(p), pack<T, 1>(a));
+    if (on1) store_word<T, 1>(reinterpret_cast<T*>(p) + 1, pack<T, 1>(b));
+  } else {
+    if (on0) store_word<T, 4 / sizeof(T)>(reinterpret_cast<T*>(p), pack<T, 4 / sizeof(T)>(v));
+  }
+}
+
+template <int N>
+__device__ __forceinline__ void wait_copies() {   // all but the last N groups have arrived
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+  __syncwarp();
+}
+__device__ __forceinline__ void end_copies() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+
+// What a thread works on: a sequence, a block of channels, a place in the cluster.
+template <class T, int L, int NW>
+struct Place {
+  static constexpr int VEC = 4 / sizeof(T);
+  int lane, warp, ncl, rank, s, c0, c, first, len, mine0, step, width;
+  bool on0, on1;
+  int64_t at0, dir;
+  __device__ __forceinline__ explicit Place(const ScanArgs& a) {
+    lane = threadIdx.x & 31;
+    warp = threadIdx.x >> 5;
+    ncl = a.cluster;
+    rank = ncl > 1 ? (int)(blockIdx.x % ncl) : 0;
+    const int unit = blockIdx.x / ncl;
+    s = unit / a.ctiles;
+    c0 = (unit % a.ctiles) * 32 * VEC;
+    c = c0 + lane * VEC;
+    on0 = c < a.channels;
+    on1 = c + 1 < a.channels;
+    width = min(32 * VEC, a.channels - c0) * (int)sizeof(T);
+    sequence_range(a, s, first, len);
+    at0 = a.reverse ? (int64_t)first + len - 1 : first;   // the scan's first token
+    dir = a.reverse ? -1 : 1;
+    mine0 = (rank * NW + warp) * L;
+    step = ncl * NW * L;
+  }
+  __device__ __forceinline__ void get(const float* p, int channels, float (&v)[VEC]) const {
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) v[i] = p && (i ? on1 : on0) ? p[(int64_t)s * channels + c + i] : 0.0f;
+  }
+  __device__ __forceinline__ void put(float* p, int channels, const float (&v)[VEC]) const {
+#pragma unroll
+    for (int i = 0; i < VEC; ++i)
+      if (i ? on1 : on0) p[(int64_t)s * channels + c + i] = v[i];
+  }
+};
+
+constexpr int kStages = 2;
+
+template <class T, Lie LIE, int L, int NW>
+__global__ void __launch_bounds__(NW * 32, 2) k_scan_forward(const ScanArgs a) {
+  pdl_enter();
+  constexpr int VEC = 4 / sizeof(T), kPart = L * kPitch<LIE>;
+  extern __shared__ __align__(16) char buffer[];   // [warp][stage][z, x][L rows]
+  __shared__ Join<VEC, NW> sm;
+  const Place<T, L, NW> at(a);
+  const int len = at.len;
+  const Rows z = rows_of<T>(a.z, a.ld_z, at.at0, at.dir, at.c0, a), x = rows_of<T>(a.x, a.ld_x, at.at0, at.dir, at.c0, a);
+  char* const mine = buffer + at.warp * (kStages * 2 * kPart);
+  auto fetch = [&](int64_t t0, int stage) {
+    copy_rows<T, LIE, L>(mine + stage * 2 * kPart, z, t0, len, at.width, at.lane);
+    copy_rows<T, LIE, L>(mine + stage * 2 * kPart + kPart, x, t0, len, at.width, at.lane);
+    end_copies();
+  };
+#pragma unroll
+  for (int i = 0; i < kStages; ++i) fetch((int64_t)at.step * i + at.mine0, i);
   float carry[VEC];
-#pragma unroll
-  for (int v = 0; v < VEC; ++v)
-    carry[v] = on && a.h0 ? a.h0[(int64_t)s * a.channels + c + v] : 0.0f;
+  at.get(a.h0, a.channels, carry);
   if (len == 0) {   // (the same for all blocks of the cluster)
-    if (a.h_last && on && rank == 0 && warp == 0)
-#pragma unroll
-      for (int v = 0; v < VEC; ++v) a.h_last[(int64_t)s * a.channels + c + v] = carry[v];
+    if (a.h_last && at.rank == 0 && at.warp == 0) at.put(a.h_last, a.channels, carry);
     return;
   }
-  if (ncl > 1) cg::this_cluster().sync();   // every block runs before anyone writes to its memory
+  if (at.ncl > 1) cg::this_cluster().sync();   // every block runs before anyone writes to its memory
 
-  const int mine0 = (rank * NW + warp) * L, step = ncl * NW * L;
-  uint32_t wz[L], wx[L];
-#pragma unroll
-  for (int i = 0; i < L; ++i) {
-    const int t = mine0 + i;
-    wz[i] = wx[i] = 0;
-    if (on && t < len) {
-      wz[i] = load_word<T, VEC>(z + t * dz);
-      wx[i] = load_word<T, VEC>(x + t * dx);
-    }
-  }
-  int par = 0;
-  for (int64_t base = 0; base < len; base += step, par ^= 1) {
-    const int t0 = (int)base + mine0;
+  const int64_t out_stride = at.dir * a.ld_h * (int64_t)sizeof(T);
+  int par = 0, stage = 0;
+  for (int64_t base = 0; base < len; base += at.step, par ^= 1) {
+    const int64_t t0 = base + at.mine0;
+    const bool full = t0 + L <= len;
+    const char* from = mine + stage * 2 * kPart;
+    const uint32_t z0 = (uint32_t)reinterpret_cast<uintptr_t>(z.row) + (uint32_t)t0 * (uint32_t)z.stride;
+    const uint32_t x0 = (uint32_t)reinterpret_cast<uintptr_t>(x.row) + (uint32_t)t0 * (uint32_t)x.stride;
     float f[L][VEC], b[L][VEC], P[VEC], S[VEC];
+    wait_copies<kStages - 1>();
 #pragma unroll
     for (int v = 0; v < VEC; ++v) { P[v] = 1.0f; S[v] = 0.0f; }
+    auto walk = [&](auto whole) {
 #pragma unroll
-    for (int i = 0; i < L; ++i) {
-      float zz[VEC], xx[VEC];
-      unpack<T, VEC>(wz[i], zz);
-      unpack<T, VEC>(wx[i], xx);
-      const bool live = t0 + i < len;
+      for (int i = 0; i < L; ++i) {
+        float zz[VEC], xx[VEC];
+        row_word<T, LIE>(from, z0, (uint32_t)z.stride, i, at.lane, zz);
+        row_word<T, LIE>(from + kPart, x0, (uint32_t)x.stride, i, at.lane, xx);
 #pragma unroll
-      for (int v = 0; v < VEC; ++v) {
-        float omf;
-        gate(zz[v], f[i][v], omf);
-        b[i][v] = omf * xx[v];
-        if (!live) { f[i][v] = 1.0f; b[i][v] = 0.0f; }
-        P[v] *= f[i][v];
-        S[v] = fmaf(f[i][v], S[v], b[i][v]);
+        for (int v = 0; v < VEC; ++v) {
+          float omf;
+          gate(zz[v], f[i][v], omf);
+          b[i][v] = omf * xx[v];
+          if (!decltype(whole)::value && t0 + i >= len) { f[i][v] = 1.0f; b[i][v] = 0.0f; }
+          P[v] *= f[i][v];
+          S[v] = fmaf(f[i][v], S[v], b[i][v]);
+        }
       }
-    }
-#pragma unroll
-    for (int i = 0; i < L; ++i) {   // the next steps' words, under way during the join
-      const int64_t t = base + step + mine0 + i;
-      if (on && t < len) {
-        wz[i] = load_word<T, VEC>(z + t * dz);
-        wx[i] = load_word<T, VEC>(x + t * dx);
-      }
-    }
+    };
+    if (full) walk(std::true_type{});
+    else walk(std::false_type{});
+    __syncwarp();   // the stage has been read by all lanes
+    fetch(t0 + (int64_t)kStages * at.step, stage);
+    stage = stage + 1 == kStages ? 0 : stage + 1;
     float cur[VEC];
-    join_runs<VEC, NW>(sm, par, ncl, rank, warp, lane, P, S, carry, cur);
+    join_runs<VEC, NW>(sm, par, at.ncl, at.rank, at.warp, at.lane, P, S, carry, cur);
+    char* out = static_cast<char*>(a.h) + ((at.at0 + at.dir * t0) * a.ld_h + at.c) * (int64_t)sizeof(T);
 #pragma unroll
-    for (int i = 0; i < L; ++i) {
+    for (int i = 0; i < L; ++i, out += out_stride) {
 #pragma unroll
       for (int v = 0; v < VEC; ++v) cur[v] = fmaf(f[i][v], cur[v], b[i][v]);
-      const int t = t0 + i;
-      if (on && t < len) store_word<T, VEC>(h + t * dh, pack<T, VEC>(cur));
+      if (full || t0 + i < len) put_word<T, LIE>(out, cur, at.on0, at.on1);
     }
-    if (a.h_last && on && t0 < len && t0 + L >= len) {
-#pragma unroll
-      for (int v = 0; v < VEC; ++v) a.h_last[(int64_t)s * a.channels + c + v] = cur[v];
-    }
+    // (steps after the last have f = 1, b = 0: they pass the state on unchanged)
+    if (a.h_last && t0 < len && t0 + L >= len) at.put(a.h_last, a.channels, cur);
   }
+  wait_copies<0>();
 }
 
 // Backward, walked from the sequence's end: position u = len-1-t.  A thread's run of L steps
 // needs h_{t-1} at each of them; it reads the stored h once, before the run's first step, and
 // recomputes the others in 32 bits from z and x, which it has to read anyway: 5 words moved a
 // step instead of 6, and the states inside a run carry no rounding of the output type.
-template <class T, int VEC, int L, int NW>
-__global__ void __launch_bounds__(NW * 32) k_scan_backward(const ScanArgs a) {
+template <class T, Lie LIE, int L, int NW>
+__global__ void __launch_bounds__(NW * 32, 2) k_scan_backward(const ScanArgs a) {
   pdl_enter();
+  constexpr int VEC = 4 / sizeof(T), kPart = L * kPitch<LIE>;
+  extern __shared__ __align__(16) char buffer[];   // [warp][stage][z, x, dh][L rows]
   __shared__ Join<VEC, NW> sm;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int ncl = a.cluster, rank = ncl > 1 ? (int)(blockIdx.x % ncl) : 0;
-  const int unit = blockIdx.x / ncl;
-  const int c = ((unit % a.ctiles) * 32 + lane) * VEC;
-  const int s = unit / a.ctiles;
-  const bool on = c < a.channels;
-  int first, len;
-  sequence_range(a, s, first, len);
-  const int64_t at0 = a.reverse ? (int64_t)first + len - 1 : first;
-  const int64_t dir = a.reverse ? -1 : 1;
-  const T* z = static_cast<const T*>(a.z) + at0 * a.ld_z + c;
-  const T* x = static_cast<const T*>(a.x) + at0 * a.ld_x + c;
-  const T* h = static_cast<const T*>(a.h_in) + at0 * a.ld_h + c;
-  const T* dh = static_cast<const T*>(a.dh) + at0 * a.ld_dh + c;
-  T* gz = static_cast<T*>(a.dz) + at0 * a.ld_dz + c;
-  T* gx = static_cast<T*>(a.dx) + at0 * a.ld_dx + c;
-  const int64_t sz = dir * a.ld_z, sx = dir * a.ld_x, sh = dir * a.ld_h, sdh = dir * a.ld_dh,
-                sgz = dir * a.ld_dz, sgx = dir * a.ld_dx;
-
+  const Place<T, L, NW> at(a);
+  const int len = at.len;
+  const Rows z = rows_of<T>(a.z, a.ld_z, at.at0, at.dir, at.c0, a), x = rows_of<T>(a.x, a.ld_x, at.at0, at.dir, at.c0, a),
+             d = rows_of<T>(a.dh, a.ld_dh, at.at0, at.dir, at.c0, a);
+  char* const mine = buffer + at.warp * (kStages * 3 * kPart);
+  // a stage holds the steps t_lo .. t_lo + L - 1 in ascending order
+  auto fetch = [&](int64_t u0, int stage) {
+    const int64_t t_lo = len - u0 - L;
+    char* to = mine + stage * 3 * kPart;
+    copy_rows<T, LIE, L>(to, z, t_lo, len, at.width, at.lane);
+    copy_rows<T, LIE, L>(to + kPart, x, t_lo, len, at.width, at.lane);
+    copy_rows<T, LIE, L>(to + 2 * kPart, d, t_lo, len, at.width, at.lane);
+    end_copies();
+  };
+#pragma unroll
+  for (int i = 0; i < kStages; ++i) fetch((int64_t)at.step * i + at.mine0, i);
   float carry[VEC], start[VEC];
-#pragma unroll
-  for (int v = 0; v < VEC; ++v) {
-    carry[v] = on && a.dh_last ? a.dh_last[(int64_t)s * a.channels + c + v] : 0.0f;
-    start[v] = on && a.h0 ? a.h0[(int64_t)s * a.channels + c + v] : 0.0f;
-  }
+  at.get(a.dh_last, a.channels, carry);
+  at.get(a.h0, a.channels, start);
   if (len == 0) {
-    if (a.dh0 && on && rank == 0 && warp == 0)
-#pragma unroll
-      for (int v = 0; v < VEC; ++v) a.dh0[(int64_t)s * a.channels + c + v] = carry[v];
+    if (a.dh0 && at.rank == 0 && at.warp == 0) at.put(a.dh0, a.channels, carry);
     return;
   }
-  if (ncl > 1) cg::this_cluster().sync();
+  if (at.ncl > 1) cg::this_cluster().sync();
 
-  const int mine0 = (rank * NW + warp) * L, step = ncl * NW * L;
-  uint32_t wz[L], wx[L], wd[L], wh = 0;
-  auto load = [&](int64_t u0) {
+  // the state before a run, stored by the forward pass
+  auto state_before = [&](int64_t u0, float (&v)[VEC]) {
+    const int64_t t = len - 1 - (u0 + L);
 #pragma unroll
-    for (int i = 0; i < L; ++i) {
-      const int64_t t = len - 1 - (u0 + i);
-      wz[i] = wx[i] = wd[i] = 0;
-      if (on && t >= 0) {
-        wz[i] = load_word<T, VEC>(z + t * sz);
-        wx[i] = load_word<T, VEC>(x + t * sx);
-        wd[i] = load_word<T, VEC>(dh + t * sdh);
+    for (int i = 0; i < VEC; ++i) v[i] = start[i];
+    if (t >= 0) {
+      const T* p = static_cast<const T*>(a.h_in) + (at.at0 + at.dir * t) * a.ld_h + at.c;
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        float one[1] = {0.0f};
+        if (i ? at.on1 : at.on0) {
+          if constexpr (sizeof(T) == 4) one[0] = __ldg(p + i);
+          else unpack<T, 1>(load_word<T, 1>(p + i), one);
+        }
+        v[i] = one[0];
       }
     }
-    const int64_t before = len - 1 - (u0 + L);   // the step before the run's first
-    if (on && before >= 0) wh = load_word<T, VEC>(h + before * sh);
   };
-  load(mine0);
-  int par = 0;
-  for (int64_t base = 0; base < len; base += step, par ^= 1) {
-    const int64_t u0 = base + mine0;
-    const int64_t t_hi = len - 1 - u0;   // may be negative: nothing of this sequence is left
-    float f[L][VEC], w1[L][VEC], d[L][VEC], g[L][VEC], P[VEC], S[VEC], hp[VEC];
-    unpack<T, VEC>(wh, hp);
-    if (t_hi - L < 0) {
+  float before[VEC];
+  state_before(at.mine0, before);
+  const int64_t zs = at.dir * a.ld_dz * (int64_t)sizeof(T), xs = at.dir * a.ld_dx * (int64_t)sizeof(T);
+  int par = 0, stage = 0;
+  for (int64_t base = 0; base < len; base += at.step, par ^= 1) {
+    const int64_t u0 = base + at.mine0;
+    const int64_t t_hi = len - 1 - u0, t_lo = t_hi - (L - 1);   // negative: nothing of this sequence is left there
+    const bool full = t_lo >= 0;
+    const char* from = mine + stage * 3 * kPart;
+    const uint32_t z0 = (uint32_t)reinterpret_cast<uintptr_t>(z.row) + (uint32_t)t_lo * (uint32_t)z.stride;
+    const uint32_t x0 = (uint32_t)reinterpret_cast<uintptr_t>(x.row) + (uint32_t)t_lo * (uint32_t)x.stride;
+    const uint32_t d0 = (uint32_t)reinterpret_cast<uintptr_t>(d.row) + (uint32_t)t_lo * (uint32_t)d.stride;
+    float f[L][VEC], w[L][VEC], e[L][VEC], P[VEC], S[VEC];   // f, 1 - f, h_{t-1} - x_t
+    wait_copies<kStages - 1>();
+    auto walk = [&](auto whole) {
+      float hp[VEC];
 #pragma unroll
-      for (int v = 0; v < VEC; ++v) hp[v] = start[v];
-    }
+      for (int v = 0; v < VEC; ++v) hp[v] = before[v];
 #pragma unroll
-    for (int i = L - 1; i >= 0; --i) {   // ascending t
-      float zz[VEC], xx[VEC];
-      unpack<T, VEC>(wz[i], zz);
-      unpack<T, VEC>(wx[i], xx);
-      unpack<T, VEC>(wd[i], g[i]);
-      const bool live = t_hi - i >= 0;
+      for (int j = 0; j < L; ++j) {
+        float zz[VEC], xx[VEC];
+        row_word<T, LIE>(from, z0, (uint32_t)z.stride, j, at.lane, zz);
+        row_word<T, LIE>(from + kPart, x0, (uint32_t)x.stride, j, at.lane, xx);
+        const bool live = decltype(whole)::value || t_lo + j >= 0;
 #pragma unroll
-      for (int v = 0; v < VEC; ++v) {
-        gate(zz[v], f[i][v], w1[i][v]);
-        d[i][v] = hp[v] - xx[v];
-        if (live) hp[v] = fmaf(f[i][v], hp[v], w1[i][v] * xx[v]);
-        else f[i][v] = 1.0f;
+        for (int v = 0; v < VEC; ++v) {
+          gate(zz[v], f[j][v], w[j][v]);
+          e[j][v] = hp[v] - xx[v];
+          if (live) hp[v] = fmaf(f[j][v], hp[v], w[j][v] * xx[v]);
+          else f[j][v] = 1.0f;
+        }
       }
-    }
 #pragma unroll
-    for (int v = 0; v < VEC; ++v) { P[v] = 1.0f; S[v] = 0.0f; }
+      for (int v = 0; v < VEC; ++v) { P[v] = 1.0f; S[v] = 0.0f; }
 #pragma unroll
-    for (int i = 0; i < L; ++i) {
+      for (int j = L - 1; j >= 0; --j) {
+        float g[VEC];
+        row_word<T, LIE>(from + 2 * kPart, d0, (uint32_t)d.stride, j, at.lane, g);
 #pragma unroll
-      for (int v = 0; v < VEC; ++v) {
-        P[v] *= f[i][v];
-        S[v] = f[i][v] * (g[i][v] + S[v]);
+        for (int v = 0; v < VEC; ++v) {
+          if (!decltype(whole)::value && t_lo + j < 0) g[v] = 0.0f;
+          P[v] *= f[j][v];
+          S[v] = f[j][v] * (g[v] + S[v]);
+        }
       }
-    }
-    load(base + step + mine0);
+    };
+    if (full) walk(std::true_type{});
+    else walk(std::false_type{});
+    state_before(u0 + at.step, before);
     float cur[VEC];
-    join_runs<VEC, NW>(sm, par, ncl, rank, warp, lane, P, S, carry, cur);
+    join_runs<VEC, NW>(sm, par, at.ncl, at.rank, at.warp, at.lane, P, S, carry, cur);
+    char* gz = static_cast<char*>(a.dz) + ((at.at0 + at.dir * t_hi) * a.ld_dz + at.c) * (int64_t)sizeof(T);
+    char* gx = static_cast<char*>(a.dx) + ((at.at0 + at.dir * t_hi) * a.ld_dx + at.c) * (int64_t)sizeof(T);
 #pragma unroll
-    for (int i = 0; i < L; ++i) {
-      float oz[VEC], ox[VEC];
+    for (int j = L - 1; j >= 0; --j, gz -= zs, gx -= xs) {
+      if (full || t_lo + j >= 0) {
+        float g[VEC], oz[VEC], ox[VEC];
+        row_word<T, LIE>(from + 2 * kPart, d0, (uint32_t)d.stride, j, at.lane, g);
 #pragma unroll
-      for (int v = 0; v < VEC; ++v) {
-        const float gt = g[i][v] + cur[v];
-        cur[v] = f[i][v] * gt;
-        ox[v] = w1[i][v] * gt;
-        oz[v] = w1[i][v] * cur[v] * d[i][v];
-      }
-      const int64_t t = t_hi - i;
-      if (on && t >= 0) {
-        store_word<T, VEC>(gz + t * sgz, pack<T, VEC>(oz));
-        store_word<T, VEC>(gx + t * sgx, pack<T, VEC>(ox));
+        for (int v = 0; v < VEC; ++v) {
+          const float gt = g[v] + cur[v];
+          cur[v] = f[j][v] * gt;
+          ox[v] = w[j][v] * gt;
+          oz[v] = w[j][v] * cur[v] * e[j][v];
+        }
+        put_word<T, LIE>(gz, oz, at.on0, at.on1);
+        put_word<T, LIE>(gx, ox, at.on0, at.on1);
       }
     }
-    // (steps before the sequence's first have f = 1, g = 0: they pass e on unchanged)
-    if (a.dh0 && on && t_hi >= 0 && t_hi < L) {
-#pragma unroll
-      for (int v = 0; v < VEC; ++v) a.dh0[(int64_t)s * a.channels + c + v] = cur[v];
-    }
+    if (a.dh0 && t_hi >= 0 && t_lo <= 0) at.put(a.dh0, a.channels, cur);
+    __syncwarp();   // the stage has been read by all lanes
+    fetch(u0 + (int64_t)kStages * at.step, stage);
+    stage = stage + 1 == kStages ? 0 : stage + 1;
   }
+  wait_copies<0>();
 }
 
 // One token a sequence: the state is read, advanced and written back where it lies.
@@ -376,7 +513,7 @@ k_scan_step(const T* z, int64_t ld_z, const T* x, int64_t ld_x, float* state, co
 
 bool aligned(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
-constexpr int kFwdL = 16, kFwdNW = 8, kBwdL = 8, kBwdNW = 16;
+constexpr int kWarps = 8, kFwdL = 16, kBwdL = 8;
 
 int cluster_for(const ScanArgs& a, int tile) {
   int64_t blocks = (int64_t)a.ctiles * a.seqs;
@@ -386,26 +523,36 @@ int cluster_for(const ScanArgs& a, int tile) {
   return ncl;
 }
 
-template <class T, int VEC>
+template <class T, Lie LIE>
 int32_t enqueue(ScanArgs a, bool backward, cudaStream_t s) {
+  constexpr int VEC = 4 / sizeof(T);
   a.ctiles = (a.channels + 32 * VEC - 1) / (32 * VEC);
-  a.cluster = cluster_for(a, backward ? kBwdL * kBwdNW : kFwdL * kFwdNW);
+  a.cluster = cluster_for(a, kWarps * (backward ? kBwdL : kFwdL));
   const int64_t grid = (int64_t)a.ctiles * a.seqs * a.cluster;
   if (grid > INT32_MAX) return DGC_EINVAL;
-  if (backward)
-    launch_cluster(k_scan_backward<T, VEC, kBwdL, kBwdNW>, dim3((unsigned)grid), dim3(kBwdNW * 32), 0, s,
-                   (unsigned)a.cluster, a);
-  else
-    launch_cluster(k_scan_forward<T, VEC, kFwdL, kFwdNW>, dim3((unsigned)grid), dim3(kFwdNW * 32), 0, s,
-                   (unsigned)a.cluster, a);
-  return check_launch();
+  auto go = [&](auto kernel, size_t smem) {
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) {
+      (void)cudaGetLastError();
+      return (int32_t)DGC_ECUDA;
+    }
+    launch_cluster(kernel, dim3((unsigned)grid), dim3(kWarps * 32), smem, s, (unsigned)a.cluster, a);
+    return check_launch();
+  };
+  if (backward) return go(k_scan_backward<T, LIE, kBwdL, kWarps>, kWarps * kStages * 3 * kBwdL * kPitch<LIE>);
+  return go(k_scan_forward<T, LIE, kFwdL, kWarps>, kWarps * kStages * 2 * kFwdL * kPitch<LIE>);
 }
 
-int32_t dispatch(const ScanArgs& a, int32_t dtype, bool backward, bool pairs, cudaStream_t s) {
-  if (dtype == DGC_F32) return enqueue<float, 1>(a, backward, s);
+int32_t dispatch(const ScanArgs& a, int32_t dtype, bool backward, Lie lie, cudaStream_t s) {
+  if (dtype == DGC_F32)
+    return lie == kAligned ? enqueue<float, kAligned>(a, backward, s) : enqueue<float, kWords>(a, backward, s);
   if (dtype == DGC_BF16)
-    return pairs ? enqueue<__nv_bfloat16, 2>(a, backward, s) : enqueue<__nv_bfloat16, 1>(a, backward, s);
-  return pairs ? enqueue<__half, 2>(a, backward, s) : enqueue<__half, 1>(a, backward, s);
+    return lie == kAligned ? enqueue<__nv_bfloat16, kAligned>(a, backward, s)
+           : lie == kWords ? enqueue<__nv_bfloat16, kWords>(a, backward, s)
+                           : enqueue<__nv_bfloat16, kHalves>(a, backward, s);
+  return lie == kAligned ? enqueue<__half, kAligned>(a, backward, s)
+         : lie == kWords ? enqueue<__half, kWords>(a, backward, s)
+                         : enqueue<__half, kHalves>(a, backward, s);
 }
 
 size_t element_size(int32_t dtype) { return dtype == DGC_F32 ? 4 : 2; }
@@ -422,6 +569,14 @@ bool bad_rows(const void* p, int64_t ld, int32_t channels, size_t elem, int64_t 
 }
 
 bool pairs_ok(const void* p, int64_t ld) { return aligned(p, 4) && ld % 2 == 0; }
+
+// The worst lie of the call's matrices.
+struct Matrix { const void* p; int64_t ld; };
+Lie lie_of(std::initializer_list<Matrix> ms, int32_t channels, size_t es) {
+  size_t bits = channels * es;
+  for (const Matrix& m : ms) bits |= reinterpret_cast<uintptr_t>(m.p) | (size_t)m.ld * es;
+  return bits % 16 == 0 ? kAligned : bits % 4 == 0 ? kWords : kHalves;
+}
 
 }  // namespace
 
@@ -443,8 +598,8 @@ int32_t dgc_gated_scan_forward(int32_t dtype, int64_t tokens, int32_t num_seqs, 
   a.ld_z = ld_gate; a.ld_x = ld_x; a.ld_h = ld_h;
   a.tokens = (int32_t)tokens; a.seqs = num_seqs; a.seq_len = (int32_t)(tokens / num_seqs);
   a.channels = channels; a.reverse = reverse != 0;
-  const bool pairs = channels % 2 == 0 && pairs_ok(gate_logits, ld_gate) && pairs_ok(x, ld_x) && pairs_ok(h, ld_h);
-  return dispatch(a, dtype, false, pairs, as_stream(stream));
+  const Lie lie = lie_of({{gate_logits, ld_gate}, {x, ld_x}, {h, ld_h}}, channels, es);
+  return dispatch(a, dtype, false, lie, as_stream(stream));
 }
 
 int32_t dgc_gated_scan_backward(int32_t dtype, int64_t tokens, int32_t num_seqs, int32_t channels,
@@ -467,9 +622,9 @@ int32_t dgc_gated_scan_backward(int32_t dtype, int64_t tokens, int32_t num_seqs,
   a.ld_z = ld_gate; a.ld_x = ld_x; a.ld_h = ld_h; a.ld_dh = ld_dh; a.ld_dz = ld_dgate; a.ld_dx = ld_dx;
   a.tokens = (int32_t)tokens; a.seqs = num_seqs; a.seq_len = (int32_t)(tokens / num_seqs);
   a.channels = channels; a.reverse = reverse != 0;
-  const bool pairs = channels % 2 == 0 && pairs_ok(gate_logits, ld_gate) && pairs_ok(x, ld_x) &&
-                     pairs_ok(h, ld_h) && pairs_ok(dh, ld_dh) && pairs_ok(dgate, ld_dgate) && pairs_ok(dx, ld_dx);
-  return dispatch(a, dtype, true, pairs, as_stream(stream));
+  const Lie lie = lie_of({{gate_logits, ld_gate}, {x, ld_x}, {h, ld_h}, {dh, ld_dh}, {dgate, ld_dgate}, {dx, ld_dx}},
+                         channels, es);
+  return dispatch(a, dtype, true, lie, as_stream(stream));
 }
 
 int32_t dgc_gated_scan_step(int32_t dtype, int32_t rows, int32_t channels, const void* gate_logits,
