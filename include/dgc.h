@@ -444,6 +444,11 @@ int32_t dgc_gated_scan_step(int32_t dtype, int32_t rows, int32_t channels, const
                             const int32_t* slots, int32_t num_slots, void* out, int64_t ld_out,
                             void* stream);
 
+/* Synchronises `stream` and returns DGC_ECUDA if, since the last check on the current device, a
+ * block of a dgc_gated_scan_forward or _backward kernel gave up waiting for another block of its
+ * cluster (every such wait is bounded; the call's results are then wrong), else DGC_OK. */
+int32_t dgc_gated_scan_check(void* stream);
+
 /* The k largest entries of every row of `logits` [rows, vocab], the form in which a teacher's
  * distribution is kept for dgc_distill_*: largest first, the lowest index first among equals
  * (-0 equals +0, NaN counts as larger than every number).  Entries of -infinity (words masked

@@ -110,6 +110,7 @@ _sigs = {
     "dgc_gated_scan_step": (ctypes.c_int32, [ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, _vp,
                                              ctypes.c_int64, _vp, ctypes.c_int64, _vp, _vp,
                                              ctypes.c_int32, _vp, ctypes.c_int64, _vp]),
+    "dgc_gated_scan_check": (ctypes.c_int32, [_vp]),
     "dgc_top_logits": (ctypes.c_int32, [ctypes.c_int32, ctypes.c_int64, ctypes.c_int32,
                                         ctypes.c_int32, _vp, ctypes.c_int64, _vp, _vp, _vp]),
     "dgc_distill_forward": (ctypes.c_int32, [ctypes.c_int32, ctypes.c_int64, ctypes.c_int32,
@@ -561,6 +562,11 @@ def gated_scan_step(gate: torch.Tensor, x: torch.Tensor, state: torch.Tensor, ou
         code, n, c, zp, zl, xp, xl, _vec(state, torch.float32, state.numel(), "state"),
         _vec(slots, torch.int32, n, "slots"), state.shape[0], op, ol, _stream(stream)),
         "dgc_gated_scan_step")
+
+
+def gated_scan_check(stream=None) -> None:
+    """Synchronises and raises DgcError if a scan kernel's bounded wait has run out."""
+    _check(_lib.dgc_gated_scan_check(_stream(stream)), "dgc_gated_scan_check")
 
 
 def top_logits(logits: torch.Tensor, idx: torch.Tensor, val: torch.Tensor, stream=None) -> None:

@@ -114,8 +114,22 @@ __device__ __forceinline__ uint32_t round_one(float v) {
 // Rounds once, to nearest even: the results leave 32 bits only here.
 template <class T, int VEC>
 __device__ __forceinline__ uint32_t pack(const float (&v)[VEC]) {
-  if constexpr (VEC == 1) return round_one<T>(v[0]);
-  else return round_one<T>(v[0]) | (round_one<T>(v[1]) << 16);
+  if constexpr (VEC == 1) {
+    return round_one<T>(v[0]);
+  } else if constexpr (std::is_same_v<T, __nv_bfloat16>) {
+    const __nv_bfloat162 p = __floats2bfloat162_rn(v[0], v[1]);
+    return *reinterpret_cast<const uint32_t*>(&p);
+  } else {
+    const __half2 p = __floats2half2_rn(v[0], v[1]);
+    return *reinterpret_cast<const uint32_t*>(&p);
+  }
+}
+
+template <class T>
+__device__ __forceinline__ float to_float(T v) {
+  if constexpr (sizeof(T) == 4) return v;
+  else if constexpr (std::is_same_v<T, __nv_bfloat16>) return __bfloat162float(v);
+  else return __half2float(v);
 }
 
 }  // namespace dgc

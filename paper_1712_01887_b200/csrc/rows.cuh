@@ -24,13 +24,6 @@ struct Row {
 };
 
 template <class T>
-__device__ __forceinline__ float to_float(T v) {
-  if constexpr (sizeof(T) == 4) return v;
-  else if constexpr (std::is_same_v<T, __nv_bfloat16>) return __bfloat162float(v);
-  else return __half2float(v);
-}
-
-template <class T>
 __device__ __forceinline__ void store_one(T* p, float v) {
   const float one[1] = {v};
   store_word<T, 1>(p, pack<T, 1>(one));

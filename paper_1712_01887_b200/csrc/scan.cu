@@ -34,6 +34,7 @@ using namespace dgc;
 namespace {
 
 constexpr int kMaxCluster = 8;
+constexpr unsigned long long kWaitNs = 1000000000ull;   // bound of a wait on a peer: a second
 
 struct ScanArgs {
   const void *z, *x, *dh, *h_in;
@@ -45,16 +46,64 @@ struct ScanArgs {
   int32_t tokens, seqs, seq_len, channels, ctiles, cluster, reverse;
 };
 
+// The channels of a lane's word, with the packed 32-bit arithmetic of sm_100 (two operations an
+// instruction, each rounded as its scalar form).
+template <int VEC> struct Val { float v[VEC]; };
+
+__device__ __forceinline__ unsigned long long bits(const Val<2>& a) {
+  unsigned long long r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a.v[0]), "f"(a.v[1]));
+  return r;
+}
+__device__ __forceinline__ Val<2> val(unsigned long long r) {
+  Val<2> a;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(a.v[0]), "=f"(a.v[1]) : "l"(r));
+  return a;
+}
+template <int VEC>
+__device__ __forceinline__ Val<VEC> fill(float x) {
+  Val<VEC> r;
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) r.v[i] = x;
+  return r;
+}
+__device__ __forceinline__ Val<2> fma_(const Val<2>& a, const Val<2>& b, const Val<2>& c) {
+  unsigned long long r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(bits(a)), "l"(bits(b)), "l"(bits(c)));
+  return val(r);
+}
+__device__ __forceinline__ Val<2> mul_(const Val<2>& a, const Val<2>& b) {
+  unsigned long long r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(bits(a)), "l"(bits(b)));
+  return val(r);
+}
+__device__ __forceinline__ Val<2> add_(const Val<2>& a, const Val<2>& b) {
+  unsigned long long r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(bits(a)), "l"(bits(b)));
+  return val(r);
+}
+__device__ __forceinline__ Val<1> fma_(const Val<1>& a, const Val<1>& b, const Val<1>& c) { return {{fmaf(a.v[0], b.v[0], c.v[0])}}; }
+__device__ __forceinline__ Val<1> mul_(const Val<1>& a, const Val<1>& b) { return {{a.v[0] * b.v[0]}}; }
+__device__ __forceinline__ Val<1> add_(const Val<1>& a, const Val<1>& b) { return {{a.v[0] + b.v[0]}}; }
+// a - b
+template <int VEC>
+__device__ __forceinline__ Val<VEC> sub_(const Val<VEC>& a, const Val<VEC>& b) { return fma_(b, fill<VEC>(-1.0f), a); }
+
 // f = sigma(z) and 1 - f, each to full relative precision (1 - f is not formed by subtraction:
-// for gates near 1 it is the weight of the input).  The exponent is held below 2^126, so that
-// e f cannot become inf * 0; a NaN passes through.
-__device__ __forceinline__ void gate(float z, float& f, float& omf) {
-  float x = z * -1.4426950408889634f, e;
-  asm("min.NaN.f32 %0, %0, 0f42FC0000;" : "+f"(x));   // 126
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(x));
-  const float t = 1.0f + e;
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(f) : "f"(t));
-  omf = e * f;
+// for gates near 1 it is the weight of the input).  The logit is held above -87, so that e f
+// cannot become inf * 0; f is then at most 2e-38 too large.  A NaN passes through.
+template <int VEC>
+__device__ __forceinline__ void gate(Val<VEC> z, Val<VEC>& f, Val<VEC>& omf) {
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) asm("max.NaN.f32 %0, %0, 0fC2AE0000;" : "+f"(z.v[i]));   // -87
+  const Val<VEC> x = mul_(z, fill<VEC>(-1.4426950408889634f));
+  Val<VEC> e;
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.v[i]) : "f"(x.v[i]));
+  const Val<VEC> t = add_(e, fill<VEC>(1.0f));
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(f.v[i]) : "f"(t.v[i]));
+  omf = mul_(e, f);
 }
 
 __device__ __forceinline__ void sequence_range(const ScanArgs& a, int s, int& first, int& len) {
@@ -70,76 +119,116 @@ __device__ __forceinline__ void sequence_range(const ScanArgs& a, int s, int& fi
   }
 }
 
-// Joins the runs of all warps of the cluster in order.  `carry` is the state before the first
-// run on entry and after the last on return; the return value `mine` is the state before this
-// warp's run.  `par` alternates from call to call: a buffer is written again only after
-// everyone has passed the barrier of the call in between, hence has read it.
+// ------------------------------------------------------------------ joining the runs
+// The maps of a block's runs, the states they start from, and the maps of the cluster's blocks.
+// Everything alternates between two buffers from call to call.
 template <int VEC, int NW>
 struct Join {
-  float2 runs[2][NW][32][VEC];
-  float2 blocks[2][kMaxCluster][32][VEC];
+  float runs[2][NW][32][2 * VEC];            // P, then S
+  float starts[2][NW][32][VEC];
+  float blocks[2][kMaxCluster][32][2 * VEC];
+  unsigned long long arrived[2];             // mbarriers of `blocks`
 };
 
+// Waits that run out (they cannot, short of a fault: the blocks of a cluster run together) are
+// counted here and not waited for again; dgc_gated_scan_check reports them.
+__device__ int g_scan_waits_out;
+
+__device__ __forceinline__ uint32_t shared_address(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
 template <int VEC, int NW>
-__device__ __forceinline__ void join_runs(Join<VEC, NW>& sm, int par, int ncl, int rank, int warp,
-                                          int lane, const float (&P)[VEC], const float (&S)[VEC],
-                                          float (&carry)[VEC], float (&mine)[VEC]) {
-#pragma unroll
-  for (int v = 0; v < VEC; ++v) sm.runs[par][warp][lane][v] = make_float2(P[v], S[v]);
-  __syncthreads();
-  if (ncl > 1) {
-    cg::cluster_group cl = cg::this_cluster();
-    if (warp < ncl) {   // warp w hands this block's map to block w of the cluster
-      float2 t[VEC];
-#pragma unroll
-      for (int v = 0; v < VEC; ++v) t[v] = make_float2(1.0f, 0.0f);
-#pragma unroll
-      for (int w = 0; w < NW; ++w) {
-#pragma unroll
-        for (int v = 0; v < VEC; ++v) {
-          const float2 r = sm.runs[par][w][lane][v];
-          t[v] = make_float2(r.x * t[v].x, fmaf(r.x, t[v].y, r.y));
-        }
-      }
-      Join<VEC, NW>* peer = cl.map_shared_rank(&sm, warp);
-#pragma unroll
-      for (int v = 0; v < VEC; ++v) peer->blocks[par][rank][lane][v] = t[v];
-    }
-    cl.sync();
-    float at_block[VEC];
-#pragma unroll
-    for (int v = 0; v < VEC; ++v) at_block[v] = carry[v];
-    for (int r = 0; r < ncl; ++r) {
-#pragma unroll
-      for (int v = 0; v < VEC; ++v) {
-        if (r == rank) at_block[v] = carry[v];
-        const float2 m = sm.blocks[par][r][lane][v];
-        carry[v] = fmaf(m.x, carry[v], m.y);
-      }
-    }
-#pragma unroll
-    for (int v = 0; v < VEC; ++v) mine[v] = at_block[v];
-#pragma unroll
-    for (int w = 0; w < NW; ++w) {
-      if (w < warp) {
-#pragma unroll
-        for (int v = 0; v < VEC; ++v) {
-          const float2 r = sm.runs[par][w][lane][v];
-          mine[v] = fmaf(r.x, mine[v], r.y);
-        }
-      }
-    }
-  } else {
-#pragma unroll
-    for (int w = 0; w < NW; ++w) {
-#pragma unroll
-      for (int v = 0; v < VEC; ++v) {
-        if (w == warp) mine[v] = carry[v];
-        const float2 r = sm.runs[par][w][lane][v];
-        carry[v] = fmaf(r.x, carry[v], r.y);
-      }
-    }
+__device__ __forceinline__ void join_begin(Join<VEC, NW>& sm, int ncl) {
+  if (ncl == 1) return;
+  if (threadIdx.x < 2)
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(shared_address(&sm.arrived[threadIdx.x])) : "memory");
+  asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  cg::this_cluster().sync();   // every block runs, its barriers are there
+}
+
+__device__ __forceinline__ unsigned long long clock_ns() {
+  unsigned long long t;
+  asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
+  return t;
+}
+
+__device__ __forceinline__ bool wait_arrived(uint32_t barrier, uint32_t phase) {
+  unsigned long long since = 0;
+  for (;;) {
+    uint32_t done;
+    asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
+                 : "=r"(done) : "r"(barrier), "r"(phase) : "memory");
+    if (done) return true;
+    if (since == 0) since = clock_ns();
+    else if (clock_ns() - since > kWaitNs) break;
   }
+  atomicAdd(&g_scan_waits_out, 1);
+  return false;
+}
+
+// Joins the runs of all warps of the cluster in order: takes this warp's map (P, S), returns the
+// state its run starts from.  The first warp does the work for the block; it alone holds
+// `carry`, the state before the cluster's first run on entry and after its last on return.
+// A block's map reaches the others by asynchronous stores that complete on their barriers, not
+// through the cluster's barrier: that one would wait for every store of results under way.
+template <int VEC, int NW>
+__device__ __forceinline__ Val<VEC> join_runs(Join<VEC, NW>& sm, int round, int ncl, int rank, int warp, int lane,
+                                              const Val<VEC>& P, const Val<VEC>& S, Val<VEC>& carry, bool& waits) {
+  const int par = round & 1;
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) { sm.runs[par][warp][lane][i] = P.v[i]; sm.runs[par][warp][lane][VEC + i] = S.v[i]; }
+  __syncthreads();
+  if (warp == 0) {
+    Val<VEC> cur = carry;
+    auto load = [&](const float (&m)[2 * VEC], Val<VEC>& p, Val<VEC>& s) {
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) { p.v[i] = m[i]; s.v[i] = m[VEC + i]; }
+    };
+    if (ncl > 1) {
+      Val<VEC> tp = P, ts = S;
+#pragma unroll
+      for (int w = 1; w < NW; ++w) {
+        Val<VEC> p, s;
+        load(sm.runs[par][w][lane], p, s);
+        tp = mul_(p, tp);
+        ts = fma_(p, ts, s);
+      }
+      const uint32_t to = shared_address(&sm.blocks[par][rank][lane][0]), bar = shared_address(&sm.arrived[par]);
+      if (lane == 0)
+        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(ncl * 32 * 2 * VEC * 4) : "memory");
+      for (int r = 0; r < ncl; ++r) {
+        uint32_t far, far_bar;
+        asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(far) : "r"(to), "r"(r));
+        asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(far_bar) : "r"(bar), "r"(r));
+        if constexpr (VEC == 2)
+          asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];"
+                       ::"r"(far), "f"(tp.v[0]), "f"(tp.v[1]), "f"(ts.v[0]), "f"(ts.v[1]), "r"(far_bar) : "memory");
+        else
+          asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];"
+                       ::"r"(far), "f"(tp.v[0]), "f"(ts.v[0]), "r"(far_bar) : "memory");
+      }
+      if (waits) waits = wait_arrived(bar, (uint32_t)(round >> 1) & 1u);
+      for (int r = 0; r < ncl; ++r) {
+        Val<VEC> p, s;
+        if (r == rank) cur = carry;
+        load(sm.blocks[par][r][lane], p, s);
+        carry = fma_(p, carry, s);
+      }
+    }
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      Val<VEC> p = P, s = S;
+      if (w > 0) load(sm.runs[par][w][lane], p, s);
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) sm.starts[par][w][lane][i] = cur.v[i];
+      cur = fma_(p, cur, s);
+    }
+    if (ncl == 1) carry = cur;
+  }
+  __syncthreads();
+  Val<VEC> start;
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) start.v[i] = sm.starts[par][warp][lane][i];
+  return start;
 }
 
 // ------------------------------------------------------------------ rows into shared memory
@@ -167,26 +256,34 @@ __device__ __forceinline__ Rows rows_of(const void* base, int64_t ld, int64_t at
   return r;
 }
 
-// Copies the warp's part of the steps [t0, t0 + n) (steps outside [0, len) are left out) in
-// aligned 16-byte granules; `width` is the part's bytes inside the matrix's columns.  Where
-// rows do not start on a boundary the granules at a part's ends also hold neighbouring
-// elements, which nobody uses; a granule that reaches outside the matrix itself is fetched by
-// elements.
+// Copies the warp's part of the steps from t0 on, those of them inside [0, len); `width` is the
+// part's bytes inside the matrix's columns.  Where rows do not start on a boundary the granules
+// at a part's ends also hold neighbouring elements, which nobody uses; a granule that reaches
+// outside the matrix itself is fetched by elements.
 template <class T, Lie LIE, int L>
 __device__ __forceinline__ void copy_rows(char* to, const Rows& m, int64_t t0, int len, int width, int lane) {
   constexpr int G = kGranules<LIE>;
-  const uint32_t dst = (uint32_t)__cvta_generic_to_shared(to);
+  const int64_t left = len - t0;
+  const int lo = t0 < 0 ? (int)min(-t0, (int64_t)L) : 0, hi = (int)max(min(left, (int64_t)L), (int64_t)0);
+  const char* p0 = m.row + t0 * m.stride;
+  if constexpr (LIE == kAligned) {
+    static_assert(G == 8 && L % 4 == 0, "");
+    const int r0 = lane / 8, g = lane % 8;
+    const uint32_t dst = shared_address(to) + r0 * kPitch<LIE> + g * 16;
+    const char* p = p0 + r0 * m.stride + g * 16;
+    const int64_t jump = 4 * m.stride;
+    const bool on = g * 16 < width;
 #pragma unroll
-  for (int k = 0; k < (L * G + 31) / 32; ++k) {
-    const int i = lane + 32 * k, r = i / G, g = i % G;
-    const int64_t t = t0 + r;
-    if (r < L && t >= 0 && t < len) {
-      const char* p = m.row + t * m.stride;
-      if (LIE == kAligned) {
-        if (g * 16 < width)
-          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + r * kPitch<LIE> + g * 16),
-                       "l"(p + g * 16) : "memory");
-      } else {
+    for (int k = 0; k < L / 4; ++k, p += jump)
+      if (on && r0 + 4 * k >= lo && r0 + 4 * k < hi)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + 4 * k * kPitch<LIE>), "l"(p) : "memory");
+  } else {
+    const uint32_t dst = shared_address(to);
+#pragma unroll
+    for (int k = 0; k < (L * G + 31) / 32; ++k) {
+      const int i = lane + 32 * k, r = i / G, g = i % G;
+      if (r >= lo && r < hi) {
+        const char* p = p0 + r * m.stride;
         const char* q = reinterpret_cast<const char*>(reinterpret_cast<uintptr_t>(p) & ~(uintptr_t)15) + g * 16;
         if (q < p + width) {
           if (q >= m.begin && q + 16 <= m.end) {
@@ -206,8 +303,9 @@ __device__ __forceinline__ void copy_rows(char* to, const Rows& m, int64_t t0, i
 // Word of this lane in row r of a copied part; `first` is the low half of the address of the
 // part's first row, `stride` the low half of the stride.
 template <class T, Lie LIE>
-__device__ __forceinline__ void row_word(const char* from, uint32_t first, uint32_t stride, int r, int lane,
-                                         float (&v)[4 / sizeof(T)]) {
+__device__ __forceinline__ Val<4 / sizeof(T)> row_word(const char* from, uint32_t first, uint32_t stride, int r,
+                                                       int lane) {
+  Val<4 / sizeof(T)> w;
   const char* p = from + r * kPitch<LIE> + lane * 4;
   if (LIE != kAligned) p += (first + r * stride) & 15u;
   if constexpr (LIE == kHalves) {
@@ -216,21 +314,22 @@ __device__ __forceinline__ void row_word(const char* from, uint32_t first, uint3
     for (int i = 0; i < 2; ++i) {
       float one[1];
       unpack<T, 1>(*reinterpret_cast<const unsigned short*>(p + 2 * i), one);
-      v[i] = one[0];
+      w.v[i] = one[0];
     }
   } else {
-    unpack<T, 4 / sizeof(T)>(*reinterpret_cast<const uint32_t*>(p), v);
+    unpack<T, 4 / sizeof(T)>(*reinterpret_cast<const uint32_t*>(p), w.v);
   }
+  return w;
 }
 
 template <class T, Lie LIE>
-__device__ __forceinline__ void put_word(char* p, const float (&v)[4 / sizeof(T)], bool on0, bool on1) {
+__device__ __forceinline__ void put_word(char* p, const Val<4 / sizeof(T)>& w, bool on0, bool on1) {
   if constexpr (LIE == kHalves) {
-    const float a[1] = {v[0]}, b[1] = {v[1]};
+    const float a[1] = {w.v[0]}, b[1] = {w.v[1]};
     if (on0) store_word<T, 1>(reinterpret_cast<T*>(p), pack<T, 1>(a));
     if (on1) store_word<T, 1>(reinterpret_cast<T*>(p) + 1, pack<T, 1>(b));
   } else {
-    if (on0) store_word<T, 4 / sizeof(T)>(reinterpret_cast<T*>(p), pack<T, 4 / sizeof(T)>(v));
+    if (on0) store_word<T, 4 / sizeof(T)>(reinterpret_cast<T*>(p), pack<T, 4 / sizeof(T)>(w.v));
   }
 }
 
@@ -266,14 +365,16 @@ struct Place {
     mine0 = (rank * NW + warp) * L;
     step = ncl * NW * L;
   }
-  __device__ __forceinline__ void get(const float* p, int channels, float (&v)[VEC]) const {
+  __device__ __forceinline__ Val<VEC> get(const float* p, int channels) const {
+    Val<VEC> w;
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) v[i] = p && (i ? on1 : on0) ? p[(int64_t)s * channels + c + i] : 0.0f;
+    for (int i = 0; i < VEC; ++i) w.v[i] = p && (i ? on1 : on0) ? p[(int64_t)s * channels + c + i] : 0.0f;
+    return w;
   }
-  __device__ __forceinline__ void put(float* p, int channels, const float (&v)[VEC]) const {
+  __device__ __forceinline__ void put(float* p, int channels, const Val<VEC>& w) const {
 #pragma unroll
     for (int i = 0; i < VEC; ++i)
-      if (i ? on1 : on0) p[(int64_t)s * channels + c + i] = v[i];
+      if (i ? on1 : on0) p[(int64_t)s * channels + c + i] = w.v[i];
   }
 };
 
@@ -296,41 +397,33 @@ __global__ void __launch_bounds__(NW * 32, 2) k_scan_forward(const ScanArgs a) {
   };
 #pragma unroll
   for (int i = 0; i < kStages; ++i) fetch((int64_t)at.step * i + at.mine0, i);
-  float carry[VEC];
-  at.get(a.h0, a.channels, carry);
+  Val<VEC> carry = at.get(a.h0, a.channels);
   if (len == 0) {   // (the same for all blocks of the cluster)
     if (a.h_last && at.rank == 0 && at.warp == 0) at.put(a.h_last, a.channels, carry);
     return;
   }
-  if (at.ncl > 1) cg::this_cluster().sync();   // every block runs before anyone writes to its memory
+  join_begin(sm, at.ncl);
 
   const int64_t out_stride = at.dir * a.ld_h * (int64_t)sizeof(T);
-  int par = 0, stage = 0;
-  for (int64_t base = 0; base < len; base += at.step, par ^= 1) {
+  bool waits = true;
+  int round = 0, stage = 0;
+  for (int64_t base = 0; base < len; base += at.step, ++round) {
     const int64_t t0 = base + at.mine0;
     const bool full = t0 + L <= len;
     const char* from = mine + stage * 2 * kPart;
     const uint32_t z0 = (uint32_t)reinterpret_cast<uintptr_t>(z.row) + (uint32_t)t0 * (uint32_t)z.stride;
     const uint32_t x0 = (uint32_t)reinterpret_cast<uintptr_t>(x.row) + (uint32_t)t0 * (uint32_t)x.stride;
-    float f[L][VEC], b[L][VEC], P[VEC], S[VEC];
+    Val<VEC> f[L], b[L], P = fill<VEC>(1.0f), S = fill<VEC>(0.0f);
     wait_copies<kStages - 1>();
-#pragma unroll
-    for (int v = 0; v < VEC; ++v) { P[v] = 1.0f; S[v] = 0.0f; }
     auto walk = [&](auto whole) {
 #pragma unroll
       for (int i = 0; i < L; ++i) {
-        float zz[VEC], xx[VEC];
-        row_word<T, LIE>(from, z0, (uint32_t)z.stride, i, at.lane, zz);
-        row_word<T, LIE>(from + kPart, x0, (uint32_t)x.stride, i, at.lane, xx);
-#pragma unroll
-        for (int v = 0; v < VEC; ++v) {
-          float omf;
-          gate(zz[v], f[i][v], omf);
-          b[i][v] = omf * xx[v];
-          if (!decltype(whole)::value && t0 + i >= len) { f[i][v] = 1.0f; b[i][v] = 0.0f; }
-          P[v] *= f[i][v];
-          S[v] = fmaf(f[i][v], S[v], b[i][v]);
-        }
+        Val<VEC> omf;
+        gate(row_word<T, LIE>(from, z0, (uint32_t)z.stride, i, at.lane), f[i], omf);
+        b[i] = mul_(omf, row_word<T, LIE>(from + kPart, x0, (uint32_t)x.stride, i, at.lane));
+        if (!decltype(whole)::value && t0 + i >= len) { f[i] = fill<VEC>(1.0f); b[i] = fill<VEC>(0.0f); }
+        P = mul_(P, f[i]);
+        S = fma_(f[i], S, b[i]);
       }
     };
     if (full) walk(std::true_type{});
@@ -338,15 +431,17 @@ __global__ void __launch_bounds__(NW * 32, 2) k_scan_forward(const ScanArgs a) {
     __syncwarp();   // the stage has been read by all lanes
     fetch(t0 + (int64_t)kStages * at.step, stage);
     stage = stage + 1 == kStages ? 0 : stage + 1;
-    float cur[VEC];
-    join_runs<VEC, NW>(sm, par, at.ncl, at.rank, at.warp, at.lane, P, S, carry, cur);
+    Val<VEC> cur = join_runs<VEC, NW>(sm, round, at.ncl, at.rank, at.warp, at.lane, P, S, carry, waits);
     char* out = static_cast<char*>(a.h) + ((at.at0 + at.dir * t0) * a.ld_h + at.c) * (int64_t)sizeof(T);
+    auto write = [&](auto whole) {
 #pragma unroll
-    for (int i = 0; i < L; ++i, out += out_stride) {
-#pragma unroll
-      for (int v = 0; v < VEC; ++v) cur[v] = fmaf(f[i][v], cur[v], b[i][v]);
-      if (full || t0 + i < len) put_word<T, LIE>(out, cur, at.on0, at.on1);
-    }
+      for (int i = 0; i < L; ++i, out += out_stride) {
+        cur = fma_(f[i], cur, b[i]);
+        if (decltype(whole)::value || t0 + i < len) put_word<T, LIE>(out, cur, at.on0, at.on1);
+      }
+    };
+    if (full) write(std::true_type{});
+    else write(std::false_type{});
     // (steps after the last have f = 1, b = 0: they pass the state on unchanged)
     if (a.h_last && t0 < len && t0 + L >= len) at.put(a.h_last, a.channels, cur);
   }
@@ -379,38 +474,30 @@ __global__ void __launch_bounds__(NW * 32, 2) k_scan_backward(const ScanArgs a) 
   };
 #pragma unroll
   for (int i = 0; i < kStages; ++i) fetch((int64_t)at.step * i + at.mine0, i);
-  float carry[VEC], start[VEC];
-  at.get(a.dh_last, a.channels, carry);
-  at.get(a.h0, a.channels, start);
+  Val<VEC> carry = at.get(a.dh_last, a.channels);
+  const Val<VEC> start = at.get(a.h0, a.channels);
   if (len == 0) {
     if (a.dh0 && at.rank == 0 && at.warp == 0) at.put(a.dh0, a.channels, carry);
     return;
   }
-  if (at.ncl > 1) cg::this_cluster().sync();
+  join_begin(sm, at.ncl);
 
   // the state before a run, stored by the forward pass
-  auto state_before = [&](int64_t u0, float (&v)[VEC]) {
+  auto state_before = [&](int64_t u0) {
     const int64_t t = len - 1 - (u0 + L);
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) v[i] = start[i];
+    Val<VEC> w = start;
     if (t >= 0) {
       const T* p = static_cast<const T*>(a.h_in) + (at.at0 + at.dir * t) * a.ld_h + at.c;
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) {
-        float one[1] = {0.0f};
-        if (i ? at.on1 : at.on0) {
-          if constexpr (sizeof(T) == 4) one[0] = __ldg(p + i);
-          else unpack<T, 1>(load_word<T, 1>(p + i), one);
-        }
-        v[i] = one[0];
-      }
+      for (int i = 0; i < VEC; ++i) w.v[i] = (i ? at.on1 : at.on0) ? to_float<T>(p[i]) : 0.0f;
     }
+    return w;
   };
-  float before[VEC];
-  state_before(at.mine0, before);
+  Val<VEC> before = state_before(at.mine0);
   const int64_t zs = at.dir * a.ld_dz * (int64_t)sizeof(T), xs = at.dir * a.ld_dx * (int64_t)sizeof(T);
-  int par = 0, stage = 0;
-  for (int64_t base = 0; base < len; base += at.step, par ^= 1) {
+  bool waits = true;
+  int round = 0, stage = 0;
+  for (int64_t base = 0; base < len; base += at.step, ++round) {
     const int64_t u0 = base + at.mine0;
     const int64_t t_hi = len - 1 - u0, t_lo = t_hi - (L - 1);   // negative: nothing of this sequence is left there
     const bool full = t_lo >= 0;
@@ -418,63 +505,45 @@ __global__ void __launch_bounds__(NW * 32, 2) k_scan_backward(const ScanArgs a) 
     const uint32_t z0 = (uint32_t)reinterpret_cast<uintptr_t>(z.row) + (uint32_t)t_lo * (uint32_t)z.stride;
     const uint32_t x0 = (uint32_t)reinterpret_cast<uintptr_t>(x.row) + (uint32_t)t_lo * (uint32_t)x.stride;
     const uint32_t d0 = (uint32_t)reinterpret_cast<uintptr_t>(d.row) + (uint32_t)t_lo * (uint32_t)d.stride;
-    float f[L][VEC], w[L][VEC], e[L][VEC], P[VEC], S[VEC];   // f, 1 - f, h_{t-1} - x_t
+    Val<VEC> f[L], w[L], e[L], P = fill<VEC>(1.0f), S = fill<VEC>(0.0f);   // f, 1 - f, h_{t-1} - x_t
     wait_copies<kStages - 1>();
     auto walk = [&](auto whole) {
-      float hp[VEC];
-#pragma unroll
-      for (int v = 0; v < VEC; ++v) hp[v] = before[v];
+      Val<VEC> hp = before;
 #pragma unroll
       for (int j = 0; j < L; ++j) {
-        float zz[VEC], xx[VEC];
-        row_word<T, LIE>(from, z0, (uint32_t)z.stride, j, at.lane, zz);
-        row_word<T, LIE>(from + kPart, x0, (uint32_t)x.stride, j, at.lane, xx);
-        const bool live = decltype(whole)::value || t_lo + j >= 0;
-#pragma unroll
-        for (int v = 0; v < VEC; ++v) {
-          gate(zz[v], f[j][v], w[j][v]);
-          e[j][v] = hp[v] - xx[v];
-          if (live) hp[v] = fmaf(f[j][v], hp[v], w[j][v] * xx[v]);
-          else f[j][v] = 1.0f;
-        }
+        gate(row_word<T, LIE>(from, z0, (uint32_t)z.stride, j, at.lane), f[j], w[j]);
+        const Val<VEC> x_t = row_word<T, LIE>(from + kPart, x0, (uint32_t)x.stride, j, at.lane);
+        e[j] = sub_(hp, x_t);
+        if (decltype(whole)::value || t_lo + j >= 0) hp = fma_(f[j], hp, mul_(w[j], x_t));
+        else f[j] = fill<VEC>(1.0f);
       }
 #pragma unroll
-      for (int v = 0; v < VEC; ++v) { P[v] = 1.0f; S[v] = 0.0f; }
-#pragma unroll
       for (int j = L - 1; j >= 0; --j) {
-        float g[VEC];
-        row_word<T, LIE>(from + 2 * kPart, d0, (uint32_t)d.stride, j, at.lane, g);
-#pragma unroll
-        for (int v = 0; v < VEC; ++v) {
-          if (!decltype(whole)::value && t_lo + j < 0) g[v] = 0.0f;
-          P[v] *= f[j][v];
-          S[v] = f[j][v] * (g[v] + S[v]);
-        }
+        Val<VEC> g = row_word<T, LIE>(from + 2 * kPart, d0, (uint32_t)d.stride, j, at.lane);
+        if (!decltype(whole)::value && t_lo + j < 0) g = fill<VEC>(0.0f);
+        P = mul_(P, f[j]);
+        S = mul_(f[j], add_(g, S));
       }
     };
     if (full) walk(std::true_type{});
     else walk(std::false_type{});
-    state_before(u0 + at.step, before);
-    float cur[VEC];
-    join_runs<VEC, NW>(sm, par, at.ncl, at.rank, at.warp, at.lane, P, S, carry, cur);
+    before = state_before(u0 + at.step);
+    Val<VEC> cur = join_runs<VEC, NW>(sm, round, at.ncl, at.rank, at.warp, at.lane, P, S, carry, waits);
     char* gz = static_cast<char*>(a.dz) + ((at.at0 + at.dir * t_hi) * a.ld_dz + at.c) * (int64_t)sizeof(T);
     char* gx = static_cast<char*>(a.dx) + ((at.at0 + at.dir * t_hi) * a.ld_dx + at.c) * (int64_t)sizeof(T);
+    auto write = [&](auto whole) {
 #pragma unroll
-    for (int j = L - 1; j >= 0; --j, gz -= zs, gx -= xs) {
-      if (full || t_lo + j >= 0) {
-        float g[VEC], oz[VEC], ox[VEC];
-        row_word<T, LIE>(from + 2 * kPart, d0, (uint32_t)d.stride, j, at.lane, g);
-#pragma unroll
-        for (int v = 0; v < VEC; ++v) {
-          const float gt = g[v] + cur[v];
-          cur[v] = f[j][v] * gt;
-          ox[v] = w[j][v] * gt;
-          oz[v] = w[j][v] * cur[v] * e[j][v];
+      for (int j = L - 1; j >= 0; --j, gz -= zs, gx -= xs) {
+        if (decltype(whole)::value || t_lo + j >= 0) {
+          const Val<VEC> gt = add_(row_word<T, LIE>(from + 2 * kPart, d0, (uint32_t)d.stride, j, at.lane), cur);
+          cur = mul_(f[j], gt);
+          put_word<T, LIE>(gx, mul_(w[j], gt), at.on0, at.on1);
+          put_word<T, LIE>(gz, mul_(mul_(w[j], cur), e[j]), at.on0, at.on1);
         }
-        put_word<T, LIE>(gz, oz, at.on0, at.on1);
-        put_word<T, LIE>(gx, ox, at.on0, at.on1);
       }
-    }
+    };
+    if (full) write(std::true_type{});
+    else write(std::false_type{});
     if (a.dh0 && t_hi >= 0 && t_lo <= 0) at.put(a.dh0, a.channels, cur);
     __syncwarp();   // the stage has been read by all lanes
     fetch(u0 + (int64_t)kStages * at.step, stage);
@@ -495,16 +564,16 @@ k_scan_step(const T* z, int64_t ld_z, const T* x, int64_t ld_x, float* state, co
        i += (int64_t)gridDim.x * blockDim.x) {
     const int r = (int)(i / words), c = (int)(i % words) * VEC;
     const int slot = slots ? __ldg(slots + r) : r;
-    float zz[VEC], xx[VEC], y[VEC];
-    unpack<T, VEC>(load_word<T, VEC>(z + r * ld_z + c), zz);
-    unpack<T, VEC>(load_word<T, VEC>(x + r * ld_x + c), xx);
+    Val<VEC> zz, xx, f, omf;
+    float y[VEC];
+    unpack<T, VEC>(load_word<T, VEC>(z + r * ld_z + c), zz.v);
+    unpack<T, VEC>(load_word<T, VEC>(x + r * ld_x + c), xx.v);
+    gate(zz, f, omf);
     const bool live = slot >= 0 && slot < num_slots;
     float* st = state + (int64_t)(live ? slot : 0) * channels + c;
 #pragma unroll
     for (int v = 0; v < VEC; ++v) {
-      float f, omf;
-      gate(zz[v], f, omf);
-      y[v] = live ? fmaf(f, st[v], omf * xx[v]) : 0.0f;
+      y[v] = live ? fmaf(f.v[v], st[v], omf.v[v] * xx.v[v]) : 0.0f;
       if (live) st[v] = y[v];
     }
     store_word<T, VEC>(out + r * ld_out + c, pack<T, VEC>(y));
@@ -654,6 +723,16 @@ int32_t dgc_gated_scan_step(int32_t dtype, int32_t rows, int32_t channels, const
   else if (dtype == DGC_BF16) pairs ? go(__nv_bfloat16{}, two{}) : go(__nv_bfloat16{}, one{});
   else pairs ? go(__half{}, two{}) : go(__half{}, one{});
   return check_launch();
+}
+
+int32_t dgc_gated_scan_check(void* stream) {
+  DGC_CUDA(cudaStreamSynchronize(as_stream(stream)));
+  int count = 0;
+  DGC_CUDA(cudaMemcpyFromSymbol(&count, g_scan_waits_out, sizeof count));
+  if (count == 0) return DGC_OK;
+  const int none = 0;
+  DGC_CUDA(cudaMemcpyToSymbol(g_scan_waits_out, &none, sizeof none));
+  return DGC_ECUDA;
 }
 
 }  // extern "C"
