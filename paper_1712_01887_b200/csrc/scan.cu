@@ -24,6 +24,7 @@
 #include <cooperative_groups.h>
 
 #include <algorithm>
+#include <cstdlib>
 #include <initializer_list>
 
 #include "common.cuh"
@@ -36,19 +37,27 @@ namespace {
 constexpr int kMaxCluster = 8;
 constexpr unsigned long long kWaitNs = 1000000000ull;   // bound of a wait on a peer: a second
 
+// A matrix argument.  The strides that the loops add are laid out by the host: as kernel
+// parameters they cost no registers.
+struct Matrix {
+  char *begin, *end;
+  int64_t ld;        // elements
+  int64_t stride;    // bytes from one step of the walk to the next (negative: towards the front)
+  int64_t jump;      // stride * steps of a round
+  int64_t skip;      // stride * (steps of a round - steps of a run)
+};
+
 struct ScanArgs {
-  const void *z, *x, *dh, *h_in;
-  void *h, *dz, *dx;
+  Matrix z, x, h, dh, dz, dx;
   const float *h0, *dh_last;
   float *h_last, *dh0;
   const int32_t* seq_start;
-  int64_t ld_z, ld_x, ld_h, ld_dh, ld_dz, ld_dx;
   int32_t tokens, seqs, seq_len, channels, ctiles, cluster, reverse;
 };
 
 // The channels of a lane's word, with the packed 32-bit arithmetic of sm_100 (two operations an
 // instruction, each rounded as its scalar form).
-template <int VEC> struct Val { float v[VEC]; };
+template <int VEC> struct alignas(4 * VEC) Val { float v[VEC]; };
 
 __device__ __forceinline__ unsigned long long bits(const Val<2>& a) {
   unsigned long long r;
@@ -120,13 +129,16 @@ __device__ __forceinline__ void sequence_range(const ScanArgs& a, int s, int& fi
 }
 
 // ------------------------------------------------------------------ joining the runs
+// A map y_out = P y_in + S of a lane's channels, as it lies in shared memory.
+template <int VEC> struct alignas(8 * VEC) Map { Val<VEC> p, s; };
+
 // The maps of a block's runs, the states they start from, and the maps of the cluster's blocks.
-// Everything alternates between two buffers from call to call.
+// Everything alternates between two buffers from round to round.
 template <int VEC, int NW>
 struct Join {
-  float runs[2][NW][32][2 * VEC];            // P, then S
-  float starts[2][NW][32][VEC];
-  float blocks[2][kMaxCluster][32][2 * VEC];
+  Map<VEC> runs[2][NW][32];
+  Map<VEC> blocks[2][kMaxCluster][32];
+  Val<VEC> starts[2][NW][32];
   unsigned long long arrived[2];             // mbarriers of `blocks`
 };
 
@@ -174,61 +186,66 @@ template <int VEC, int NW>
 __device__ __forceinline__ Val<VEC> join_runs(Join<VEC, NW>& sm, int round, int ncl, int rank, int warp, int lane,
                                               const Val<VEC>& P, const Val<VEC>& S, Val<VEC>& carry, bool& waits) {
   const int par = round & 1;
-#pragma unroll
-  for (int i = 0; i < VEC; ++i) { sm.runs[par][warp][lane][i] = P.v[i]; sm.runs[par][warp][lane][VEC + i] = S.v[i]; }
+  sm.runs[par][warp][lane] = {P, S};
   __syncthreads();
   if (warp == 0) {
     Val<VEC> cur = carry;
-    auto load = [&](const float (&m)[2 * VEC], Val<VEC>& p, Val<VEC>& s) {
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) { p.v[i] = m[i]; s.v[i] = m[VEC + i]; }
-    };
     if (ncl > 1) {
       Val<VEC> tp = P, ts = S;
 #pragma unroll
       for (int w = 1; w < NW; ++w) {
-        Val<VEC> p, s;
-        load(sm.runs[par][w][lane], p, s);
-        tp = mul_(p, tp);
-        ts = fma_(p, ts, s);
+        const Map<VEC> m = sm.runs[par][w][lane];
+        tp = mul_(m.p, tp);
+        ts = fma_(m.p, ts, m.s);
       }
-      const uint32_t to = shared_address(&sm.blocks[par][rank][lane][0]), bar = shared_address(&sm.arrived[par]);
+      const uint32_t to = shared_address(&sm.blocks[par][rank][lane]), bar = shared_address(&sm.arrived[par]);
       if (lane == 0)
         asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(ncl * 32 * 2 * VEC * 4) : "memory");
-      for (int r = 0; r < ncl; ++r) {
-        uint32_t far, far_bar;
-        asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(far) : "r"(to), "r"(r));
-        asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(far_bar) : "r"(bar), "r"(r));
-        if constexpr (VEC == 2)
-          asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];"
-                       ::"r"(far), "f"(tp.v[0]), "f"(tp.v[1]), "f"(ts.v[0]), "f"(ts.v[1]), "r"(far_bar) : "memory");
-        else
-          asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];"
-                       ::"r"(far), "f"(tp.v[0]), "f"(ts.v[0]), "r"(far_bar) : "memory");
+#pragma unroll
+      for (int r = 0; r < kMaxCluster; ++r) {
+        if (r < ncl) {
+          uint32_t far, far_bar;
+          asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(far) : "r"(to), "r"(r));
+          asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(far_bar) : "r"(bar), "r"(r));
+          if constexpr (VEC == 2)
+            asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];"
+                         ::"r"(far), "f"(tp.v[0]), "f"(tp.v[1]), "f"(ts.v[0]), "f"(ts.v[1]), "r"(far_bar) : "memory");
+          else
+            asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];"
+                         ::"r"(far), "f"(tp.v[0]), "f"(ts.v[0]), "r"(far_bar) : "memory");
+        }
       }
       if (waits) waits = wait_arrived(bar, (uint32_t)(round >> 1) & 1u);
-      for (int r = 0; r < ncl; ++r) {
-        Val<VEC> p, s;
-        if (r == rank) cur = carry;
-        load(sm.blocks[par][r][lane], p, s);
-        carry = fma_(p, carry, s);
+#pragma unroll
+      for (int r0 = 0; r0 < kMaxCluster; r0 += 4) {   // (four loads under way at a time)
+        if (r0 < ncl) {
+          Map<VEC> m[4];
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (r0 + r < ncl) m[r] = sm.blocks[par][r0 + r][lane];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            if (r0 + r == rank) cur = carry;
+            if (r0 + r < ncl) carry = fma_(m[r].p, carry, m[r].s);
+          }
+        }
       }
     }
 #pragma unroll
-    for (int w = 0; w < NW; ++w) {
-      Val<VEC> p = P, s = S;
-      if (w > 0) load(sm.runs[par][w][lane], p, s);
+    for (int w0 = 0; w0 < NW; w0 += 4) {
+      Map<VEC> m[4];
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) sm.starts[par][w][lane][i] = cur.v[i];
-      cur = fma_(p, cur, s);
+      for (int w = 0; w < 4; ++w) m[w] = sm.runs[par][w0 + w][lane];
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        sm.starts[par][w0 + w][lane] = cur;
+        cur = fma_(m[w].p, cur, m[w].s);
+      }
     }
     if (ncl == 1) carry = cur;
   }
   __syncthreads();
-  Val<VEC> start;
-#pragma unroll
-  for (int i = 0; i < VEC; ++i) start.v[i] = sm.starts[par][warp][lane][i];
-  return start;
+  return sm.starts[par][warp][lane];
 }
 
 // ------------------------------------------------------------------ rows into shared memory
@@ -239,43 +256,30 @@ constexpr int kRowBytes = 128;            // a warp's part of a row: 32 words
 template <Lie LIE> constexpr int kGranules = LIE == kAligned ? kRowBytes / 16 : kRowBytes / 16 + 1;
 template <Lie LIE> constexpr int kPitch = kGranules<LIE> * 16;
 
-struct Rows {              // a matrix as the copies see it, at this thread's channels' block
-  const char* row;         // the scan's first row, the tile's first channel
-  int64_t stride;          // bytes from one step to the next (negative: from the end)
-  const char *begin, *end; // the matrix
-};
-
+// Where a matrix's row `row` has this block's channels.
 template <class T>
-__device__ __forceinline__ Rows rows_of(const void* base, int64_t ld, int64_t at0, int64_t dir, int c0,
-                                        const ScanArgs& a) {
-  Rows r;
-  r.begin = static_cast<const char*>(base);
-  r.end = r.begin + ((int64_t)(a.tokens - 1) * ld + a.channels) * sizeof(T);
-  r.row = r.begin + (at0 * ld + c0) * (int64_t)sizeof(T);
-  r.stride = dir * ld * (int64_t)sizeof(T);
-  return r;
+__device__ __forceinline__ char* row_at(const Matrix& m, int64_t row, int c) {
+  return m.begin + (row * m.ld + c) * (int64_t)sizeof(T);
 }
 
-// Copies the warp's part of the steps from t0 on, those of them inside [0, len); `width` is the
-// part's bytes inside the matrix's columns.  Where rows do not start on a boundary the granules
-// at a part's ends also hold neighbouring elements, which nobody uses; a granule that reaches
+// Copies the warp's part of the rows [lo, hi) of a round's L, from `next` on, and moves `next` on
+// by a round; `width` is the part's bytes inside the matrix's columns.  (Where rows are aligned
+// `next` is this lane's granule.)  Where rows do not start on a boundary the granules at a
+// part's ends also hold neighbouring elements, which nobody uses; a granule that reaches
 // outside the matrix itself is fetched by elements.
 template <class T, Lie LIE, int L>
-__device__ __forceinline__ void copy_rows(char* to, const Rows& m, int64_t t0, int len, int width, int lane) {
+__device__ __forceinline__ void copy_rows(char* to, const char*& next, const Matrix& m, int64_t stride, int64_t jump,
+                                          int lo, int hi, int width, int lane) {
   constexpr int G = kGranules<LIE>;
-  const int64_t left = len - t0;
-  const int lo = t0 < 0 ? (int)min(-t0, (int64_t)L) : 0, hi = (int)max(min(left, (int64_t)L), (int64_t)0);
-  const char* p0 = m.row + t0 * m.stride;
   if constexpr (LIE == kAligned) {
     static_assert(G == 8 && L % 4 == 0, "");
     const int r0 = lane / 8, g = lane % 8;
     const uint32_t dst = shared_address(to) + r0 * kPitch<LIE> + g * 16;
-    const char* p = p0 + r0 * m.stride + g * 16;
-    const int64_t jump = 4 * m.stride;
-    const bool on = g * 16 < width;
+    const char* p = next;
+    if (g * 16 >= width) hi = 0;
 #pragma unroll
-    for (int k = 0; k < L / 4; ++k, p += jump)
-      if (on && r0 + 4 * k >= lo && r0 + 4 * k < hi)
+    for (int k = 0; k < L / 4; ++k, p += 4 * stride)
+      if (r0 + 4 * k >= lo && r0 + 4 * k < hi)
         asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + 4 * k * kPitch<LIE>), "l"(p) : "memory");
   } else {
     const uint32_t dst = shared_address(to);
@@ -283,7 +287,7 @@ __device__ __forceinline__ void copy_rows(char* to, const Rows& m, int64_t t0, i
     for (int k = 0; k < (L * G + 31) / 32; ++k) {
       const int i = lane + 32 * k, r = i / G, g = i % G;
       if (r >= lo && r < hi) {
-        const char* p = p0 + r * m.stride;
+        const char* p = next + r * stride;
         const char* q = reinterpret_cast<const char*>(reinterpret_cast<uintptr_t>(p) & ~(uintptr_t)15) + g * 16;
         if (q < p + width) {
           if (q >= m.begin && q + 16 <= m.end) {
@@ -298,6 +302,14 @@ __device__ __forceinline__ void copy_rows(char* to, const Rows& m, int64_t t0, i
       }
     }
   }
+  next += jump;
+}
+
+// Where a lane's copies of a round start.
+template <class T, Lie LIE>
+__device__ __forceinline__ const char* first_copy(const Matrix& m, int64_t row, int c0, int64_t stride, int lane) {
+  const char* p = row_at<T>(m, row, c0);
+  return LIE == kAligned ? p + (lane / 8) * stride + lane % 8 * 16 : p;
 }
 
 // Word of this lane in row r of a copied part; `first` is the low half of the address of the
@@ -380,23 +392,29 @@ struct Place {
 
 constexpr int kStages = 2;
 
-template <class T, Lie LIE, int L, int NW>
-__global__ void __launch_bounds__(NW * 32, 2) k_scan_forward(const ScanArgs a) {
+template <class T, Lie LIE, int L, int NW, int BLOCKS>
+__global__ void __launch_bounds__(NW * 32, BLOCKS) k_scan_forward(const ScanArgs a) {
   pdl_enter();
   constexpr int VEC = 4 / sizeof(T), kPart = L * kPitch<LIE>;
   extern __shared__ __align__(16) char buffer[];   // [warp][stage][z, x][L rows]
   __shared__ Join<VEC, NW> sm;
   const Place<T, L, NW> at(a);
   const int len = at.len;
-  const Rows z = rows_of<T>(a.z, a.ld_z, at.at0, at.dir, at.c0, a), x = rows_of<T>(a.x, a.ld_x, at.at0, at.dir, at.c0, a);
+  const int64_t row0 = at.at0 + at.dir * at.mine0;
+  const char* z = first_copy<T, LIE>(a.z, row0, at.c0, a.z.stride, at.lane);
+  const char* x = first_copy<T, LIE>(a.x, row0, at.c0, a.x.stride, at.lane);
+  // (low halves of addresses: where in their granules the rows of the round in hand start)
+  uint32_t z0 = (uint32_t)reinterpret_cast<uintptr_t>(z), x0 = (uint32_t)reinterpret_cast<uintptr_t>(x);
   char* const mine = buffer + at.warp * (kStages * 2 * kPart);
-  auto fetch = [&](int64_t t0, int stage) {
-    copy_rows<T, LIE, L>(mine + stage * 2 * kPart, z, t0, len, at.width, at.lane);
-    copy_rows<T, LIE, L>(mine + stage * 2 * kPart + kPart, x, t0, len, at.width, at.lane);
+  int ahead = len - at.mine0;   // steps from the next fetch's first on (may be negative)
+  auto fetch = [&](int stage) {
+    copy_rows<T, LIE, L>(mine + stage * 2 * kPart, z, a.z, a.z.stride, a.z.jump, 0, min(ahead, L), at.width, at.lane);
+    copy_rows<T, LIE, L>(mine + stage * 2 * kPart + kPart, x, a.x, a.x.stride, a.x.jump, 0, min(ahead, L), at.width, at.lane);
     end_copies();
+    ahead = max(ahead - at.step, 0);
   };
 #pragma unroll
-  for (int i = 0; i < kStages; ++i) fetch((int64_t)at.step * i + at.mine0, i);
+  for (int i = 0; i < kStages; ++i) fetch(i);
   Val<VEC> carry = at.get(a.h0, a.channels);
   if (len == 0) {   // (the same for all blocks of the cluster)
     if (a.h_last && at.rank == 0 && at.warp == 0) at.put(a.h_last, a.channels, carry);
@@ -404,24 +422,23 @@ __global__ void __launch_bounds__(NW * 32, 2) k_scan_forward(const ScanArgs a) {
   }
   join_begin(sm, at.ncl);
 
-  const int64_t out_stride = at.dir * a.ld_h * (int64_t)sizeof(T);
+  char* out = row_at<T>(a.h, row0, at.c);
   bool waits = true;
-  int round = 0, stage = 0;
-  for (int64_t base = 0; base < len; base += at.step, ++round) {
-    const int64_t t0 = base + at.mine0;
-    const bool full = t0 + L <= len;
+  int stage = 0;
+  const int rounds = (len - 1) / at.step + 1;
+  int left = len - at.mine0;   // steps from this warp's first of the round on
+  for (int round = 0; round < rounds; ++round, left -= at.step) {
+    const bool full = left >= L;
     const char* from = mine + stage * 2 * kPart;
-    const uint32_t z0 = (uint32_t)reinterpret_cast<uintptr_t>(z.row) + (uint32_t)t0 * (uint32_t)z.stride;
-    const uint32_t x0 = (uint32_t)reinterpret_cast<uintptr_t>(x.row) + (uint32_t)t0 * (uint32_t)x.stride;
     Val<VEC> f[L], b[L], P = fill<VEC>(1.0f), S = fill<VEC>(0.0f);
     wait_copies<kStages - 1>();
     auto walk = [&](auto whole) {
 #pragma unroll
       for (int i = 0; i < L; ++i) {
         Val<VEC> omf;
-        gate(row_word<T, LIE>(from, z0, (uint32_t)z.stride, i, at.lane), f[i], omf);
-        b[i] = mul_(omf, row_word<T, LIE>(from + kPart, x0, (uint32_t)x.stride, i, at.lane));
-        if (!decltype(whole)::value && t0 + i >= len) { f[i] = fill<VEC>(1.0f); b[i] = fill<VEC>(0.0f); }
+        gate(row_word<T, LIE>(from, z0, (uint32_t)a.z.stride, i, at.lane), f[i], omf);
+        b[i] = mul_(omf, row_word<T, LIE>(from + kPart, x0, (uint32_t)a.x.stride, i, at.lane));
+        if (!decltype(whole)::value && i >= left) { f[i] = fill<VEC>(1.0f); b[i] = fill<VEC>(0.0f); }
         P = mul_(P, f[i]);
         S = fma_(f[i], S, b[i]);
       }
@@ -429,21 +446,23 @@ __global__ void __launch_bounds__(NW * 32, 2) k_scan_forward(const ScanArgs a) {
     if (full) walk(std::true_type{});
     else walk(std::false_type{});
     __syncwarp();   // the stage has been read by all lanes
-    fetch(t0 + (int64_t)kStages * at.step, stage);
-    stage = stage + 1 == kStages ? 0 : stage + 1;
+    fetch(stage);
+    stage ^= 1;
+    z0 += (uint32_t)a.z.jump;
+    x0 += (uint32_t)a.x.jump;
     Val<VEC> cur = join_runs<VEC, NW>(sm, round, at.ncl, at.rank, at.warp, at.lane, P, S, carry, waits);
-    char* out = static_cast<char*>(a.h) + ((at.at0 + at.dir * t0) * a.ld_h + at.c) * (int64_t)sizeof(T);
     auto write = [&](auto whole) {
 #pragma unroll
-      for (int i = 0; i < L; ++i, out += out_stride) {
+      for (int i = 0; i < L; ++i, out += a.h.stride) {
         cur = fma_(f[i], cur, b[i]);
-        if (decltype(whole)::value || t0 + i < len) put_word<T, LIE>(out, cur, at.on0, at.on1);
+        if (decltype(whole)::value || i < left) put_word<T, LIE>(out, cur, at.on0, at.on1);
       }
     };
     if (full) write(std::true_type{});
     else write(std::false_type{});
+    out += a.h.skip;
     // (steps after the last have f = 1, b = 0: they pass the state on unchanged)
-    if (a.h_last && t0 < len && t0 + L >= len) at.put(a.h_last, a.channels, cur);
+    if (a.h_last && left > 0 && left <= L) at.put(a.h_last, a.channels, cur);
   }
   wait_copies<0>();
 }
@@ -452,28 +471,34 @@ __global__ void __launch_bounds__(NW * 32, 2) k_scan_forward(const ScanArgs a) {
 // needs h_{t-1} at each of them; it reads the stored h once, before the run's first step, and
 // recomputes the others in 32 bits from z and x, which it has to read anyway: 5 words moved a
 // step instead of 6, and the states inside a run carry no rounding of the output type.
-template <class T, Lie LIE, int L, int NW>
-__global__ void __launch_bounds__(NW * 32, 2) k_scan_backward(const ScanArgs a) {
+template <class T, Lie LIE, int L, int NW, int BLOCKS>
+__global__ void __launch_bounds__(NW * 32, BLOCKS) k_scan_backward(const ScanArgs a) {
   pdl_enter();
   constexpr int VEC = 4 / sizeof(T), kPart = L * kPitch<LIE>;
   extern __shared__ __align__(16) char buffer[];   // [warp][stage][z, x, dh][L rows]
   __shared__ Join<VEC, NW> sm;
   const Place<T, L, NW> at(a);
   const int len = at.len;
-  const Rows z = rows_of<T>(a.z, a.ld_z, at.at0, at.dir, at.c0, a), x = rows_of<T>(a.x, a.ld_x, at.at0, at.dir, at.c0, a),
-             d = rows_of<T>(a.dh, a.ld_dh, at.at0, at.dir, at.c0, a);
+  // a stage holds the steps t_lo .. t_lo + L - 1 in ascending order; the rounds descend
+  const int64_t row0 = at.at0 + at.dir * (int64_t)(len - L - at.mine0);
+  const char* z = first_copy<T, LIE>(a.z, row0, at.c0, a.z.stride, at.lane);
+  const char* x = first_copy<T, LIE>(a.x, row0, at.c0, a.x.stride, at.lane);
+  const char* d = first_copy<T, LIE>(a.dh, row0, at.c0, a.dh.stride, at.lane);
+  uint32_t z0 = (uint32_t)reinterpret_cast<uintptr_t>(z), x0 = (uint32_t)reinterpret_cast<uintptr_t>(x),
+           d0 = (uint32_t)reinterpret_cast<uintptr_t>(d);
   char* const mine = buffer + at.warp * (kStages * 3 * kPart);
-  // a stage holds the steps t_lo .. t_lo + L - 1 in ascending order
-  auto fetch = [&](int64_t u0, int stage) {
-    const int64_t t_lo = len - u0 - L;
+  int ahead = len - at.mine0;   // steps of the next fetch and before it (may be negative)
+  auto fetch = [&](int stage) {
     char* to = mine + stage * 3 * kPart;
-    copy_rows<T, LIE, L>(to, z, t_lo, len, at.width, at.lane);
-    copy_rows<T, LIE, L>(to + kPart, x, t_lo, len, at.width, at.lane);
-    copy_rows<T, LIE, L>(to + 2 * kPart, d, t_lo, len, at.width, at.lane);
+    const int lo = ahead > 0 ? max(L - ahead, 0) : L;
+    copy_rows<T, LIE, L>(to, z, a.z, a.z.stride, -a.z.jump, lo, L, at.width, at.lane);
+    copy_rows<T, LIE, L>(to + kPart, x, a.x, a.x.stride, -a.x.jump, lo, L, at.width, at.lane);
+    copy_rows<T, LIE, L>(to + 2 * kPart, d, a.dh, a.dh.stride, -a.dh.jump, lo, L, at.width, at.lane);
     end_copies();
+    ahead = max(ahead - at.step, 0);
   };
 #pragma unroll
-  for (int i = 0; i < kStages; ++i) fetch((int64_t)at.step * i + at.mine0, i);
+  for (int i = 0; i < kStages; ++i) fetch(i);
   Val<VEC> carry = at.get(a.dh_last, a.channels);
   const Val<VEC> start = at.get(a.h0, a.channels);
   if (len == 0) {
@@ -482,60 +507,65 @@ __global__ void __launch_bounds__(NW * 32, 2) k_scan_backward(const ScanArgs a) 
   }
   join_begin(sm, at.ncl);
 
-  // the state before a run, stored by the forward pass
-  auto state_before = [&](int64_t u0) {
-    const int64_t t = len - 1 - (u0 + L);
-    Val<VEC> w = start;
-    if (t >= 0) {
-      const T* p = static_cast<const T*>(a.h_in) + (at.at0 + at.dir * t) * a.ld_h + at.c;
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) w.v[i] = (i ? at.on1 : at.on0) ? to_float<T>(p[i]) : 0.0f;
+  // the state before a run, stored by the forward pass: fetched a round ahead, as it lies
+  uint32_t before[2] = {0, 0};
+  auto fetch_state = [&](int left) {
+    if (left > L) {
+      const T* p = reinterpret_cast<const T*>(row_at<T>(a.h, at.at0 + at.dir * (int64_t)(left - L - 1), at.c));
+      if constexpr (LIE == kHalves) {
+        if (at.on0) before[0] = load_word<T, 1>(p);
+        if (at.on1) before[1] = load_word<T, 1>(p + 1);
+      } else {
+        if (at.on0) before[0] = load_word<T, VEC>(p);
+      }
     }
-    return w;
   };
-  Val<VEC> before = state_before(at.mine0);
-  const int64_t zs = at.dir * a.ld_dz * (int64_t)sizeof(T), xs = at.dir * a.ld_dx * (int64_t)sizeof(T);
+  int left = len - at.mine0;   // steps up to this warp's last of the round (t_hi + 1)
+  char* gz = row_at<T>(a.dz, at.at0 + at.dir * (int64_t)(left - 1), at.c);
+  char* gx = row_at<T>(a.dx, at.at0 + at.dir * (int64_t)(left - 1), at.c);
+  fetch_state(left);
   bool waits = true;
-  int round = 0, stage = 0;
-  for (int64_t base = 0; base < len; base += at.step, ++round) {
-    const int64_t u0 = base + at.mine0;
-    const int64_t t_hi = len - 1 - u0, t_lo = t_hi - (L - 1);   // negative: nothing of this sequence is left there
-    const bool full = t_lo >= 0;
+  int stage = 0;
+  const int rounds = (len - 1) / at.step + 1;
+  for (int round = 0; round < rounds; ++round, left -= at.step) {
+    const bool full = left >= L;
+    const int none = L - left;   // steps j of the run below this are before the sequence's first
     const char* from = mine + stage * 3 * kPart;
-    const uint32_t z0 = (uint32_t)reinterpret_cast<uintptr_t>(z.row) + (uint32_t)t_lo * (uint32_t)z.stride;
-    const uint32_t x0 = (uint32_t)reinterpret_cast<uintptr_t>(x.row) + (uint32_t)t_lo * (uint32_t)x.stride;
-    const uint32_t d0 = (uint32_t)reinterpret_cast<uintptr_t>(d.row) + (uint32_t)t_lo * (uint32_t)d.stride;
     Val<VEC> f[L], w[L], e[L], P = fill<VEC>(1.0f), S = fill<VEC>(0.0f);   // f, 1 - f, h_{t-1} - x_t
+    Val<VEC> hp;
+    if constexpr (LIE == kHalves) {
+      unpack<T, 2>(before[0] | before[1] << 16, hp.v);
+    } else {
+      unpack<T, VEC>(before[0], hp.v);
+    }
+    if (left <= L) hp = start;
     wait_copies<kStages - 1>();
     auto walk = [&](auto whole) {
-      Val<VEC> hp = before;
 #pragma unroll
       for (int j = 0; j < L; ++j) {
-        gate(row_word<T, LIE>(from, z0, (uint32_t)z.stride, j, at.lane), f[j], w[j]);
-        const Val<VEC> x_t = row_word<T, LIE>(from + kPart, x0, (uint32_t)x.stride, j, at.lane);
+        gate(row_word<T, LIE>(from, z0, (uint32_t)a.z.stride, j, at.lane), f[j], w[j]);
+        const Val<VEC> x_t = row_word<T, LIE>(from + kPart, x0, (uint32_t)a.x.stride, j, at.lane);
         e[j] = sub_(hp, x_t);
-        if (decltype(whole)::value || t_lo + j >= 0) hp = fma_(f[j], hp, mul_(w[j], x_t));
+        if (decltype(whole)::value || j >= none) hp = fma_(f[j], hp, mul_(w[j], x_t));
         else f[j] = fill<VEC>(1.0f);
       }
 #pragma unroll
       for (int j = L - 1; j >= 0; --j) {
-        Val<VEC> g = row_word<T, LIE>(from + 2 * kPart, d0, (uint32_t)d.stride, j, at.lane);
-        if (!decltype(whole)::value && t_lo + j < 0) g = fill<VEC>(0.0f);
+        Val<VEC> g = row_word<T, LIE>(from + 2 * kPart, d0, (uint32_t)a.dh.stride, j, at.lane);
+        if (!decltype(whole)::value && j < none) g = fill<VEC>(0.0f);
         P = mul_(P, f[j]);
         S = mul_(f[j], add_(g, S));
       }
     };
     if (full) walk(std::true_type{});
     else walk(std::false_type{});
-    before = state_before(u0 + at.step);
+    fetch_state(left - at.step);
     Val<VEC> cur = join_runs<VEC, NW>(sm, round, at.ncl, at.rank, at.warp, at.lane, P, S, carry, waits);
-    char* gz = static_cast<char*>(a.dz) + ((at.at0 + at.dir * t_hi) * a.ld_dz + at.c) * (int64_t)sizeof(T);
-    char* gx = static_cast<char*>(a.dx) + ((at.at0 + at.dir * t_hi) * a.ld_dx + at.c) * (int64_t)sizeof(T);
     auto write = [&](auto whole) {
 #pragma unroll
-      for (int j = L - 1; j >= 0; --j, gz -= zs, gx -= xs) {
-        if (decltype(whole)::value || t_lo + j >= 0) {
-          const Val<VEC> gt = add_(row_word<T, LIE>(from + 2 * kPart, d0, (uint32_t)d.stride, j, at.lane), cur);
+      for (int j = L - 1; j >= 0; --j, gz -= a.dz.stride, gx -= a.dx.stride) {
+        if (decltype(whole)::value || j >= none) {
+          const Val<VEC> gt = add_(row_word<T, LIE>(from + 2 * kPart, d0, (uint32_t)a.dh.stride, j, at.lane), cur);
           cur = mul_(f[j], gt);
           put_word<T, LIE>(gx, mul_(w[j], gt), at.on0, at.on1);
           put_word<T, LIE>(gz, mul_(mul_(w[j], cur), e[j]), at.on0, at.on1);
@@ -544,10 +574,15 @@ __global__ void __launch_bounds__(NW * 32, 2) k_scan_backward(const ScanArgs a) 
     };
     if (full) write(std::true_type{});
     else write(std::false_type{});
-    if (a.dh0 && t_hi >= 0 && t_lo <= 0) at.put(a.dh0, a.channels, cur);
+    gz -= a.dz.skip;
+    gx -= a.dx.skip;
+    if (a.dh0 && left > 0 && left <= L) at.put(a.dh0, a.channels, cur);
     __syncwarp();   // the stage has been read by all lanes
-    fetch(u0 + (int64_t)kStages * at.step, stage);
-    stage = stage + 1 == kStages ? 0 : stage + 1;
+    fetch(stage);
+    stage ^= 1;
+    z0 -= (uint32_t)a.z.jump;
+    x0 -= (uint32_t)a.x.jump;
+    d0 -= (uint32_t)a.dh.jump;
   }
   wait_copies<0>();
 }
@@ -582,11 +617,20 @@ k_scan_step(const T* z, int64_t ld_z, const T* x, int64_t ld_x, float* state, co
 
 bool aligned(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
-constexpr int kWarps = 8, kFwdL = 16, kBwdL = 8;
-
+#ifndef FL
+#define FL 16
+#define FW 8
+#define FB 2
+#endif
+#ifndef BL
+#define BL 8
+#define BW 8
+#define BB 2
+#endif
 int cluster_for(const ScanArgs& a, int tile) {
   int64_t blocks = (int64_t)a.ctiles * a.seqs;
   const int64_t len = a.tokens / std::max(a.seqs, 1);
+  if (getenv("NCL")) return atoi(getenv("NCL"));
   int ncl = 1;
   while (ncl < kMaxCluster && blocks * ncl < 296 && (int64_t)ncl * tile < len) ncl *= 2;
   return ncl;
@@ -595,21 +639,28 @@ int cluster_for(const ScanArgs& a, int tile) {
 template <class T, Lie LIE>
 int32_t enqueue(ScanArgs a, bool backward, cudaStream_t s) {
   constexpr int VEC = 4 / sizeof(T);
+  const int L = backward ? BL : FL, NW = backward ? BW : FW;
   a.ctiles = (a.channels + 32 * VEC - 1) / (32 * VEC);
-  a.cluster = cluster_for(a, kWarps * (backward ? kBwdL : kFwdL));
+  a.cluster = cluster_for(a, L * NW);
   const int64_t grid = (int64_t)a.ctiles * a.seqs * a.cluster;
   if (grid > INT32_MAX) return DGC_EINVAL;
+  for (Matrix* m : {&a.z, &a.x, &a.h, &a.dh, &a.dz, &a.dx}) {
+    m->end = m->begin + ((int64_t)(a.tokens - 1) * m->ld + a.channels) * (int64_t)sizeof(T);
+    m->stride = (a.reverse ? -m->ld : m->ld) * (int64_t)sizeof(T);
+    m->jump = m->stride * (a.cluster * NW * L);
+    m->skip = m->stride * (a.cluster * NW * L - L);
+  }
   auto go = [&](auto kernel, size_t smem) {
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) {
       (void)cudaGetLastError();
       return (int32_t)DGC_ECUDA;
     }
-    launch_cluster(kernel, dim3((unsigned)grid), dim3(kWarps * 32), smem, s, (unsigned)a.cluster, a);
+    launch_cluster(kernel, dim3((unsigned)grid), dim3(NW * 32), smem, s, (unsigned)a.cluster, a);
     return check_launch();
   };
-  if (backward) return go(k_scan_backward<T, LIE, kBwdL, kWarps>, kWarps * kStages * 3 * kBwdL * kPitch<LIE>);
-  return go(k_scan_forward<T, LIE, kFwdL, kWarps>, kWarps * kStages * 2 * kFwdL * kPitch<LIE>);
+  if (backward) return go(k_scan_backward<T, LIE, BL, BW, BB>, NW * kStages * 3 * L * kPitch<LIE>);
+  return go(k_scan_forward<T, LIE, FL, FW, FB>, NW * kStages * 2 * L * kPitch<LIE>);
 }
 
 int32_t dispatch(const ScanArgs& a, int32_t dtype, bool backward, Lie lie, cudaStream_t s) {
@@ -639,11 +690,17 @@ bool bad_rows(const void* p, int64_t ld, int32_t channels, size_t elem, int64_t 
 
 bool pairs_ok(const void* p, int64_t ld) { return aligned(p, 4) && ld % 2 == 0; }
 
+Matrix matrix(const void* p, int64_t ld) {
+  Matrix m{};
+  m.begin = static_cast<char*>(const_cast<void*>(p));
+  m.ld = ld;
+  return m;
+}
+
 // The worst lie of the call's matrices.
-struct Matrix { const void* p; int64_t ld; };
 Lie lie_of(std::initializer_list<Matrix> ms, int32_t channels, size_t es) {
   size_t bits = channels * es;
-  for (const Matrix& m : ms) bits |= reinterpret_cast<uintptr_t>(m.p) | (size_t)m.ld * es;
+  for (const Matrix& m : ms) bits |= reinterpret_cast<uintptr_t>(m.begin) | (size_t)m.ld * es;
   return bits % 16 == 0 ? kAligned : bits % 4 == 0 ? kWords : kHalves;
 }
 
@@ -663,11 +720,11 @@ int32_t dgc_gated_scan_forward(int32_t dtype, int64_t tokens, int32_t num_seqs, 
     return DGC_EINVAL;
   if (tokens == 0 && !h_last) return DGC_OK;
   ScanArgs a{};
-  a.z = gate_logits; a.x = x; a.h = h; a.h0 = h0; a.h_last = h_last; a.seq_start = seq_start;
-  a.ld_z = ld_gate; a.ld_x = ld_x; a.ld_h = ld_h;
+  a.z = matrix(gate_logits, ld_gate); a.x = matrix(x, ld_x); a.h = matrix(h, ld_h);
+  a.h0 = h0; a.h_last = h_last; a.seq_start = seq_start;
   a.tokens = (int32_t)tokens; a.seqs = num_seqs; a.seq_len = (int32_t)(tokens / num_seqs);
   a.channels = channels; a.reverse = reverse != 0;
-  const Lie lie = lie_of({{gate_logits, ld_gate}, {x, ld_x}, {h, ld_h}}, channels, es);
+  const Lie lie = lie_of({a.z, a.x, a.h}, channels, es);
   return dispatch(a, dtype, false, lie, as_stream(stream));
 }
 
@@ -686,13 +743,12 @@ int32_t dgc_gated_scan_backward(int32_t dtype, int64_t tokens, int32_t num_seqs,
     return DGC_EINVAL;
   if (tokens == 0 && !dh0) return DGC_OK;
   ScanArgs a{};
-  a.z = gate_logits; a.x = x; a.h_in = h; a.dh = dh; a.dz = dgate; a.dx = dx; a.h0 = h0;
-  a.dh_last = dh_last; a.dh0 = dh0; a.seq_start = seq_start;
-  a.ld_z = ld_gate; a.ld_x = ld_x; a.ld_h = ld_h; a.ld_dh = ld_dh; a.ld_dz = ld_dgate; a.ld_dx = ld_dx;
+  a.z = matrix(gate_logits, ld_gate); a.x = matrix(x, ld_x); a.h = matrix(h, ld_h);
+  a.dh = matrix(dh, ld_dh); a.dz = matrix(dgate, ld_dgate); a.dx = matrix(dx, ld_dx);
+  a.h0 = h0; a.dh_last = dh_last; a.dh0 = dh0; a.seq_start = seq_start;
   a.tokens = (int32_t)tokens; a.seqs = num_seqs; a.seq_len = (int32_t)(tokens / num_seqs);
   a.channels = channels; a.reverse = reverse != 0;
-  const Lie lie = lie_of({{gate_logits, ld_gate}, {x, ld_x}, {h, ld_h}, {dh, ld_dh}, {dgate, ld_dgate}, {dx, ld_dx}},
-                         channels, es);
+  const Lie lie = lie_of({a.z, a.x, a.h, a.dh, a.dz, a.dx}, channels, es);
   return dispatch(a, dtype, true, lie, as_stream(stream));
 }
 
