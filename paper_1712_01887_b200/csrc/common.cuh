@@ -126,6 +126,13 @@ __device__ __forceinline__ uint32_t pack(const float (&v)[VEC]) {
 }
 
 template <class T>
+__device__ __forceinline__ T from_float(float v) {
+  if constexpr (sizeof(T) == 4) return v;
+  else if constexpr (std::is_same_v<T, __nv_bfloat16>) return __float2bfloat16_rn(v);
+  else return __float2half_rn(v);
+}
+
+template <class T>
 __device__ __forceinline__ float to_float(T v) {
   if constexpr (sizeof(T) == 4) return v;
   else if constexpr (std::is_same_v<T, __nv_bfloat16>) return __bfloat162float(v);

@@ -24,7 +24,6 @@
 #include <cooperative_groups.h>
 
 #include <algorithm>
-#include <cstdlib>
 #include <initializer_list>
 
 #include "common.cuh"
@@ -43,8 +42,6 @@ struct Matrix {
   char *begin, *end;
   int64_t ld;        // elements
   int64_t stride;    // bytes from one step of the walk to the next (negative: towards the front)
-  int64_t jump;      // stride * steps of a round
-  int64_t skip;      // stride * (steps of a round - steps of a run)
 };
 
 struct ScanArgs {
@@ -52,7 +49,7 @@ struct ScanArgs {
   const float *h0, *dh_last;
   float *h_last, *dh0;
   const int32_t* seq_start;
-  int32_t tokens, seqs, seq_len, channels, ctiles, cluster, reverse;
+  int32_t tokens, seqs, seq_len, channels, ctiles, cluster, reverse, longest_first;
 };
 
 // The channels of a lane's word, with the packed 32-bit arithmetic of sm_100 (two operations an
@@ -128,19 +125,52 @@ __device__ __forceinline__ void sequence_range(const ScanArgs& a, int s, int& fi
   }
 }
 
+// The sequence that is `place`-th in length (the longest first, the first first among equals):
+// blocks start in this order, so that the last to start have little left to do.
+constexpr int kSorted = 128;
+__device__ __forceinline__ int by_length(const ScanArgs& a, int place) {
+  __shared__ __align__(16) int lens[kSorted];
+  __shared__ int found;
+  const int t = threadIdx.x;
+  int first, len = -1;
+  if (t < kSorted) {
+    if (t < a.seqs) sequence_range(a, t, first, len);
+    lens[t] = len;
+  }
+  __syncthreads();
+  if (t < a.seqs) {
+    int before = 0;
+    for (int j = 0; j < a.seqs; ++j) before += lens[j] > len || (lens[j] == len && j < t);
+    if (before == place) found = t;
+  }
+  __syncthreads();
+  return found;
+}
+
 // ------------------------------------------------------------------ joining the runs
 // A map y_out = P y_in + S of a lane's channels, as it lies in shared memory.
 template <int VEC> struct alignas(8 * VEC) Map { Val<VEC> p, s; };
 
-// The maps of a block's runs, the states they start from, and the maps of the cluster's blocks.
-// Everything alternates between two buffers from round to round.
-template <int VEC, int NW>
+// A block's warps work in G groups that take the rounds in turn.  By group: the maps of a round's
+// runs and the states they start from; by round: the maps of the cluster's blocks and the state
+// before the round.  (Slots of `blocks`: a block sends round i + 4 after it has every block's map
+// of round i + 2, and the warp that sent that one has read round i by then.)
+constexpr int kBlockSlots = 4;
+template <int VEC, int NW, int G>
 struct Join {
-  Map<VEC> runs[2][NW][32];
-  Map<VEC> blocks[2][kMaxCluster][32];
-  Val<VEC> starts[2][NW][32];
-  unsigned long long arrived[2];             // mbarriers of `blocks`
+  Map<VEC> runs[G][NW][32];
+  Val<VEC> starts[G][NW][32];
+  Map<VEC> blocks[kBlockSlots][kMaxCluster][32];
+  Val<VEC> carry[2][32];
+  unsigned long long arrived[kBlockSlots];   // mbarriers of `blocks`
 };
+
+// Named barriers: one of each group, two between the groups' joining warps.
+template <int THREADS>
+__device__ __forceinline__ void bar_sync(int id) { asm volatile("barrier.cta.sync %0, %1;" ::"r"(id), "n"(THREADS) : "memory"); }
+template <int THREADS>
+__device__ __forceinline__ void bar_arrive(int id) { asm volatile("barrier.cta.arrive %0, %1;" ::"r"(id), "n"(THREADS) : "memory"); }
+constexpr int kGroupBarrier = 1, kCarryBarrier = 3;
 
 // Waits that run out (they cannot, short of a fault: the blocks of a cluster run together) are
 // counted here and not waited for again; dgc_gated_scan_check reports them.
@@ -148,10 +178,10 @@ __device__ int g_scan_waits_out;
 
 __device__ __forceinline__ uint32_t shared_address(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
-template <int VEC, int NW>
-__device__ __forceinline__ void join_begin(Join<VEC, NW>& sm, int ncl) {
+template <int VEC, int NW, int G>
+__device__ __forceinline__ void join_begin(Join<VEC, NW, G>& sm, int ncl) {
   if (ncl == 1) return;
-  if (threadIdx.x < 2)
+  if (threadIdx.x < kBlockSlots)
     asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(shared_address(&sm.arrived[threadIdx.x])) : "memory");
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   cg::this_cluster().sync();   // every block runs, its barriers are there
@@ -177,28 +207,29 @@ __device__ __forceinline__ bool wait_arrived(uint32_t barrier, uint32_t phase) {
   return false;
 }
 
-// Joins the runs of all warps of the cluster in order: takes this warp's map (P, S), returns the
-// state its run starts from.  The first warp does the work for the block; it alone holds
-// `carry`, the state before the cluster's first run on entry and after its last on return.
-// A block's map reaches the others by asynchronous stores that complete on their barriers, not
-// through the cluster's barrier: that one would wait for every store of results under way.
-template <int VEC, int NW>
-__device__ __forceinline__ Val<VEC> join_runs(Join<VEC, NW>& sm, int round, int ncl, int rank, int warp, int lane,
-                                              const Val<VEC>& P, const Val<VEC>& S, Val<VEC>& carry, bool& waits) {
-  const int par = round & 1;
-  sm.runs[par][warp][lane] = {P, S};
-  __syncthreads();
+// Joins the runs of a round in order: takes this warp's map (P, S), returns the state its run
+// starts from.  The group's first warp does the work for the block; with one group it keeps
+// `carry`, the state before the round, itself, with two it has it from the other group's first
+// warp, which joined the round before.  A block's map reaches the others by asynchronous stores
+// that complete on their barriers, not through the cluster's barrier: that one would wait for
+// every store of results under way.
+template <int VEC, int NW, int G>
+__device__ __forceinline__ Val<VEC> join_runs(Join<VEC, NW, G>& sm, int round, bool last, int ncl, int rank, int group,
+                                              int warp, int lane, const Val<VEC>& P, const Val<VEC>& S,
+                                              Val<VEC>& carry, bool& waits) {
+  sm.runs[group][warp][lane] = {P, S};
+  bar_sync<NW * 32>(kGroupBarrier + group);
   if (warp == 0) {
-    Val<VEC> cur = carry;
+    const int slot = round % kBlockSlots;
     if (ncl > 1) {
       Val<VEC> tp = P, ts = S;
 #pragma unroll
       for (int w = 1; w < NW; ++w) {
-        const Map<VEC> m = sm.runs[par][w][lane];
+        const Map<VEC> m = sm.runs[group][w][lane];
         tp = mul_(m.p, tp);
         ts = fma_(m.p, ts, m.s);
       }
-      const uint32_t to = shared_address(&sm.blocks[par][rank][lane]), bar = shared_address(&sm.arrived[par]);
+      const uint32_t to = shared_address(&sm.blocks[slot][rank][lane]), bar = shared_address(&sm.arrived[slot]);
       if (lane == 0)
         asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(ncl * 32 * 2 * VEC * 4) : "memory");
 #pragma unroll
@@ -215,14 +246,21 @@ __device__ __forceinline__ Val<VEC> join_runs(Join<VEC, NW>& sm, int round, int 
                          ::"r"(far), "f"(tp.v[0]), "f"(ts.v[0]), "r"(far_bar) : "memory");
         }
       }
-      if (waits) waits = wait_arrived(bar, (uint32_t)(round >> 1) & 1u);
+      if (waits) waits = wait_arrived(bar, (uint32_t)(round / kBlockSlots) & 1u);
+    }
+    if (G == 2 && round > 0) {
+      bar_sync<64>(kCarryBarrier + (round & 1));
+      carry = sm.carry[round & 1][lane];
+    }
+    Val<VEC> cur = carry;
+    if (ncl > 1) {
 #pragma unroll
       for (int r0 = 0; r0 < kMaxCluster; r0 += 4) {   // (four loads under way at a time)
         if (r0 < ncl) {
           Map<VEC> m[4];
 #pragma unroll
           for (int r = 0; r < 4; ++r)
-            if (r0 + r < ncl) m[r] = sm.blocks[par][r0 + r][lane];
+            if (r0 + r < ncl) m[r] = sm.blocks[slot][r0 + r][lane];
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
             if (r0 + r == rank) cur = carry;
@@ -230,22 +268,32 @@ __device__ __forceinline__ Val<VEC> join_runs(Join<VEC, NW>& sm, int round, int 
           }
         }
       }
+      if (G == 2 && !last) {
+        sm.carry[(round + 1) & 1][lane] = carry;
+        bar_arrive<64>(kCarryBarrier + ((round + 1) & 1));
+      }
     }
 #pragma unroll
     for (int w0 = 0; w0 < NW; w0 += 4) {
       Map<VEC> m[4];
 #pragma unroll
-      for (int w = 0; w < 4; ++w) m[w] = sm.runs[par][w0 + w][lane];
+      for (int w = 0; w < 4; ++w) m[w] = sm.runs[group][w0 + w][lane];
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
-        sm.starts[par][w0 + w][lane] = cur;
+        sm.starts[group][w0 + w][lane] = cur;
         cur = fma_(m[w].p, cur, m[w].s);
       }
     }
-    if (ncl == 1) carry = cur;
+    if (ncl == 1) {
+      carry = cur;
+      if (G == 2 && !last) {
+        sm.carry[(round + 1) & 1][lane] = carry;
+        bar_arrive<64>(kCarryBarrier + ((round + 1) & 1));
+      }
+    }
   }
-  __syncthreads();
-  return sm.starts[par][warp][lane];
+  bar_sync<NW * 32>(kGroupBarrier + group);
+  return sm.starts[group][warp][lane];
 }
 
 // ------------------------------------------------------------------ rows into shared memory
@@ -353,19 +401,19 @@ __device__ __forceinline__ void wait_copies() {   // all but the last N groups h
 __device__ __forceinline__ void end_copies() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 
 // What a thread works on: a sequence, a block of channels, a place in the cluster.
-template <class T, int L, int NW>
+template <class T, int L, int NW, int G>
 struct Place {
   static constexpr int VEC = 4 / sizeof(T);
-  int lane, warp, ncl, rank, s, c0, c, first, len, mine0, step, width;
+  int lane, warp, group, ncl, rank, s, c0, c, first, len, mine0, step, width;
   bool on0, on1;
   int64_t at0, dir;
   __device__ __forceinline__ explicit Place(const ScanArgs& a) {
     lane = threadIdx.x & 31;
-    warp = threadIdx.x >> 5;
-    ncl = a.cluster;
-    rank = ncl > 1 ? (int)(blockIdx.x % ncl) : 0;
-    const int unit = blockIdx.x / ncl;
-    s = unit / a.ctiles;
+    warp = (threadIdx.x >> 5) % NW;
+    group = (threadIdx.x >> 5) / NW;
+    rank = a.cluster > 1 ? (int)(blockIdx.x % a.cluster) : 0;
+    const int unit = blockIdx.x / a.cluster;
+    s = a.longest_first ? by_length(a, unit / a.ctiles) : unit / a.ctiles;
     c0 = (unit % a.ctiles) * 32 * VEC;
     c = c0 + lane * VEC;
     on0 = c < a.channels;
@@ -374,8 +422,11 @@ struct Place {
     sequence_range(a, s, first, len);
     at0 = a.reverse ? (int64_t)first + len - 1 : first;   // the scan's first token
     dir = a.reverse ? -1 : 1;
-    mine0 = (rank * NW + warp) * L;
-    step = ncl * NW * L;
+    // a short sequence is left to the cluster's first blocks
+    constexpr int share = NW * L * G;
+    ncl = min(a.cluster, max(1, (len - 1) / share + 1));
+    mine0 = ((group * ncl + rank) * NW + warp) * L;
+    step = ncl * NW * L * G;   // from one of a group's rounds to its next
   }
   __device__ __forceinline__ Val<VEC> get(const float* p, int channels) const {
     Val<VEC> w;
@@ -392,24 +443,26 @@ struct Place {
 
 constexpr int kStages = 2;
 
-template <class T, Lie LIE, int L, int NW, int BLOCKS>
-__global__ void __launch_bounds__(NW * 32, BLOCKS) k_scan_forward(const ScanArgs a) {
+template <class T, Lie LIE, int L, int NW, int G, int BLOCKS>
+__global__ void __launch_bounds__(NW * G * 32, BLOCKS) k_scan_forward(const ScanArgs a) {
   pdl_enter();
   constexpr int VEC = 4 / sizeof(T), kPart = L * kPitch<LIE>;
-  extern __shared__ __align__(16) char buffer[];   // [warp][stage][z, x][L rows]
-  __shared__ Join<VEC, NW> sm;
-  const Place<T, L, NW> at(a);
+  // (on a 128-byte boundary: a row's part that lies across one is read in two steps, 15 % slower)
+  extern __shared__ __align__(1024) char buffer[];   // [warp][stage][z, x][L rows]
+  __shared__ Join<VEC, NW, G> sm;
+  const Place<T, L, NW, G> at(a);
+  if (at.rank >= at.ncl) return;
   const int len = at.len;
   const int64_t row0 = at.at0 + at.dir * at.mine0;
   const char* z = first_copy<T, LIE>(a.z, row0, at.c0, a.z.stride, at.lane);
   const char* x = first_copy<T, LIE>(a.x, row0, at.c0, a.x.stride, at.lane);
   // (low halves of addresses: where in their granules the rows of the round in hand start)
   uint32_t z0 = (uint32_t)reinterpret_cast<uintptr_t>(z), x0 = (uint32_t)reinterpret_cast<uintptr_t>(x);
-  char* const mine = buffer + at.warp * (kStages * 2 * kPart);
+  char* const mine = buffer + (at.group * NW + at.warp) * (kStages * 2 * kPart);
   int ahead = len - at.mine0;   // steps from the next fetch's first on (may be negative)
   auto fetch = [&](int stage) {
-    copy_rows<T, LIE, L>(mine + stage * 2 * kPart, z, a.z, a.z.stride, a.z.jump, 0, min(ahead, L), at.width, at.lane);
-    copy_rows<T, LIE, L>(mine + stage * 2 * kPart + kPart, x, a.x, a.x.stride, a.x.jump, 0, min(ahead, L), at.width, at.lane);
+    copy_rows<T, LIE, L>(mine + stage * 2 * kPart, z, a.z, a.z.stride, a.z.stride * at.step, 0, min(ahead, L), at.width, at.lane);
+    copy_rows<T, LIE, L>(mine + stage * 2 * kPart + kPart, x, a.x, a.x.stride, a.x.stride * at.step, 0, min(ahead, L), at.width, at.lane);
     end_copies();
     ahead = max(ahead - at.step, 0);
   };
@@ -417,7 +470,7 @@ __global__ void __launch_bounds__(NW * 32, BLOCKS) k_scan_forward(const ScanArgs
   for (int i = 0; i < kStages; ++i) fetch(i);
   Val<VEC> carry = at.get(a.h0, a.channels);
   if (len == 0) {   // (the same for all blocks of the cluster)
-    if (a.h_last && at.rank == 0 && at.warp == 0) at.put(a.h_last, a.channels, carry);
+    if (a.h_last && at.rank == 0 && threadIdx.x < 32) at.put(a.h_last, a.channels, carry);
     return;
   }
   join_begin(sm, at.ncl);
@@ -425,9 +478,9 @@ __global__ void __launch_bounds__(NW * 32, BLOCKS) k_scan_forward(const ScanArgs
   char* out = row_at<T>(a.h, row0, at.c);
   bool waits = true;
   int stage = 0;
-  const int rounds = (len - 1) / at.step + 1;
+  const int rounds = (len - 1) / (at.step / G) + 1;   // of the block
   int left = len - at.mine0;   // steps from this warp's first of the round on
-  for (int round = 0; round < rounds; ++round, left -= at.step) {
+  for (int round = at.group; round < rounds; round += G, left -= at.step) {
     const bool full = left >= L;
     const char* from = mine + stage * 2 * kPart;
     Val<VEC> f[L], b[L], P = fill<VEC>(1.0f), S = fill<VEC>(0.0f);
@@ -448,9 +501,9 @@ __global__ void __launch_bounds__(NW * 32, BLOCKS) k_scan_forward(const ScanArgs
     __syncwarp();   // the stage has been read by all lanes
     fetch(stage);
     stage ^= 1;
-    z0 += (uint32_t)a.z.jump;
-    x0 += (uint32_t)a.x.jump;
-    Val<VEC> cur = join_runs<VEC, NW>(sm, round, at.ncl, at.rank, at.warp, at.lane, P, S, carry, waits);
+    z0 += (uint32_t)a.z.stride * (uint32_t)at.step;
+    x0 += (uint32_t)a.x.stride * (uint32_t)at.step;
+    Val<VEC> cur = join_runs<VEC, NW, G>(sm, round, round + 1 == rounds, at.ncl, at.rank, at.group, at.warp, at.lane, P, S, carry, waits);
     auto write = [&](auto whole) {
 #pragma unroll
       for (int i = 0; i < L; ++i, out += a.h.stride) {
@@ -460,7 +513,7 @@ __global__ void __launch_bounds__(NW * 32, BLOCKS) k_scan_forward(const ScanArgs
     };
     if (full) write(std::true_type{});
     else write(std::false_type{});
-    out += a.h.skip;
+    out += a.h.stride * (at.step - L);
     // (steps after the last have f = 1, b = 0: they pass the state on unchanged)
     if (a.h_last && left > 0 && left <= L) at.put(a.h_last, a.channels, cur);
   }
@@ -471,13 +524,15 @@ __global__ void __launch_bounds__(NW * 32, BLOCKS) k_scan_forward(const ScanArgs
 // needs h_{t-1} at each of them; it reads the stored h once, before the run's first step, and
 // recomputes the others in 32 bits from z and x, which it has to read anyway: 5 words moved a
 // step instead of 6, and the states inside a run carry no rounding of the output type.
-template <class T, Lie LIE, int L, int NW, int BLOCKS>
-__global__ void __launch_bounds__(NW * 32, BLOCKS) k_scan_backward(const ScanArgs a) {
+template <class T, Lie LIE, int L, int NW, int G, int BLOCKS>
+__global__ void __launch_bounds__(NW * G * 32, BLOCKS) k_scan_backward(const ScanArgs a) {
   pdl_enter();
   constexpr int VEC = 4 / sizeof(T), kPart = L * kPitch<LIE>;
-  extern __shared__ __align__(16) char buffer[];   // [warp][stage][z, x, dh][L rows]
-  __shared__ Join<VEC, NW> sm;
-  const Place<T, L, NW> at(a);
+  // (on a 128-byte boundary: a row's part that lies across one is read in two steps, 15 % slower)
+  extern __shared__ __align__(1024) char buffer[];   // [warp][stage][z, x, dh][L rows]
+  __shared__ Join<VEC, NW, G> sm;
+  const Place<T, L, NW, G> at(a);
+  if (at.rank >= at.ncl) return;
   const int len = at.len;
   // a stage holds the steps t_lo .. t_lo + L - 1 in ascending order; the rounds descend
   const int64_t row0 = at.at0 + at.dir * (int64_t)(len - L - at.mine0);
@@ -486,14 +541,14 @@ __global__ void __launch_bounds__(NW * 32, BLOCKS) k_scan_backward(const ScanArg
   const char* d = first_copy<T, LIE>(a.dh, row0, at.c0, a.dh.stride, at.lane);
   uint32_t z0 = (uint32_t)reinterpret_cast<uintptr_t>(z), x0 = (uint32_t)reinterpret_cast<uintptr_t>(x),
            d0 = (uint32_t)reinterpret_cast<uintptr_t>(d);
-  char* const mine = buffer + at.warp * (kStages * 3 * kPart);
+  char* const mine = buffer + (at.group * NW + at.warp) * (kStages * 3 * kPart);
   int ahead = len - at.mine0;   // steps of the next fetch and before it (may be negative)
   auto fetch = [&](int stage) {
     char* to = mine + stage * 3 * kPart;
     const int lo = ahead > 0 ? max(L - ahead, 0) : L;
-    copy_rows<T, LIE, L>(to, z, a.z, a.z.stride, -a.z.jump, lo, L, at.width, at.lane);
-    copy_rows<T, LIE, L>(to + kPart, x, a.x, a.x.stride, -a.x.jump, lo, L, at.width, at.lane);
-    copy_rows<T, LIE, L>(to + 2 * kPart, d, a.dh, a.dh.stride, -a.dh.jump, lo, L, at.width, at.lane);
+    copy_rows<T, LIE, L>(to, z, a.z, a.z.stride, -a.z.stride * at.step, lo, L, at.width, at.lane);
+    copy_rows<T, LIE, L>(to + kPart, x, a.x, a.x.stride, -a.x.stride * at.step, lo, L, at.width, at.lane);
+    copy_rows<T, LIE, L>(to + 2 * kPart, d, a.dh, a.dh.stride, -a.dh.stride * at.step, lo, L, at.width, at.lane);
     end_copies();
     ahead = max(ahead - at.step, 0);
   };
@@ -502,7 +557,7 @@ __global__ void __launch_bounds__(NW * 32, BLOCKS) k_scan_backward(const ScanArg
   Val<VEC> carry = at.get(a.dh_last, a.channels);
   const Val<VEC> start = at.get(a.h0, a.channels);
   if (len == 0) {
-    if (a.dh0 && at.rank == 0 && at.warp == 0) at.put(a.dh0, a.channels, carry);
+    if (a.dh0 && at.rank == 0 && threadIdx.x < 32) at.put(a.dh0, a.channels, carry);
     return;
   }
   join_begin(sm, at.ncl);
@@ -526,8 +581,8 @@ __global__ void __launch_bounds__(NW * 32, BLOCKS) k_scan_backward(const ScanArg
   fetch_state(left);
   bool waits = true;
   int stage = 0;
-  const int rounds = (len - 1) / at.step + 1;
-  for (int round = 0; round < rounds; ++round, left -= at.step) {
+  const int rounds = (len - 1) / (at.step / G) + 1;   // of the block
+  for (int round = at.group; round < rounds; round += G, left -= at.step) {
     const bool full = left >= L;
     const int none = L - left;   // steps j of the run below this are before the sequence's first
     const char* from = mine + stage * 3 * kPart;
@@ -560,7 +615,7 @@ __global__ void __launch_bounds__(NW * 32, BLOCKS) k_scan_backward(const ScanArg
     if (full) walk(std::true_type{});
     else walk(std::false_type{});
     fetch_state(left - at.step);
-    Val<VEC> cur = join_runs<VEC, NW>(sm, round, at.ncl, at.rank, at.warp, at.lane, P, S, carry, waits);
+    Val<VEC> cur = join_runs<VEC, NW, G>(sm, round, round + 1 == rounds, at.ncl, at.rank, at.group, at.warp, at.lane, P, S, carry, waits);
     auto write = [&](auto whole) {
 #pragma unroll
       for (int j = L - 1; j >= 0; --j, gz -= a.dz.stride, gx -= a.dx.stride) {
@@ -574,81 +629,75 @@ __global__ void __launch_bounds__(NW * 32, BLOCKS) k_scan_backward(const ScanArg
     };
     if (full) write(std::true_type{});
     else write(std::false_type{});
-    gz -= a.dz.skip;
-    gx -= a.dx.skip;
+    gz -= a.dz.stride * (at.step - L);
+    gx -= a.dx.stride * (at.step - L);
     if (a.dh0 && left > 0 && left <= L) at.put(a.dh0, a.channels, cur);
     __syncwarp();   // the stage has been read by all lanes
     fetch(stage);
     stage ^= 1;
-    z0 -= (uint32_t)a.z.jump;
-    x0 -= (uint32_t)a.x.jump;
-    d0 -= (uint32_t)a.dh.jump;
+    z0 -= (uint32_t)a.z.stride * (uint32_t)at.step;
+    x0 -= (uint32_t)a.x.stride * (uint32_t)at.step;
+    d0 -= (uint32_t)a.dh.stride * (uint32_t)at.step;
   }
   wait_copies<0>();
 }
 
-// One token a sequence: the state is read, advanced and written back where it lies.
-template <class T, int VEC>
+// One token a sequence: the state is read, advanced and written back where it lies.  A thread
+// takes N neighbouring channels (4, in words of 16 bytes of state, where everything is aligned
+// for that), a block's rows are given by the grid's second dimension: no divisions.
+template <class T, int N>
 __global__ void __launch_bounds__(256)
 k_scan_step(const T* z, int64_t ld_z, const T* x, int64_t ld_x, float* state, const int32_t* slots,
             int32_t num_slots, T* out, int64_t ld_out, int32_t rows, int32_t channels) {
   pdl_enter();
-  const int words = (channels + VEC - 1) / VEC;
-  const int64_t total = (int64_t)rows * words;
-  for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < total;
-       i += (int64_t)gridDim.x * blockDim.x) {
-    const int r = (int)(i / words), c = (int)(i % words) * VEC;
+  const int c = (blockIdx.x * 256 + threadIdx.x) * N;
+  if (c >= channels) return;
+  for (int r = blockIdx.y; r < rows; r += gridDim.y) {
     const int slot = slots ? __ldg(slots + r) : r;
-    Val<VEC> zz, xx, f, omf;
-    float y[VEC];
-    unpack<T, VEC>(load_word<T, VEC>(z + r * ld_z + c), zz.v);
-    unpack<T, VEC>(load_word<T, VEC>(x + r * ld_x + c), xx.v);
-    gate(zz, f, omf);
     const bool live = slot >= 0 && slot < num_slots;
     float* st = state + (int64_t)(live ? slot : 0) * channels + c;
+    struct alignas(sizeof(T) * N) Pack { T v[N]; };
+    struct alignas(4 * N) State { float v[N]; };
+    const Pack zw = *reinterpret_cast<const Pack*>(z + r * ld_z + c), xw = *reinterpret_cast<const Pack*>(x + r * ld_x + c);
+    State h{};
+    if (live) h = *reinterpret_cast<const State*>(st);
+    Pack o;
 #pragma unroll
-    for (int v = 0; v < VEC; ++v) {
-      y[v] = live ? fmaf(f.v[v], st[v], omf.v[v] * xx.v[v]) : 0.0f;
-      if (live) st[v] = y[v];
+    for (int i = 0; i < N; ++i) {
+      Val<1> f, omf;
+      gate(Val<1>{{to_float<T>(zw.v[i])}}, f, omf);
+      h.v[i] = live ? fmaf(f.v[0], h.v[i], omf.v[0] * to_float<T>(xw.v[i])) : 0.0f;
+      o.v[i] = from_float<T>(h.v[i]);
     }
-    store_word<T, VEC>(out + r * ld_out + c, pack<T, VEC>(y));
+    if (live) *reinterpret_cast<State*>(st) = h;
+    *reinterpret_cast<Pack*>(out + r * ld_out + c) = o;
   }
 }
 
 bool aligned(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
-#ifndef FL
-#define FL 16
-#define FW 8
-#define FB 2
-#endif
-#ifndef BL
-#define BL 8
-#define BW 8
-#define BB 2
-#endif
-int cluster_for(const ScanArgs& a, int tile) {
-  int64_t blocks = (int64_t)a.ctiles * a.seqs;
-  const int64_t len = a.tokens / std::max(a.seqs, 1);
-  if (getenv("NCL")) return atoi(getenv("NCL"));
-  int ncl = 1;
-  while (ncl < kMaxCluster && blocks * ncl < 296 && (int64_t)ncl * tile < len) ncl *= 2;
-  return ncl;
-}
+constexpr int kWarps = 8, kFwdL = 16, kBwdL = 8, kSms = 148;
 
-template <class T, Lie LIE>
+template <class T, Lie LIE, int G>
 int32_t enqueue(ScanArgs a, bool backward, cudaStream_t s) {
-  constexpr int VEC = 4 / sizeof(T);
-  const int L = backward ? BL : FL, NW = backward ? BW : FW;
+  constexpr int VEC = 4 / sizeof(T), BLOCKS = 3 - G;
+  const int L = backward ? kBwdL : kFwdL;
   a.ctiles = (a.channels + 32 * VEC - 1) / (32 * VEC);
-  a.cluster = cluster_for(a, L * NW);
-  const int64_t grid = (int64_t)a.ctiles * a.seqs * a.cluster;
+  const int64_t units = (int64_t)a.ctiles * a.seqs;
+  // As many blocks of a cluster as there are SMs for, and steps: 4 blocks a sequence instead of 1
+  // take 65536 x 2048 bf16 from 515 to 164 us; where the SMs have enough to do without, the
+  // exchange costs (40 -> 56 us for 16 x 1024 x 1001).
+  a.cluster = 1;
+  if (G == 2)
+    while (a.cluster < kMaxCluster && units * (a.cluster + 1) <= kSms &&
+           (int64_t)a.cluster * (L * kWarps * G) < a.tokens / a.seqs)
+      ++a.cluster;
+  a.longest_first = a.seq_start && a.seqs > 1 && a.seqs <= kSorted && units > kSms;
+  const int64_t grid = units * a.cluster;
   if (grid > INT32_MAX) return DGC_EINVAL;
   for (Matrix* m : {&a.z, &a.x, &a.h, &a.dh, &a.dz, &a.dx}) {
     m->end = m->begin + ((int64_t)(a.tokens - 1) * m->ld + a.channels) * (int64_t)sizeof(T);
     m->stride = (a.reverse ? -m->ld : m->ld) * (int64_t)sizeof(T);
-    m->jump = m->stride * (a.cluster * NW * L);
-    m->skip = m->stride * (a.cluster * NW * L - L);
   }
   auto go = [&](auto kernel, size_t smem) {
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
@@ -656,11 +705,24 @@ int32_t enqueue(ScanArgs a, bool backward, cudaStream_t s) {
       (void)cudaGetLastError();
       return (int32_t)DGC_ECUDA;
     }
-    launch_cluster(kernel, dim3((unsigned)grid), dim3(NW * 32), smem, s, (unsigned)a.cluster, a);
+    launch_cluster(kernel, dim3((unsigned)grid), dim3(kWarps * G * 32), smem, s, (unsigned)a.cluster, a);
     return check_launch();
   };
-  if (backward) return go(k_scan_backward<T, LIE, BL, BW, BB>, NW * kStages * 3 * L * kPitch<LIE>);
-  return go(k_scan_forward<T, LIE, FL, FW, FB>, NW * kStages * 2 * L * kPitch<LIE>);
+  const size_t smem = G * kWarps * kStages * kPitch<LIE> * (backward ? 3 * kBwdL : 2 * kFwdL);
+  if (backward) return go(k_scan_backward<T, LIE, kBwdL, kWarps, G, BLOCKS>, smem);
+  return go(k_scan_forward<T, LIE, kFwdL, kWarps, G, BLOCKS>, smem);
+}
+
+// One group of warps and two blocks an SM, or two groups and one block.  Two groups put a whole SM
+// behind a sequence: right where sequences are long (17 against 105 us for one of 8192 steps x
+// 512 bf16 channels, where the cluster then helps too; 59 against 69 us for 37 of 1081 steps on
+// average, uneven), wrong where they are many and short (51 against 41 us for 64 of 400 x 1024).
+template <class T, Lie LIE>
+int32_t enqueue(const ScanArgs& a, bool backward, cudaStream_t s) {
+  const int32_t len = a.tokens / a.seqs, words = 32 * 4 / (int)sizeof(T);
+  const int64_t units = (int64_t)((a.channels + words - 1) / words) * a.seqs;
+  const bool two = len >= 640 || (len > kFwdL * kWarps && units < kSms);
+  return two ? enqueue<T, LIE, 2>(a, backward, s) : enqueue<T, LIE, 1>(a, backward, s);
 }
 
 int32_t dispatch(const ScanArgs& a, int32_t dtype, bool backward, Lie lie, cudaStream_t s) {
@@ -687,8 +749,6 @@ bool bad_shape(int32_t dtype, int64_t tokens, int32_t seqs, int32_t channels, co
 bool bad_rows(const void* p, int64_t ld, int32_t channels, size_t elem, int64_t tokens) {
   return ld < channels || (tokens > 0 && (!p || !aligned(p, elem)));
 }
-
-bool pairs_ok(const void* p, int64_t ld) { return aligned(p, 4) && ld % 2 == 0; }
 
 Matrix matrix(const void* p, int64_t ld) {
   Matrix m{};
@@ -764,20 +824,21 @@ int32_t dgc_gated_scan_step(int32_t dtype, int32_t rows, int32_t channels, const
   if (rows == 0) return DGC_OK;
   if (!state || !aligned(state, 4) || (!slots && num_slots < rows)) return DGC_EINVAL;
   cudaStream_t s = as_stream(stream);
-  const bool pairs = channels % 2 == 0 && pairs_ok(gate_logits, ld_gate) && pairs_ok(x, ld_x) && pairs_ok(out, ld_out);
-  auto go = [&](auto tag, auto vec) {
+  size_t bits = (channels | ld_gate | ld_x | ld_out) * es;
+  for (const void* p : {gate_logits, x, static_cast<const void*>(out)}) bits |= reinterpret_cast<uintptr_t>(p);
+  const bool four = bits % (4 * es) == 0 && aligned(state, 16);
+  auto go = [&](auto tag, auto n) {
     using T = decltype(tag);
-    constexpr int VEC = decltype(vec)::value;
-    const int64_t total = (int64_t)rows * (channels / VEC);
-    const int grid = (int)std::min<int64_t>((total + 255) / 256, 148 * 8);
-    launch(k_scan_step<T, VEC>, grid, 256, 0, s, static_cast<const T*>(gate_logits), ld_gate,
+    constexpr int N = decltype(n)::value;
+    const dim3 grid((channels + 256 * N - 1) / (256 * N), std::min(rows, 65535));
+    launch(k_scan_step<T, N>, grid, 256, 0, s, static_cast<const T*>(gate_logits), ld_gate,
            static_cast<const T*>(x), ld_x, state, slots, num_slots, static_cast<T*>(out), ld_out, rows, channels);
   };
   using one = std::integral_constant<int, 1>;
-  using two = std::integral_constant<int, 2>;
-  if (dtype == DGC_F32) go(float{}, one{});
-  else if (dtype == DGC_BF16) pairs ? go(__nv_bfloat16{}, two{}) : go(__nv_bfloat16{}, one{});
-  else pairs ? go(__half{}, two{}) : go(__half{}, one{});
+  using all = std::integral_constant<int, 4>;
+  if (dtype == DGC_F32) four ? go(float{}, all{}) : go(float{}, one{});
+  else if (dtype == DGC_BF16) four ? go(__nv_bfloat16{}, all{}) : go(__nv_bfloat16{}, one{});
+  else four ? go(__half{}, all{}) : go(__half{}, one{});
   return check_launch();
 }
 
