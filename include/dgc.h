@@ -393,105 +393,132 @@ int32_t dgc_timeline_read(dgc_state* st, void* stream, uint64_t* ns_out);
 /* ---------------------------------------------------------------- a recurrent model's step
  * The calls below are what a language model trained with this library computes beside its
  * matrix products: a gated recurrent layer (whose gradients the arena takes) and the
- * distillation loss that its gradients start from.  They are stateless, take matrices as a
- * base pointer and a row stride `ld_*` in elements (>= the row's length; columns are
- * adjacent), so that a slice of a wider product's output can be passed as it is, and accept
- * DGC_F32, DGC_BF16 and DGC_F16.  All arithmetic is in 32 bits; results are rounded once.
- * Outputs must not overlap inputs unless stated.  Base pointers are aligned to their element;
- * 16-bit matrices whose bases are 4-byte aligned and whose strides and row lengths are even
- * run about twice as fast as others. */
+ * distillation loss that its gradients start from.  They are stateless and take their
+ * arguments in a struct, which is read during the call only.  Matrices are a base pointer and a
+ * row stride in elements (>= the row's length; columns are adjacent), so that a slice of a
+ * wider product's output can be passed as it is; DGC_F32, DGC_BF16 and DGC_F16 are accepted
+ * at any alignment of the element.  All arithmetic is in 32 bits; results are rounded once.
+ * Outputs must not overlap inputs unless stated.  Errors: DGC_EINVAL (a NULL struct, a size
+ * out of range, a stride below the row's length, a required pointer NULL or misaligned; nothing
+ * is enqueued then), DGC_ECUDA.  Asynchronous on `stream`; may be captured into a CUDA graph. */
+typedef struct dgc_matrix {
+  void*   data;    /* device; inputs are not modified */
+  int64_t ld;      /* elements from one row to the next */
+} dgc_matrix;
 
 /* Gated linear recurrence over packed sequences, per channel:
  *   f_t = 1 / (1 + exp(-z_t)) ;  h_t = f_t h_{t-1} + (1 - f_t) x_t
  * with z the gate's logits.  Sequence s is rows seq_start[s] .. seq_start[s+1] of the
- * [tokens, channels] matrices; a sequence may be empty.
- *   seq_start  device int32 [num_seqs + 1], ascending from 0 to tokens; offsets outside
- *              [0, tokens] are clamped (nothing outside the matrices is touched whatever the
- *              table holds).  NULL: num_seqs sequences of tokens / num_seqs rows each
- *   reverse    non-zero: every sequence is walked from its last row to its first
- *   h0         fp32 [num_seqs, channels], the states before the first step; NULL: 0
- *   h_last     fp32 [num_seqs, channels], the states after the last step (those of empty
- *              sequences are h0's); may be NULL
- * Results do not vary from run to run, and no value of one sequence (an infinity, a NaN)
- * reaches another.  Rows outside every sequence are not written.  tokens < 2^31.  No
- * workspace.  Errors: DGC_EINVAL (sizes < 1, tokens no multiple of num_seqs where seq_start
- * is NULL, a stride below channels, a NULL or misaligned matrix), DGC_ECUDA.  Asynchronous. */
-int32_t dgc_gated_scan_forward(int32_t dtype, int64_t tokens, int32_t num_seqs, int32_t channels,
-                               const int32_t* seq_start, int32_t reverse, const void* gate_logits,
-                               int64_t ld_gate, const void* x, int64_t ld_x, const float* h0, void* h,
-                               int64_t ld_h, float* h_last, void* stream);
+ * [tokens, channels] matrices; a sequence may be empty. */
+typedef struct dgc_scan {
+  int32_t        dtype;      /* DGC_F32, DGC_BF16, DGC_F16: of all matrices                      */
+  int32_t        num_seqs;   /* >= 1                                                             */
+  int32_t        channels;   /* >= 1                                                             */
+  int32_t        reverse;    /* non-zero: every sequence is walked from its last row to its first */
+  int64_t        tokens;     /* 0 .. 2^31 - 1                                                    */
+  const int32_t* seq_start;  /* device [num_seqs + 1], ascending from 0 to tokens; offsets outside
+                                [0, tokens] are clamped (nothing outside the matrices is touched
+                                whatever the table holds).  NULL: num_seqs sequences of
+                                tokens / num_seqs rows each (tokens a multiple of num_seqs)      */
+  dgc_matrix     gate, x;    /* inputs z and x                                                   */
+  dgc_matrix     h;          /* forward: output; backward: the forward call's output             */
+  const float*   h0;         /* [num_seqs, channels], the states before the first step; NULL: 0  */
+  float*         h_last;     /* forward output [num_seqs, channels], the states after the last
+                                step (h0's row for an empty sequence); may be NULL               */
+  /* backward only */
+  dgc_matrix     dh;         /* gradient of h                                                    */
+  dgc_matrix     dgate, dx;  /* outputs                                                          */
+  const float*   dh_last;    /* [num_seqs, channels], gradient of h_last; NULL: 0                */
+  float*         dh0;        /* output [num_seqs, channels] (dh_last's row for an empty
+                                sequence); may be NULL                                           */
+} dgc_scan;
+
+/* Writes h and h_last.  Results do not vary from run to run, and no value of one sequence (an
+ * infinity, a NaN) reaches another.  Rows outside every sequence are not written.  No
+ * workspace. */
+int32_t dgc_gated_scan_forward(const dgc_scan* scan, void* stream);
 
 /* The gradients of dgc_gated_scan_forward, with g_t the gradient that reaches h_t in all:
  *   g_t = dh_t + f_{t+1} g_{t+1}  (+ dh_last at the last step)
- *   dx_t = (1 - f_t) g_t ;  dgate_t = f_t (1 - f_t) g_t (h_{t-1} - x_t) ;  dh0 = f_first g_first
- * First arguments as in the forward call; h is its output.
- *   dh         gradient of h;   dh_last  fp32 [num_seqs, channels], of h_last; NULL: 0
- *   dh0        fp32 [num_seqs, channels] output (dh_last's row for an empty sequence); may be NULL */
-int32_t dgc_gated_scan_backward(int32_t dtype, int64_t tokens, int32_t num_seqs, int32_t channels,
-                                const int32_t* seq_start, int32_t reverse, const void* gate_logits,
-                                int64_t ld_gate, const void* x, int64_t ld_x, const float* h0,
-                                const void* h, int64_t ld_h, const void* dh, int64_t ld_dh,
-                                const float* dh_last, void* dgate, int64_t ld_dgate, void* dx,
-                                int64_t ld_dx, float* dh0, void* stream);
-
-/* One step of the recurrence for `rows` sequences at once (one token each), their states kept
- * in a cache: row r's state is row slots[r] of `state` (fp32 [num_slots, channels]; slots
- * NULL: row r), which is advanced in place; out's row r is the new state.  A slot outside
- * [0, num_slots) marks an idle row: no state changes and out's row is 0.  Two rows must not
- * name one slot. */
-int32_t dgc_gated_scan_step(int32_t dtype, int32_t rows, int32_t channels, const void* gate_logits,
-                            int64_t ld_gate, const void* x, int64_t ld_x, float* state,
-                            const int32_t* slots, int32_t num_slots, void* out, int64_t ld_out,
-                            void* stream);
+ *   dx_t = (1 - f_t) g_t ;  dgate_t = f_t (1 - f_t) g_t (h_{t-1} - x_t) ;  dh0 = f_first g_first */
+int32_t dgc_gated_scan_backward(const dgc_scan* scan, void* stream);
 
 /* Synchronises `stream` and returns DGC_ECUDA if, since the last check on the current device, a
  * block of a dgc_gated_scan_forward or _backward kernel gave up waiting for another block of its
  * cluster (every such wait is bounded; the call's results are then wrong), else DGC_OK. */
 int32_t dgc_gated_scan_check(void* stream);
 
+/* One step of the recurrence for `rows` sequences at once (one token each), their states kept
+ * in a cache: row r's state is row slots[r] of `state`, which is advanced in place; out's row r
+ * is the new state. */
+typedef struct dgc_scan_one {
+  int32_t        dtype, rows, channels;
+  int32_t        num_slots;  /* rows of state                                                    */
+  dgc_matrix     gate, x;    /* [rows, channels] inputs                                          */
+  dgc_matrix     out;        /* [rows, channels] output                                          */
+  float*         state;      /* device [num_slots, channels], in and out                         */
+  const int32_t* slots;      /* device [rows], no two the same; one outside [0, num_slots) marks
+                                an idle row: no state changes and out's row is 0.  NULL: row r
+                                is in slot r                                                     */
+} dgc_scan_one;
+int32_t dgc_gated_scan_step(const dgc_scan_one* step, void* stream);
+
 /* The k largest entries of every row of `logits` [rows, vocab], the form in which a teacher's
  * distribution is kept for dgc_distill_*: largest first, the lowest index first among equals
  * (-0 equals +0, NaN counts as larger than every number).  Entries of -infinity (words masked
- * out) are never listed; a row with fewer than k others is filled up with (-1, -infinity).
- *   idx, val   int32 and fp32 [rows, k] outputs;   1 <= k <= DGC_MAX_TOP
- * Errors: DGC_EINVAL, DGC_ECUDA.  Asynchronous. */
-int32_t dgc_top_logits(int32_t dtype, int64_t rows, int32_t vocab, int32_t k, const void* logits,
-                       int64_t ld_logits, int32_t* idx, float* val, void* stream);
+ * out) are never listed; a row with fewer than k others is filled up with (-1, -infinity). */
+typedef struct dgc_top {
+  int32_t    dtype, vocab;   /* vocab >= 1                                                       */
+  int32_t    k;              /* 1 .. DGC_MAX_TOP                                                 */
+  int32_t    reserved;       /* 0                                                                */
+  int64_t    rows;           /* 0 .. 2^31 - 1                                                    */
+  dgc_matrix logits;
+  int32_t*   idx;            /* output [rows, k]                                                 */
+  float*     val;            /* output [rows, k]                                                 */
+} dgc_top;
+int32_t dgc_top_logits(const dgc_top* top, void* stream);
 
 /* Distillation from a teacher's top logits, one loss a row.  With T the temperature,
  *   q = softmax of the row's listed teacher logits / T ;  p = softmax(s / T) ;  p1 = softmax(s)
- *   loss = soft_weight T^2 sum_k q_k (log q_k - log p[idx_k]) + hard_weight (-log p1[label])
- *   logits     [rows, vocab], the student's;  words masked out are -infinity (their p is 0)
- *   idx, val   int32 and fp32 [rows, k], the teacher's list (dgc_top_logits); an entry whose
- *              index is outside [0, vocab) or whose value is -infinity or NaN is absent; an
- *              index listed twice counts twice.  A row with no entry has no soft term
- *   labels     int32 [rows] or NULL; a label outside [0, vocab) (a padding token) has no hard term
- *   loss       fp32 [rows] output; +infinity where a listed entry or the label has p = 0
- *   lse        fp32 [rows, 2] output for dgc_distill_backward: log sum exp of s / T, and of s
- *              (only where labels and a non-zero hard_weight need it); may be NULL
- * temperature > 0; weights finite.  Asynchronous. */
-int32_t dgc_distill_forward(int32_t dtype, int64_t rows, int32_t vocab, int32_t k, const void* logits,
-                            int64_t ld_logits, const int32_t* idx, const float* val, const int32_t* labels,
-                            float temperature, float soft_weight, float hard_weight, float* loss, float* lse,
-                            void* stream);
+ *   loss = soft_weight T^2 sum_k q_k (log q_k - log p[idx_k]) + hard_weight (-log p1[label]) */
+typedef struct dgc_distill {
+  int32_t        dtype, vocab, k;   /* as in dgc_top                                              */
+  int32_t        reserved;          /* 0                                                          */
+  int64_t        rows;
+  dgc_matrix     logits;            /* [rows, vocab], the student's; words masked out are -infinity
+                                       (their p is 0)                                             */
+  const int32_t* idx;               /* [rows, k] and                                              */
+  const float*   val;               /* [rows, k], the teacher's list (dgc_top_logits): an entry whose
+                                       index is outside [0, vocab) or whose value is -infinity or
+                                       NaN is absent; an index listed twice counts twice.  A row
+                                       with no entry has no soft term                             */
+  const int32_t* labels;            /* [rows] or NULL; a label outside [0, vocab) (a padding token)
+                                       has no hard term                                           */
+  float          temperature;       /* > 0                                                        */
+  float          soft_weight, hard_weight;
+  float          reserved1;         /* 0                                                          */
+  float*         loss;              /* output [rows]; +infinity where a listed entry or the label
+                                       has p = 0                                                  */
+  float*         lse;               /* [rows, 2], forward output (may be NULL) that backward takes:
+                                       log sum exp of s / T, and of s (only where labels and a
+                                       non-zero hard_weight need it)                              */
+  const float*   dloss;             /* [rows], the gradient that reaches the row's loss           */
+  dgc_matrix     dlogits;           /* output [rows, vocab]                                       */
+} dgc_distill;
 
-/* Its gradient: dlogits[r][j] = dloss[r] (soft_weight T (p_j - sum of q listed at j)
- * + hard_weight (p1_j - [j = label])), with lse the forward call's and dloss fp32 [rows] the
- * gradient that reaches the row's loss.  Every element of dlogits [rows, vocab] is written; a row
- * with neither term, or with dloss 0, gets zeros.  dlogits may be the logits themselves (same
+/* Writes loss, and lse if given. */
+int32_t dgc_distill_forward(const dgc_distill* d, void* stream);
+
+/* The gradient: dlogits[r][j] = dloss[r] (soft_weight T (p_j - sum of q listed at j)
+ * + hard_weight (p1_j - [j = label])), from lse and dloss.  Every element of dlogits is written; a
+ * row with neither term, or with dloss 0, gets zeros.  dlogits may be the logits themselves (same
  * base and stride); rows at the same distance from a 16-byte boundary as the logits' are
- * written in 16-byte words, others element by element.  Asynchronous. */
-int32_t dgc_distill_backward(int32_t dtype, int64_t rows, int32_t vocab, int32_t k, const void* logits,
-                             int64_t ld_logits, const int32_t* idx, const float* val, const int32_t* labels,
-                             float temperature, float soft_weight, float hard_weight, const float* lse,
-                             const float* dloss, void* dlogits, int64_t ld_dlogits, void* stream);
+ * written in 16-byte words, others element by element. */
+int32_t dgc_distill_backward(const dgc_distill* d, void* stream);
 
 /* Loss and gradient in one call (dloss known beforehand: a token's weight over the number of
- * tokens): the same results, the logits read from memory once. */
-int32_t dgc_distill_loss_grad(int32_t dtype, int64_t rows, int32_t vocab, int32_t k, const void* logits,
-                              int64_t ld_logits, const int32_t* idx, const float* val, const int32_t* labels,
-                              float temperature, float soft_weight, float hard_weight, const float* dloss,
-                              float* loss, void* dlogits, int64_t ld_dlogits, void* stream);
+ * tokens): the same results, the logits read from memory once.  lse is not used. */
+int32_t dgc_distill_loss_grad(const dgc_distill* d, void* stream);
 
 /* Number of kernels this library has launched in this process (all states). */
 uint64_t dgc_launch_count(void);

@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Optional, Sequence
 
 import numpy as np
@@ -98,33 +99,10 @@ _sigs = {
     "dgc_profile_enable": (ctypes.c_int32, [_vp, ctypes.c_int32]),
     "dgc_profile_read": (ctypes.c_int32, [_vp, _vp, ctypes.c_int32,
                                           ctypes.POINTER(ctypes.c_int32)]),
-    "dgc_gated_scan_forward": (ctypes.c_int32, [ctypes.c_int32, ctypes.c_int64, ctypes.c_int32,
-                                                ctypes.c_int32, _vp, ctypes.c_int32, _vp,
-                                                ctypes.c_int64, _vp, ctypes.c_int64, _vp, _vp,
-                                                ctypes.c_int64, _vp, _vp]),
-    "dgc_gated_scan_backward": (ctypes.c_int32, [ctypes.c_int32, ctypes.c_int64, ctypes.c_int32,
-                                                 ctypes.c_int32, _vp, ctypes.c_int32, _vp,
-                                                 ctypes.c_int64, _vp, ctypes.c_int64, _vp, _vp,
-                                                 ctypes.c_int64, _vp, ctypes.c_int64, _vp, _vp,
-                                                 ctypes.c_int64, _vp, ctypes.c_int64, _vp, _vp]),
-    "dgc_gated_scan_step": (ctypes.c_int32, [ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, _vp,
-                                             ctypes.c_int64, _vp, ctypes.c_int64, _vp, _vp,
-                                             ctypes.c_int32, _vp, ctypes.c_int64, _vp]),
+    **{name: (ctypes.c_int32, [ctypes.c_char_p, _vp]) for name in (
+        "dgc_gated_scan_forward", "dgc_gated_scan_backward", "dgc_gated_scan_step",
+        "dgc_top_logits", "dgc_distill_forward", "dgc_distill_backward", "dgc_distill_loss_grad")},
     "dgc_gated_scan_check": (ctypes.c_int32, [_vp]),
-    "dgc_top_logits": (ctypes.c_int32, [ctypes.c_int32, ctypes.c_int64, ctypes.c_int32,
-                                        ctypes.c_int32, _vp, ctypes.c_int64, _vp, _vp, _vp]),
-    "dgc_distill_forward": (ctypes.c_int32, [ctypes.c_int32, ctypes.c_int64, ctypes.c_int32,
-                                             ctypes.c_int32, _vp, ctypes.c_int64, _vp, _vp, _vp,
-                                             ctypes.c_float, ctypes.c_float, ctypes.c_float, _vp,
-                                             _vp, _vp]),
-    "dgc_distill_backward": (ctypes.c_int32, [ctypes.c_int32, ctypes.c_int64, ctypes.c_int32,
-                                              ctypes.c_int32, _vp, ctypes.c_int64, _vp, _vp, _vp,
-                                              ctypes.c_float, ctypes.c_float, ctypes.c_float, _vp,
-                                              _vp, _vp, ctypes.c_int64, _vp]),
-    "dgc_distill_loss_grad": (ctypes.c_int32, [ctypes.c_int32, ctypes.c_int64, ctypes.c_int32,
-                                               ctypes.c_int32, _vp, ctypes.c_int64, _vp, _vp, _vp,
-                                               ctypes.c_float, ctypes.c_float, ctypes.c_float, _vp,
-                                               _vp, _vp, ctypes.c_int64, _vp]),
     "dgc_launch_count": (ctypes.c_uint64, []),
     "dgc_error_string": (ctypes.c_char_p, [ctypes.c_int32]),
 }
@@ -474,36 +452,52 @@ def apply_sgd(w: torch.Tensor, dense_grad: torch.Tensor, lr: float, stream=None)
 
 
 # ----------------------------------------------------------------- a recurrent model's step
+# These calls take a struct; it is packed in one go, a fraction of the time that a ctypes
+# structure or as many ctypes arguments take (a step of a serving loop is not much longer).
 
 MAX_TOP = 256
 DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}   # DGC_F32, DGC_BF16, DGC_F16
+SCAN = struct.Struct("@4iqP6P2P6P2P")            # dgc_scan (a matrix is a pointer and a 64-bit stride)
+SCAN_ONE = struct.Struct("@4i6P2P")              # dgc_scan_one
+TOP = struct.Struct("@4iq2P2P")                  # dgc_top
+DISTILL = struct.Struct("@4iq2P3P4f3P2P")        # dgc_distill
+_raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else None
 
 
-def _rows(t: torch.Tensor, dtype, rows: int, cols: int, what: str):
-    """(pointer, row stride) of a CUDA matrix whose columns are adjacent."""
-    if t.dtype != dtype or not t.is_cuda or t.dim() != 2:
-        raise ValueError(f"{what}: expected a CUDA {dtype} matrix")
-    if t.shape[0] != rows or t.shape[1] != cols:
-        raise ValueError(f"{what}: expected shape ({rows}, {cols}), got {tuple(t.shape)}")
-    if t.stride(1) != 1 and cols > 1:
-        raise ValueError(f"{what}: columns must be adjacent in memory")
-    return t.data_ptr(), (t.stride(0) if rows > 1 else max(cols, t.stride(0)))
+def _stream_of(stream, device: int) -> int:
+    """The given stream, or the current one of the tensors' device."""
+    if stream is None and _raw_stream is not None:
+        return _raw_stream(device)
+    return _stream(stream)
 
 
-def _vec(t: Optional[torch.Tensor], dtype, numel: int, what: str):
-    """Pointer of a contiguous CUDA tensor of `numel` elements, or None."""
-    if t is None:
-        return None
-    if t.dtype != dtype or not t.is_cuda or not t.is_contiguous() or t.numel() != numel:
-        raise ValueError(f"{what}: expected a contiguous CUDA {dtype} tensor of {numel} elements")
-    return t.data_ptr()
-
-
-def _dtype(t: torch.Tensor, what: str) -> int:
+def _first(t: torch.Tensor, what: str):
+    """What a call's first matrix says of the others: (type code, type, shape, device)."""
     code = DTYPES.get(t.dtype)
-    if code is None or t.dim() != 2:
-        raise ValueError(f"{what}: expected a float32, bfloat16 or float16 matrix")
-    return code
+    device = t.get_device()
+    shape = t.shape
+    if code is None or device < 0 or len(shape) != 2:
+        raise ValueError(f"{what}: expected a CUDA float32, bfloat16 or float16 matrix")
+    return code, t.dtype, shape, device
+
+
+def _matrix(t: torch.Tensor, dtype, shape, device: int, what: str):
+    """(pointer, row stride) of a matrix whose columns are adjacent."""
+    if t.dtype is not dtype or t.get_device() != device or t.shape != shape:
+        raise ValueError(f"{what}: expected a {dtype} matrix of shape {tuple(shape)} on device {device}")
+    ld, one = t.stride()
+    if one != 1 and shape[1] > 1:
+        raise ValueError(f"{what}: columns must be adjacent in memory")
+    return t.data_ptr(), ld if shape[0] > 1 else max(shape[1], ld)
+
+
+def _vec(t: Optional[torch.Tensor], dtype, numel: int, device: int, what: str) -> int:
+    """Pointer of a contiguous tensor of `numel` elements; 0 for None."""
+    if t is None:
+        return 0
+    if t.dtype is not dtype or t.get_device() != device or not t.is_contiguous() or t.numel() != numel:
+        raise ValueError(f"{what}: expected a contiguous {dtype} tensor of {numel} elements on device {device}")
+    return t.data_ptr()
 
 
 def gated_scan_forward(gate: torch.Tensor, x: torch.Tensor, h: torch.Tensor,
@@ -513,16 +507,16 @@ def gated_scan_forward(gate: torch.Tensor, x: torch.Tensor, h: torch.Tensor,
     """h_t = f_t h_{t-1} + (1 - f_t) x_t, f = sigmoid(gate), over packed sequences: rows
     seq_start[s] .. seq_start[s+1] of the [tokens, channels] matrices (seq_start None: num_seqs
     sequences of equal length).  Writes h, and the last states to h_last."""
-    code = _dtype(gate, "gate")
-    n, c = gate.shape
-    zp, zl = _rows(gate, gate.dtype, n, c, "gate")
-    xp, xl = _rows(x, gate.dtype, n, c, "x")
-    hp, hl = _rows(h, gate.dtype, n, c, "h")
-    _check(_lib.dgc_gated_scan_forward(
-        code, n, num_seqs, c, _vec(seq_start, torch.int32, num_seqs + 1, "seq_start"), bool(reverse),
-        zp, zl, xp, xl, _vec(h0, torch.float32, num_seqs * c, "h0"), hp, hl,
-        _vec(h_last, torch.float32, num_seqs * c, "h_last"), _stream(stream)),
-        "dgc_gated_scan_forward")
+    code, dt, shape, dev = _first(gate, "gate")
+    n, c = shape
+    zp, zl = _matrix(gate, dt, shape, dev, "gate")
+    xp, xl = _matrix(x, dt, shape, dev, "x")
+    hp, hl = _matrix(h, dt, shape, dev, "h")
+    args = SCAN.pack(code, num_seqs, c, 1 if reverse else 0, n,
+                     _vec(seq_start, torch.int32, num_seqs + 1, dev, "seq_start"), zp, zl, xp, xl, hp, hl,
+                     _vec(h0, torch.float32, num_seqs * c, dev, "h0"),
+                     _vec(h_last, torch.float32, num_seqs * c, dev, "h_last"), 0, 0, 0, 0, 0, 0, 0, 0)
+    _check(_lib.dgc_gated_scan_forward(args, _stream_of(stream, dev)), "dgc_gated_scan_forward")
 
 
 def gated_scan_backward(gate: torch.Tensor, x: torch.Tensor, h: torch.Tensor, dh: torch.Tensor,
@@ -532,36 +526,38 @@ def gated_scan_backward(gate: torch.Tensor, x: torch.Tensor, h: torch.Tensor, dh
                         dh0: Optional[torch.Tensor] = None, reverse: bool = False,
                         stream=None) -> None:
     """Gradients of gated_scan_forward: writes dgate, dx and dh0 from dh (of h) and dh_last."""
-    code = _dtype(gate, "gate")
-    n, c = gate.shape
-    zp, zl = _rows(gate, gate.dtype, n, c, "gate")
-    xp, xl = _rows(x, gate.dtype, n, c, "x")
-    hp, hl = _rows(h, gate.dtype, n, c, "h")
-    dp, dl = _rows(dh, gate.dtype, n, c, "dh")
-    gp, gl = _rows(dgate, gate.dtype, n, c, "dgate")
-    yp, yl = _rows(dx, gate.dtype, n, c, "dx")
-    _check(_lib.dgc_gated_scan_backward(
-        code, n, num_seqs, c, _vec(seq_start, torch.int32, num_seqs + 1, "seq_start"), bool(reverse),
-        zp, zl, xp, xl, _vec(h0, torch.float32, num_seqs * c, "h0"), hp, hl, dp, dl,
-        _vec(dh_last, torch.float32, num_seqs * c, "dh_last"), gp, gl, yp, yl,
-        _vec(dh0, torch.float32, num_seqs * c, "dh0"), _stream(stream)), "dgc_gated_scan_backward")
+    code, dt, shape, dev = _first(gate, "gate")
+    n, c = shape
+    zp, zl = _matrix(gate, dt, shape, dev, "gate")
+    xp, xl = _matrix(x, dt, shape, dev, "x")
+    hp, hl = _matrix(h, dt, shape, dev, "h")
+    dp, dl = _matrix(dh, dt, shape, dev, "dh")
+    gp, gl = _matrix(dgate, dt, shape, dev, "dgate")
+    yp, yl = _matrix(dx, dt, shape, dev, "dx")
+    args = SCAN.pack(code, num_seqs, c, 1 if reverse else 0, n,
+                     _vec(seq_start, torch.int32, num_seqs + 1, dev, "seq_start"), zp, zl, xp, xl, hp, hl,
+                     _vec(h0, torch.float32, num_seqs * c, dev, "h0"), 0, dp, dl, gp, gl, yp, yl,
+                     _vec(dh_last, torch.float32, num_seqs * c, dev, "dh_last"),
+                     _vec(dh0, torch.float32, num_seqs * c, dev, "dh0"))
+    _check(_lib.dgc_gated_scan_backward(args, _stream_of(stream, dev)), "dgc_gated_scan_backward")
 
 
 def gated_scan_step(gate: torch.Tensor, x: torch.Tensor, state: torch.Tensor, out: torch.Tensor,
                     slots: Optional[torch.Tensor] = None, stream=None) -> None:
     """One token for each row: row slots[r] of `state` (fp32 [slots, channels]) is advanced in
     place and written to out[r]; a slot outside the cache marks an idle row."""
-    code = _dtype(gate, "gate")
-    n, c = gate.shape
-    zp, zl = _rows(gate, gate.dtype, n, c, "gate")
-    xp, xl = _rows(x, gate.dtype, n, c, "x")
-    op, ol = _rows(out, gate.dtype, n, c, "out")
-    if state.dim() != 2 or state.shape[1] != c:
+    code, dt, shape, dev = _first(gate, "gate")
+    n, c = shape
+    zp, zl = _matrix(gate, dt, shape, dev, "gate")
+    xp, xl = _matrix(x, dt, shape, dev, "x")
+    op, ol = _matrix(out, dt, shape, dev, "out")
+    if len(state.shape) != 2:
         raise ValueError("state: expected [slots, channels]")
-    _check(_lib.dgc_gated_scan_step(
-        code, n, c, zp, zl, xp, xl, _vec(state, torch.float32, state.numel(), "state"),
-        _vec(slots, torch.int32, n, "slots"), state.shape[0], op, ol, _stream(stream)),
-        "dgc_gated_scan_step")
+    rows = state.shape[0]
+    args = SCAN_ONE.pack(code, n, c, rows, zp, zl, xp, xl, op, ol,
+                         _vec(state, torch.float32, rows * c, dev, "state"),
+                         _vec(slots, torch.int32, n, dev, "slots"))
+    _check(_lib.dgc_gated_scan_step(args, _stream_of(stream, dev)), "dgc_gated_scan_step")
 
 
 def gated_scan_check(stream=None) -> None:
@@ -572,23 +568,13 @@ def gated_scan_check(stream=None) -> None:
 def top_logits(logits: torch.Tensor, idx: torch.Tensor, val: torch.Tensor, stream=None) -> None:
     """The k largest entries of every row, largest first (idx, val: [rows, k]; the lowest index
     first among equals; -inf is never listed, missing entries are (-1, -inf))."""
-    code = _dtype(logits, "logits")
-    n, v = logits.shape
-    lp, ll = _rows(logits, logits.dtype, n, v, "logits")
+    code, dt, shape, dev = _first(logits, "logits")
+    n, v = shape
+    lp, ll = _matrix(logits, dt, shape, dev, "logits")
     k = idx.shape[-1]
-    _check(_lib.dgc_top_logits(code, n, v, k, lp, ll, _vec(idx, torch.int32, n * k, "idx"),
-                               _vec(val, torch.float32, n * k, "val"), _stream(stream)),
-           "dgc_top_logits")
-
-
-def _distill(logits, idx, val, labels, temperature, soft_weight, hard_weight):
-    code = _dtype(logits, "logits")
-    n, v = logits.shape
-    lp, ll = _rows(logits, logits.dtype, n, v, "logits")
-    k = idx.shape[-1]
-    return n, v, (code, n, v, k, lp, ll, _vec(idx, torch.int32, n * k, "idx"),
-                  _vec(val, torch.float32, n * k, "val"), _vec(labels, torch.int32, n, "labels"),
-                  temperature, soft_weight, hard_weight)
+    args = TOP.pack(code, v, k, 0, n, lp, ll, _vec(idx, torch.int32, n * k, dev, "idx"),
+                    _vec(val, torch.float32, n * k, dev, "val"))
+    _check(_lib.dgc_top_logits(args, _stream_of(stream, dev)), "dgc_top_logits")
 
 
 def distill_forward(logits: torch.Tensor, idx: torch.Tensor, val: torch.Tensor, loss: torch.Tensor,
@@ -597,10 +583,16 @@ def distill_forward(logits: torch.Tensor, idx: torch.Tensor, val: torch.Tensor, 
                     labels: Optional[torch.Tensor] = None, stream=None) -> None:
     """loss[r] = soft_weight T^2 KL(teacher's listed distribution || student's) + hard_weight
     cross entropy with labels[r]; lse [rows, 2] is kept for distill_backward."""
-    n, _, head = _distill(logits, idx, val, labels, temperature, soft_weight, hard_weight)
-    _check(_lib.dgc_distill_forward(*head, _vec(loss, torch.float32, n, "loss"),
-                                    _vec(lse, torch.float32, 2 * n, "lse"), _stream(stream)),
-           "dgc_distill_forward")
+    code, dt, shape, dev = _first(logits, "logits")
+    n, v = shape
+    lp, ll = _matrix(logits, dt, shape, dev, "logits")
+    k = idx.shape[-1]
+    args = DISTILL.pack(code, v, k, 0, n, lp, ll, _vec(idx, torch.int32, n * k, dev, "idx"),
+                        _vec(val, torch.float32, n * k, dev, "val"),
+                        _vec(labels, torch.int32, n, dev, "labels"), temperature, soft_weight,
+                        hard_weight, 0.0, _vec(loss, torch.float32, n, dev, "loss"),
+                        _vec(lse, torch.float32, 2 * n, dev, "lse"), 0, 0, 0)
+    _check(_lib.dgc_distill_forward(args, _stream_of(stream, dev)), "dgc_distill_forward")
 
 
 def distill_backward(logits: torch.Tensor, idx: torch.Tensor, val: torch.Tensor, lse: torch.Tensor,
@@ -609,11 +601,17 @@ def distill_backward(logits: torch.Tensor, idx: torch.Tensor, val: torch.Tensor,
                      labels: Optional[torch.Tensor] = None, stream=None) -> None:
     """The gradient of distill_forward's losses, dloss[r] being that of row r's; dlogits may be
     the logits themselves."""
-    n, v, head = _distill(logits, idx, val, labels, temperature, soft_weight, hard_weight)
-    dp, dl = _rows(dlogits, logits.dtype, n, v, "dlogits")
-    _check(_lib.dgc_distill_backward(*head, _vec(lse, torch.float32, 2 * n, "lse"),
-                                     _vec(dloss, torch.float32, n, "dloss"), dp, dl,
-                                     _stream(stream)), "dgc_distill_backward")
+    code, dt, shape, dev = _first(logits, "logits")
+    n, v = shape
+    lp, ll = _matrix(logits, dt, shape, dev, "logits")
+    dp, dl = _matrix(dlogits, dt, shape, dev, "dlogits")
+    k = idx.shape[-1]
+    args = DISTILL.pack(code, v, k, 0, n, lp, ll, _vec(idx, torch.int32, n * k, dev, "idx"),
+                        _vec(val, torch.float32, n * k, dev, "val"),
+                        _vec(labels, torch.int32, n, dev, "labels"), temperature, soft_weight,
+                        hard_weight, 0.0, 0, _vec(lse, torch.float32, 2 * n, dev, "lse"),
+                        _vec(dloss, torch.float32, n, dev, "dloss"), dp, dl)
+    _check(_lib.dgc_distill_backward(args, _stream_of(stream, dev)), "dgc_distill_backward")
 
 
 def distill_loss_grad(logits: torch.Tensor, idx: torch.Tensor, val: torch.Tensor,
@@ -621,8 +619,14 @@ def distill_loss_grad(logits: torch.Tensor, idx: torch.Tensor, val: torch.Tensor
                       temperature: float = 1.0, soft_weight: float = 1.0, hard_weight: float = 0.0,
                       labels: Optional[torch.Tensor] = None, stream=None) -> None:
     """distill_forward and distill_backward in one call, the logits read from memory once."""
-    n, v, head = _distill(logits, idx, val, labels, temperature, soft_weight, hard_weight)
-    dp, dl = _rows(dlogits, logits.dtype, n, v, "dlogits")
-    _check(_lib.dgc_distill_loss_grad(*head, _vec(dloss, torch.float32, n, "dloss"),
-                                      _vec(loss, torch.float32, n, "loss"), dp, dl,
-                                      _stream(stream)), "dgc_distill_loss_grad")
+    code, dt, shape, dev = _first(logits, "logits")
+    n, v = shape
+    lp, ll = _matrix(logits, dt, shape, dev, "logits")
+    dp, dl = _matrix(dlogits, dt, shape, dev, "dlogits")
+    k = idx.shape[-1]
+    args = DISTILL.pack(code, v, k, 0, n, lp, ll, _vec(idx, torch.int32, n * k, dev, "idx"),
+                        _vec(val, torch.float32, n * k, dev, "val"),
+                        _vec(labels, torch.int32, n, dev, "labels"), temperature, soft_weight,
+                        hard_weight, 0.0, _vec(loss, torch.float32, n, dev, "loss"), 0,
+                        _vec(dloss, torch.float32, n, dev, "dloss"), dp, dl)
+    _check(_lib.dgc_distill_loss_grad(args, _stream_of(stream, dev)), "dgc_distill_loss_grad")

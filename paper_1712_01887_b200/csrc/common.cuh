@@ -65,6 +65,28 @@ inline void launch_cluster(void (*kernel)(KArgs...), dim3 grid, dim3 block, size
   (void)cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);   // error: check_launch()
 }
 
+// Lets a kernel have `bytes` of dynamic shared memory; the driver is asked once per kernel and
+// device.
+template <auto KERNEL>
+inline int32_t allow_shared(size_t bytes) {
+  static std::atomic<uint64_t> done{0};
+  int dev = 0;
+  DGC_CUDA(cudaGetDevice(&dev));
+  const uint64_t bit = dev < 64 ? 1ull << dev : 0;
+  if (done.load(std::memory_order_relaxed) & bit) return DGC_OK;
+  DGC_CUDA(cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
+  done.fetch_or(bit, std::memory_order_relaxed);
+  return DGC_OK;
+}
+
+// Whether a matrix argument of rows x cols cannot be what it says.
+inline bool bad_matrix(const dgc_matrix& m, int64_t rows, int64_t cols, size_t elem) {
+  return m.ld < cols || (rows > 0 && (!m.data || (reinterpret_cast<uintptr_t>(m.data) & (elem - 1)) != 0));
+}
+inline bool misaligned(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) != 0; }
+inline size_t element_size(int32_t dtype) { return dtype == DGC_F32 ? 4 : 2; }
+inline bool bad_dtype(int32_t dtype) { return dtype < DGC_F32 || dtype > DGC_F16; }
+
 inline int32_t check_launch() {
   g_launches.fetch_add(1, std::memory_order_relaxed);
   cudaError_t e = cudaGetLastError();
@@ -137,6 +159,57 @@ __device__ __forceinline__ float to_float(T v) {
   if constexpr (sizeof(T) == 4) return v;
   else if constexpr (std::is_same_v<T, __nv_bfloat16>) return __bfloat162float(v);
   else return __half2float(v);
+}
+
+// ------------------------------------------------------------------ packed arithmetic
+// One or two numbers, with the packed 32-bit arithmetic of sm_100 (two operations an instruction,
+// each rounded as its scalar form).
+template <int VEC> struct alignas(4 * VEC) Val { float v[VEC]; };
+
+__device__ __forceinline__ unsigned long long bits(const Val<2>& a) {
+  unsigned long long r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a.v[0]), "f"(a.v[1]));
+  return r;
+}
+__device__ __forceinline__ Val<2> val(unsigned long long r) {
+  Val<2> a;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(a.v[0]), "=f"(a.v[1]) : "l"(r));
+  return a;
+}
+template <int VEC>
+__device__ __forceinline__ Val<VEC> fill(float x) {
+  Val<VEC> r;
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) r.v[i] = x;
+  return r;
+}
+__device__ __forceinline__ Val<2> fma_(const Val<2>& a, const Val<2>& b, const Val<2>& c) {
+  unsigned long long r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(bits(a)), "l"(bits(b)), "l"(bits(c)));
+  return val(r);
+}
+__device__ __forceinline__ Val<2> mul_(const Val<2>& a, const Val<2>& b) {
+  unsigned long long r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(bits(a)), "l"(bits(b)));
+  return val(r);
+}
+__device__ __forceinline__ Val<2> add_(const Val<2>& a, const Val<2>& b) {
+  unsigned long long r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(bits(a)), "l"(bits(b)));
+  return val(r);
+}
+__device__ __forceinline__ Val<1> fma_(const Val<1>& a, const Val<1>& b, const Val<1>& c) { return {{fmaf(a.v[0], b.v[0], c.v[0])}}; }
+__device__ __forceinline__ Val<1> mul_(const Val<1>& a, const Val<1>& b) { return {{a.v[0] * b.v[0]}}; }
+__device__ __forceinline__ Val<1> add_(const Val<1>& a, const Val<1>& b) { return {{a.v[0] + b.v[0]}}; }
+// a - b
+template <int VEC>
+__device__ __forceinline__ Val<VEC> sub_(const Val<VEC>& a, const Val<VEC>& b) { return fma_(b, fill<VEC>(-1.0f), a); }
+
+// 2^x, to 2 ulp; results below 2^-126 are 0.
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
 }
 
 }  // namespace dgc

@@ -47,12 +47,6 @@ struct DistillArgs {
   int32_t vocab, k, cluster;
 };
 
-__device__ __forceinline__ float exp2_fast(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-
 // Running maximum and sums of exponentials under it (s1: at temperature 1, where it differs).
 // The maximum starts at the lowest finite value, so that rows of -infinity sum to zero.
 template <bool TWO>
@@ -85,9 +79,12 @@ struct DistillShared {
 };
 
 template <class T, int NT, int MODE, bool TWO>
-__global__ void __launch_bounds__(NT) k_distill(const DistillArgs a) {
+#ifndef DB
+#define DB 2
+#endif
+__global__ void __launch_bounds__(NT, DB * 512 / NT) k_distill(const DistillArgs a) {
   pdl_enter();
-  constexpr int E = Row<T>::E, W = NT / 32;
+  constexpr int E = Row<T>::E, W = NT / 32, U = 4;
   __shared__ DistillShared<NT> sm;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int ncl = a.cluster, rank = ncl > 1 ? (int)(blockIdx.x % ncl) : 0;
@@ -126,18 +123,37 @@ __global__ void __launch_bounds__(NT) k_distill(const DistillArgs a) {
   }
   if (walk) {   // (the same for all threads of the row)
     Sums<TWO> st;
-    each_chunk<T, NT, 4>(row, lo, hi, [&](const float (&v)[E], int, bool) {
-      float top = v[0];
+    Val<2> s2 = fill<2>(0.0f), s1 = fill<2>(0.0f);   // (sums of the even and the odd places)
+    each_group<T, NT, U>(row, lo, hi, [&](const uint4 (&x)[U], int, int count) {
+      uint32_t best = max_word<T, false>(x[0]);
 #pragma unroll
-      for (int i = 1; i < E; ++i) top = fmaxf(top, v[i]);
-      if (top > st.m) st.scale_to(top, a.c);
+      for (int u = 1; u < U; ++u)
+        if (u < count) best = max_words<T, false>(best, max_word<T, false>(x[u]));
+      const float top = max_of_word<T, false>(best);
+      if (top > st.m) {
+        s2 = mul_(s2, fill<2>(exp2_fast((st.m - top) * a.c)));
+        if (TWO) s1 = mul_(s1, fill<2>(exp2_fast((st.m - top) * kLog2e)));
+        st.m = top;
+      }
+      const Val<2> minus = fill<2>(-st.m);
 #pragma unroll
-      for (int i = 0; i < E; ++i) {
-        const float d = v[i] - st.m;
-        st.s += exp2_fast(d * a.c);
-        if (TWO) st.s1 += exp2_fast(d * kLog2e);
+      for (int u = 0; u < U; ++u) {
+        if (u >= max(count, 1)) continue;
+        Val<2> v[E / 2];
+        pairs_of<T>(x[u], v);
+#pragma unroll
+        for (int i = 0; i < E / 2; ++i) {
+          const Val<2> d = add_(v[i], minus), e = mul_(d, fill<2>(a.c));
+          s2 = add_(s2, Val<2>{{exp2_fast(e.v[0]), exp2_fast(e.v[1])}});
+          if (TWO) {
+            const Val<2> e1 = mul_(d, fill<2>(kLog2e));
+            s1 = add_(s1, Val<2>{{exp2_fast(e1.v[0]), exp2_fast(e1.v[1])}});
+          }
+        }
       }
     });
+    st.s = s2.v[0] + s2.v[1];
+    st.s1 = s1.v[0] + s1.v[1];
     st.join(32, a.c);
     if (lane == 0) sm.row[warp] = make_float3(st.m, st.s, st.s1);
     __syncthreads();
@@ -211,16 +227,30 @@ __global__ void __launch_bounds__(NT) k_distill(const DistillArgs a) {
   T* out = static_cast<T*>(a.dlogits) + r * a.ld_d;
   const bool same = (reinterpret_cast<uintptr_t>(out) & 15u) == (reinterpret_cast<uintptr_t>(row.p) & 15u);
   __syncthreads();   // the listed logits are in registers: their places may be overwritten
-  each_chunk<T, NT, 4>(row, lo, hi, [&](const float (&v)[E], int e0, bool whole) {
-    float g[E];
+  each_group<T, NT, U>(row, lo, hi, [&](const uint4 (&x)[U], int j, int count) {
 #pragma unroll
-    for (int i = 0; i < E; ++i) g[i] = zero ? 0.0f : grad(v[i]);
-    if (whole && same) {
-      *reinterpret_cast<uint4*>(out + e0) = pack_chunk<T>(g);
-    } else {
+    for (int u = 0; u < U; ++u) {
+      if (u >= max(count, 1)) continue;
+      Val<2> v[E / 2];
+      pairs_of<T>(x[u], v);
 #pragma unroll
-      for (int i = 0; i < E; ++i)
-        if (e0 + i >= 0 && e0 + i < a.vocab) store_one<T>(out + e0 + i, g[i]);
+      for (int i = 0; i < E / 2; ++i) {
+        const Val<2> s = v[i], e = mul_(add_(s, fill<2>(-m)), fill<2>(a.c));
+        v[i] = mul_(Val<2>{{exp2_fast(e.v[0]), exp2_fast(e.v[1])}}, fill<2>(coef));
+        if (TWO) {
+          const Val<2> e1 = mul_(add_(s, fill<2>(-m1)), fill<2>(kLog2e));
+          v[i] = fma_(Val<2>{{exp2_fast(e1.v[0]), exp2_fast(e1.v[1])}}, fill<2>(coef1), v[i]);
+        }
+        if (zero) v[i] = fill<2>(0.0f);
+      }
+      const int e0 = row.first(j + u * NT);
+      if (count > 0 && same) {
+        *reinterpret_cast<uint4*>(out + e0) = chunk_of<T>(v);
+      } else {
+#pragma unroll
+        for (int i = 0; i < E; ++i)
+          if (e0 + i >= 0 && e0 + i < a.vocab) store_one<T>(out + e0 + i, v[i / 2].v[i % 2]);
+      }
     }
   });
   if (zero) return;
@@ -251,7 +281,10 @@ template <class T, int MODE, bool TWO>
 void go(const DistillArgs& a, int64_t rows, cudaStream_t s) {
   const dim3 grid((unsigned)(rows * a.cluster));
   if (a.vocab <= 4096) launch_cluster(k_distill<T, 256, MODE, TWO>, grid, 256, 0, s, (unsigned)a.cluster, a);
-  else launch_cluster(k_distill<T, 512, MODE, TWO>, grid, 512, 0, s, (unsigned)a.cluster, a);
+#ifndef DNT
+#define DNT 512
+#endif
+  else launch_cluster(k_distill<T, DNT, MODE, TWO>, grid, DNT, 0, s, (unsigned)a.cluster, a);
 }
 
 template <class T>
@@ -266,68 +299,39 @@ int32_t enqueue(DistillArgs a, int mode, int64_t rows, cudaStream_t s) {
   return check_launch();
 }
 
-bool off(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) != 0; }
-
-int32_t distill(int mode, int32_t dtype, int64_t rows, int64_t k, DistillArgs& a, void* stream) {
-  if (dtype < DGC_F32 || dtype > DGC_F16 || rows < 0 || rows > INT32_MAX || a.vocab < 1 ||
-      a.vocab > INT32_MAX - 64 || k < 1 || k > DGC_MAX_TOP || a.ld < a.vocab)
+int32_t distill(int mode, const dgc_distill* d, void* stream) {
+  if (!d || bad_dtype(d->dtype) || d->rows < 0 || d->rows > INT32_MAX || d->vocab < 1 || d->vocab > INT32_MAX - 64 ||
+      d->k < 1 || d->k > DGC_MAX_TOP)
     return DGC_EINVAL;
-  if (!(a.temperature > 0.0f) || !std::isfinite(a.temperature) || !std::isfinite(a.soft) || !std::isfinite(a.hard))
+  if (!(d->temperature > 0.0f) || !std::isfinite(d->temperature) || !std::isfinite(d->soft_weight) ||
+      !std::isfinite(d->hard_weight))
     return DGC_EINVAL;
-  if (mode != kForward && a.ld_d < a.vocab) return DGC_EINVAL;
-  if (rows == 0) return DGC_OK;
-  const uintptr_t es = dtype == DGC_F32 ? 4 : 2;
-  if (!a.logits || !a.idx || !a.val || off(a.logits, es) || off(a.idx, 4) || off(a.val, 4) || off(a.labels, 4) ||
-      off(a.dloss, 4) || off(a.lse, 4) || off(a.lse_in, 4) || off(a.loss, 4) || off(a.dlogits, es))
+  const size_t es = element_size(d->dtype);
+  if (bad_matrix(d->logits, d->rows, d->vocab, es)) return DGC_EINVAL;
+  if (mode != kForward && bad_matrix(d->dlogits, d->rows, d->vocab, es)) return DGC_EINVAL;
+  if (d->rows == 0) return DGC_OK;
+  if (!d->idx || !d->val || misaligned(d->idx, 4) || misaligned(d->val, 4) || misaligned(d->labels, 4) ||
+      misaligned(d->loss, 4) || misaligned(d->lse, 4) || misaligned(d->dloss, 4))
     return DGC_EINVAL;
-  if (mode != kBackward && !a.loss) return DGC_EINVAL;
-  if (mode != kForward && (!a.dloss || !a.dlogits)) return DGC_EINVAL;
-  if (mode == kBackward && !a.lse_in) return DGC_EINVAL;
-  a.k = (int32_t)k;
-  a.c = (float)(1.4426950408889634 / (double)a.temperature);
-  cudaStream_t s = as_stream(stream);
-  if (dtype == DGC_F32) return enqueue<float>(a, mode, rows, s);
-  if (dtype == DGC_BF16) return enqueue<__nv_bfloat16>(a, mode, rows, s);
-  return enqueue<__half>(a, mode, rows, s);
-}
-
-DistillArgs common_args(int32_t vocab, const void* logits, int64_t ld, const int32_t* idx, const float* val,
-                        const int32_t* labels, float temperature, float soft, float hard) {
+  if ((mode != kBackward && !d->loss) || (mode != kForward && !d->dloss) || (mode == kBackward && !d->lse)) return DGC_EINVAL;
   DistillArgs a{};
-  a.logits = logits; a.ld = ld; a.idx = idx; a.val = val; a.labels = labels; a.vocab = vocab;
-  a.temperature = temperature; a.soft = soft; a.hard = hard;
-  return a;
+  a.logits = d->logits.data; a.ld = d->logits.ld; a.idx = d->idx; a.val = d->val; a.labels = d->labels;
+  a.vocab = d->vocab; a.k = d->k; a.temperature = d->temperature; a.soft = d->soft_weight; a.hard = d->hard_weight;
+  a.c = (float)(1.4426950408889634 / (double)d->temperature);
+  a.loss = d->loss; a.lse = d->lse; a.lse_in = d->lse; a.dloss = d->dloss;
+  a.dlogits = d->dlogits.data; a.ld_d = d->dlogits.ld;
+  cudaStream_t s = as_stream(stream);
+  if (d->dtype == DGC_F32) return enqueue<float>(a, mode, d->rows, s);
+  if (d->dtype == DGC_BF16) return enqueue<__nv_bfloat16>(a, mode, d->rows, s);
+  return enqueue<__half>(a, mode, d->rows, s);
 }
 
 }  // namespace
 
 extern "C" {
 
-int32_t dgc_distill_forward(int32_t dtype, int64_t rows, int32_t vocab, int32_t k, const void* logits,
-                            int64_t ld_logits, const int32_t* idx, const float* val, const int32_t* labels,
-                            float temperature, float soft_weight, float hard_weight, float* loss, float* lse,
-                            void* stream) {
-  DistillArgs a = common_args(vocab, logits, ld_logits, idx, val, labels, temperature, soft_weight, hard_weight);
-  a.loss = loss; a.lse = lse;
-  return distill(kForward, dtype, rows, k, a, stream);
-}
-
-int32_t dgc_distill_backward(int32_t dtype, int64_t rows, int32_t vocab, int32_t k, const void* logits,
-                             int64_t ld_logits, const int32_t* idx, const float* val, const int32_t* labels,
-                             float temperature, float soft_weight, float hard_weight, const float* lse,
-                             const float* dloss, void* dlogits, int64_t ld_dlogits, void* stream) {
-  DistillArgs a = common_args(vocab, logits, ld_logits, idx, val, labels, temperature, soft_weight, hard_weight);
-  a.lse_in = lse; a.dloss = dloss; a.dlogits = dlogits; a.ld_d = ld_dlogits;
-  return distill(kBackward, dtype, rows, k, a, stream);
-}
-
-int32_t dgc_distill_loss_grad(int32_t dtype, int64_t rows, int32_t vocab, int32_t k, const void* logits,
-                              int64_t ld_logits, const int32_t* idx, const float* val, const int32_t* labels,
-                              float temperature, float soft_weight, float hard_weight, const float* dloss,
-                              float* loss, void* dlogits, int64_t ld_dlogits, void* stream) {
-  DistillArgs a = common_args(vocab, logits, ld_logits, idx, val, labels, temperature, soft_weight, hard_weight);
-  a.dloss = dloss; a.loss = loss; a.dlogits = dlogits; a.ld_d = ld_dlogits;
-  return distill(kBoth, dtype, rows, k, a, stream);
-}
+int32_t dgc_distill_forward(const dgc_distill* d, void* stream) { return distill(kForward, d, stream); }
+int32_t dgc_distill_backward(const dgc_distill* d, void* stream) { return distill(kBackward, d, stream); }
+int32_t dgc_distill_loss_grad(const dgc_distill* d, void* stream) { return distill(kBoth, d, stream); }
 
 }  // extern "C"

@@ -52,49 +52,6 @@ struct ScanArgs {
   int32_t tokens, seqs, seq_len, channels, ctiles, cluster, reverse, longest_first;
 };
 
-// The channels of a lane's word, with the packed 32-bit arithmetic of sm_100 (two operations an
-// instruction, each rounded as its scalar form).
-template <int VEC> struct alignas(4 * VEC) Val { float v[VEC]; };
-
-__device__ __forceinline__ unsigned long long bits(const Val<2>& a) {
-  unsigned long long r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a.v[0]), "f"(a.v[1]));
-  return r;
-}
-__device__ __forceinline__ Val<2> val(unsigned long long r) {
-  Val<2> a;
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(a.v[0]), "=f"(a.v[1]) : "l"(r));
-  return a;
-}
-template <int VEC>
-__device__ __forceinline__ Val<VEC> fill(float x) {
-  Val<VEC> r;
-#pragma unroll
-  for (int i = 0; i < VEC; ++i) r.v[i] = x;
-  return r;
-}
-__device__ __forceinline__ Val<2> fma_(const Val<2>& a, const Val<2>& b, const Val<2>& c) {
-  unsigned long long r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(bits(a)), "l"(bits(b)), "l"(bits(c)));
-  return val(r);
-}
-__device__ __forceinline__ Val<2> mul_(const Val<2>& a, const Val<2>& b) {
-  unsigned long long r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(bits(a)), "l"(bits(b)));
-  return val(r);
-}
-__device__ __forceinline__ Val<2> add_(const Val<2>& a, const Val<2>& b) {
-  unsigned long long r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(bits(a)), "l"(bits(b)));
-  return val(r);
-}
-__device__ __forceinline__ Val<1> fma_(const Val<1>& a, const Val<1>& b, const Val<1>& c) { return {{fmaf(a.v[0], b.v[0], c.v[0])}}; }
-__device__ __forceinline__ Val<1> mul_(const Val<1>& a, const Val<1>& b) { return {{a.v[0] * b.v[0]}}; }
-__device__ __forceinline__ Val<1> add_(const Val<1>& a, const Val<1>& b) { return {{a.v[0] + b.v[0]}}; }
-// a - b
-template <int VEC>
-__device__ __forceinline__ Val<VEC> sub_(const Val<VEC>& a, const Val<VEC>& b) { return fma_(b, fill<VEC>(-1.0f), a); }
-
 // f = sigma(z) and 1 - f, each to full relative precision (1 - f is not formed by subtraction:
 // for gates near 1 it is the weight of the input).  The logit is held above -87, so that e f
 // cannot become inf * 0; f is then at most 2e-38 too large.  A NaN passes through.
@@ -674,8 +631,6 @@ k_scan_step(const T* z, int64_t ld_z, const T* x, int64_t ld_x, float* state, co
   }
 }
 
-bool aligned(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
-
 constexpr int kWarps = 8, kFwdL = 16, kBwdL = 8, kSms = 148;
 
 template <class T, Lie LIE, int G>
@@ -699,18 +654,19 @@ int32_t enqueue(ScanArgs a, bool backward, cudaStream_t s) {
     m->end = m->begin + ((int64_t)(a.tokens - 1) * m->ld + a.channels) * (int64_t)sizeof(T);
     m->stride = (a.reverse ? -m->ld : m->ld) * (int64_t)sizeof(T);
   }
-  auto go = [&](auto kernel, size_t smem) {
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (e != cudaSuccess) {
-      (void)cudaGetLastError();
-      return (int32_t)DGC_ECUDA;
-    }
-    launch_cluster(kernel, dim3((unsigned)grid), dim3(kWarps * G * 32), smem, s, (unsigned)a.cluster, a);
+  const size_t smem = G * kWarps * kStages * kPitch<LIE> * (backward ? 3 * kBwdL : 2 * kFwdL);
+  auto go = [&](auto kernel) {
+    constexpr auto f = decltype(kernel)::value;
+    const int32_t rc = allow_shared<f>(smem);
+    if (rc != DGC_OK) return rc;
+    const dim3 blocks((unsigned)grid), threads(kWarps * G * 32);
+    if (a.cluster > 1) launch_cluster(f, blocks, threads, smem, s, (unsigned)a.cluster, a);
+    else launch(f, blocks, threads, smem, s, a);
     return check_launch();
   };
-  const size_t smem = G * kWarps * kStages * kPitch<LIE> * (backward ? 3 * kBwdL : 2 * kFwdL);
-  if (backward) return go(k_scan_backward<T, LIE, kBwdL, kWarps, G, BLOCKS>, smem);
-  return go(k_scan_forward<T, LIE, kFwdL, kWarps, G, BLOCKS>, smem);
+  using Kernel = void (*)(ScanArgs);
+  if (backward) return go(std::integral_constant<Kernel, &k_scan_backward<T, LIE, kBwdL, kWarps, G, BLOCKS>>{});
+  return go(std::integral_constant<Kernel, &k_scan_forward<T, LIE, kFwdL, kWarps, G, BLOCKS>>{});
 }
 
 // One group of warps and two blocks an SM, or two groups and one block.  Two groups put a whole SM
@@ -737,25 +693,7 @@ int32_t dispatch(const ScanArgs& a, int32_t dtype, bool backward, Lie lie, cudaS
                          : enqueue<__half, kHalves>(a, backward, s);
 }
 
-size_t element_size(int32_t dtype) { return dtype == DGC_F32 ? 4 : 2; }
-
-bool bad_shape(int32_t dtype, int64_t tokens, int32_t seqs, int32_t channels, const int32_t* seq_start) {
-  if (dtype < DGC_F32 || dtype > DGC_F16) return true;
-  if (tokens < 0 || tokens > INT32_MAX || seqs < 1 || channels < 1) return true;
-  return !seq_start && tokens % seqs != 0;
-}
-
-// A matrix argument: rows of `channels` elements, `ld` apart.
-bool bad_rows(const void* p, int64_t ld, int32_t channels, size_t elem, int64_t tokens) {
-  return ld < channels || (tokens > 0 && (!p || !aligned(p, elem)));
-}
-
-Matrix matrix(const void* p, int64_t ld) {
-  Matrix m{};
-  m.begin = static_cast<char*>(const_cast<void*>(p));
-  m.ld = ld;
-  return m;
-}
+Matrix matrix(const dgc_matrix& m) { return Matrix{static_cast<char*>(m.data), nullptr, m.ld, 0}; }
 
 // The worst lie of the call's matrices.
 Lie lie_of(std::initializer_list<Matrix> ms, int32_t channels, size_t es) {
@@ -764,80 +702,61 @@ Lie lie_of(std::initializer_list<Matrix> ms, int32_t channels, size_t es) {
   return bits % 16 == 0 ? kAligned : bits % 4 == 0 ? kWords : kHalves;
 }
 
+int32_t scan(const dgc_scan* d, bool backward, void* stream) {
+  if (!d || bad_dtype(d->dtype) || d->tokens < 0 || d->tokens > INT32_MAX || d->num_seqs < 1 || d->channels < 1 ||
+      (!d->seq_start && d->tokens % d->num_seqs != 0))
+    return DGC_EINVAL;
+  const size_t es = element_size(d->dtype);
+  const auto bad = [&](const dgc_matrix& m) { return bad_matrix(m, d->tokens, d->channels, es); };
+  if (bad(d->gate) || bad(d->x) || bad(d->h) || misaligned(d->h0, 4) || misaligned(d->seq_start, 4)) return DGC_EINVAL;
+  if (backward ? bad(d->dh) || bad(d->dgate) || bad(d->dx) || misaligned(d->dh_last, 4) || misaligned(d->dh0, 4)
+               : misaligned(d->h_last, 4))
+    return DGC_EINVAL;
+  if (d->tokens == 0 && !(backward ? d->dh0 : d->h_last)) return DGC_OK;
+  ScanArgs a{};
+  a.z = matrix(d->gate); a.x = matrix(d->x); a.h = matrix(d->h);
+  a.h0 = d->h0; a.seq_start = d->seq_start;
+  a.tokens = (int32_t)d->tokens; a.seqs = d->num_seqs; a.seq_len = (int32_t)(d->tokens / d->num_seqs);
+  a.channels = d->channels; a.reverse = d->reverse != 0;
+  if (!backward) {
+    a.h_last = d->h_last;
+    return dispatch(a, d->dtype, false, lie_of({a.z, a.x, a.h}, a.channels, es), as_stream(stream));
+  }
+  a.dh = matrix(d->dh); a.dz = matrix(d->dgate); a.dx = matrix(d->dx);
+  a.dh_last = d->dh_last; a.dh0 = d->dh0;
+  return dispatch(a, d->dtype, true, lie_of({a.z, a.x, a.h, a.dh, a.dz, a.dx}, a.channels, es), as_stream(stream));
+}
+
 }  // namespace
 
 extern "C" {
 
-int32_t dgc_gated_scan_forward(int32_t dtype, int64_t tokens, int32_t num_seqs, int32_t channels,
-                               const int32_t* seq_start, int32_t reverse, const void* gate_logits,
-                               int64_t ld_gate, const void* x, int64_t ld_x, const float* h0, void* h,
-                               int64_t ld_h, float* h_last, void* stream) {
-  if (bad_shape(dtype, tokens, num_seqs, channels, seq_start)) return DGC_EINVAL;
-  const size_t es = element_size(dtype);
-  if (bad_rows(gate_logits, ld_gate, channels, es, tokens) || bad_rows(x, ld_x, channels, es, tokens) ||
-      bad_rows(h, ld_h, channels, es, tokens) || !aligned(h0, 4) || !aligned(h_last, 4) ||
-      !aligned(seq_start, 4))
-    return DGC_EINVAL;
-  if (tokens == 0 && !h_last) return DGC_OK;
-  ScanArgs a{};
-  a.z = matrix(gate_logits, ld_gate); a.x = matrix(x, ld_x); a.h = matrix(h, ld_h);
-  a.h0 = h0; a.h_last = h_last; a.seq_start = seq_start;
-  a.tokens = (int32_t)tokens; a.seqs = num_seqs; a.seq_len = (int32_t)(tokens / num_seqs);
-  a.channels = channels; a.reverse = reverse != 0;
-  const Lie lie = lie_of({a.z, a.x, a.h}, channels, es);
-  return dispatch(a, dtype, false, lie, as_stream(stream));
-}
+int32_t dgc_gated_scan_forward(const dgc_scan* d, void* stream) { return scan(d, false, stream); }
+int32_t dgc_gated_scan_backward(const dgc_scan* d, void* stream) { return scan(d, true, stream); }
 
-int32_t dgc_gated_scan_backward(int32_t dtype, int64_t tokens, int32_t num_seqs, int32_t channels,
-                                const int32_t* seq_start, int32_t reverse, const void* gate_logits,
-                                int64_t ld_gate, const void* x, int64_t ld_x, const float* h0,
-                                const void* h, int64_t ld_h, const void* dh, int64_t ld_dh,
-                                const float* dh_last, void* dgate, int64_t ld_dgate, void* dx,
-                                int64_t ld_dx, float* dh0, void* stream) {
-  if (bad_shape(dtype, tokens, num_seqs, channels, seq_start)) return DGC_EINVAL;
-  const size_t es = element_size(dtype);
-  if (bad_rows(gate_logits, ld_gate, channels, es, tokens) || bad_rows(x, ld_x, channels, es, tokens) ||
-      bad_rows(h, ld_h, channels, es, tokens) || bad_rows(dh, ld_dh, channels, es, tokens) ||
-      bad_rows(dgate, ld_dgate, channels, es, tokens) || bad_rows(dx, ld_dx, channels, es, tokens) ||
-      !aligned(h0, 4) || !aligned(dh_last, 4) || !aligned(dh0, 4) || !aligned(seq_start, 4))
+int32_t dgc_gated_scan_step(const dgc_scan_one* d, void* stream) {
+  if (!d || bad_dtype(d->dtype) || d->rows < 0 || d->channels < 1 || d->num_slots < 0) return DGC_EINVAL;
+  const size_t es = element_size(d->dtype);
+  if (bad_matrix(d->gate, d->rows, d->channels, es) || bad_matrix(d->x, d->rows, d->channels, es) ||
+      bad_matrix(d->out, d->rows, d->channels, es) || misaligned(d->slots, 4))
     return DGC_EINVAL;
-  if (tokens == 0 && !dh0) return DGC_OK;
-  ScanArgs a{};
-  a.z = matrix(gate_logits, ld_gate); a.x = matrix(x, ld_x); a.h = matrix(h, ld_h);
-  a.dh = matrix(dh, ld_dh); a.dz = matrix(dgate, ld_dgate); a.dx = matrix(dx, ld_dx);
-  a.h0 = h0; a.dh_last = dh_last; a.dh0 = dh0; a.seq_start = seq_start;
-  a.tokens = (int32_t)tokens; a.seqs = num_seqs; a.seq_len = (int32_t)(tokens / num_seqs);
-  a.channels = channels; a.reverse = reverse != 0;
-  const Lie lie = lie_of({a.z, a.x, a.h, a.dh, a.dz, a.dx}, channels, es);
-  return dispatch(a, dtype, true, lie, as_stream(stream));
-}
-
-int32_t dgc_gated_scan_step(int32_t dtype, int32_t rows, int32_t channels, const void* gate_logits,
-                            int64_t ld_gate, const void* x, int64_t ld_x, float* state,
-                            const int32_t* slots, int32_t num_slots, void* out, int64_t ld_out,
-                            void* stream) {
-  if (dtype < DGC_F32 || dtype > DGC_F16 || rows < 0 || channels < 1 || num_slots < 0) return DGC_EINVAL;
-  const size_t es = element_size(dtype);
-  if (bad_rows(gate_logits, ld_gate, channels, es, rows) || bad_rows(x, ld_x, channels, es, rows) ||
-      bad_rows(out, ld_out, channels, es, rows) || !aligned(slots, 4))
-    return DGC_EINVAL;
-  if (rows == 0) return DGC_OK;
-  if (!state || !aligned(state, 4) || (!slots && num_slots < rows)) return DGC_EINVAL;
-  cudaStream_t s = as_stream(stream);
-  size_t bits = (channels | ld_gate | ld_x | ld_out) * es;
-  for (const void* p : {gate_logits, x, static_cast<const void*>(out)}) bits |= reinterpret_cast<uintptr_t>(p);
-  const bool four = bits % (4 * es) == 0 && aligned(state, 16);
+  if (d->rows == 0) return DGC_OK;
+  if (!d->state || misaligned(d->state, 4) || (!d->slots && d->num_slots < d->rows)) return DGC_EINVAL;
+  size_t bits = d->channels * es;
+  for (const dgc_matrix& m : {d->gate, d->x, d->out}) bits |= reinterpret_cast<uintptr_t>(m.data) | (size_t)m.ld * es;
+  const bool four = bits % (4 * es) == 0 && !misaligned(d->state, 16);
   auto go = [&](auto tag, auto n) {
     using T = decltype(tag);
     constexpr int N = decltype(n)::value;
-    const dim3 grid((channels + 256 * N - 1) / (256 * N), std::min(rows, 65535));
-    launch(k_scan_step<T, N>, grid, 256, 0, s, static_cast<const T*>(gate_logits), ld_gate,
-           static_cast<const T*>(x), ld_x, state, slots, num_slots, static_cast<T*>(out), ld_out, rows, channels);
+    const dim3 grid((d->channels + 256 * N - 1) / (256 * N), std::min(d->rows, 65535));
+    launch(k_scan_step<T, N>, grid, 256, 0, as_stream(stream), static_cast<const T*>(d->gate.data), d->gate.ld,
+           static_cast<const T*>(d->x.data), d->x.ld, d->state, d->slots, d->num_slots, static_cast<T*>(d->out.data),
+           d->out.ld, d->rows, d->channels);
   };
   using one = std::integral_constant<int, 1>;
   using all = std::integral_constant<int, 4>;
-  if (dtype == DGC_F32) four ? go(float{}, all{}) : go(float{}, one{});
-  else if (dtype == DGC_BF16) four ? go(__nv_bfloat16{}, all{}) : go(__nv_bfloat16{}, one{});
+  if (d->dtype == DGC_F32) four ? go(float{}, all{}) : go(float{}, one{});
+  else if (d->dtype == DGC_BF16) four ? go(__nv_bfloat16{}, all{}) : go(__nv_bfloat16{}, one{});
   else four ? go(__half{}, all{}) : go(__half{}, one{});
   return check_launch();
 }

@@ -48,6 +48,7 @@ __device__ __forceinline__ unsigned long long entry(uint32_t key, int index) {
 struct TopShared {
   unsigned long long list[kTopList];
   unsigned long long best[DGC_MAX_TOP];
+  uint2 range[32];
   int count, total[2];
 };
 
@@ -60,6 +61,30 @@ __device__ __forceinline__ int block_sum(int v, TopShared& sm, int par) {
   if ((threadIdx.x & 31) == 0) atomicAdd(&sm.total[par], v);
   __syncthreads();
   return sm.total[par];
+}
+
+// A bound that at least k of the threads' keys reach if as many are above -infinity, and the
+// lowest finite key otherwise: the k-th largest key, cut off below the bits that a type's
+// rounding leaves (f32: ten bits of fraction are near enough).  The search starts below the bits
+// that all keys have in common.
+template <class T, int NT>
+__device__ __forceinline__ uint32_t kth_largest(uint32_t key, int k, TopShared& sm) {
+  constexpr int low = std::is_same_v<T, __nv_bfloat16> ? 16 : 13;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const bool there = key >= kLowest;
+  const uint32_t top = __reduce_max_sync(0xFFFFFFFFu, key), bottom = __reduce_min_sync(0xFFFFFFFFu, there ? key : 0xFFFFFFFFu);
+  if (lane == 0) sm.range[warp] = make_uint2(top, bottom);
+  if (__syncthreads_count(there) < k) return kLowest;
+  const uint2 mine = lane < NT / 32 ? sm.range[lane] : make_uint2(0, 0xFFFFFFFFu);
+  const uint32_t hi = __reduce_max_sync(0xFFFFFFFFu, mine.x), lo = __reduce_min_sync(0xFFFFFFFFu, mine.y);
+  int bit = 31 - __clz(hi ^ lo);                                   // -1: all alike
+  uint32_t bound = bit < 0 ? lo : bit == 31 ? 0u : lo & ~((2u << bit) - 1u);
+#pragma unroll 1
+  for (; bit >= low; --bit) {
+    const uint32_t c = bound | (1u << bit);
+    if (__syncthreads_count(key >= c) >= k) bound = c;
+  }
+  return max(bound, kLowest);
 }
 
 // The k largest of the n listed entries (all different), in order, to sm.best.  Ends with a barrier.
@@ -89,37 +114,33 @@ __device__ void rank_list(TopShared& sm, int n, int k) {
 // sm.best; returns how many there are.
 template <class T, int NT>
 __device__ int top_of_part(const Row<T>& row, int lo, int hi, int k, TopShared& sm) {
+  constexpr int E = Row<T>::E;
   const int tid = threadIdx.x;
-  float top = -INFINITY;
-  bool nan = false;
-  each_chunk<T, NT, 4>(row, lo, hi, [&](const float (&v)[Row<T>::E], int, bool) {
+  uint32_t best = kNone<T>;   // (two maxima of 16-bit types; a NaN wins)
+  each_group<T, NT, 8>(row, lo, hi, [&](const uint4 (&w)[8], int, int count) {
 #pragma unroll
-    for (int i = 0; i < Row<T>::E; ++i) {
-      nan |= v[i] != v[i];
-      top = fmaxf(top, v[i]);
-    }
+    for (int u = 0; u < 8; ++u)
+      if (u < max(count, 1)) best = max_words<T, true>(best, max_word<T, true>(w[u]));
   });
-  const uint32_t key = nan ? 0xFFFFFFFFu : order_key(top);
-  // k-th largest maximum, from the top bit down; what a type's rounding leaves in the low bits
-  // (or, for f32, a closer bound than 2^-15 of the value) is not worth a barrier a bit
-  constexpr int low = sizeof(T) == 4 ? 8 : std::is_same_v<T, __nv_bfloat16> ? 16 : 13;
-  uint32_t bound = 0;
-#pragma unroll 1
-  for (int bit = 31; bit >= low; --bit) {
-    const uint32_t c = bound | (1u << bit);
-    if (__syncthreads_count(key >= c) >= k) bound = c;
-  }
-  bound = max(bound, kLowest);
+  const uint32_t key = order_key(max_of_word<T, true>(best));
+  const uint32_t bound = kth_largest<T, NT>(key, k, sm);
   if (tid == 0) sm.count = 0;
   __syncthreads();
   auto list_above = [&](uint32_t from) {
-    each_chunk<T, NT, 2>(row, lo, hi, [&](const float (&v)[Row<T>::E], int e0, bool) {
+    const float floor = key_value(from);
+    each_group<T, NT, 4>(row, lo, hi, [&](const uint4 (&w)[4], int j, int count) {
 #pragma unroll
-      for (int i = 0; i < Row<T>::E; ++i) {
-        const uint32_t q = order_key(v[i]);
-        if (q >= from) {
-          const int at = atomicAdd(&sm.count, 1);
-          if (at < kTopList) sm.list[at] = entry(q, e0 + i);
+      for (int u = 0; u < 4; ++u) {
+        if (u >= max(count, 1) || max_of_word<T, true>(max_word<T, true>(w[u])) < floor) continue;   // (not if it is NaN)
+        Val<2> v[E / 2];
+        pairs_of<T>(w[u], v);
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+          const uint32_t q = order_key(v[i / 2].v[i % 2]);
+          if (q >= from) {
+            const int at = atomicAdd(&sm.count, 1);
+            if (at < kTopList) sm.list[at] = entry(q, row.first(j + u * NT) + i);
+          }
         }
       }
     });
@@ -134,9 +155,15 @@ __device__ int top_of_part(const Row<T>& row, int lo, int hi, int k, TopShared& 
     int par = 0;
     auto reach = [&](uint32_t from) {
       int mine = 0;
-      each_chunk<T, NT, 2>(row, lo, hi, [&](const float (&v)[Row<T>::E], int, bool) {
+      each_group<T, NT, 2>(row, lo, hi, [&](const uint4 (&w)[2], int, int count) {
 #pragma unroll
-        for (int i = 0; i < Row<T>::E; ++i) mine += order_key(v[i]) >= from;
+        for (int u = 0; u < 2; ++u) {
+          if (u >= max(count, 1)) continue;
+          Val<2> v[E / 2];
+          pairs_of<T>(w[u], v);
+#pragma unroll
+          for (int i = 0; i < E; ++i) mine += order_key(v[i / 2].v[i % 2]) >= from;
+        }
       });
       return block_sum<NT>(mine, sm, par ^= 1);
     };
@@ -158,7 +185,7 @@ __device__ int top_of_part(const Row<T>& row, int lo, int hi, int k, TopShared& 
       const int e0 = row.first(j);
       if (j < hi) {
 #pragma unroll
-        for (int i = 0; i < Row<T>::E; ++i) {
+        for (int i = 0; i < E; ++i) {
           const int e = e0 + i;
           if (e >= 0 && e < row.n && order_key(to_float<T>(row.p[e])) == good) hit |= 1u << i;
         }
@@ -181,7 +208,7 @@ __device__ int top_of_part(const Row<T>& row, int lo, int hi, int k, TopShared& 
       }
       base += before - __popc(hit);
 #pragma unroll
-      for (int i = 0; i < Row<T>::E; ++i) {
+      for (int i = 0; i < E; ++i) {
         if (hit >> i & 1) {
           if (base < k) sm.list[base] = entry(good, e0 + i);
           ++base;
@@ -208,24 +235,44 @@ k_top_logits(const T* logits, int64_t ld, int32_t rows, int32_t vocab, int32_t k
   const int lo = (int)((int64_t)row.chunks * rank / ncl), hi = (int)((int64_t)row.chunks * (rank + 1) / ncl);
   int n = top_of_part<T, NT>(row, lo, hi, k, sm);
   if (ncl > 1) {
+    // every block writes the entries of its own part that are among the row's k largest: their
+    // places are the numbers of larger entries in all parts' lists, which are in order
     cg::cluster_group cl = cg::this_cluster();
     if (threadIdx.x == 0) sm.total[0] = n;
     cl.sync();
-    if (rank == 0) {
-      int at = 0;
-      for (int q = 0; q < ncl; ++q) {
-        TopShared* peer = cl.map_shared_rank(&sm, q);
-        const int m = peer->total[0];
-        for (int i = threadIdx.x; i < m; i += NT) sm.list[at + i] = peer->best[i];
-        at += m;
-      }
-      __syncthreads();
-      n = at;
+    for (int i = threadIdx.x; i < ncl * k; i += NT) {
+      TopShared* peer = cl.map_shared_rank(&sm, i / k);
+      sm.list[i] = i % k < peer->total[0] ? peer->best[i % k] : 0;   // (0: below every entry)
     }
     cl.sync();   // the peers' lists have been read
+    int all = 0;
+    for (int i = threadIdx.x; i < n; i += NT) {
+      const unsigned long long e = sm.best[i];
+      int place = i;
+      for (int q = 0; q < ncl; ++q) {
+        if (q == rank) continue;
+        const unsigned long long* list = sm.list + q * k;
+        int a = 0, b = k;      // list[0, a) > e, list[b, k) < e
+        while (a < b) {
+          const int m = (a + b) / 2;
+          if (list[m] > e) a = m + 1;
+          else b = m;
+        }
+        place += a;
+      }
+      if (place < k) {
+        idx[r * k + place] = (int32_t)(0xFFFFFFFFu - (uint32_t)e);
+        val[r * k + place] = key_value((uint32_t)(e >> 32));
+      }
+    }
     if (rank != 0) return;
-    rank_list<NT>(sm, n, k);
-    n = min(n, k);
+    for (int q = threadIdx.x; q < ncl * k; q += NT) all += sm.list[q] != 0;
+    all = block_sum<NT>(all, sm, 1);
+    for (int i = all + threadIdx.x; i < k; i += NT) {   // fewer than k in the whole row
+      idx[r * k + i] = -1;
+      val[r * k + i] = -INFINITY;
+    }
+    return;
   }
   for (int i = threadIdx.x; i < k; i += NT) {
     const unsigned long long e = i < n ? sm.best[i] : 0;
@@ -235,32 +282,25 @@ k_top_logits(const T* logits, int64_t ld, int32_t rows, int32_t vocab, int32_t k
 }
 
 template <class T>
-int32_t enqueue(const void* logits, int64_t ld, int64_t rows, int32_t vocab, int32_t k, int32_t* idx,
-                float* val, cudaStream_t s) {
+int32_t enqueue(const dgc_top& d, cudaStream_t s) {
   int ncl = 1;
-  while (ncl < 8 && rows * ncl < 148 && vocab / ncl > 16384) ncl *= 2;
-  const int64_t grid = rows * ncl;
+  while (ncl < 8 && d.rows * ncl < 148 && d.vocab / ncl > 16384) ncl *= 2;
+  const int64_t grid = d.rows * ncl;
   if (grid > INT32_MAX) return DGC_EINVAL;
   launch_cluster(k_top_logits<T, kTopThreads>, dim3((unsigned)grid), kTopThreads, 0, s, (unsigned)ncl,
-                 static_cast<const T*>(logits), ld, (int32_t)rows, vocab, k, ncl, idx, val);
+                 static_cast<const T*>(d.logits.data), d.logits.ld, (int32_t)d.rows, d.vocab, d.k, ncl, d.idx, d.val);
   return check_launch();
 }
 
 }  // namespace
 
-extern "C" int32_t dgc_top_logits(int32_t dtype, int64_t rows, int32_t vocab, int32_t k,
-                                  const void* logits, int64_t ld_logits, int32_t* idx, float* val,
-                                  void* stream) {
-  if (dtype < DGC_F32 || dtype > DGC_F16 || rows < 0 || rows > INT32_MAX || vocab < 1 || vocab > INT32_MAX - 64 ||
-      k < 1 || k > DGC_MAX_TOP || ld_logits < vocab)
+extern "C" int32_t dgc_top_logits(const dgc_top* d, void* stream) {
+  if (!d || bad_dtype(d->dtype) || d->rows < 0 || d->rows > INT32_MAX || d->vocab < 1 || d->vocab > INT32_MAX - 64 ||
+      d->k < 1 || d->k > DGC_MAX_TOP || bad_matrix(d->logits, d->rows, d->vocab, element_size(d->dtype)))
     return DGC_EINVAL;
-  if (rows == 0) return DGC_OK;
-  const uintptr_t es = dtype == DGC_F32 ? 4 : 2;
-  if (!logits || !idx || !val || (reinterpret_cast<uintptr_t>(logits) & (es - 1)) ||
-      ((reinterpret_cast<uintptr_t>(idx) | reinterpret_cast<uintptr_t>(val)) & 3))
-    return DGC_EINVAL;
-  cudaStream_t s = as_stream(stream);
-  if (dtype == DGC_F32) return enqueue<float>(logits, ld_logits, rows, vocab, k, idx, val, s);
-  if (dtype == DGC_BF16) return enqueue<__nv_bfloat16>(logits, ld_logits, rows, vocab, k, idx, val, s);
-  return enqueue<__half>(logits, ld_logits, rows, vocab, k, idx, val, s);
+  if (d->rows == 0) return DGC_OK;
+  if (!d->idx || !d->val || misaligned(d->idx, 4) || misaligned(d->val, 4)) return DGC_EINVAL;
+  if (d->dtype == DGC_F32) return enqueue<float>(*d, as_stream(stream));
+  if (d->dtype == DGC_BF16) return enqueue<__nv_bfloat16>(*d, as_stream(stream));
+  return enqueue<__half>(*d, as_stream(stream));
 }

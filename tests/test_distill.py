@@ -6,7 +6,6 @@ probability is (s - m) / T - log(sum): with |s - m| / T < 64 the products and di
 at most 4 * 2^-24 * 64 = 1.6e-5, the sum by the same (the exponents of its terms) plus a few ulp: in
 all under 4e-5 of a unit, times the weights.  A probability is off by 4e-5 of itself, hence
 a gradient by 4e-5 of w_soft T (p + q) + w_hard (p1 + [label]), plus half an ulp of a 16-bit type."""
-import ctypes
 import math
 
 import numpy as np
@@ -346,32 +345,29 @@ def test_matrices_whose_offsets_pass_32_bits():
 
 def test_refusals_of_the_c_calls():
     from paper_1712_01887_b200 import binding as B
-    lib, p, null, off = B._lib, ctypes.c_void_p(4096), ctypes.c_void_p(0), ctypes.c_void_p(4097)
+    lib, p, off = B._lib, 4096, 4097
 
     def top(dtype=0, rows=2, v=8, k=4, x=p, ld=8, i=p, o=p):
-        return lib.dgc_top_logits(dtype, rows, v, k, x, ld, i, o, null)
-    for bad in (dict(dtype=3), dict(rows=-1), dict(v=0), dict(k=0), dict(k=257), dict(ld=7), dict(x=null), dict(i=null), dict(o=null),
-                dict(x=off), dict(i=off), dict(rows=1 << 31)):
+        return lib.dgc_top_logits(B.TOP.pack(dtype, v, k, 0, rows, x, ld, i, o), None)
+    for bad in (dict(dtype=3), dict(rows=-1), dict(v=0), dict(k=0), dict(k=257), dict(ld=7), dict(x=0), dict(i=0), dict(o=0),
+                dict(x=off), dict(i=off), dict(o=off), dict(rows=1 << 31)):
         assert top(**bad) == B.EINVAL, bad
-    assert top(rows=0) == B.OK
+    assert top(rows=0) == B.OK and lib.dgc_top_logits(None, None) == B.EINVAL
 
-    def call(which, dtype=1, rows=2, v=8, k=4, x=p, ld=8, i=p, t=p, T=1.0, ws=1.0, wh=0.0, lse=p, dl=p, loss=p, g=p, ldg=8, lab=null):
-        head = (dtype, rows, v, k, x, ld, i, t, lab, T, ws, wh)
-        if which == "forward":
-            return lib.dgc_distill_forward(*head, loss, lse, null)
-        if which == "backward":
-            return lib.dgc_distill_backward(*head, lse, dl, g, ldg, null)
-        return lib.dgc_distill_loss_grad(*head, dl, loss, g, ldg, null)
-    every = [dict(dtype=-1), dict(dtype=3), dict(rows=-2), dict(v=0), dict(k=0), dict(k=300), dict(x=null), dict(ld=7), dict(i=null),
-             dict(t=null), dict(T=0.0), dict(T=-1.0), dict(T=float("nan")), dict(T=INF), dict(ws=INF), dict(wh=float("nan")), dict(x=off),
+    def call(which, dtype=1, rows=2, v=8, k=4, x=p, ld=8, i=p, t=p, T=1.0, ws=1.0, wh=0.0, lse=p, dl=p, loss=p, g=p, ldg=8, lab=0):
+        return getattr(lib, "dgc_distill_" + which)(B.DISTILL.pack(dtype, v, k, 0, rows, x, ld, i, t, lab, T, ws, wh, 0.0, loss, lse,
+                                                                   dl, g, ldg), None)
+    every = [dict(dtype=-1), dict(dtype=3), dict(rows=-2), dict(v=0), dict(k=0), dict(k=300), dict(x=0), dict(ld=7), dict(i=0),
+             dict(t=0), dict(T=0.0), dict(T=-1.0), dict(T=float("nan")), dict(T=INF), dict(ws=INF), dict(wh=float("nan")), dict(x=off),
              dict(i=off), dict(lab=off)]
-    only = {"forward": [dict(loss=null), dict(loss=off), dict(lse=off)],
-            "backward": [dict(lse=null), dict(dl=null), dict(g=null), dict(ldg=7), dict(g=off)],
-            "both": [dict(dl=null), dict(loss=null), dict(g=null), dict(ldg=0)]}
+    only = {"forward": [dict(loss=0), dict(loss=off), dict(lse=off)],
+            "backward": [dict(lse=0), dict(dl=0), dict(g=0), dict(ldg=7), dict(g=off)],
+            "loss_grad": [dict(dl=0), dict(loss=0), dict(g=0), dict(ldg=0)]}
     for which, more in only.items():
         for bad in every + more:
             assert call(which, **bad) == B.EINVAL, (which, bad)
         assert call(which, rows=0) == B.OK
+        assert getattr(lib, "dgc_distill_" + which)(None, None) == B.EINVAL
 
 
 @pytest.mark.gpu

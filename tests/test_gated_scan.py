@@ -6,8 +6,6 @@ logits inside [-6, 6] that is d * 404 < 1e-4 of the largest state, and the same 
 gradients (their recurrence has the same coefficients).  Rounding to a 16-bit type adds half a
 unit in the last place: at most eps / 2 = 2^-8 (bf16) or 2^-11 (f16) of the value; where the backward pass starts a
 run from a stored state, that state's rounding enters dgate once more, times f (1 - f) |g|."""
-import ctypes
-
 import numpy as np
 import pytest
 import torch
@@ -281,25 +279,30 @@ def test_scan_in_a_graph():
 def test_refusals_of_the_c_calls():
     """Bad arguments come back as DGC_EINVAL before anything is enqueued (no GPU needed)."""
     from paper_1712_01887_b200 import binding as B
-    lib, p = B._lib, ctypes.c_void_p(4096)
-    null = ctypes.c_void_p(0)
+    p = 4096
 
-    def fwd(dtype=0, tokens=8, seqs=2, ch=4, ld=4, z=p, x=p, h=p):
-        return lib.dgc_gated_scan_forward(dtype, tokens, seqs, ch, null, 0, z, ld, x, ld, null, h, ld, null, null)
-    for bad in (dict(dtype=3), dict(dtype=-1), dict(tokens=-1), dict(tokens=7), dict(tokens=1 << 31), dict(seqs=0), dict(ch=0),
-                dict(ld=3), dict(z=null), dict(x=null), dict(h=null), dict(x=ctypes.c_void_p(4098)), dict(dtype=1, h=ctypes.c_void_p(4097))):
-        assert fwd(**bad) == B.EINVAL, bad
+    def scan(call, dtype=0, tokens=8, seqs=2, ch=4, table=0, z=p, ldz=4, x=p, ldx=4, h=p, ldh=4, h0=0, last=0, dh=p, lddh=4, dz=p,
+             lddz=4, dx=p, lddx=4, dlast=0, dh0=0):
+        return call(B.SCAN.pack(dtype, seqs, ch, 0, tokens, table, z, ldz, x, ldx, h, ldh, h0, last, dh, lddh, dz, lddz, dx, lddx,
+                                dlast, dh0), None)
+    both = [dict(dtype=3), dict(dtype=-1), dict(tokens=-1), dict(tokens=7), dict(tokens=1 << 31), dict(seqs=0), dict(seqs=-1), dict(ch=0),
+            dict(ch=-4), dict(ldz=3), dict(ldx=0), dict(ldh=-4), dict(z=0), dict(x=0), dict(h=0), dict(x=p + 2), dict(dtype=1, h=p + 1),
+            dict(table=p + 2), dict(h0=p + 1)]
+    for bad in both + [dict(last=p + 2)]:
+        assert scan(B._lib.dgc_gated_scan_forward, **bad) == B.EINVAL, bad
+    for bad in both + [dict(dh=0), dict(dz=0), dict(dx=0), dict(lddh=3), dict(lddz=3), dict(lddx=3), dict(dh=p + 1), dict(dlast=p + 1),
+                       dict(dh0=p + 2)]:
+        assert scan(B._lib.dgc_gated_scan_backward, **bad) == B.EINVAL, bad
 
-    def bwd(dtype=0, tokens=8, seqs=2, ch=4, ld=4, dh=p, dx=p):
-        return lib.dgc_gated_scan_backward(dtype, tokens, seqs, ch, null, 0, p, 4, p, 4, null, p, 4, dh, ld, null, p, 4, dx, 4, null, null)
-    for bad in (dict(dtype=9), dict(tokens=9), dict(seqs=-1), dict(ch=-4), dict(ld=2), dict(dh=null), dict(dx=null), dict(dh=ctypes.c_void_p(4097))):
-        assert bwd(**bad) == B.EINVAL, bad
-
-    def step(dtype=0, rows=2, ch=4, ld=4, state=p, slots=null, n=2):
-        return lib.dgc_gated_scan_step(dtype, rows, ch, p, ld, p, 4, state, slots, n, p, 4, null)
-    for bad in (dict(dtype=5), dict(rows=-1), dict(ch=0), dict(ld=1), dict(state=null), dict(n=1), dict(n=-1), dict(slots=ctypes.c_void_p(4097))):
+    def step(dtype=0, rows=2, ch=4, n=2, z=p, ldz=4, x=p, ldx=4, out=p, ldo=4, state=p, slots=0):
+        return B._lib.dgc_gated_scan_step(B.SCAN_ONE.pack(dtype, rows, ch, n, z, ldz, x, ldx, out, ldo, state, slots), None)
+    for bad in (dict(dtype=5), dict(rows=-1), dict(ch=0), dict(ldz=1), dict(ldx=3), dict(ldo=2), dict(z=0), dict(x=p + 2), dict(out=0),
+                dict(state=0), dict(state=p + 2), dict(n=1), dict(n=-1), dict(slots=p + 1)):
         assert step(**bad) == B.EINVAL, bad
-    assert step(rows=0) == B.OK and fwd(tokens=0) == B.OK
+    assert step(rows=0) == B.OK and scan(B._lib.dgc_gated_scan_forward, tokens=0) == B.OK
+    assert scan(B._lib.dgc_gated_scan_backward, tokens=0) == B.OK
+    for call in (B._lib.dgc_gated_scan_forward, B._lib.dgc_gated_scan_backward, B._lib.dgc_gated_scan_step):
+        assert call(None, None) == B.EINVAL
 
 
 @pytest.mark.gpu
