@@ -10,10 +10,12 @@
 // reads the row again (out of L2: the block has just read it) and writes p scaled; the few places
 // that the list and the label name are then written once more with their q taken off.
 //
-// Exponentials are 2^((s - m) c), c = log2(e) / T, with m the row's maximum: the difference comes
-// first, so that rows of very large or very low logits (a mask of the type's lowest value in
-// every place) lose nothing and cannot overflow.  Sums are 32-bit: a thread adds at most a few
-// hundred terms, the rest is a tree.
+// Exponentials are 2^(s c - round(m c)), c = log2(e) / T, m the row's maximum: the rounding of m c is
+// the same factor in every term and cancels in p, and where the loss needs logarithms the same
+// expression is used.  Rows whose maximum is out of the range where m c is safe (a mask of the
+// type's lowest value in every place) or that hold no finite number are found by their sum and
+// done again as 2^((s - m) c).  Sums are 32-bit: a thread adds at most a few hundred terms, the
+// rest is a tree.
 
 #include <cooperative_groups.h>
 
@@ -44,25 +46,29 @@ struct DistillArgs {
   float *loss, *lse;
   int64_t ld, ld_d;
   float temperature, c, soft, hard;   // c = log2(e) / temperature
+  float lowest;                       // below it, and above its opposite, exponents are taken with care
   int32_t vocab, k, cluster;
 };
 
-// Running maximum and sums of exponentials under it (s1: at temperature 1, where it differs).
-// The maximum starts at the lowest finite value, so that rows of -infinity sum to zero.
-template <bool TWO>
+// A maximum and the sums of exponentials under it (s1: at temperature 1, where it differs).
+// CAREFUL: exponents are (s - m) c, in any range; else s c - m c, see above.
+template <bool TWO, bool CAREFUL>
 struct Sums {
-  float m = -FLT_MAX, s = 0.0f, s1 = 0.0f;
+  float m, s = 0.0f, s1 = 0.0f;
+  __device__ __forceinline__ explicit Sums(float lowest) : m(lowest) {}
   __device__ __forceinline__ void scale_to(float to, float c) {
-    s *= exp2_fast((m - to) * c);
-    if (TWO) s1 *= exp2_fast((m - to) * kLog2e);
+    s *= exp2_fast(CAREFUL ? (m - to) * c : __fadd_rn(__fmul_rn(m, c), -__fmul_rn(to, c)));
+    if (TWO) s1 *= exp2_fast(CAREFUL ? (m - to) * kLog2e : __fadd_rn(__fmul_rn(m, kLog2e), -__fmul_rn(to, kLog2e)));
     m = to;
   }
-  // joins the pairs of `width` neighbouring lanes; every lane gets the result
-  __device__ __forceinline__ void join(int width, float c) {
+  // joins what the warp's lanes hold; every lane gets the result
+  __device__ __forceinline__ void join(float c) {
     float top = m;
-    for (int d = width / 2; d; d /= 2) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+#pragma unroll
+    for (int d = 16; d; d /= 2) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
     scale_to(top, c);
-    for (int d = width / 2; d; d /= 2) {
+#pragma unroll
+    for (int d = 16; d; d /= 2) {
       s += __shfl_xor_sync(0xFFFFFFFFu, s, d);
       if (TWO) s1 += __shfl_xor_sync(0xFFFFFFFFu, s1, d);
     }
@@ -72,58 +78,94 @@ struct Sums {
 template <int NT>
 struct DistillShared {
   float3 row[NT / 32], part[kMaxCluster];   // maximum, sum, sum at temperature 1
-  float2 teacher[NT / 32];
-  float loss[NT / 32];
+  float2 teacher[DGC_MAX_TOP / 32];
+  float loss[DGC_MAX_TOP / 32];
   int idx[DGC_MAX_TOP];
   float q[DGC_MAX_TOP];
 };
 
+// Chunks of a thread under way at once, and blocks of 256 threads an SM.  The loss alone reads
+// memory only: more blocks hide more (4096 x 50021 bf16: 72 us with five, 83 with four of more
+// registers).  The gradient's second walk lives on L2, which more rows in work at once would not
+// fit (168 us with four, 206 with five); 32-bit rows have half the arithmetic to a byte and gain
+// from more loads instead (2048 x 32768: 104 us with eight and three, 120 with four and four).
+template <class T, int MODE> constexpr int kAhead = sizeof(T) == 4 && MODE != kForward ? 8 : 4;
+template <class T, int MODE> constexpr int kBlocks = MODE == kForward ? 5 : sizeof(T) == 4 ? 3 : 4;
+
 template <class T, int NT, int MODE, bool TWO>
-#ifndef DB
-#define DB 2
-#endif
-__global__ void __launch_bounds__(NT, DB * 512 / NT) k_distill(const DistillArgs a) {
+__global__ void __launch_bounds__(NT, kBlocks<T, MODE>) k_distill(const DistillArgs a) {
   pdl_enter();
-  constexpr int E = Row<T>::E, W = NT / 32, U = 4;
+  constexpr int E = Row<T>::E, W = NT / 32, U = kAhead<T, MODE>;
   __shared__ DistillShared<NT> sm;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int ncl = a.cluster, rank = ncl > 1 ? (int)(blockIdx.x % ncl) : 0;
-  const int64_t r = blockIdx.x / ncl;
+  const int ncl = a.cluster;
+  Part part = part_of(ncl);
+  const int64_t r = part.row;
   const Row<T> row(static_cast<const T*>(a.logits) + r * a.ld, a.vocab);
-  const int lo = (int)((int64_t)row.chunks * rank / ncl), hi = (int)((int64_t)row.chunks * (rank + 1) / ncl);
+  take_part(part, row, ncl);
+  const int rank = part.rank, lo = part.lo, hi = part.hi;
 
-  // the teacher's entry and the student's logit of thread k, the label
-  int mine = -1;
-  float t = -INFINITY, sk = 0.0f, sy = 0.0f;
+  // the teacher's entry of thread k, the label: on their way while the row is walked
+  int mine = -1, y = -1;
+  float t = -INFINITY, sk = 0.0f, sy = 0.0f, w = 0.0f;
   if (tid < a.k) {
     mine = a.idx[r * a.k + tid];
     t = a.val[r * a.k + tid];
+  }
+  if (a.labels) y = a.labels[r];
+  if (MODE != kForward) w = a.dloss[r];
+  // and, after the walk, the student's logits there (the row is then in L2)
+  const auto pick = [&] {
     if (mine < 0 || mine >= a.vocab || !(t > -INFINITY)) mine = -1;
     else sk = to_float<T>(row.p[mine]);
-  }
-  int y = a.labels ? a.labels[r] : -1;
-  if (y < 0 || y >= a.vocab) y = -1;
-  else sy = to_float<T>(row.p[y]);
-  const float w = MODE == kForward ? 0.0f : a.dloss[r];
+    if (y < 0 || y >= a.vocab) y = -1;
+    else sy = to_float<T>(row.p[y]);
+  };
 
-  Sums<false> te;
-  if (mine >= 0) { te.m = fmaxf(t, -FLT_MAX); te.s = 1.0f; }
-  te.join(32, a.c);
-  if (lane == 0) sm.teacher[warp] = make_float2(te.m, te.s);
-
-  // p = 2^((s - m) c) / sum,  p1 = 2^((s - m1) log2 e) / sum1
-  float m = 0.0f, m1 = 0.0f, sum = 1.0f, sum1 = 1.0f;
-  bool walk = MODE != kBackward;
+  // p = 2^(s c - mc) / sum,  p1 = 2^(s log2(e) - mc1) / sum1;  careful: 2^((s - m) c) and so on
+  float m = 0.0f, mc = 0.0f, mc1 = 0.0f, sum = 1.0f, sum1 = 1.0f;
+  bool careful = false, walk = MODE != kBackward;
   if (MODE == kBackward) {
     const float2 lse = make_float2(a.lse_in[2 * r], a.lse_in[2 * r + 1]);
-    m = lse.x * a.temperature;
-    m1 = lse.y;
+    mc = lse.x * kLog2e;
+    mc1 = lse.y * kLog2e;
     // 32 bits of a large logarithm are too few for p: such rows are summed once more
     walk = !(fabsf(lse.x) < kLseExact && fabsf(lse.y) < kLseExact);
   }
+  // joins the threads' sums over the row's blocks
+  const auto over_row = [&](auto st) {
+    using S = decltype(st);
+    st.join(a.c);
+    if (lane == 0) sm.row[warp] = make_float3(st.m, st.s, st.s1);
+    __syncthreads();
+    const float lowest = sm.row[0].x;   // (any of the maxima will do for lanes without one)
+    st = S(lowest);
+    if (lane < W) { st.m = sm.row[lane].x; st.s = sm.row[lane].y; st.s1 = sm.row[lane].z; }
+    st.join(a.c);
+    if (ncl > 1) {
+      cg::cluster_group cl = cg::this_cluster();
+      cl.sync();   // every block of the cluster runs
+      if (tid < ncl) cl.map_shared_rank(&sm, tid)->part[rank] = make_float3(st.m, st.s, st.s1);
+      cl.sync();
+      st = S(sm.part[0].x);
+      if (lane < ncl) { st.m = sm.part[lane].x; st.s = sm.part[lane].y; st.s1 = sm.part[lane].z; }
+      st.join(a.c);
+    }
+    return st;
+  };
+  const auto teacher = [&] {   // (after the walk: the list's way from memory is then long over)
+    if (warp * 32 < a.k) {
+      Sums<false, true> te(-FLT_MAX);
+      if (mine >= 0) { te.m = fmaxf(t, -FLT_MAX); te.s = 1.0f; }
+      te.join(a.c);
+      if (lane == 0) sm.teacher[warp] = make_float2(te.m, te.s);
+    }
+  };
   if (walk) {   // (the same for all threads of the row)
-    Sums<TWO> st;
+    Sums<TWO, false> st(a.lowest);
     Val<2> s2 = fill<2>(0.0f), s1 = fill<2>(0.0f);   // (sums of the even and the odd places)
+    Val<2> minus = fill<2>(-(st.m * a.c)), minus1 = fill<2>(-(st.m * kLog2e));
+    const Val<2> c = fill<2>(a.c), c1 = fill<2>(kLog2e);
     each_group<T, NT, U>(row, lo, hi, [&](const uint4 (&x)[U], int, int count) {
       uint32_t best = max_word<T, false>(x[0]);
 #pragma unroll
@@ -131,11 +173,13 @@ __global__ void __launch_bounds__(NT, DB * 512 / NT) k_distill(const DistillArgs
         if (u < count) best = max_words<T, false>(best, max_word<T, false>(x[u]));
       const float top = max_of_word<T, false>(best);
       if (top > st.m) {
-        s2 = mul_(s2, fill<2>(exp2_fast((st.m - top) * a.c)));
-        if (TWO) s1 = mul_(s1, fill<2>(exp2_fast((st.m - top) * kLog2e)));
+        const Val<2> now = fill<2>(-(top * a.c)), now1 = fill<2>(-(top * kLog2e));
+        s2 = mul_(s2, fill<2>(exp2_fast(now.v[0] - minus.v[0])));
+        if (TWO) s1 = mul_(s1, fill<2>(exp2_fast(now1.v[0] - minus1.v[0])));
         st.m = top;
+        minus = now;
+        minus1 = now1;
       }
-      const Val<2> minus = fill<2>(-st.m);
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         if (u >= max(count, 1)) continue;
@@ -143,70 +187,86 @@ __global__ void __launch_bounds__(NT, DB * 512 / NT) k_distill(const DistillArgs
         pairs_of<T>(x[u], v);
 #pragma unroll
         for (int i = 0; i < E / 2; ++i) {
-          const Val<2> d = add_(v[i], minus), e = mul_(d, fill<2>(a.c));
+          const Val<2> e = fma_(v[i], c, minus);
           s2 = add_(s2, Val<2>{{exp2_fast(e.v[0]), exp2_fast(e.v[1])}});
           if (TWO) {
-            const Val<2> e1 = mul_(d, fill<2>(kLog2e));
+            const Val<2> e1 = fma_(v[i], c1, minus1);
             s1 = add_(s1, Val<2>{{exp2_fast(e1.v[0]), exp2_fast(e1.v[1])}});
           }
         }
       }
     });
+    pick();
     st.s = s2.v[0] + s2.v[1];
     st.s1 = s1.v[0] + s1.v[1];
-    st.join(32, a.c);
-    if (lane == 0) sm.row[warp] = make_float3(st.m, st.s, st.s1);
-    __syncthreads();
-    st = Sums<TWO>();
-    if (lane < W) { st.m = sm.row[lane].x; st.s = sm.row[lane].y; st.s1 = sm.row[lane].z; }
-    st.join(32, a.c);
-    if (ncl > 1) {
-      cg::cluster_group cl = cg::this_cluster();
-      cl.sync();   // every block of the cluster runs
-      if (tid < ncl) cl.map_shared_rank(&sm, tid)->part[rank] = make_float3(st.m, st.s, st.s1);
-      cl.sync();
-      st = Sums<TWO>();
-      if (lane < ncl) { st.m = sm.part[lane].x; st.s = sm.part[lane].y; st.s1 = sm.part[lane].z; }
-      st.join(32, a.c);
-    }
-    m = m1 = st.m;
+    teacher();
+    st = over_row(st);
+    mc = st.m * a.c;
+    mc1 = st.m * kLog2e;
     sum = st.s;
     sum1 = TWO ? st.s1 : st.s;
-  } else {
-    __syncthreads();
-  }
-  te = Sums<false>();
-  if (lane < W) { te.m = sm.teacher[lane].x; te.s = sm.teacher[lane].y; }
-  te.join(32, a.c);
-
-  const bool taught = te.s > 0.0f, labelled = y >= 0;
-  float q = 0.0f, logq = 0.0f;
-  if (mine >= 0) {
-    const float x = (fmaxf(t, -FLT_MAX) - te.m) * a.c;
-    q = __fdividef(exp2_fast(x), te.s);
-    logq = x * kLn2 - logf(te.s);
-  }
-  if (MODE != kBackward && rank == 0) {
-    float part = 0.0f;
-    if (!(q <= 0.0f)) {
-      const float logp = sk == -INFINITY ? -INFINITY : (sk - m) * a.c * kLn2 - logf(sum);
-      part = q * (logq - logp);
-    }
+    careful = !(sum > 0.0f && fabsf(st.m) < -a.lowest);
+    if (careful) {   // (the same for all threads of the row) out of the ordinary range, or not finite
+      __syncthreads();
+      Sums<TWO, true> ca(-FLT_MAX);
+      each_group<T, NT, 1>(row, lo, hi, [&](const uint4 (&x)[1], int, int) {
+        Val<2> v[E / 2];
+        pairs_of<T>(x[0], v);
+        const float top = max_of_word<T, false>(max_word<T, false>(x[0]));
+        if (top > ca.m) ca.scale_to(top, a.c);
 #pragma unroll
-    for (int d = 16; d; d /= 2) part += __shfl_xor_sync(0xFFFFFFFFu, part, d);
-    if (lane == 0) sm.loss[warp] = part;
+        for (int i = 0; i < E; ++i) {
+          const float d = v[i / 2].v[i % 2] - ca.m;
+          ca.s += exp2_fast(d * a.c);
+          if (TWO) ca.s1 += exp2_fast(d * kLog2e);
+        }
+      });
+      ca = over_row(ca);
+      m = ca.m;
+      sum = ca.s;
+      sum1 = TWO ? ca.s1 : ca.s;
+    }
+  } else {
+    pick();
+    teacher();
     __syncthreads();
-    if (tid == 0) {
-      float soft = 0.0f;
-      for (int i = 0; i < W; ++i) soft += sm.loss[i];
-      float loss = taught ? a.soft * a.temperature * a.temperature * soft : 0.0f;
-      if (labelled && a.hard != 0.0f)
-        loss -= a.hard * (sy == -INFINITY ? -INFINITY : (sy - m1) - logf(sum1));
-      a.loss[r] = loss;
-      if (MODE == kForward && a.lse) {
-        a.lse[2 * r] = sum == 0.0f ? -INFINITY : m / a.temperature + logf(sum);
-        a.lse[2 * r + 1] = TWO ? (sum1 == 0.0f ? -INFINITY : m1 + logf(sum1)) : a.lse[2 * r];
-      }
+  }
+  const auto exponent = [&](float v) { return careful ? (v - m) * a.c : fmaf(v, a.c, -mc); };
+  const auto exponent1 = [&](float v) { return careful ? (v - m) * kLog2e : fmaf(v, kLog2e, -mc1); };
+
+  float tm = -FLT_MAX, ts = 0.0f;   // the teacher's maximum and sum
+  for (int i = 0; i * 32 < a.k; ++i) tm = fmaxf(tm, sm.teacher[i].x);
+  for (int i = 0; i * 32 < a.k; ++i) ts += sm.teacher[i].y * exp2_fast((sm.teacher[i].x - tm) * a.c);
+  const bool taught = ts > 0.0f, labelled = y >= 0;
+  float q = 0.0f;
+  if (warp * 32 < a.k) {
+    float logq = 0.0f;
+    if (mine >= 0) {
+      const float x = (fmaxf(t, -FLT_MAX) - tm) * a.c;
+      q = __fdividef(exp2_fast(x), ts);
+      logq = x * kLn2 - logf(ts);
+    }
+    if (MODE != kForward && tid < a.k) { sm.idx[tid] = mine; sm.q[tid] = q; }
+    if (MODE != kBackward && rank == 0) {
+      float kl = 0.0f;
+      if (!(q <= 0.0f)) kl = q * (logq - (sk == -INFINITY ? -INFINITY : exponent(sk) * kLn2 - logf(sum)));
+#pragma unroll
+      for (int d = 16; d; d /= 2) kl += __shfl_xor_sync(0xFFFFFFFFu, kl, d);
+      if (lane == 0) sm.loss[warp] = kl;
+    }
+  }
+  __syncthreads();   // (also: the listed logits are in registers, their places may be overwritten)
+  if (MODE != kBackward && rank == 0 && tid == 0) {
+    float soft = 0.0f;
+    for (int i = 0; i * 32 < a.k; ++i) soft += sm.loss[i];
+    float loss = taught ? a.soft * a.temperature * a.temperature * soft : 0.0f;
+    if (labelled && a.hard != 0.0f)
+      loss -= a.hard * (sy == -INFINITY ? -INFINITY : exponent1(sy) * kLn2 - logf(sum1));
+    a.loss[r] = loss;
+    if (MODE == kForward && a.lse) {
+      const float lse = sum == 0.0f ? -INFINITY : (careful ? m / a.temperature : mc * kLn2) + logf(sum);
+      a.lse[2 * r] = lse;
+      a.lse[2 * r + 1] = !TWO ? lse : sum1 == 0.0f ? -INFINITY : (careful ? m : mc1 * kLn2) + logf(sum1);
     }
   }
   if (MODE == kForward) return;
@@ -218,41 +278,53 @@ __global__ void __launch_bounds__(NT, DB * 512 / NT) k_distill(const DistillArgs
   if (sum == 0.0f) coef = coef1 = 0.0f;   // a row of -infinity: p is 0
   const bool zero = wq == 0.0f && wy == 0.0f;
   if (!TWO) coef += coef1;
-  auto grad = [&](float v) {
-    float g = exp2_fast((v - m) * a.c) * coef;
-    if (TWO) g = fmaf(exp2_fast((v - m1) * kLog2e), coef1, g);
+  const auto grad = [&](float v) {
+    float g = exp2_fast(exponent(v)) * coef;
+    if (TWO) g = fmaf(exp2_fast(exponent1(v)), coef1, g);
     return g;
   };
-  if (tid < a.k) { sm.idx[tid] = mine; sm.q[tid] = q; }
   T* out = static_cast<T*>(a.dlogits) + r * a.ld_d;
   const bool same = (reinterpret_cast<uintptr_t>(out) & 15u) == (reinterpret_cast<uintptr_t>(row.p) & 15u);
-  __syncthreads();   // the listed logits are in registers: their places may be overwritten
-  each_group<T, NT, U>(row, lo, hi, [&](const uint4 (&x)[U], int j, int count) {
+  const auto put = [&](const Val<2> (&v)[E / 2], int e0, bool whole) {
+    if (whole && same) {
+      __stcs(reinterpret_cast<uint4*>(out + e0), chunk_of<T>(v));   // (not to be read again here: the rows are)
+    } else {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (u >= max(count, 1)) continue;
-      Val<2> v[E / 2];
-      pairs_of<T>(x[u], v);
-#pragma unroll
-      for (int i = 0; i < E / 2; ++i) {
-        const Val<2> s = v[i], e = mul_(add_(s, fill<2>(-m)), fill<2>(a.c));
-        v[i] = mul_(Val<2>{{exp2_fast(e.v[0]), exp2_fast(e.v[1])}}, fill<2>(coef));
-        if (TWO) {
-          const Val<2> e1 = mul_(add_(s, fill<2>(-m1)), fill<2>(kLog2e));
-          v[i] = fma_(Val<2>{{exp2_fast(e1.v[0]), exp2_fast(e1.v[1])}}, fill<2>(coef1), v[i]);
-        }
-        if (zero) v[i] = fill<2>(0.0f);
-      }
-      const int e0 = row.first(j + u * NT);
-      if (count > 0 && same) {
-        *reinterpret_cast<uint4*>(out + e0) = chunk_of<T>(v);
-      } else {
-#pragma unroll
-        for (int i = 0; i < E; ++i)
-          if (e0 + i >= 0 && e0 + i < a.vocab) store_one<T>(out + e0 + i, v[i / 2].v[i % 2]);
-      }
+      for (int i = 0; i < E; ++i)
+        if (e0 + i >= 0 && e0 + i < a.vocab) store_one<T>(out + e0 + i, v[i / 2].v[i % 2]);
     }
-  });
+  };
+  if (careful || zero) {
+    each_group<T, NT, 1>(row, lo, hi, [&](const uint4 (&x)[1], int j, int count) {
+      Val<2> v[E / 2];
+      pairs_of<T>(x[0], v);
+#pragma unroll
+      for (int i = 0; i < E; ++i) v[i / 2].v[i % 2] = zero ? 0.0f : grad(v[i / 2].v[i % 2]);
+      put(v, row.first(j), count > 0);
+    });
+  } else {
+    const Val<2> c = fill<2>(a.c), minus = fill<2>(-mc), k = fill<2>(coef);
+    const Val<2> c1 = fill<2>(kLog2e), minus1 = fill<2>(-mc1), k1 = fill<2>(coef1);
+    each_group<T, NT, U>(row, lo, hi, [&](const uint4 (&x)[U], int j, int count) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (u >= max(count, 1)) continue;
+        Val<2> v[E / 2];
+        pairs_of<T>(x[u], v);
+#pragma unroll
+        for (int i = 0; i < E / 2; ++i) {
+          const Val<2> e = fma_(v[i], c, minus);
+          Val<2> g = mul_(Val<2>{{exp2_fast(e.v[0]), exp2_fast(e.v[1])}}, k);
+          if (TWO) {
+            const Val<2> e1 = fma_(v[i], c1, minus1);
+            g = fma_(Val<2>{{exp2_fast(e1.v[0]), exp2_fast(e1.v[1])}}, k1, g);
+          }
+          v[i] = g;
+        }
+        put(v, row.first(j + u * NT), count > 0);
+      }
+    });
+  }
   if (zero) return;
   __syncthreads();
   const int e_lo = max(row.first(lo), 0), e_hi = hi == row.chunks ? a.vocab : row.first(hi);
@@ -278,25 +350,24 @@ __global__ void __launch_bounds__(NT, DB * 512 / NT) k_distill(const DistillArgs
 }
 
 template <class T, int MODE, bool TWO>
-void go(const DistillArgs& a, int64_t rows, cudaStream_t s) {
-  const dim3 grid((unsigned)(rows * a.cluster));
-  if (a.vocab <= 4096) launch_cluster(k_distill<T, 256, MODE, TWO>, grid, 256, 0, s, (unsigned)a.cluster, a);
-#ifndef DNT
-#define DNT 512
-#endif
-  else launch_cluster(k_distill<T, DNT, MODE, TWO>, grid, DNT, 0, s, (unsigned)a.cluster, a);
-}
-
-template <class T>
-int32_t enqueue(DistillArgs a, int mode, int64_t rows, cudaStream_t s) {
+int32_t choose(DistillArgs a, int64_t rows, cudaStream_t s) {
+  constexpr int NT = 256;
+  // blocks for a row: few rows are spread over the SMs
   a.cluster = 1;
   while (a.cluster < kMaxCluster && rows * a.cluster < 148 && a.vocab / a.cluster > 8192) a.cluster *= 2;
   if (rows * a.cluster > INT32_MAX) return DGC_EINVAL;
-  const bool two = a.labels && a.hard != 0.0f && a.temperature != 1.0f;
-  if (mode == kForward) two ? go<T, kForward, true>(a, rows, s) : go<T, kForward, false>(a, rows, s);
-  else if (mode == kBackward) two ? go<T, kBackward, true>(a, rows, s) : go<T, kBackward, false>(a, rows, s);
-  else two ? go<T, kBoth, true>(a, rows, s) : go<T, kBoth, false>(a, rows, s);
+  const dim3 grid((unsigned)(rows * a.cluster));
+  if (a.cluster > 1) launch_cluster(k_distill<T, NT, MODE, TWO>, grid, NT, 0, s, (unsigned)a.cluster, a);
+  else launch(k_distill<T, NT, MODE, TWO>, grid, NT, 0, s, a);
   return check_launch();
+}
+
+template <class T>
+int32_t enqueue(const DistillArgs& a, int mode, int64_t rows, cudaStream_t s) {
+  const bool two = a.labels && a.hard != 0.0f && a.temperature != 1.0f;
+  if (mode == kForward) return two ? choose<T, kForward, true>(a, rows, s) : choose<T, kForward, false>(a, rows, s);
+  if (mode == kBackward) return two ? choose<T, kBackward, true>(a, rows, s) : choose<T, kBackward, false>(a, rows, s);
+  return two ? choose<T, kBoth, true>(a, rows, s) : choose<T, kBoth, false>(a, rows, s);
 }
 
 int32_t distill(int mode, const dgc_distill* d, void* stream) {
@@ -318,6 +389,7 @@ int32_t distill(int mode, const dgc_distill* d, void* stream) {
   a.logits = d->logits.data; a.ld = d->logits.ld; a.idx = d->idx; a.val = d->val; a.labels = d->labels;
   a.vocab = d->vocab; a.k = d->k; a.temperature = d->temperature; a.soft = d->soft_weight; a.hard = d->hard_weight;
   a.c = (float)(1.4426950408889634 / (double)d->temperature);
+  a.lowest = -1e30f / std::max(1.0f, a.c);
   a.loss = d->loss; a.lse = d->lse; a.lse_in = d->lse; a.dloss = d->dloss;
   a.dlogits = d->dlogits.data; a.ld_d = d->dlogits.ld;
   cudaStream_t s = as_stream(stream);

@@ -23,6 +23,19 @@ struct Row {
   __device__ __forceinline__ int first(int chunk) const { return chunk * E - shift; }
 };
 
+// A cluster's block: its row, its place, and its part [lo, hi) of the row's chunks.  (A division
+// of 64-bit numbers here would cost a warp more than its share of a row of 10 KB.)
+struct Part { int64_t row; int rank, lo, hi; };
+__device__ __forceinline__ Part part_of(unsigned ncl) {
+  if (ncl == 1) return Part{(int64_t)blockIdx.x, 0, 0, 0};
+  return Part{(int64_t)(blockIdx.x / ncl), (int)(blockIdx.x % ncl), 0, 0};
+}
+template <class T>
+__device__ __forceinline__ void take_part(Part& p, const Row<T>& row, unsigned ncl) {   // chunks < 2^29, ncl <= 8
+  p.lo = ncl == 1 ? 0 : (int)((unsigned)row.chunks * (unsigned)p.rank / ncl);
+  p.hi = ncl == 1 ? row.chunks : (int)((unsigned)row.chunks * (unsigned)(p.rank + 1) / ncl);
+}
+
 template <class T>
 __device__ __forceinline__ void store_one(T* p, float v) {
   const float one[1] = {v};
@@ -92,30 +105,11 @@ __device__ __forceinline__ float max_of_word(uint32_t w) {
   }
 }
 
-// f(chunks, first chunk, count) for the chunks [lo, hi) of a row, dealt to the block's NT threads
-// in turn, U at a time: their loads are under way at once; chunk u is the first + u NT, and the
-// first `count` are there.  A chunk that lies partly outside the row comes alone, as
-// f(chunks, chunk, 0), with -infinity in the places outside.  Plain loads (not the read-only
-// path): the gradient may be written over the logits.
+// The chunks among [lo, hi) that lie partly outside the row, for f as below.
 template <class T, int NT, int U, class F>
-__device__ __forceinline__ void each_group(const Row<T>& r, int lo, int hi, F&& f) {
+__device__ __forceinline__ void odd_chunks(const Row<T>& r, int lo, int hi, bool tail, uint4 (&w)[U], F&& f) {
   constexpr int E = Row<T>::E;
   const int tid = threadIdx.x;
-  const bool tail = (r.n + r.shift) % E != 0;
-  const int a = max(lo, r.shift ? 1 : 0), b = min(hi, r.chunks - (tail ? 1 : 0));
-  uint4 w[U];
-  int j = a + tid;
-  for (; j + (U - 1) * NT < b; j += NT * U) {
-#pragma unroll
-    for (int u = 0; u < U; ++u) w[u] = r.base[j + u * NT];
-    f(w, j, U);
-  }
-  if (j < b) {
-#pragma unroll
-    for (int u = 0; u < U - 1; ++u)
-      if (j + u * NT < b) w[u] = r.base[j + u * NT];
-    f(w, j, (b - 1 - j) / NT + 1);
-  }
   int odd = -1;   // the chunks that are partly outside: one for thread 0, one for the last thread
   if (tid == 0 && lo == 0 && hi > 0 && r.shift) odd = 0;
   if (tid == NT - 1 && hi == r.chunks && lo < hi && tail && !(r.chunks == 1 && r.shift)) odd = r.chunks - 1;
@@ -137,6 +131,41 @@ __device__ __forceinline__ void each_group(const Row<T>& r, int lo, int hi, F&& 
     w[0] = make_uint4(u[0], u[1], u[2], u[3]);
     f(w, odd, 0);
   }
+}
+
+// f(chunks, first chunk, count) for the chunks [lo, hi) of a row, dealt to the block's NT threads
+// in turn, U at a time: their loads are under way at once; chunk u is the first + u NT, and the
+// first `count` are there.  A chunk that lies partly outside the row comes alone, as
+// f(chunks, chunk, 0), with -infinity in the places outside.  Plain loads (not the read-only
+// path): the gradient may be written over the logits.
+// Groups for which `wanted()` is false are left out (it is asked once a group, in order; a chunk
+// partly outside comes in any case).
+template <class T, int NT, int U, class W, class F>
+__device__ __forceinline__ void each_group_if(const Row<T>& r, int lo, int hi, W&& wanted, F&& f) {
+  constexpr int E = Row<T>::E;
+  const int tid = threadIdx.x;
+  const bool tail = (r.n + r.shift) % E != 0;
+  const int a = max(lo, r.shift ? 1 : 0), b = min(hi, r.chunks - (tail ? 1 : 0));
+  uint4 w[U];
+  int j = a + tid;
+  for (; j + (U - 1) * NT < b; j += NT * U) {
+    if (!wanted()) continue;
+#pragma unroll
+    for (int u = 0; u < U; ++u) w[u] = r.base[j + u * NT];
+    f(w, j, U);
+  }
+  if (j < b && wanted()) {
+#pragma unroll
+    for (int u = 0; u < U - 1; ++u)
+      if (j + u * NT < b) w[u] = r.base[j + u * NT];
+    f(w, j, (b - 1 - j) / NT + 1);
+  }
+  odd_chunks<T, NT, U>(r, lo, hi, tail, w, f);
+}
+
+template <class T, int NT, int U, class F>
+__device__ __forceinline__ void each_group(const Row<T>& r, int lo, int hi, F&& f) {
+  each_group_if<T, NT, U>(r, lo, hi, [] { return true; }, f);
 }
 
 }  // namespace dgc

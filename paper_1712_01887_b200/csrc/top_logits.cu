@@ -3,16 +3,22 @@
 // The list is in the library's form, (int32 index, fp32 value), largest value first and the
 // lowest index first among equals.  A row is read once from memory:
 //
-//   1. every thread takes the maximum of the elements it is dealt;
-//   2. the k-th largest of these maxima is a bound that at least k elements reach, and that
-//      few others do (about k + k^2 / 2 threads of them when the row is in no special order);
-//   3. the threads whose maximum reaches it, and only those, look at their elements again
-//      (k of the block's threads, out of L2) and list the ones that reach it;
+//   1. every thread takes the maximum of the elements it is dealt, and of each group of them;
+//   2. the k-th largest of the threads' maxima is a bound that at least k elements reach, and
+//      that few others do (74 in all for k = 64 and 256 threads when the row is in no special
+//      order), found bit by bit with a counting barrier each;
+//   3. the groups whose maximum reaches it, and only those, are looked at again (out of L2),
+//      and the elements that reach it are listed;
 //   4. a listed entry's place is the number of listed entries that come before it.
 //
 // Where more entries reach the bound than the list holds (a row of equal values, an order that
 // deals all large values to a few threads), the k-th value is found by bisection over the row,
 // then its equals are taken in index order: slow, and always right.
+//
+// What bounds it: memory, and the latency of the steps between (4096 x 50021 bf16, k = 64: 91 us,
+// 4.5 TB/s of the 6.6 measured for a copy).  Five blocks of 256 threads an SM hide that better than
+// two of 512 (134 us); looking at whole rows again in step 3 took 107 us; the code that looks at one
+// chunk is there once and not unrolled over a group (170 us: it did not fit the instruction cache).
 
 #include <cooperative_groups.h>
 
@@ -25,8 +31,7 @@ using namespace dgc;
 
 namespace {
 
-constexpr int kTopThreads = 512;
-constexpr int kTopList = 4096;            // candidates a block can hold
+template <int NT> constexpr int kTopGroups = NT == 512 ? 4 : 8;
 constexpr int kTopRank = 512;             // up to this many are ranked directly
 constexpr uint32_t kLowest = 0x00800000u; // order key of the lowest finite value; -infinity is below
 
@@ -45,16 +50,18 @@ __device__ __forceinline__ unsigned long long entry(uint32_t key, int index) {
   return ((unsigned long long)key << 32) | (0xFFFFFFFFu - (uint32_t)index);
 }
 
+template <int NT, int LIST>   // LIST: candidates a block can hold
 struct TopShared {
-  unsigned long long list[kTopList];
+  uint32_t groups[kTopGroups<NT>][NT];   // a thread's maxima by group of chunks; the last slot takes the rest
+  unsigned long long list[LIST];
   unsigned long long best[DGC_MAX_TOP];
   uint2 range[32];
   int count, total[2];
 };
 
 // Sum over the block of a per-thread count.
-template <int NT>
-__device__ __forceinline__ int block_sum(int v, TopShared& sm, int par) {
+template <int NT, int LIST>
+__device__ __forceinline__ int block_sum(int v, TopShared<NT, LIST>& sm, int par) {
   v = __reduce_add_sync(0xFFFFFFFFu, v);
   if (threadIdx.x == 0) sm.total[par] = 0;
   __syncthreads();
@@ -67,8 +74,8 @@ __device__ __forceinline__ int block_sum(int v, TopShared& sm, int par) {
 // lowest finite key otherwise: the k-th largest key, cut off below the bits that a type's
 // rounding leaves (f32: ten bits of fraction are near enough).  The search starts below the bits
 // that all keys have in common.
-template <class T, int NT>
-__device__ __forceinline__ uint32_t kth_largest(uint32_t key, int k, TopShared& sm) {
+template <class T, int NT, int LIST>
+__device__ __forceinline__ uint32_t kth_largest(uint32_t key, int k, TopShared<NT, LIST>& sm) {
   constexpr int low = std::is_same_v<T, __nv_bfloat16> ? 16 : 13;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const bool there = key >= kLowest;
@@ -88,8 +95,8 @@ __device__ __forceinline__ uint32_t kth_largest(uint32_t key, int k, TopShared& 
 }
 
 // The k largest of the n listed entries (all different), in order, to sm.best.  Ends with a barrier.
-template <int NT>
-__device__ void rank_list(TopShared& sm, int n, int k) {
+template <int NT, int LIST>
+__device__ void rank_list(TopShared<NT, LIST>& sm, int n, int k) {
   const int tid = threadIdx.x;
   unsigned long long floor = 0;   // entries below it are out
   if (n > kTopRank && n > k) {
@@ -112,36 +119,57 @@ __device__ void rank_list(TopShared& sm, int n, int k) {
 
 // The row's part [lo, hi) in chunks: its k largest entries above -infinity, in order, to
 // sm.best; returns how many there are.
-template <class T, int NT>
-__device__ int top_of_part(const Row<T>& row, int lo, int hi, int k, TopShared& sm) {
-  constexpr int E = Row<T>::E;
+template <class T, int NT, int LIST>
+__device__ int top_of_part(const Row<T>& row, int lo, int hi, int k, TopShared<NT, LIST>& sm) {
+  constexpr int E = Row<T>::E, U = NT == 512 ? 8 : 6;
   const int tid = threadIdx.x;
   uint32_t best = kNone<T>;   // (two maxima of 16-bit types; a NaN wins)
-  each_group<T, NT, 8>(row, lo, hi, [&](const uint4 (&w)[8], int, int count) {
+  int group = 0;
+  each_group<T, NT, U>(row, lo, hi, [&](const uint4 (&w)[U], int, int count) {
+    uint32_t here = max_word<T, true>(w[0]);
 #pragma unroll
-    for (int u = 0; u < 8; ++u)
-      if (u < max(count, 1)) best = max_words<T, true>(best, max_word<T, true>(w[u]));
+    for (int u = 1; u < U; ++u)
+      if (u < count) here = max_words<T, true>(here, max_word<T, true>(w[u]));
+    if (count > 0) {
+      if (group < kTopGroups<NT>) sm.groups[group][tid] = here;
+      else sm.groups[kTopGroups<NT> - 1][tid] = max_words<T, true>(here, sm.groups[kTopGroups<NT> - 1][tid]);
+      ++group;
+    }
+    best = max_words<T, true>(best, here);
   });
   const uint32_t key = order_key(max_of_word<T, true>(best));
   const uint32_t bound = kth_largest<T, NT>(key, k, sm);
   if (tid == 0) sm.count = 0;
   __syncthreads();
-  auto list_above = [&](uint32_t from) {
+  const auto list_above = [&](uint32_t from) {
     const float floor = key_value(from);
-    each_group<T, NT, 4>(row, lo, hi, [&](const uint4 (&w)[4], int j, int count) {
+    const auto list = [&](const uint4& w, int e0) {
+      Val<2> v[E / 2];
+      pairs_of<T>(w, v);
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        if (u >= max(count, 1) || max_of_word<T, true>(max_word<T, true>(w[u])) < floor) continue;   // (not if it is NaN)
-        Val<2> v[E / 2];
-        pairs_of<T>(w[u], v);
-#pragma unroll
-        for (int i = 0; i < E; ++i) {
-          const uint32_t q = order_key(v[i / 2].v[i % 2]);
-          if (q >= from) {
-            const int at = atomicAdd(&sm.count, 1);
-            if (at < kTopList) sm.list[at] = entry(q, row.first(j + u * NT) + i);
-          }
+      for (int i = 0; i < E; ++i) {
+        const float x = v[i / 2].v[i % 2];
+        if (!(x < floor) && order_key(x) >= from) {   // (a NaN floor or x is not less)
+          const int at = atomicAdd(&sm.count, 1);
+          if (at < LIST) sm.list[at] = entry(order_key(x), e0 + i);
         }
+      }
+    };
+    const auto reaches = [&](uint32_t w) { return !(max_of_word<T, true>(w) < floor); };
+    int g = 0;
+    each_group_if<T, NT, U>(row, lo, hi, [&] { return reaches(sm.groups[min(g++, kTopGroups<NT> - 1)][tid]); },
+                            [&](const uint4 (&w)[U], int j, int count) {
+      if (count == 0) {
+        list(w[0], row.first(j));
+        return;
+      }
+      uint32_t which = 0;   // chunks to look at one by one: few, so the code for one is there once
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (u < count && reaches(max_word<T, true>(w[u]))) which |= 1u << u;
+      for (; which; which &= which - 1) {
+        const int chunk = j + (__ffs(which) - 1) * NT;
+        list(row.base[chunk], row.first(chunk));
       }
     });
   };
@@ -149,7 +177,7 @@ __device__ int top_of_part(const Row<T>& row, int lo, int hi, int k, TopShared& 
   __syncthreads();
   int n = sm.count;
   __syncthreads();
-  if (n > kTopList) {
+  if (n > LIST) {
     // bisection for the k-th value: `good` is reached by k entries or more, `bad` by fewer
     uint32_t good = bound, bad = 0xFFFFFFFFu;
     int par = 0;
@@ -223,16 +251,17 @@ __device__ int top_of_part(const Row<T>& row, int lo, int hi, int k, TopShared& 
 }
 
 // One cluster a row: its blocks take parts of the row, the first block joins their lists.
-template <class T, int NT>
-__global__ void __launch_bounds__(NT)
+template <class T, int NT, int LIST>
+__global__ void __launch_bounds__(NT, NT == 128 ? 8 : NT == 256 ? 5 : 2)
 k_top_logits(const T* logits, int64_t ld, int32_t rows, int32_t vocab, int32_t k, int32_t ncl,
              int32_t* idx, float* val) {
   pdl_enter();
-  __shared__ TopShared sm;
-  const int rank = ncl > 1 ? (int)(blockIdx.x % ncl) : 0;
-  const int64_t r = blockIdx.x / ncl;
+  __shared__ TopShared<NT, LIST> sm;
+  Part part = part_of(ncl);
+  const int64_t r = part.row;
   const Row<T> row(logits + r * ld, vocab);
-  const int lo = (int)((int64_t)row.chunks * rank / ncl), hi = (int)((int64_t)row.chunks * (rank + 1) / ncl);
+  take_part(part, row, ncl);
+  const int rank = part.rank, lo = part.lo, hi = part.hi;
   int n = top_of_part<T, NT>(row, lo, hi, k, sm);
   if (ncl > 1) {
     // every block writes the entries of its own part that are among the row's k largest: their
@@ -241,7 +270,7 @@ k_top_logits(const T* logits, int64_t ld, int32_t rows, int32_t vocab, int32_t k
     if (threadIdx.x == 0) sm.total[0] = n;
     cl.sync();
     for (int i = threadIdx.x; i < ncl * k; i += NT) {
-      TopShared* peer = cl.map_shared_rank(&sm, i / k);
+      TopShared<NT, LIST>* peer = cl.map_shared_rank(&sm, i / k);
       sm.list[i] = i % k < peer->total[0] ? peer->best[i % k] : 0;   // (0: below every entry)
     }
     cl.sync();   // the peers' lists have been read
@@ -281,15 +310,29 @@ k_top_logits(const T* logits, int64_t ld, int32_t rows, int32_t vocab, int32_t k
   }
 }
 
-template <class T>
-int32_t enqueue(const dgc_top& d, cudaStream_t s) {
-  int ncl = 1;
-  while (ncl < 8 && d.rows * ncl < 148 && d.vocab / ncl > 16384) ncl *= 2;
+template <class T, int NT, int LIST>
+int32_t go(const dgc_top& d, int ncl, cudaStream_t s) {
   const int64_t grid = d.rows * ncl;
   if (grid > INT32_MAX) return DGC_EINVAL;
-  launch_cluster(k_top_logits<T, kTopThreads>, dim3((unsigned)grid), kTopThreads, 0, s, (unsigned)ncl,
-                 static_cast<const T*>(d.logits.data), d.logits.ld, (int32_t)d.rows, d.vocab, d.k, ncl, d.idx, d.val);
+  if (ncl > 1)
+    launch_cluster(k_top_logits<T, NT, LIST>, dim3((unsigned)grid), NT, 0, s, (unsigned)ncl, static_cast<const T*>(d.logits.data),
+                   d.logits.ld, (int32_t)d.rows, d.vocab, d.k, ncl, d.idx, d.val);
+  else
+    launch(k_top_logits<T, NT, LIST>, dim3((unsigned)grid), NT, 0, s, static_cast<const T*>(d.logits.data), d.logits.ld,
+           (int32_t)d.rows, d.vocab, d.k, ncl, d.idx, d.val);
   return check_launch();
+}
+
+template <class T>
+int32_t enqueue(const dgc_top& d, cudaStream_t s) {
+  // few rows are spread over the SMs: 8 blocks for each of 3 rows of 250007 (f32) take 13 us, one 57
+  int ncl = 1;
+  while (ncl < 8 && d.rows * ncl < 148 && d.vocab / ncl > 16384) ncl *= 2;
+  // Threads: few for short rows (8000 x 1000 bf16: 77 us with 128, 92 with 256), many for long lists, whose
+  // bound is the tighter the more maxima there are, and where a row's time counts.
+  if ((int64_t)d.vocab * (int)sizeof(T) <= 8192 && d.k <= 128) return go<T, 128, 1024>(d, ncl, s);
+  if (ncl > 1 || d.k > 128) return go<T, 512, 4096>(d, ncl, s);
+  return go<T, 256, 2048>(d, ncl, s);
 }
 
 }  // namespace
