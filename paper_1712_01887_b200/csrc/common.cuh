@@ -79,6 +79,35 @@ inline int32_t allow_shared(size_t bytes) {
   return DGC_OK;
 }
 
+// Whether the device runs the kernel in clusters of more than the portable eight blocks; asked
+// once per kernel and device.
+template <auto KERNEL>
+inline bool allow_cluster(int blocks, int threads, size_t shared) {
+  static std::atomic<uint64_t> asked{0}, yes{0};
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev >= 64) return (void)cudaGetLastError(), false;
+  const uint64_t bit = 1ull << dev;
+  if (!(asked.load(std::memory_order_acquire) & bit)) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = blocks;
+    cfg.blockDim = threads;
+    cfg.dynamicSmemBytes = shared;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = blocks;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    int n = 0;
+    if (cudaFuncSetAttribute(KERNEL, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess &&
+        cudaOccupancyMaxActiveClusters(&n, KERNEL, &cfg) == cudaSuccess && n > 0)
+      yes.fetch_or(bit, std::memory_order_relaxed);
+    (void)cudaGetLastError();
+    asked.fetch_or(bit, std::memory_order_release);
+  }
+  return yes.load(std::memory_order_relaxed) & bit;
+}
+
 // Whether a matrix argument of rows x cols cannot be what it says.
 inline bool bad_matrix(const dgc_matrix& m, int64_t rows, int64_t cols, size_t elem) {
   return m.ld < cols || (rows > 0 && (!m.data || (reinterpret_cast<uintptr_t>(m.data) & (elem - 1)) != 0));

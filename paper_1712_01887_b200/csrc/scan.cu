@@ -33,7 +33,7 @@ using namespace dgc;
 
 namespace {
 
-constexpr int kMaxCluster = 8;
+constexpr int kMaxCluster = 16, kPortableCluster = 8;
 constexpr unsigned long long kWaitNs = 1000000000ull;   // bound of a wait on a peer: a second
 
 // A matrix argument.  The strides that the loops add are laid out by the host: as kernel
@@ -113,11 +113,11 @@ template <int VEC> struct alignas(8 * VEC) Map { Val<VEC> p, s; };
 // before the round.  (Slots of `blocks`: a block sends round i + 4 after it has every block's map
 // of round i + 2, and the warp that sent that one has read round i by then.)
 constexpr int kBlockSlots = 4;
-template <int VEC, int NW, int G>
+template <int VEC, int NW, int G, int CL>   // CL: the most blocks of a cluster
 struct Join {
   Map<VEC> runs[G][NW][32];
   Val<VEC> starts[G][NW][32];
-  Map<VEC> blocks[kBlockSlots][kMaxCluster][32];
+  Map<VEC> blocks[kBlockSlots][CL][32];
   Val<VEC> carry[2][32];
   unsigned long long arrived[kBlockSlots];   // mbarriers of `blocks`
 };
@@ -135,8 +135,8 @@ __device__ int g_scan_waits_out;
 
 __device__ __forceinline__ uint32_t shared_address(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
-template <int VEC, int NW, int G>
-__device__ __forceinline__ void join_begin(Join<VEC, NW, G>& sm, int ncl) {
+template <int VEC, int NW, int G, int CL>
+__device__ __forceinline__ void join_begin(Join<VEC, NW, G, CL>& sm, int ncl) {
   if (ncl == 1) return;
   if (threadIdx.x < kBlockSlots)
     asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(shared_address(&sm.arrived[threadIdx.x])) : "memory");
@@ -170,8 +170,8 @@ __device__ __forceinline__ bool wait_arrived(uint32_t barrier, uint32_t phase) {
 // warp, which joined the round before.  A block's map reaches the others by asynchronous stores
 // that complete on their barriers, not through the cluster's barrier: that one would wait for
 // every store of results under way.
-template <int VEC, int NW, int G>
-__device__ __forceinline__ Val<VEC> join_runs(Join<VEC, NW, G>& sm, int round, bool last, int ncl, int rank, int group,
+template <int VEC, int NW, int G, int CL>
+__device__ __forceinline__ Val<VEC> join_runs(Join<VEC, NW, G, CL>& sm, int round, bool last, int ncl, int rank, int group,
                                               int warp, int lane, const Val<VEC>& P, const Val<VEC>& S,
                                               Val<VEC>& carry, bool& waits) {
   sm.runs[group][warp][lane] = {P, S};
@@ -190,7 +190,7 @@ __device__ __forceinline__ Val<VEC> join_runs(Join<VEC, NW, G>& sm, int round, b
       if (lane == 0)
         asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(ncl * 32 * 2 * VEC * 4) : "memory");
 #pragma unroll
-      for (int r = 0; r < kMaxCluster; ++r) {
+      for (int r = 0; r < CL; ++r) {
         if (r < ncl) {
           uint32_t far, far_bar;
           asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(far) : "r"(to), "r"(r));
@@ -212,7 +212,7 @@ __device__ __forceinline__ Val<VEC> join_runs(Join<VEC, NW, G>& sm, int round, b
     Val<VEC> cur = carry;
     if (ncl > 1) {
 #pragma unroll
-      for (int r0 = 0; r0 < kMaxCluster; r0 += 4) {   // (four loads under way at a time)
+      for (int r0 = 0; r0 < CL; r0 += 4) {   // (four loads under way at a time)
         if (r0 < ncl) {
           Map<VEC> m[4];
 #pragma unroll
@@ -400,13 +400,13 @@ struct Place {
 
 constexpr int kStages = 2;
 
-template <class T, Lie LIE, int L, int NW, int G, int BLOCKS>
+template <class T, Lie LIE, int L, int NW, int G, int BLOCKS, int CL>
 __global__ void __launch_bounds__(NW * G * 32, BLOCKS) k_scan_forward(const ScanArgs a) {
   pdl_enter();
   constexpr int VEC = 4 / sizeof(T), kPart = L * kPitch<LIE>;
   // (on a 128-byte boundary: a row's part that lies across one is read in two steps, 15 % slower)
   extern __shared__ __align__(1024) char buffer[];   // [warp][stage][z, x][L rows]
-  __shared__ Join<VEC, NW, G> sm;
+  __shared__ Join<VEC, NW, G, CL> sm;
   const Place<T, L, NW, G> at(a);
   if (at.rank >= at.ncl) return;
   const int len = at.len;
@@ -460,7 +460,7 @@ __global__ void __launch_bounds__(NW * G * 32, BLOCKS) k_scan_forward(const Scan
     stage ^= 1;
     z0 += (uint32_t)a.z.stride * (uint32_t)at.step;
     x0 += (uint32_t)a.x.stride * (uint32_t)at.step;
-    Val<VEC> cur = join_runs<VEC, NW, G>(sm, round, round + 1 == rounds, at.ncl, at.rank, at.group, at.warp, at.lane, P, S, carry, waits);
+    Val<VEC> cur = join_runs(sm, round, round + 1 == rounds, at.ncl, at.rank, at.group, at.warp, at.lane, P, S, carry, waits);
     auto write = [&](auto whole) {
 #pragma unroll
       for (int i = 0; i < L; ++i, out += a.h.stride) {
@@ -481,13 +481,13 @@ __global__ void __launch_bounds__(NW * G * 32, BLOCKS) k_scan_forward(const Scan
 // needs h_{t-1} at each of them; it reads the stored h once, before the run's first step, and
 // recomputes the others in 32 bits from z and x, which it has to read anyway: 5 words moved a
 // step instead of 6, and the states inside a run carry no rounding of the output type.
-template <class T, Lie LIE, int L, int NW, int G, int BLOCKS>
+template <class T, Lie LIE, int L, int NW, int G, int BLOCKS, int CL>
 __global__ void __launch_bounds__(NW * G * 32, BLOCKS) k_scan_backward(const ScanArgs a) {
   pdl_enter();
   constexpr int VEC = 4 / sizeof(T), kPart = L * kPitch<LIE>;
   // (on a 128-byte boundary: a row's part that lies across one is read in two steps, 15 % slower)
   extern __shared__ __align__(1024) char buffer[];   // [warp][stage][z, x, dh][L rows]
-  __shared__ Join<VEC, NW, G> sm;
+  __shared__ Join<VEC, NW, G, CL> sm;
   const Place<T, L, NW, G> at(a);
   if (at.rank >= at.ncl) return;
   const int len = at.len;
@@ -572,7 +572,7 @@ __global__ void __launch_bounds__(NW * G * 32, BLOCKS) k_scan_backward(const Sca
     if (full) walk(std::true_type{});
     else walk(std::false_type{});
     fetch_state(left - at.step);
-    Val<VEC> cur = join_runs<VEC, NW, G>(sm, round, round + 1 == rounds, at.ncl, at.rank, at.group, at.warp, at.lane, P, S, carry, waits);
+    Val<VEC> cur = join_runs(sm, round, round + 1 == rounds, at.ncl, at.rank, at.group, at.warp, at.lane, P, S, carry, waits);
     auto write = [&](auto whole) {
 #pragma unroll
       for (int j = L - 1; j >= 0; --j, gz -= a.dz.stride, gx -= a.dx.stride) {
@@ -633,7 +633,7 @@ k_scan_step(const T* z, int64_t ld_z, const T* x, int64_t ld_x, float* state, co
 
 constexpr int kWarps = 8, kFwdL = 16, kBwdL = 8, kSms = 148;
 
-template <class T, Lie LIE, int G>
+template <class T, Lie LIE, int G, int CL>
 int32_t enqueue(ScanArgs a, bool backward, cudaStream_t s) {
   constexpr int VEC = 4 / sizeof(T), BLOCKS = 3 - G;
   const int L = backward ? kBwdL : kFwdL;
@@ -644,11 +644,11 @@ int32_t enqueue(ScanArgs a, bool backward, cudaStream_t s) {
   // exchange costs (40 -> 56 us for 16 x 1024 x 1001).
   a.cluster = 1;
   if (G == 2)
-    while (a.cluster < kMaxCluster && units * (a.cluster + 1) <= kSms &&
+    while (a.cluster < CL && units * (a.cluster + 1) <= kSms &&
            (int64_t)a.cluster * (L * kWarps * G) < a.tokens / a.seqs)
       ++a.cluster;
   a.longest_first = a.seq_start && a.seqs > 1 && a.seqs <= kSorted && units > kSms;
-  const int64_t grid = units * a.cluster;
+  int64_t grid = units * a.cluster;
   if (grid > INT32_MAX) return DGC_EINVAL;
   for (Matrix* m : {&a.z, &a.x, &a.h, &a.dh, &a.dz, &a.dx}) {
     m->end = m->begin + ((int64_t)(a.tokens - 1) * m->ld + a.channels) * (int64_t)sizeof(T);
@@ -659,14 +659,18 @@ int32_t enqueue(ScanArgs a, bool backward, cudaStream_t s) {
     constexpr auto f = decltype(kernel)::value;
     const int32_t rc = allow_shared<f>(smem);
     if (rc != DGC_OK) return rc;
+    if (CL > kPortableCluster && !allow_cluster<f>(CL, kWarps * G * 32, smem)) {
+      a.cluster = std::min(a.cluster, kPortableCluster);
+      grid = units * a.cluster;
+    }
     const dim3 blocks((unsigned)grid), threads(kWarps * G * 32);
     if (a.cluster > 1) launch_cluster(f, blocks, threads, smem, s, (unsigned)a.cluster, a);
     else launch(f, blocks, threads, smem, s, a);
     return check_launch();
   };
   using Kernel = void (*)(ScanArgs);
-  if (backward) return go(std::integral_constant<Kernel, &k_scan_backward<T, LIE, kBwdL, kWarps, G, BLOCKS>>{});
-  return go(std::integral_constant<Kernel, &k_scan_forward<T, LIE, kFwdL, kWarps, G, BLOCKS>>{});
+  if (backward) return go(std::integral_constant<Kernel, &k_scan_backward<T, LIE, kBwdL, kWarps, G, BLOCKS, CL>>{});
+  return go(std::integral_constant<Kernel, &k_scan_forward<T, LIE, kFwdL, kWarps, G, BLOCKS, CL>>{});
 }
 
 // One group of warps and two blocks an SM, or two groups and one block.  Two groups put a whole SM
@@ -678,7 +682,12 @@ int32_t enqueue(const ScanArgs& a, bool backward, cudaStream_t s) {
   const int32_t len = a.tokens / a.seqs, words = 32 * 4 / (int)sizeof(T);
   const int64_t units = (int64_t)((a.channels + words - 1) / words) * a.seqs;
   const bool two = len >= 640 || (len > kFwdL * kWarps && units < kSms);
-  return two ? enqueue<T, LIE, 2>(a, backward, s) : enqueue<T, LIE, 1>(a, backward, s);
+  // More blocks of a cluster than the portable eight where next to nothing else is there to do
+  // (77 against 131 us for one sequence of 60000 x 100 f16); beyond four clusters of sixteen not all
+  // find room at once (8 of them: 19 against 14 us for 8192 x 512 bf16).
+  if (two && units <= 4 && len > 2 * kPortableCluster * kBwdL * kWarps)
+    return enqueue<T, LIE, 2, kMaxCluster>(a, backward, s);
+  return two ? enqueue<T, LIE, 2, kPortableCluster>(a, backward, s) : enqueue<T, LIE, 1, kPortableCluster>(a, backward, s);
 }
 
 int32_t dispatch(const ScanArgs& a, int32_t dtype, bool backward, Lie lie, cudaStream_t s) {
