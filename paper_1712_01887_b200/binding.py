@@ -464,21 +464,24 @@ DISTILL = struct.Struct("@4iq2P3P4f3P2P")        # dgc_distill
 _raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else None
 
 
-def _stream_of(stream, device: int) -> int:
-    """The given stream, or the current one of the tensors' device."""
-    if stream is None and _raw_stream is not None:
-        return _raw_stream(device)
-    return _stream(stream)
+def _enqueue(call, name: str, args: bytes, stream, device: int) -> None:
+    """Calls with the given stream, or the current one of the tensors' device."""
+    rc = call(args, _raw_stream(device) if stream is None and _raw_stream else _stream(stream))
+    if rc:
+        _check(rc, name)
 
 
 def _first(t: torch.Tensor, what: str):
-    """What a call's first matrix says of the others: (type code, type, shape, device)."""
-    code = DTYPES.get(t.dtype)
-    device = t.get_device()
-    shape = t.shape
+    """A call's first matrix, and what it says of the others: (type code, type, shape, device,
+    pointer, row stride)."""
+    dt, shape, device = t.dtype, t.shape, t.get_device()
+    code = DTYPES.get(dt)
     if code is None or device < 0 or len(shape) != 2:
         raise ValueError(f"{what}: expected a CUDA float32, bfloat16 or float16 matrix")
-    return code, t.dtype, shape, device
+    ld, one = t.stride()
+    if one != 1 and shape[1] > 1:
+        raise ValueError(f"{what}: columns must be adjacent in memory")
+    return code, dt, shape, device, t.data_ptr(), ld if shape[0] > 1 else max(shape[1], ld)
 
 
 def _matrix(t: torch.Tensor, dtype, shape, device: int, what: str):
@@ -507,16 +510,15 @@ def gated_scan_forward(gate: torch.Tensor, x: torch.Tensor, h: torch.Tensor,
     """h_t = f_t h_{t-1} + (1 - f_t) x_t, f = sigmoid(gate), over packed sequences: rows
     seq_start[s] .. seq_start[s+1] of the [tokens, channels] matrices (seq_start None: num_seqs
     sequences of equal length).  Writes h, and the last states to h_last."""
-    code, dt, shape, dev = _first(gate, "gate")
+    code, dt, shape, dev, zp, zl = _first(gate, "gate")
     n, c = shape
-    zp, zl = _matrix(gate, dt, shape, dev, "gate")
     xp, xl = _matrix(x, dt, shape, dev, "x")
     hp, hl = _matrix(h, dt, shape, dev, "h")
     args = SCAN.pack(code, num_seqs, c, 1 if reverse else 0, n,
                      _vec(seq_start, torch.int32, num_seqs + 1, dev, "seq_start"), zp, zl, xp, xl, hp, hl,
                      _vec(h0, torch.float32, num_seqs * c, dev, "h0"),
                      _vec(h_last, torch.float32, num_seqs * c, dev, "h_last"), 0, 0, 0, 0, 0, 0, 0, 0)
-    _check(_lib.dgc_gated_scan_forward(args, _stream_of(stream, dev)), "dgc_gated_scan_forward")
+    _enqueue(_lib.dgc_gated_scan_forward, "dgc_gated_scan_forward", args, stream, dev)
 
 
 def gated_scan_backward(gate: torch.Tensor, x: torch.Tensor, h: torch.Tensor, dh: torch.Tensor,
@@ -526,9 +528,8 @@ def gated_scan_backward(gate: torch.Tensor, x: torch.Tensor, h: torch.Tensor, dh
                         dh0: Optional[torch.Tensor] = None, reverse: bool = False,
                         stream=None) -> None:
     """Gradients of gated_scan_forward: writes dgate, dx and dh0 from dh (of h) and dh_last."""
-    code, dt, shape, dev = _first(gate, "gate")
+    code, dt, shape, dev, zp, zl = _first(gate, "gate")
     n, c = shape
-    zp, zl = _matrix(gate, dt, shape, dev, "gate")
     xp, xl = _matrix(x, dt, shape, dev, "x")
     hp, hl = _matrix(h, dt, shape, dev, "h")
     dp, dl = _matrix(dh, dt, shape, dev, "dh")
@@ -539,25 +540,22 @@ def gated_scan_backward(gate: torch.Tensor, x: torch.Tensor, h: torch.Tensor, dh
                      _vec(h0, torch.float32, num_seqs * c, dev, "h0"), 0, dp, dl, gp, gl, yp, yl,
                      _vec(dh_last, torch.float32, num_seqs * c, dev, "dh_last"),
                      _vec(dh0, torch.float32, num_seqs * c, dev, "dh0"))
-    _check(_lib.dgc_gated_scan_backward(args, _stream_of(stream, dev)), "dgc_gated_scan_backward")
+    _enqueue(_lib.dgc_gated_scan_backward, "dgc_gated_scan_backward", args, stream, dev)
 
 
 def gated_scan_step(gate: torch.Tensor, x: torch.Tensor, state: torch.Tensor, out: torch.Tensor,
                     slots: Optional[torch.Tensor] = None, stream=None) -> None:
     """One token for each row: row slots[r] of `state` (fp32 [slots, channels]) is advanced in
     place and written to out[r]; a slot outside the cache marks an idle row."""
-    code, dt, shape, dev = _first(gate, "gate")
+    code, dt, shape, dev, zp, zl = _first(gate, "gate")
     n, c = shape
-    zp, zl = _matrix(gate, dt, shape, dev, "gate")
     xp, xl = _matrix(x, dt, shape, dev, "x")
     op, ol = _matrix(out, dt, shape, dev, "out")
-    if len(state.shape) != 2:
-        raise ValueError("state: expected [slots, channels]")
     rows = state.shape[0]
     args = SCAN_ONE.pack(code, n, c, rows, zp, zl, xp, xl, op, ol,
                          _vec(state, torch.float32, rows * c, dev, "state"),
                          _vec(slots, torch.int32, n, dev, "slots"))
-    _check(_lib.dgc_gated_scan_step(args, _stream_of(stream, dev)), "dgc_gated_scan_step")
+    _enqueue(_lib.dgc_gated_scan_step, "dgc_gated_scan_step", args, stream, dev)
 
 
 def gated_scan_check(stream=None) -> None:
@@ -568,13 +566,12 @@ def gated_scan_check(stream=None) -> None:
 def top_logits(logits: torch.Tensor, idx: torch.Tensor, val: torch.Tensor, stream=None) -> None:
     """The k largest entries of every row, largest first (idx, val: [rows, k]; the lowest index
     first among equals; -inf is never listed, missing entries are (-1, -inf))."""
-    code, dt, shape, dev = _first(logits, "logits")
+    code, dt, shape, dev, lp, ll = _first(logits, "logits")
     n, v = shape
-    lp, ll = _matrix(logits, dt, shape, dev, "logits")
     k = idx.shape[-1]
     args = TOP.pack(code, v, k, 0, n, lp, ll, _vec(idx, torch.int32, n * k, dev, "idx"),
                     _vec(val, torch.float32, n * k, dev, "val"))
-    _check(_lib.dgc_top_logits(args, _stream_of(stream, dev)), "dgc_top_logits")
+    _enqueue(_lib.dgc_top_logits, "dgc_top_logits", args, stream, dev)
 
 
 def distill_forward(logits: torch.Tensor, idx: torch.Tensor, val: torch.Tensor, loss: torch.Tensor,
@@ -583,16 +580,15 @@ def distill_forward(logits: torch.Tensor, idx: torch.Tensor, val: torch.Tensor, 
                     labels: Optional[torch.Tensor] = None, stream=None) -> None:
     """loss[r] = soft_weight T^2 KL(teacher's listed distribution || student's) + hard_weight
     cross entropy with labels[r]; lse [rows, 2] is kept for distill_backward."""
-    code, dt, shape, dev = _first(logits, "logits")
+    code, dt, shape, dev, lp, ll = _first(logits, "logits")
     n, v = shape
-    lp, ll = _matrix(logits, dt, shape, dev, "logits")
     k = idx.shape[-1]
     args = DISTILL.pack(code, v, k, 0, n, lp, ll, _vec(idx, torch.int32, n * k, dev, "idx"),
                         _vec(val, torch.float32, n * k, dev, "val"),
                         _vec(labels, torch.int32, n, dev, "labels"), temperature, soft_weight,
                         hard_weight, 0.0, _vec(loss, torch.float32, n, dev, "loss"),
                         _vec(lse, torch.float32, 2 * n, dev, "lse"), 0, 0, 0)
-    _check(_lib.dgc_distill_forward(args, _stream_of(stream, dev)), "dgc_distill_forward")
+    _enqueue(_lib.dgc_distill_forward, "dgc_distill_forward", args, stream, dev)
 
 
 def distill_backward(logits: torch.Tensor, idx: torch.Tensor, val: torch.Tensor, lse: torch.Tensor,
@@ -601,9 +597,8 @@ def distill_backward(logits: torch.Tensor, idx: torch.Tensor, val: torch.Tensor,
                      labels: Optional[torch.Tensor] = None, stream=None) -> None:
     """The gradient of distill_forward's losses, dloss[r] being that of row r's; dlogits may be
     the logits themselves."""
-    code, dt, shape, dev = _first(logits, "logits")
+    code, dt, shape, dev, lp, ll = _first(logits, "logits")
     n, v = shape
-    lp, ll = _matrix(logits, dt, shape, dev, "logits")
     dp, dl = _matrix(dlogits, dt, shape, dev, "dlogits")
     k = idx.shape[-1]
     args = DISTILL.pack(code, v, k, 0, n, lp, ll, _vec(idx, torch.int32, n * k, dev, "idx"),
@@ -611,7 +606,7 @@ def distill_backward(logits: torch.Tensor, idx: torch.Tensor, val: torch.Tensor,
                         _vec(labels, torch.int32, n, dev, "labels"), temperature, soft_weight,
                         hard_weight, 0.0, 0, _vec(lse, torch.float32, 2 * n, dev, "lse"),
                         _vec(dloss, torch.float32, n, dev, "dloss"), dp, dl)
-    _check(_lib.dgc_distill_backward(args, _stream_of(stream, dev)), "dgc_distill_backward")
+    _enqueue(_lib.dgc_distill_backward, "dgc_distill_backward", args, stream, dev)
 
 
 def distill_loss_grad(logits: torch.Tensor, idx: torch.Tensor, val: torch.Tensor,
@@ -619,9 +614,8 @@ def distill_loss_grad(logits: torch.Tensor, idx: torch.Tensor, val: torch.Tensor
                       temperature: float = 1.0, soft_weight: float = 1.0, hard_weight: float = 0.0,
                       labels: Optional[torch.Tensor] = None, stream=None) -> None:
     """distill_forward and distill_backward in one call, the logits read from memory once."""
-    code, dt, shape, dev = _first(logits, "logits")
+    code, dt, shape, dev, lp, ll = _first(logits, "logits")
     n, v = shape
-    lp, ll = _matrix(logits, dt, shape, dev, "logits")
     dp, dl = _matrix(dlogits, dt, shape, dev, "dlogits")
     k = idx.shape[-1]
     args = DISTILL.pack(code, v, k, 0, n, lp, ll, _vec(idx, torch.int32, n * k, dev, "idx"),
@@ -629,4 +623,4 @@ def distill_loss_grad(logits: torch.Tensor, idx: torch.Tensor, val: torch.Tensor
                         _vec(labels, torch.int32, n, dev, "labels"), temperature, soft_weight,
                         hard_weight, 0.0, _vec(loss, torch.float32, n, dev, "loss"), 0,
                         _vec(dloss, torch.float32, n, dev, "dloss"), dp, dl)
-    _check(_lib.dgc_distill_loss_grad(args, _stream_of(stream, dev)), "dgc_distill_loss_grad")
+    _enqueue(_lib.dgc_distill_loss_grad, "dgc_distill_loss_grad", args, stream, dev)

@@ -88,14 +88,13 @@ constexpr int kSorted = 128;
 __device__ __forceinline__ int by_length(const ScanArgs& a, int place) {
   __shared__ __align__(16) int lens[kSorted];
   __shared__ int found;
-  const int t = threadIdx.x;
-  int first, len = -1;
-  if (t < kSorted) {
-    if (t < a.seqs) sequence_range(a, t, first, len);
-    lens[t] = len;
+  for (int t = threadIdx.x; t < a.seqs; t += blockDim.x) {
+    int first;
+    sequence_range(a, t, first, lens[t]);
   }
   __syncthreads();
-  if (t < a.seqs) {
+  for (int t = threadIdx.x; t < a.seqs; t += blockDim.x) {
+    const int len = lens[t];
     int before = 0;
     for (int j = 0; j < a.seqs; ++j) before += lens[j] > len || (lens[j] == len && j < t);
     if (before == place) found = t;
@@ -230,13 +229,14 @@ __device__ __forceinline__ Val<VEC> join_runs(Join<VEC, NW, G, CL>& sm, int roun
         bar_arrive<64>(kCarryBarrier + ((round + 1) & 1));
       }
     }
+    constexpr int Q = NW < 4 ? NW : 4;
 #pragma unroll
-    for (int w0 = 0; w0 < NW; w0 += 4) {
-      Map<VEC> m[4];
+    for (int w0 = 0; w0 < NW; w0 += Q) {
+      Map<VEC> m[Q];
 #pragma unroll
-      for (int w = 0; w < 4; ++w) m[w] = sm.runs[group][w0 + w][lane];
+      for (int w = 0; w < Q; ++w) m[w] = sm.runs[group][w0 + w][lane];
 #pragma unroll
-      for (int w = 0; w < 4; ++w) {
+      for (int w = 0; w < Q; ++w) {
         sm.starts[group][w0 + w][lane] = cur;
         cur = fma_(m[w].p, cur, m[w].s);
       }
@@ -631,11 +631,11 @@ k_scan_step(const T* z, int64_t ld_z, const T* x, int64_t ld_x, float* state, co
   }
 }
 
-constexpr int kWarps = 8, kFwdL = 16, kBwdL = 8, kSms = 148;
+constexpr int kFwdL = 16, kBwdL = 8, kSms = 148;
 
-template <class T, Lie LIE, int G, int CL>
+template <class T, Lie LIE, int NW, int G, int CL>
 int32_t enqueue(ScanArgs a, bool backward, cudaStream_t s) {
-  constexpr int VEC = 4 / sizeof(T), BLOCKS = 3 - G;
+  constexpr int VEC = 4 / sizeof(T), BLOCKS = 16 / (NW * G);   // 16 warps of 128 registers an SM
   const int L = backward ? kBwdL : kFwdL;
   a.ctiles = (a.channels + 32 * VEC - 1) / (32 * VEC);
   const int64_t units = (int64_t)a.ctiles * a.seqs;
@@ -645,7 +645,7 @@ int32_t enqueue(ScanArgs a, bool backward, cudaStream_t s) {
   a.cluster = 1;
   if (G == 2)
     while (a.cluster < CL && units * (a.cluster + 1) <= kSms &&
-           (int64_t)a.cluster * (L * kWarps * G) < a.tokens / a.seqs)
+           (int64_t)a.cluster * (L * NW * G) < a.tokens / a.seqs)
       ++a.cluster;
   a.longest_first = a.seq_start && a.seqs > 1 && a.seqs <= kSorted && units > kSms;
   int64_t grid = units * a.cluster;
@@ -654,40 +654,49 @@ int32_t enqueue(ScanArgs a, bool backward, cudaStream_t s) {
     m->end = m->begin + ((int64_t)(a.tokens - 1) * m->ld + a.channels) * (int64_t)sizeof(T);
     m->stride = (a.reverse ? -m->ld : m->ld) * (int64_t)sizeof(T);
   }
-  const size_t smem = G * kWarps * kStages * kPitch<LIE> * (backward ? 3 * kBwdL : 2 * kFwdL);
+  const size_t smem = G * NW * kStages * kPitch<LIE> * (backward ? 3 * kBwdL : 2 * kFwdL);
   auto go = [&](auto kernel) {
     constexpr auto f = decltype(kernel)::value;
     const int32_t rc = allow_shared<f>(smem);
     if (rc != DGC_OK) return rc;
-    if (CL > kPortableCluster && !allow_cluster<f>(CL, kWarps * G * 32, smem)) {
+    if (CL > kPortableCluster && !allow_cluster<f>(CL, NW * G * 32, smem)) {
       a.cluster = std::min(a.cluster, kPortableCluster);
       grid = units * a.cluster;
     }
-    const dim3 blocks((unsigned)grid), threads(kWarps * G * 32);
+    const dim3 blocks((unsigned)grid), threads(NW * G * 32);
     if (a.cluster > 1) launch_cluster(f, blocks, threads, smem, s, (unsigned)a.cluster, a);
     else launch(f, blocks, threads, smem, s, a);
     return check_launch();
   };
   using Kernel = void (*)(ScanArgs);
-  if (backward) return go(std::integral_constant<Kernel, &k_scan_backward<T, LIE, kBwdL, kWarps, G, BLOCKS, CL>>{});
-  return go(std::integral_constant<Kernel, &k_scan_forward<T, LIE, kFwdL, kWarps, G, BLOCKS, CL>>{});
+  if (backward) return go(std::integral_constant<Kernel, &k_scan_backward<T, LIE, kBwdL, NW, G, BLOCKS, CL>>{});
+  return go(std::integral_constant<Kernel, &k_scan_forward<T, LIE, kFwdL, NW, G, BLOCKS, CL>>{});
 }
 
-// One group of warps and two blocks an SM, or two groups and one block.  Two groups put a whole SM
-// behind a sequence: right where sequences are long (17 against 105 us for one of 8192 steps x
-// 512 bf16 channels, where the cluster then helps too; 59 against 69 us for 37 of 1081 steps on
-// average, uneven), wrong where they are many and short (51 against 41 us for 64 of 400 x 1024).
+// Which blocks.  All have 16 warps of 128 registers an SM; they differ in how many of them work at
+// one sequence (forward / backward, bf16 unless stated):
+//   four blocks of 4 warps   where there are blocks for all slots, or runs end early:
+//                            32 x 1024 steps x 1024 channels 35 / 63 us against 44 / 70 with 8 warps,
+//                            20 x 35 x 1500 f32 5.1 / 7.4 against 9.5 / 9.1
+//   two blocks of 8 warps    in between: 16 x 512 x 1024 10 / 18 us against 11 / 22 with 4 warps and
+//                            12 / 18 with 16
+//   one block of 2 x 8 warps puts a whole SM behind a sequence, where they are long and few, or uneven
+//                            (the longest then decides): 20 of 500 on average x 1024 16 / 24 us against
+//                            20 / 37; clusters are for these
+// More blocks of a cluster than the portable eight where next to nothing else is there to do
+// (69 against 131 us for one sequence of 60000 x 100 f16); beyond four clusters of sixteen not all
+// find room at once (8 of them: 19 against 14 us for 8192 x 512).
 template <class T, Lie LIE>
 int32_t enqueue(const ScanArgs& a, bool backward, cudaStream_t s) {
   const int32_t len = a.tokens / a.seqs, words = 32 * 4 / (int)sizeof(T);
   const int64_t units = (int64_t)((a.channels + words - 1) / words) * a.seqs;
-  const bool two = len >= 640 || (len > kFwdL * kWarps && units < kSms);
-  // More blocks of a cluster than the portable eight where next to nothing else is there to do
-  // (77 against 131 us for one sequence of 60000 x 100 f16); beyond four clusters of sixteen not all
-  // find room at once (8 of them: 19 against 14 us for 8192 x 512 bf16).
-  if (two && units <= 4 && len > 2 * kPortableCluster * kBwdL * kWarps)
-    return enqueue<T, LIE, 2, kMaxCluster>(a, backward, s);
-  return two ? enqueue<T, LIE, 2, kPortableCluster>(a, backward, s) : enqueue<T, LIE, 1, kPortableCluster>(a, backward, s);
+  const bool uneven = a.seq_start != nullptr;
+  if (len <= 64 || (units >= 500 && len <= (uneven ? 200 : 1024)))
+    return enqueue<T, LIE, 4, 1, kPortableCluster>(a, backward, s);
+  if (len < (uneven ? 400 : 640) && (len <= 128 || units >= kSms))
+    return enqueue<T, LIE, 8, 1, kPortableCluster>(a, backward, s);
+  if (units <= 4 && len > 1024) return enqueue<T, LIE, 8, 2, kMaxCluster>(a, backward, s);
+  return enqueue<T, LIE, 8, 2, kPortableCluster>(a, backward, s);
 }
 
 int32_t dispatch(const ScanArgs& a, int32_t dtype, bool backward, Lie lie, cudaStream_t s) {
