@@ -499,25 +499,25 @@ typedef struct dgc_distill {
   float          reserved1;         /* 0                                                          */
   float*         loss;              /* output [rows]; +infinity where a listed entry or the label
                                        has p = 0                                                  */
-  float*         lse;               /* [rows, 2], forward output (may be NULL) that backward takes:
-                                       log sum exp of s / T, and of s (only where labels and a
-                                       non-zero hard_weight need it)                              */
+  float*         stats;             /* [rows, 2], forward output (may be NULL) that backward takes as it
+                                       is: what the walk over the row found.  The two calls agree in
+                                       all arguments above                                        */
   const float*   dloss;             /* [rows], the gradient that reaches the row's loss           */
   dgc_matrix     dlogits;           /* output [rows, vocab]                                       */
 } dgc_distill;
 
-/* Writes loss, and lse if given. */
+/* Writes loss, and stats if given. */
 int32_t dgc_distill_forward(const dgc_distill* d, void* stream);
 
 /* The gradient: dlogits[r][j] = dloss[r] (soft_weight T (p_j - sum of q listed at j)
- * + hard_weight (p1_j - [j = label])), from lse and dloss.  Every element of dlogits is written; a
+ * + hard_weight (p1_j - [j = label])), from stats and dloss.  Every element of dlogits is written; a
  * row with neither term, or with dloss 0, gets zeros.  dlogits may be the logits themselves (same
  * base and stride); rows at the same distance from a 16-byte boundary as the logits' are
  * written in 16-byte words, others element by element. */
 int32_t dgc_distill_backward(const dgc_distill* d, void* stream);
 
 /* Loss and gradient in one call (dloss known beforehand: a token's weight over the number of
- * tokens): the same results, the logits read from memory once.  lse is not used. */
+ * tokens): the same results, the logits read from memory once.  stats is not used. */
 int32_t dgc_distill_loss_grad(const dgc_distill* d, void* stream);
 
 /* Number of kernels this library has launched in this process (all states). */

@@ -575,11 +575,11 @@ def top_logits(logits: torch.Tensor, idx: torch.Tensor, val: torch.Tensor, strea
 
 
 def distill_forward(logits: torch.Tensor, idx: torch.Tensor, val: torch.Tensor, loss: torch.Tensor,
-                    lse: Optional[torch.Tensor] = None, temperature: float = 1.0,
+                    stats: Optional[torch.Tensor] = None, temperature: float = 1.0,
                     soft_weight: float = 1.0, hard_weight: float = 0.0,
                     labels: Optional[torch.Tensor] = None, stream=None) -> None:
     """loss[r] = soft_weight T^2 KL(teacher's listed distribution || student's) + hard_weight
-    cross entropy with labels[r]; lse [rows, 2] is kept for distill_backward."""
+    cross entropy with labels[r]; stats [rows, 2] is kept for distill_backward."""
     code, dt, shape, dev, lp, ll = _first(logits, "logits")
     n, v = shape
     k = idx.shape[-1]
@@ -587,11 +587,11 @@ def distill_forward(logits: torch.Tensor, idx: torch.Tensor, val: torch.Tensor, 
                         _vec(val, torch.float32, n * k, dev, "val"),
                         _vec(labels, torch.int32, n, dev, "labels"), temperature, soft_weight,
                         hard_weight, 0.0, _vec(loss, torch.float32, n, dev, "loss"),
-                        _vec(lse, torch.float32, 2 * n, dev, "lse"), 0, 0, 0)
+                        _vec(stats, torch.float32, 2 * n, dev, "stats"), 0, 0, 0)
     _enqueue(_lib.dgc_distill_forward, "dgc_distill_forward", args, stream, dev)
 
 
-def distill_backward(logits: torch.Tensor, idx: torch.Tensor, val: torch.Tensor, lse: torch.Tensor,
+def distill_backward(logits: torch.Tensor, idx: torch.Tensor, val: torch.Tensor, stats: torch.Tensor,
                      dloss: torch.Tensor, dlogits: torch.Tensor, temperature: float = 1.0,
                      soft_weight: float = 1.0, hard_weight: float = 0.0,
                      labels: Optional[torch.Tensor] = None, stream=None) -> None:
@@ -604,7 +604,7 @@ def distill_backward(logits: torch.Tensor, idx: torch.Tensor, val: torch.Tensor,
     args = DISTILL.pack(code, v, k, 0, n, lp, ll, _vec(idx, torch.int32, n * k, dev, "idx"),
                         _vec(val, torch.float32, n * k, dev, "val"),
                         _vec(labels, torch.int32, n, dev, "labels"), temperature, soft_weight,
-                        hard_weight, 0.0, 0, _vec(lse, torch.float32, 2 * n, dev, "lse"),
+                        hard_weight, 0.0, 0, _vec(stats, torch.float32, 2 * n, dev, "stats"),
                         _vec(dloss, torch.float32, n, dev, "dloss"), dp, dl)
     _enqueue(_lib.dgc_distill_backward, "dgc_distill_backward", args, stream, dev)
 

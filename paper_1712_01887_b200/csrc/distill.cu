@@ -32,7 +32,7 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kMaxCluster = 8;
-constexpr float kLseExact = 64.0f;   // 32-bit logarithms up to here give p to 4e-6
+constexpr float kLeast = 0x1p-110f, kMost = 0x1p110f;   // two sums kept from forward to backward
 enum { kForward = 0, kBackward = 1, kBoth = 2 };
 
 struct DistillArgs {
@@ -42,8 +42,8 @@ struct DistillArgs {
   const float* val;
   const int32_t* labels;
   const float* dloss;
-  const float* lse_in;
-  float *loss, *lse;
+  const float* stats_in;
+  float *loss, *stats;
   int64_t ld, ld_d;
   float temperature, c, soft, hard;   // c = log2(e) / temperature
   float lowest;                       // below it, and above its opposite, exponents are taken with care
@@ -126,11 +126,22 @@ __global__ void __launch_bounds__(NT, kBlocks<T, MODE>) k_distill(const DistillA
   float m = 0.0f, mc = 0.0f, mc1 = 0.0f, sum = 1.0f, sum1 = 1.0f;
   bool careful = false, walk = MODE != kBackward;
   if (MODE == kBackward) {
-    const float2 lse = make_float2(a.lse_in[2 * r], a.lse_in[2 * r + 1]);
-    mc = lse.x * kLog2e;
-    mc1 = lse.y * kLog2e;
-    // 32 bits of a large logarithm are too few for p: such rows are summed once more
-    walk = !(fabsf(lse.x) < kLseExact && fabsf(lse.y) < kLseExact);
+    // What the forward call left: m c and the sum, so that p comes out as it would there; with two
+    // sums, these as z 2^n each: p = 2^(s c - n) / z (a logarithm would cost p the bits before the
+    // point).  Rows out of the ordinary have 0 there and are summed once more.
+    const float x = a.stats_in[2 * r], x1 = a.stats_in[2 * r + 1];
+    walk = TWO ? !(x > kLeast && x < kMost && x1 > kLeast && x1 < kMost) : !(x1 > 0.0f);
+    mc = x;
+    sum = x1;
+    if (TWO) {
+      const uint32_t u = __float_as_uint(x), u1 = __float_as_uint(x1);
+      mc = (float)((int)(u >> 23) - 127);
+      mc1 = (float)((int)(u1 >> 23) - 127);
+      sum = __uint_as_float((u & 0x7FFFFFu) | 0x3F800000u);
+      sum1 = __uint_as_float((u1 & 0x7FFFFFu) | 0x3F800000u);
+    } else {
+      sum1 = sum;
+    }
   }
   // joins the threads' sums over the row's blocks
   const auto over_row = [&](auto st) {
@@ -263,10 +274,13 @@ __global__ void __launch_bounds__(NT, kBlocks<T, MODE>) k_distill(const DistillA
     if (labelled && a.hard != 0.0f)
       loss -= a.hard * (sy == -INFINITY ? -INFINITY : exponent1(sy) * kLn2 - logf(sum1));
     a.loss[r] = loss;
-    if (MODE == kForward && a.lse) {
-      const float lse = sum == 0.0f ? -INFINITY : (careful ? m / a.temperature : mc * kLn2) + logf(sum);
-      a.lse[2 * r] = lse;
-      a.lse[2 * r + 1] = !TWO ? lse : sum1 == 0.0f ? -INFINITY : (careful ? m : mc1 * kLn2) + logf(sum1);
+    if (MODE == kForward && a.stats) {
+      const auto total = [](float s, float e) {   // s 2^e, or 0: to be summed again
+        const float n = rintf(e);
+        return fabsf(e) < 100.0f ? ldexpf(s * exp2f(e - n), (int)n) : 0.0f;
+      };
+      a.stats[2 * r] = careful ? 0.0f : TWO ? total(sum, mc) : mc;
+      a.stats[2 * r + 1] = careful ? 0.0f : TWO ? total(sum1, mc1) : sum;
     }
   }
   if (MODE == kForward) return;
@@ -382,15 +396,15 @@ int32_t distill(int mode, const dgc_distill* d, void* stream) {
   if (mode != kForward && bad_matrix(d->dlogits, d->rows, d->vocab, es)) return DGC_EINVAL;
   if (d->rows == 0) return DGC_OK;
   if (!d->idx || !d->val || misaligned(d->idx, 4) || misaligned(d->val, 4) || misaligned(d->labels, 4) ||
-      misaligned(d->loss, 4) || misaligned(d->lse, 4) || misaligned(d->dloss, 4))
+      misaligned(d->loss, 4) || misaligned(d->stats, 4) || misaligned(d->dloss, 4))
     return DGC_EINVAL;
-  if ((mode != kBackward && !d->loss) || (mode != kForward && !d->dloss) || (mode == kBackward && !d->lse)) return DGC_EINVAL;
+  if ((mode != kBackward && !d->loss) || (mode != kForward && !d->dloss) || (mode == kBackward && !d->stats)) return DGC_EINVAL;
   DistillArgs a{};
   a.logits = d->logits.data; a.ld = d->logits.ld; a.idx = d->idx; a.val = d->val; a.labels = d->labels;
   a.vocab = d->vocab; a.k = d->k; a.temperature = d->temperature; a.soft = d->soft_weight; a.hard = d->hard_weight;
   a.c = (float)(1.4426950408889634 / (double)d->temperature);
   a.lowest = -1e30f / std::max(1.0f, a.c);
-  a.loss = d->loss; a.lse = d->lse; a.lse_in = d->lse; a.dloss = d->dloss;
+  a.loss = d->loss; a.stats = d->stats; a.stats_in = d->stats; a.dloss = d->dloss;
   a.dlogits = d->dlogits.data; a.ld_d = d->dlogits.ld;
   cudaStream_t s = as_stream(stream);
   if (d->dtype == DGC_F32) return enqueue<float>(a, mode, d->rows, s);

@@ -205,12 +205,12 @@ def _check_distill(B, s, idx, val, lab, w, T=1.0, soft=1.0, hard=0.0, place="sam
         bad = (x - grad).abs() > tol
         assert not bad.any() and torch.isfinite(x).all(), (int(bad.sum()), float(((x - grad).abs() / tol).max()))
     ld = logits()
-    loss, lse = torch.full((R,), -9.0, device="cuda"), torch.empty(R, 2, device="cuda")
-    B.distill_forward(ld, dev(idx), dev(val), loss, lse, **how)
+    loss, stats = torch.full((R,), -9.0, device="cuda"), torch.empty(R, 2, device="cuda")
+    B.distill_forward(ld, dev(idx), dev(val), loss, stats, **how)
     near_loss(loss)
     whole = torch.full((R, V + 4), -5.0, dtype=dt, device="cuda")
     out = whole[:, 1:V + 1] if place == "odd" else torch.full((R, V), -5.0, dtype=dt, device="cuda")
-    B.distill_backward(ld, dev(idx), dev(val), lse, dev(w), out, **how)
+    B.distill_backward(ld, dev(idx), dev(val), stats, dev(w), out, **how)
     near_grad(out)
     loss2 = torch.full((R,), -9.0, device="cuda")
     out2 = torch.full((R, V), -5.0, dtype=dt, device="cuda")
@@ -225,7 +225,7 @@ def _check_distill(B, s, idx, val, lab, w, T=1.0, soft=1.0, hard=0.0, place="sam
     assert torch.equal(over, out2)
     near_loss(loss2)
     over = logits()
-    B.distill_backward(over, dev(idx), dev(val), lse, dev(w), over, **how)
+    B.distill_backward(over, dev(idx), dev(val), stats, dev(w), over, **how)
     assert torch.equal(over, out)
 
 
@@ -281,15 +281,15 @@ def test_distill_where_the_student_cannot_say_the_word():
     s[0, int(idx[0, 1])] = -INF
     s[1, int(lab[1])] = -INF
     s[2] = -INF
-    loss, lse, out = torch.empty(3, device="cuda"), torch.empty(3, 2, device="cuda"), torch.empty(3, 700, device="cuda")
+    loss, stats, out = torch.empty(3, device="cuda"), torch.empty(3, 2, device="cuda"), torch.empty(3, 700, device="cuda")
     how = dict(temperature=2.0, soft_weight=1.0, hard_weight=0.5, labels=lab.cuda())
     _, grad, size = plain_distill(s, idx, val, lab, 2.0, 1.0, 0.5, w)
     B.distill_loss_grad(s.cuda(), idx.cuda(), val.cuda(), w.cuda(), loss, out, **how)
     assert torch.equal(loss.cpu(), torch.full((3,), INF))
     assert ((out.double().cpu() - grad).abs() <= TOL * size + 1e-38).all()
-    B.distill_forward(s.cuda(), idx.cuda(), val.cuda(), loss, lse, **how)
-    assert torch.equal(loss.cpu(), torch.full((3,), INF)) and (lse[2] == -INF).all()
-    B.distill_backward(s.cuda(), idx.cuda(), val.cuda(), lse, w.cuda(), out, **how)
+    B.distill_forward(s.cuda(), idx.cuda(), val.cuda(), loss, stats, **how)
+    assert torch.equal(loss.cpu(), torch.full((3,), INF)) and (stats[2] == 0).all()
+    B.distill_backward(s.cuda(), idx.cuda(), val.cuda(), stats, w.cuda(), out, **how)
     assert ((out.double().cpu() - grad).abs() <= TOL * size + 1e-38).all()
 
 
@@ -354,14 +354,14 @@ def test_refusals_of_the_c_calls():
         assert top(**bad) == B.EINVAL, bad
     assert top(rows=0) == B.OK and lib.dgc_top_logits(None, None) == B.EINVAL
 
-    def call(which, dtype=1, rows=2, v=8, k=4, x=p, ld=8, i=p, t=p, T=1.0, ws=1.0, wh=0.0, lse=p, dl=p, loss=p, g=p, ldg=8, lab=0):
-        return getattr(lib, "dgc_distill_" + which)(B.DISTILL.pack(dtype, v, k, 0, rows, x, ld, i, t, lab, T, ws, wh, 0.0, loss, lse,
+    def call(which, dtype=1, rows=2, v=8, k=4, x=p, ld=8, i=p, t=p, T=1.0, ws=1.0, wh=0.0, stats=p, dl=p, loss=p, g=p, ldg=8, lab=0):
+        return getattr(lib, "dgc_distill_" + which)(B.DISTILL.pack(dtype, v, k, 0, rows, x, ld, i, t, lab, T, ws, wh, 0.0, loss, stats,
                                                                    dl, g, ldg), None)
     every = [dict(dtype=-1), dict(dtype=3), dict(rows=-2), dict(v=0), dict(k=0), dict(k=300), dict(x=0), dict(ld=7), dict(i=0),
              dict(t=0), dict(T=0.0), dict(T=-1.0), dict(T=float("nan")), dict(T=INF), dict(ws=INF), dict(wh=float("nan")), dict(x=off),
              dict(i=off), dict(lab=off)]
-    only = {"forward": [dict(loss=0), dict(loss=off), dict(lse=off)],
-            "backward": [dict(lse=0), dict(dl=0), dict(g=0), dict(ldg=7), dict(g=off)],
+    only = {"forward": [dict(loss=0), dict(loss=off), dict(stats=off)],
+            "backward": [dict(stats=0), dict(dl=0), dict(g=0), dict(ldg=7), dict(g=off)],
             "loss_grad": [dict(dl=0), dict(loss=0), dict(g=0), dict(ldg=0)]}
     for which, more in only.items():
         for bad in every + more:
