@@ -5,7 +5,8 @@
  * the two accumulators U^k and V^k of that algorithm for a whole gradient set
  * (tensors j = 0..M laid out in one fp32 arena) and compresses one gradient
  * per call.  The receive side (`dgc_decode_accumulate`, `dgc_apply_sgd`) is
- * stateless.
+ * stateless, and so are the operators of a recurrent model's step
+ * (`dgc_gated_scan_*`, `dgc_top_logits`, `dgc_distill_*`).
  *
  * Conventions
  *  - "device" pointers are CUDA device memory of the state's device, owned by

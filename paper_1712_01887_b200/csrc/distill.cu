@@ -93,7 +93,7 @@ template <class T, int MODE> constexpr int kAhead = sizeof(T) == 4 && MODE != kF
 template <class T, int MODE> constexpr int kBlocks = MODE == kForward ? 5 : sizeof(T) == 4 ? 3 : 4;
 
 template <class T, int NT, int MODE, bool TWO>
-__global__ void __launch_bounds__(NT, kBlocks<T, MODE>) k_distill(const DistillArgs a) {
+__global__ void __launch_bounds__(NT, kBlocks<T, MODE> * 256 / NT) k_distill(const DistillArgs a) {
   pdl_enter();
   constexpr int E = Row<T>::E, W = NT / 32, U = kAhead<T, MODE>;
   __shared__ DistillShared<NT> sm;
@@ -363,17 +363,23 @@ __global__ void __launch_bounds__(NT, kBlocks<T, MODE>) k_distill(const DistillA
   }
 }
 
-template <class T, int MODE, bool TWO>
-int32_t choose(DistillArgs a, int64_t rows, cudaStream_t s) {
-  constexpr int NT = 256;
-  // blocks for a row: few rows are spread over the SMs
-  a.cluster = 1;
-  while (a.cluster < kMaxCluster && rows * a.cluster < 148 && a.vocab / a.cluster > 8192) a.cluster *= 2;
+template <class T, int NT, int MODE, bool TWO>
+int32_t go(const DistillArgs& a, int64_t rows, cudaStream_t s) {
   if (rows * a.cluster > INT32_MAX) return DGC_EINVAL;
   const dim3 grid((unsigned)(rows * a.cluster));
   if (a.cluster > 1) launch_cluster(k_distill<T, NT, MODE, TWO>, grid, NT, 0, s, (unsigned)a.cluster, a);
   else launch(k_distill<T, NT, MODE, TWO>, grid, NT, 0, s, a);
   return check_launch();
+}
+
+template <class T, int MODE, bool TWO>
+int32_t choose(DistillArgs a, int64_t rows, cudaStream_t s) {
+  // blocks for a row: few rows are spread over the SMs
+  a.cluster = 1;
+  while (a.cluster < kMaxCluster && rows * a.cluster < 148 && a.vocab / a.cluster > 8192) a.cluster *= 2;
+  // a short row is little work beside what a warp does once a row
+  if ((int64_t)a.vocab * (int)sizeof(T) <= 8192 && a.k <= 128) return go<T, 128, MODE, TWO>(a, rows, s);
+  return go<T, 256, MODE, TWO>(a, rows, s);
 }
 
 template <class T>

@@ -31,9 +31,10 @@ __device__ __forceinline__ Part part_of(unsigned ncl) {
   return Part{(int64_t)(blockIdx.x / ncl), (int)(blockIdx.x % ncl), 0, 0};
 }
 template <class T>
-__device__ __forceinline__ void take_part(Part& p, const Row<T>& row, unsigned ncl) {   // chunks < 2^29, ncl <= 8
-  p.lo = ncl == 1 ? 0 : (int)((unsigned)row.chunks * (unsigned)p.rank / ncl);
-  p.hi = ncl == 1 ? row.chunks : (int)((unsigned)row.chunks * (unsigned)(p.rank + 1) / ncl);
+__device__ __forceinline__ void take_part(Part& p, const Row<T>& row, unsigned ncl) {
+  const int share = ncl == 1 ? row.chunks : (int)(((unsigned)row.chunks + ncl - 1) / ncl);
+  p.lo = min(p.rank * share, row.chunks);
+  p.hi = min(p.lo + share, row.chunks);
 }
 
 template <class T>
