@@ -432,11 +432,19 @@ typedef struct dgc_scan {
   const float*   dh_last;    /* [num_seqs, channels], gradient of h_last; NULL: 0                */
   float*         dh0;        /* output [num_seqs, channels] (dh_last's row for an empty
                                 sequence); may be NULL                                           */
+  /* both */
+  void*          workspace;  /* device scratch of dgc_gated_scan_workspace_bytes() bytes, 8-byte
+                                aligned, or NULL.  With it a few long sequences of few channels are
+                                worked on by the whole GPU and not by a cluster each             */
+  int64_t        workspace_bytes;
 } dgc_scan;
 
+/* Bytes of workspace that make the two calls below faster for this struct's dtype, tokens,
+ * num_seqs and channels (0: none would; a shorter one is DGC_ECAPACITY).  Host only. */
+int64_t dgc_gated_scan_workspace_bytes(const dgc_scan* scan);
+
 /* Writes h and h_last.  Results do not vary from run to run, and no value of one sequence (an
- * infinity, a NaN) reaches another.  Rows outside every sequence are not written.  No
- * workspace. */
+ * infinity, a NaN) reaches another.  Rows outside every sequence are not written. */
 int32_t dgc_gated_scan_forward(const dgc_scan* scan, void* stream);
 
 /* The gradients of dgc_gated_scan_forward, with g_t the gradient that reaches h_t in all:

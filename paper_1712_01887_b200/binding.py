@@ -103,6 +103,7 @@ _sigs = {
         "dgc_gated_scan_forward", "dgc_gated_scan_backward", "dgc_gated_scan_step",
         "dgc_top_logits", "dgc_distill_forward", "dgc_distill_backward", "dgc_distill_loss_grad")},
     "dgc_gated_scan_check": (ctypes.c_int32, [_vp]),
+    "dgc_gated_scan_workspace_bytes": (ctypes.c_int64, [ctypes.c_char_p]),
     "dgc_launch_count": (ctypes.c_uint64, []),
     "dgc_error_string": (ctypes.c_char_p, [ctypes.c_int32]),
 }
@@ -457,7 +458,7 @@ def apply_sgd(w: torch.Tensor, dense_grad: torch.Tensor, lr: float, stream=None)
 
 MAX_TOP = 256
 DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}   # DGC_F32, DGC_BF16, DGC_F16
-SCAN = struct.Struct("@4iqP6P2P6P2P")            # dgc_scan (a matrix is a pointer and a 64-bit stride)
+SCAN = struct.Struct("@4iqP6P2P6P2PPq")          # dgc_scan (a matrix is a pointer and a 64-bit stride)
 SCAN_ONE = struct.Struct("@4i6P2P")              # dgc_scan_one
 TOP = struct.Struct("@4iq2P2P")                  # dgc_top
 DISTILL = struct.Struct("@4iq2P3P4f3P2P")        # dgc_distill
@@ -503,6 +504,18 @@ def _vec(t: Optional[torch.Tensor], dtype, numel: int, device: int, what: str) -
     return t.data_ptr()
 
 
+def _scan(call, name: str, args: bytes, tokens: int, num_seqs: int, stream, device: int) -> None:
+    """The scan calls, with a workspace where one is of use (asked for long sequences only)."""
+    if tokens >= 2048 * num_seqs > 0:
+        need = int(_lib.dgc_gated_scan_workspace_bytes(args))
+        if need > 0:
+            work = torch.empty(need, dtype=torch.uint8, device=f"cuda:{device}")
+            if stream is not None:   # the allocator must not hand it out again before that stream is done
+                work.record_stream(torch.cuda.ExternalStream(_stream(stream), device=device))
+            args = args[:-16] + struct.pack("@Pq", work.data_ptr(), need)
+    _enqueue(call, name, args, stream, device)
+
+
 def gated_scan_forward(gate: torch.Tensor, x: torch.Tensor, h: torch.Tensor,
                        seq_start: Optional[torch.Tensor] = None, num_seqs: int = 1,
                        h0: Optional[torch.Tensor] = None, h_last: Optional[torch.Tensor] = None,
@@ -517,8 +530,8 @@ def gated_scan_forward(gate: torch.Tensor, x: torch.Tensor, h: torch.Tensor,
     args = SCAN.pack(code, num_seqs, c, 1 if reverse else 0, n,
                      _vec(seq_start, torch.int32, num_seqs + 1, dev, "seq_start"), zp, zl, xp, xl, hp, hl,
                      _vec(h0, torch.float32, num_seqs * c, dev, "h0"),
-                     _vec(h_last, torch.float32, num_seqs * c, dev, "h_last"), 0, 0, 0, 0, 0, 0, 0, 0)
-    _enqueue(_lib.dgc_gated_scan_forward, "dgc_gated_scan_forward", args, stream, dev)
+                     _vec(h_last, torch.float32, num_seqs * c, dev, "h_last"), 0, 0, 0, 0, 0, 0, 0, 0, 0, 0)
+    _scan(_lib.dgc_gated_scan_forward, "dgc_gated_scan_forward", args, n, num_seqs, stream, dev)
 
 
 def gated_scan_backward(gate: torch.Tensor, x: torch.Tensor, h: torch.Tensor, dh: torch.Tensor,
@@ -539,8 +552,8 @@ def gated_scan_backward(gate: torch.Tensor, x: torch.Tensor, h: torch.Tensor, dh
                      _vec(seq_start, torch.int32, num_seqs + 1, dev, "seq_start"), zp, zl, xp, xl, hp, hl,
                      _vec(h0, torch.float32, num_seqs * c, dev, "h0"), 0, dp, dl, gp, gl, yp, yl,
                      _vec(dh_last, torch.float32, num_seqs * c, dev, "dh_last"),
-                     _vec(dh0, torch.float32, num_seqs * c, dev, "dh0"))
-    _enqueue(_lib.dgc_gated_scan_backward, "dgc_gated_scan_backward", args, stream, dev)
+                     _vec(dh0, torch.float32, num_seqs * c, dev, "dh0"), 0, 0)
+    _scan(_lib.dgc_gated_scan_backward, "dgc_gated_scan_backward", args, n, num_seqs, stream, dev)
 
 
 def gated_scan_step(gate: torch.Tensor, x: torch.Tensor, state: torch.Tensor, out: torch.Tensor,

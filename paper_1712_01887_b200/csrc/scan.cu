@@ -15,10 +15,11 @@
 // asynchronous copies, a stage ahead, whatever the alignment of the rows (see copy_rows).  Every
 // thread walks its run once to reduce it to (P, S), the runs are joined in order through shared
 // memory (the blocks' through the cluster's), and a second walk over the coefficients kept in
-// registers starts from the true state.  One pass over the data, no workspace, and a fixed
-// order of the additions: results do not vary from run to run.
+// registers starts from the true state.  One pass over the data, and a fixed order of the
+// additions: results do not vary from run to run.  A few long, narrow sequences go another way,
+// by a workspace: see there.
 //
-// A sequence is one cluster's work, so nothing (no infinity, no NaN) can cross from one
+// A sequence's runs are joined among themselves alone, so nothing (no infinity, no NaN) can cross from one
 // sequence into its neighbour in the pack.
 
 #include <cooperative_groups.h>
@@ -599,6 +600,284 @@ __global__ void __launch_bounds__(NW * G * 32, BLOCKS) k_scan_backward(const Sca
   wait_copies<0>();
 }
 
+// ------------------------------------------------------------------ few and narrow sequences
+// A few long sequences of few channels leave most SMs idle above, and a cluster's rounds are a
+// chain.  With a workspace they are cut into runs of kRun steps that any warp can take: one kernel
+// reduces every run to its map, one joins the maps of a sequence and leaves every run's start, one
+// walks the runs again from there and writes.  The rows are read twice, the second time mostly out
+// of L2; which calls take this way, and what it measured, stands at wide_bytes.
+constexpr int kRun = 64, kWideWarps = 4, kJoinWarps = 16;
+
+// Run c of sequence s has the slot first / kRun + s + c: different ones for all runs, below
+// tokens / kRun + seqs.
+struct WideArgs {
+  ScanArgs a;
+  float2* maps;      // [slots][channels]: P and S; after the join, P is the start
+};
+
+template <class T>
+struct WidePlace {   // a warp's run and channels
+  static constexpr int VEC = 4 / sizeof(T);
+  int lane, s, c0, c, first, len, at, width;   // at: the run's first step
+  bool on0, on1, any;
+  int64_t slot, at0, dir;
+  __device__ __forceinline__ explicit WidePlace(const ScanArgs& a) {
+    lane = threadIdx.x & 31;
+    slot = (int64_t)blockIdx.x * kWideWarps + (threadIdx.x >> 5);
+    c0 = blockIdx.y * 32 * VEC;
+    c = c0 + lane * VEC;
+    on0 = c < a.channels;
+    on1 = c + 1 < a.channels;
+    width = min(32 * VEC, a.channels - c0) * (int)sizeof(T);
+    any = false;
+    for (int q0 = 0; q0 < a.seqs && !any; q0 += 32) {   // whose run is it: 32 sequences at a time
+      const int q = q0 + lane;
+      int f = 0, l = 0;
+      if (q < a.seqs) sequence_range(a, q, f, l);
+      const int64_t run = slot - (f / kRun + q);
+      const uint32_t hit = __ballot_sync(0xFFFFFFFFu, q < a.seqs && run >= 0 && run * kRun < l);
+      if (hit) {
+        const int who = __ffs(hit) - 1;
+        any = true;
+        s = q0 + who;
+        first = __shfl_sync(0xFFFFFFFFu, f, who);
+        len = __shfl_sync(0xFFFFFFFFu, l, who);
+        at = (int)(__shfl_sync(0xFFFFFFFFu, (int)run, who) * kRun);
+      }
+    }
+    if (any) {
+      at0 = a.reverse ? (int64_t)first + len - 1 : first;
+      dir = a.reverse ? -1 : 1;
+    }
+  }
+};
+
+// Maps of the runs: forward of z and x, backward of z and dh (walked from the run's end).
+template <class T, Lie LIE, bool BACK>
+__global__ void __launch_bounds__(kWideWarps * 32) k_wide_reduce(const WideArgs w) {
+  pdl_enter();
+  constexpr int VEC = 4 / sizeof(T), L = 16, kPart = L * kPitch<LIE>;
+  __shared__ __align__(128) char buffer[kWideWarps][2][2][kPart];
+  const ScanArgs& a = w.a;
+  const WidePlace<T> at(a);
+  if (!at.any) return;   // (a warp on its own: nothing below waits for another)
+  const Matrix& second = BACK ? a.dh : a.x;
+  char (*mine)[2][kPart] = buffer[threadIdx.x >> 5];
+  const int n = min(at.len - at.at, kRun);             // steps of the run
+  const int stages = (n + L - 1) / L;
+  const auto stage_of = [&](int i) { return BACK ? stages - 1 - i : i; };
+  const auto fetch = [&](int i) {
+    if (i < stages) {
+      const int64_t row = at.at0 + at.dir * (int64_t)(at.at + stage_of(i) * L);
+      const int hi = min(n - stage_of(i) * L, L);
+      const char* p = first_copy<T, LIE>(a.z, row, at.c0, a.z.stride, at.lane);
+      copy_rows<T, LIE, L>(mine[i & 1][0], p, a.z, a.z.stride, 0, 0, hi, at.width, at.lane);
+      p = first_copy<T, LIE>(second, row, at.c0, second.stride, at.lane);
+      copy_rows<T, LIE, L>(mine[i & 1][1], p, second, second.stride, 0, 0, hi, at.width, at.lane);
+    }
+    end_copies();
+  };
+  fetch(0);
+  fetch(1);
+  Val<VEC> P = fill<VEC>(1.0f), S = fill<VEC>(0.0f);
+  for (int i = 0; i < stages; ++i) {
+    wait_copies<1>();
+    const int t0 = stage_of(i) * L;
+    const int64_t row = at.at0 + at.dir * (int64_t)(at.at + t0);
+    const uint32_t z0 = (uint32_t)reinterpret_cast<uintptr_t>(row_at<T>(a.z, row, at.c0));
+    const uint32_t y0 = (uint32_t)reinterpret_cast<uintptr_t>(row_at<T>(second, row, at.c0));
+#pragma unroll
+    for (int k = 0; k < L; ++k) {
+      const int j = BACK ? L - 1 - k : k;
+      Val<VEC> f, omf;
+      gate(row_word<T, LIE>(mine[i & 1][0], z0, (uint32_t)a.z.stride, j, at.lane), f, omf);
+      const Val<VEC> y = row_word<T, LIE>(mine[i & 1][1], y0, (uint32_t)second.stride, j, at.lane);
+      if (t0 + j < n) {
+        P = mul_(P, f);
+        S = BACK ? mul_(f, add_(y, S)) : fma_(f, S, mul_(omf, y));
+      }
+    }
+    __syncwarp();
+    fetch(i + 2);
+  }
+  wait_copies<0>();
+  float2* m = w.maps + at.slot * a.channels + at.c;
+#pragma unroll
+  for (int v = 0; v < VEC; ++v)
+    if (v ? at.on1 : at.on0) m[v] = make_float2(P.v[v], S.v[v]);
+}
+
+// The starts of a sequence's runs, in the order of the walk, and the state after the last.
+__global__ void __launch_bounds__(kJoinWarps * 32) k_wide_join(const WideArgs w, int back) {
+  pdl_enter();
+  __shared__ float2 parts[kJoinWarps][32];
+  const ScanArgs& a = w.a;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, s = blockIdx.y, c = blockIdx.x * 32 + lane;
+  const bool on = c < a.channels;
+  int first, len;
+  sequence_range(a, s, first, len);
+  const int runs = (len + kRun - 1) / kRun, share = (runs + kJoinWarps - 1) / kJoinWarps;
+  const int lo = min(warp * share, runs), hi = min(lo + share, runs);
+  float2* maps = w.maps + (int64_t)(first / kRun + s) * a.channels + c;
+  const auto map = [&](int i) -> float2& { return maps[(int64_t)(back ? runs - 1 - i : i) * a.channels]; };
+  float2 t = make_float2(1.0f, 0.0f);
+  if (on) {
+#pragma unroll 8
+    for (int i = lo; i < hi; ++i) {
+      const float2 m = map(i);
+      t = make_float2(m.x * t.x, fmaf(m.x, t.y, m.y));
+    }
+  }
+  parts[warp][lane] = t;
+  __syncthreads();
+  if (!on) return;
+  const float* from = back ? a.dh_last : a.h0;
+  float cur = from ? from[(int64_t)s * a.channels + c] : 0.0f;
+  for (int q = 0; q < warp; ++q) cur = fmaf(parts[q][lane].x, cur, parts[q][lane].y);
+  for (int i0 = lo; i0 < hi; i0 += 8) {   // eight loads before the stores that they could meet
+    float2 m[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) m[k] = map(min(i0 + k, hi - 1));
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (i0 + k < hi) {
+        map(i0 + k).x = cur;
+        cur = fmaf(m[k].x, cur, m[k].y);
+      }
+  }
+  float* to = back ? a.dh0 : a.h_last;
+  if (to && warp == kJoinWarps - 1) to[(int64_t)s * a.channels + c] = cur;
+}
+
+template <class T, Lie LIE>
+__global__ void __launch_bounds__(kWideWarps * 32) k_wide_forward(const WideArgs w) {
+  pdl_enter();
+  constexpr int VEC = 4 / sizeof(T), L = 16, kPart = L * kPitch<LIE>;
+  __shared__ __align__(128) char buffer[kWideWarps][2][2][kPart];
+  const ScanArgs& a = w.a;
+  const WidePlace<T> at(a);
+  if (!at.any) return;
+  char (*mine)[2][kPart] = buffer[threadIdx.x >> 5];
+  const int n = min(at.len - at.at, kRun), stages = (n + L - 1) / L;
+  const auto fetch = [&](int i) {
+    if (i < stages) {
+      const int64_t row = at.at0 + at.dir * (int64_t)(at.at + i * L);
+      const int hi = min(n - i * L, L);
+      const char* p = first_copy<T, LIE>(a.z, row, at.c0, a.z.stride, at.lane);
+      copy_rows<T, LIE, L>(mine[i & 1][0], p, a.z, a.z.stride, 0, 0, hi, at.width, at.lane);
+      p = first_copy<T, LIE>(a.x, row, at.c0, a.x.stride, at.lane);
+      copy_rows<T, LIE, L>(mine[i & 1][1], p, a.x, a.x.stride, 0, 0, hi, at.width, at.lane);
+    }
+    end_copies();
+  };
+  fetch(0);
+  fetch(1);
+  const float2* m = w.maps + at.slot * a.channels + at.c;
+  Val<VEC> cur;
+#pragma unroll
+  for (int v = 0; v < VEC; ++v) cur.v[v] = (v ? at.on1 : at.on0) ? m[v].x : 0.0f;
+  char* out = row_at<T>(a.h, at.at0 + at.dir * (int64_t)at.at, at.c);
+  for (int i = 0; i < stages; ++i) {
+    wait_copies<1>();
+    const int64_t row = at.at0 + at.dir * (int64_t)(at.at + i * L);
+    const uint32_t z0 = (uint32_t)reinterpret_cast<uintptr_t>(row_at<T>(a.z, row, at.c0));
+    const uint32_t x0 = (uint32_t)reinterpret_cast<uintptr_t>(row_at<T>(a.x, row, at.c0));
+#pragma unroll
+    for (int j = 0; j < L; ++j, out += a.h.stride) {
+      Val<VEC> f, omf;
+      gate(row_word<T, LIE>(mine[i & 1][0], z0, (uint32_t)a.z.stride, j, at.lane), f, omf);
+      cur = fma_(f, cur, mul_(omf, row_word<T, LIE>(mine[i & 1][1], x0, (uint32_t)a.x.stride, j, at.lane)));
+      if (i * L + j < n) put_word<T, LIE>(out, cur, at.on0, at.on1);
+    }
+    __syncwarp();
+    fetch(i + 2);
+  }
+  wait_copies<0>();
+}
+
+template <class T, Lie LIE>
+__global__ void __launch_bounds__(kWideWarps * 32) k_wide_backward(const WideArgs w) {
+  pdl_enter();
+  constexpr int VEC = 4 / sizeof(T), L = 8, kPart = L * kPitch<LIE>;
+  __shared__ __align__(128) char buffer[kWideWarps][2][3][kPart];
+  const ScanArgs& a = w.a;
+  const WidePlace<T> at(a);
+  if (!at.any) return;
+  char (*mine)[3][kPart] = buffer[threadIdx.x >> 5];
+  const int n = min(at.len - at.at, kRun), stages = (n + L - 1) / L;
+  uint32_t before[2] = {0, 0};   // the stored state before the next stage's first step, as it lies
+  const auto fetch_state = [&](int i) {
+    const int64_t t = at.at + (stages - 1 - i) * L - 1;
+    if (i < stages && t >= 0) {
+      const T* p = reinterpret_cast<const T*>(row_at<T>(a.h, at.at0 + at.dir * t, at.c));
+      if constexpr (LIE == kHalves) {
+        if (at.on0) before[0] = load_word<T, 1>(p);
+        if (at.on1) before[1] = load_word<T, 1>(p + 1);
+      } else {
+        if (at.on0) before[0] = load_word<T, VEC>(p);
+      }
+    }
+  };
+  const auto fetch = [&](int i) {
+    if (i < stages) {
+      const int64_t row = at.at0 + at.dir * (int64_t)(at.at + (stages - 1 - i) * L);
+      const int hi = min(n - (stages - 1 - i) * L, L);
+      const Matrix* from[3] = {&a.z, &a.x, &a.dh};
+#pragma unroll
+      for (int q = 0; q < 3; ++q) {
+        const char* p = first_copy<T, LIE>(*from[q], row, at.c0, from[q]->stride, at.lane);
+        copy_rows<T, LIE, L>(mine[i & 1][q], p, *from[q], from[q]->stride, 0, 0, hi, at.width, at.lane);
+      }
+    }
+    end_copies();
+  };
+  fetch(0);
+  fetch(1);
+  fetch_state(0);
+  const float2* m = w.maps + at.slot * a.channels + at.c;
+  Val<VEC> cur, start;
+#pragma unroll
+  for (int v = 0; v < VEC; ++v) {
+    const bool on = v ? at.on1 : at.on0;
+    cur.v[v] = on ? m[v].x : 0.0f;
+    start.v[v] = on && a.h0 ? a.h0[(int64_t)at.s * a.channels + at.c + v] : 0.0f;
+  }
+  for (int i = 0; i < stages; ++i) {
+    const int t0 = (stages - 1 - i) * L;
+    const int64_t row = at.at0 + at.dir * (int64_t)(at.at + t0);
+    const uint32_t z0 = (uint32_t)reinterpret_cast<uintptr_t>(row_at<T>(a.z, row, at.c0));
+    const uint32_t x0 = (uint32_t)reinterpret_cast<uintptr_t>(row_at<T>(a.x, row, at.c0));
+    const uint32_t d0 = (uint32_t)reinterpret_cast<uintptr_t>(row_at<T>(a.dh, row, at.c0));
+    Val<VEC> hp, f[L], omf[L], e[L];
+    if constexpr (LIE == kHalves) unpack<T, 2>(before[0] | before[1] << 16, hp.v);
+    else unpack<T, VEC>(before[0], hp.v);
+    if (at.at + t0 == 0) hp = start;
+    fetch_state(i + 1);
+    wait_copies<1>();
+#pragma unroll
+    for (int j = 0; j < L; ++j) {
+      gate(row_word<T, LIE>(mine[i & 1][0], z0, (uint32_t)a.z.stride, j, at.lane), f[j], omf[j]);
+      const Val<VEC> x_t = row_word<T, LIE>(mine[i & 1][1], x0, (uint32_t)a.x.stride, j, at.lane);
+      e[j] = sub_(hp, x_t);
+      hp = fma_(f[j], hp, mul_(omf[j], x_t));   // (past the run's end: not used)
+    }
+    char* gz = row_at<T>(a.dz, row + at.dir * (L - 1), at.c);
+    char* gx = row_at<T>(a.dx, row + at.dir * (L - 1), at.c);
+#pragma unroll
+    for (int j = L - 1; j >= 0; --j, gz -= a.dz.stride, gx -= a.dx.stride) {
+      if (t0 + j < n) {
+        const Val<VEC> gt = add_(row_word<T, LIE>(mine[i & 1][2], d0, (uint32_t)a.dh.stride, j, at.lane), cur);
+        cur = mul_(f[j], gt);
+        put_word<T, LIE>(gx, mul_(omf[j], gt), at.on0, at.on1);
+        put_word<T, LIE>(gz, mul_(mul_(omf[j], cur), e[j]), at.on0, at.on1);
+      }
+    }
+    __syncwarp();
+    fetch(i + 2);
+  }
+  wait_copies<0>();
+}
+
 // One token a sequence: the state is read, advanced and written back where it lies.  A thread
 // takes N neighbouring channels (4, in words of 16 bytes of state, where everything is aligned
 // for that), a block's rows are given by the grid's second dimension: no divisions.
@@ -632,6 +911,48 @@ k_scan_step(const T* z, int64_t ld_z, const T* x, int64_t ld_x, float* state, co
 }
 
 constexpr int kFwdL = 16, kBwdL = 8, kSms = 148;
+constexpr int kWideUnits = 16, kWideShort = 2048, kWideLong = 8192, kWideWork = 32768;
+
+template <class T>
+void lay_out(ScanArgs& a) {
+  for (Matrix* m : {&a.z, &a.x, &a.h, &a.dh, &a.dz, &a.dx}) {
+    m->end = m->begin + ((int64_t)(a.tokens - 1) * m->ld + a.channels) * (int64_t)sizeof(T);
+    m->stride = (a.reverse ? -m->ld : m->ld) * (int64_t)sizeof(T);
+  }
+}
+
+// Bytes of workspace with which a call goes by runs; 0 where it would not.  Its three launches take
+// 9 us forward and 13 backward at the least, whatever they work on; a cluster a sequence takes
+// (forward / backward, runs against clusters, bf16 unless stated, in a graph)
+//   60000 steps x  100 f16   36 / 46 against 68 / 112 us      8192 x  256    9.3 / 13.8 against 9.4 / 13.9
+//   30000 x 1024             68 / 91 against 81 / 131         4096 x  256    9.8 / 13.9 against 6.7 /  9.3
+//   16384 x   64 f16        9.8 / 14 against 14 /  23         2048 x 1024    9.3 / 13.4 against 10.8 / 15.0
+int64_t wide_bytes(int64_t tokens, int32_t seqs, int32_t channels, size_t es) {
+  const int32_t words = 128 / (int32_t)es;
+  const int64_t units = (int64_t)((channels + words - 1) / words) * seqs;
+  const int64_t len = tokens / seqs;
+  if (units > kWideUnits || len < kWideShort || (len < kWideLong && len * units < kWideWork)) return 0;
+  return (tokens / kRun + seqs) * channels * (int64_t)sizeof(float2);
+}
+
+template <class T, Lie LIE>
+int32_t enqueue_wide(ScanArgs a, float2* maps, bool backward, cudaStream_t s) {
+  lay_out<T>(a);
+  const WideArgs w{a, maps};
+  constexpr int words = 128 / (int)sizeof(T);
+  const int64_t slots = (int64_t)a.tokens / kRun + a.seqs;
+  const dim3 grid((unsigned)((slots + kWideWarps - 1) / kWideWarps), (a.channels + words - 1) / words);
+  const dim3 threads(kWideWarps * 32), join((a.channels + 31) / 32, a.seqs);
+  if (backward) launch(k_wide_reduce<T, LIE, true>, grid, threads, 0, s, w);
+  else launch(k_wide_reduce<T, LIE, false>, grid, threads, 0, s, w);
+  int32_t rc = check_launch();
+  if (rc != DGC_OK) return rc;
+  launch(k_wide_join, join, dim3(kJoinWarps * 32), 0, s, w, backward ? 1 : 0);
+  if ((rc = check_launch()) != DGC_OK) return rc;
+  if (backward) launch(k_wide_backward<T, LIE>, grid, threads, 0, s, w);
+  else launch(k_wide_forward<T, LIE>, grid, threads, 0, s, w);
+  return check_launch();
+}
 
 template <class T, Lie LIE, int NW, int G, int CL>
 int32_t enqueue(ScanArgs a, bool backward, cudaStream_t s) {
@@ -650,10 +971,7 @@ int32_t enqueue(ScanArgs a, bool backward, cudaStream_t s) {
   a.longest_first = a.seq_start && a.seqs > 1 && a.seqs <= kSorted && units > kSms;
   int64_t grid = units * a.cluster;
   if (grid > INT32_MAX) return DGC_EINVAL;
-  for (Matrix* m : {&a.z, &a.x, &a.h, &a.dh, &a.dz, &a.dx}) {
-    m->end = m->begin + ((int64_t)(a.tokens - 1) * m->ld + a.channels) * (int64_t)sizeof(T);
-    m->stride = (a.reverse ? -m->ld : m->ld) * (int64_t)sizeof(T);
-  }
+  lay_out<T>(a);
   const size_t smem = G * NW * kStages * kPitch<LIE> * (backward ? 3 * kBwdL : 2 * kFwdL);
   auto go = [&](auto kernel) {
     constexpr auto f = decltype(kernel)::value;
@@ -684,10 +1002,11 @@ int32_t enqueue(ScanArgs a, bool backward, cudaStream_t s) {
 //                            (the longest then decides): 20 of 500 on average x 1024 16 / 24 us against
 //                            20 / 37; clusters are for these
 // More blocks of a cluster than the portable eight where next to nothing else is there to do
-// (69 against 131 us for one sequence of 60000 x 100 f16); beyond four clusters of sixteen not all
+// (69 against 131 us for one sequence of 60000 x 100 f16 without a workspace); beyond four clusters of sixteen not all
 // find room at once (8 of them: 19 against 14 us for 8192 x 512).
 template <class T, Lie LIE>
-int32_t enqueue(const ScanArgs& a, bool backward, cudaStream_t s) {
+int32_t enqueue(const ScanArgs& a, float2* maps, bool backward, cudaStream_t s) {
+  if (maps) return enqueue_wide<T, LIE>(a, maps, backward, s);
   const int32_t len = a.tokens / a.seqs, words = 32 * 4 / (int)sizeof(T);
   const int64_t units = (int64_t)((a.channels + words - 1) / words) * a.seqs;
   const bool uneven = a.seq_start != nullptr;
@@ -699,16 +1018,16 @@ int32_t enqueue(const ScanArgs& a, bool backward, cudaStream_t s) {
   return enqueue<T, LIE, 8, 2, kPortableCluster>(a, backward, s);
 }
 
-int32_t dispatch(const ScanArgs& a, int32_t dtype, bool backward, Lie lie, cudaStream_t s) {
+int32_t dispatch(const ScanArgs& a, float2* maps, int32_t dtype, bool backward, Lie lie, cudaStream_t s) {
   if (dtype == DGC_F32)
-    return lie == kAligned ? enqueue<float, kAligned>(a, backward, s) : enqueue<float, kWords>(a, backward, s);
+    return lie == kAligned ? enqueue<float, kAligned>(a, maps, backward, s) : enqueue<float, kWords>(a, maps, backward, s);
   if (dtype == DGC_BF16)
-    return lie == kAligned ? enqueue<__nv_bfloat16, kAligned>(a, backward, s)
-           : lie == kWords ? enqueue<__nv_bfloat16, kWords>(a, backward, s)
-                           : enqueue<__nv_bfloat16, kHalves>(a, backward, s);
-  return lie == kAligned ? enqueue<__half, kAligned>(a, backward, s)
-         : lie == kWords ? enqueue<__half, kWords>(a, backward, s)
-                         : enqueue<__half, kHalves>(a, backward, s);
+    return lie == kAligned ? enqueue<__nv_bfloat16, kAligned>(a, maps, backward, s)
+           : lie == kWords ? enqueue<__nv_bfloat16, kWords>(a, maps, backward, s)
+                           : enqueue<__nv_bfloat16, kHalves>(a, maps, backward, s);
+  return lie == kAligned ? enqueue<__half, kAligned>(a, maps, backward, s)
+         : lie == kWords ? enqueue<__half, kWords>(a, maps, backward, s)
+                         : enqueue<__half, kHalves>(a, maps, backward, s);
 }
 
 Matrix matrix(const dgc_matrix& m) { return Matrix{static_cast<char*>(m.data), nullptr, m.ld, 0}; }
@@ -726,7 +1045,9 @@ int32_t scan(const dgc_scan* d, bool backward, void* stream) {
     return DGC_EINVAL;
   const size_t es = element_size(d->dtype);
   const auto bad = [&](const dgc_matrix& m) { return bad_matrix(m, d->tokens, d->channels, es); };
-  if (bad(d->gate) || bad(d->x) || bad(d->h) || misaligned(d->h0, 4) || misaligned(d->seq_start, 4)) return DGC_EINVAL;
+  if (bad(d->gate) || bad(d->x) || bad(d->h) || misaligned(d->h0, 4) || misaligned(d->seq_start, 4) ||
+      misaligned(d->workspace, 8) || d->workspace_bytes < 0)
+    return DGC_EINVAL;
   if (backward ? bad(d->dh) || bad(d->dgate) || bad(d->dx) || misaligned(d->dh_last, 4) || misaligned(d->dh0, 4)
                : misaligned(d->h_last, 4))
     return DGC_EINVAL;
@@ -736,13 +1057,16 @@ int32_t scan(const dgc_scan* d, bool backward, void* stream) {
   a.h0 = d->h0; a.seq_start = d->seq_start;
   a.tokens = (int32_t)d->tokens; a.seqs = d->num_seqs; a.seq_len = (int32_t)(d->tokens / d->num_seqs);
   a.channels = d->channels; a.reverse = d->reverse != 0;
+  const int64_t wide = d->workspace ? wide_bytes(d->tokens, d->num_seqs, d->channels, es) : 0;
+  if (wide && d->workspace_bytes < wide) return DGC_ECAPACITY;
+  float2* const maps = wide ? static_cast<float2*>(d->workspace) : nullptr;
   if (!backward) {
     a.h_last = d->h_last;
-    return dispatch(a, d->dtype, false, lie_of({a.z, a.x, a.h}, a.channels, es), as_stream(stream));
+    return dispatch(a, maps, d->dtype, false, lie_of({a.z, a.x, a.h}, a.channels, es), as_stream(stream));
   }
   a.dh = matrix(d->dh); a.dz = matrix(d->dgate); a.dx = matrix(d->dx);
   a.dh_last = d->dh_last; a.dh0 = d->dh0;
-  return dispatch(a, d->dtype, true, lie_of({a.z, a.x, a.h, a.dh, a.dz, a.dx}, a.channels, es), as_stream(stream));
+  return dispatch(a, maps, d->dtype, true, lie_of({a.z, a.x, a.h, a.dh, a.dz, a.dx}, a.channels, es), as_stream(stream));
 }
 
 }  // namespace
@@ -751,6 +1075,12 @@ extern "C" {
 
 int32_t dgc_gated_scan_forward(const dgc_scan* d, void* stream) { return scan(d, false, stream); }
 int32_t dgc_gated_scan_backward(const dgc_scan* d, void* stream) { return scan(d, true, stream); }
+
+int64_t dgc_gated_scan_workspace_bytes(const dgc_scan* d) {
+  if (!d || bad_dtype(d->dtype) || d->tokens < 0 || d->tokens > INT32_MAX || d->num_seqs < 1 || d->channels < 1)
+    return DGC_EINVAL;
+  return wide_bytes(d->tokens, d->num_seqs, d->channels, element_size(d->dtype));
+}
 
 int32_t dgc_gated_scan_step(const dgc_scan_one* d, void* stream) {
   if (!d || bad_dtype(d->dtype) || d->rows < 0 || d->channels < 1 || d->num_slots < 0) return DGC_EINVAL;

@@ -161,6 +161,20 @@ def test_scan_of_many_sequences_and_long_ones():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dt", DT, ids=str)
+@pytest.mark.parametrize("lens,C,joint,packed", [
+    ([8192], 64, 0, False), ([16385], 33, 0, True), ([8447], 1, 1, True), ([0, 20000, 64, 1, 32764], 10, 2, True),
+    ([24000, 63, 1025], 130, 0, True), ([8192, 8192], 100, 4, False), ([4096], 512, 0, True)])
+@pytest.mark.parametrize("reverse", [False, True])
+def test_long_and_narrow_sequences_go_by_runs(lens, C, joint, packed, reverse, dt):
+    """The sizes that take a workspace: runs that end inside a stage, empty sequences, one step."""
+    B = _bind()
+    assert B._lib.dgc_gated_scan_workspace_bytes(B.SCAN.pack(B.DTYPES[dt], len(lens), C, 0, sum(lens), *[0] * 19)) > 0
+    _check(B, lens, C, dt, joint, reverse, packed=packed, seed=C)
+    _check(B, lens, C, dt, joint, reverse, packed=packed, seed=C + 1, with_h0=False)
+
+
+@pytest.mark.gpu
 def test_extreme_gates_and_neighbours_that_are_not_finite():
     """Gates of +-inf and of the type's lowest value are exactly 1 and 0; a sequence full of NaN
     and infinities leaves its neighbours in the pack untouched, bit for bit."""
@@ -282,17 +296,25 @@ def test_refusals_of_the_c_calls():
     p = 4096
 
     def scan(call, dtype=0, tokens=8, seqs=2, ch=4, table=0, z=p, ldz=4, x=p, ldx=4, h=p, ldh=4, h0=0, last=0, dh=p, lddh=4, dz=p,
-             lddz=4, dx=p, lddx=4, dlast=0, dh0=0):
+             lddz=4, dx=p, lddx=4, dlast=0, dh0=0, work=0, size=0):
         return call(B.SCAN.pack(dtype, seqs, ch, 0, tokens, table, z, ldz, x, ldx, h, ldh, h0, last, dh, lddh, dz, lddz, dx, lddx,
-                                dlast, dh0), None)
+                                dlast, dh0, work, size), None)
     both = [dict(dtype=3), dict(dtype=-1), dict(tokens=-1), dict(tokens=7), dict(tokens=1 << 31), dict(seqs=0), dict(seqs=-1), dict(ch=0),
             dict(ch=-4), dict(ldz=3), dict(ldx=0), dict(ldh=-4), dict(z=0), dict(x=0), dict(h=0), dict(x=p + 2), dict(dtype=1, h=p + 1),
-            dict(table=p + 2), dict(h0=p + 1)]
+            dict(table=p + 2), dict(h0=p + 1), dict(work=p + 4, size=64), dict(work=p, size=-1)]
     for bad in both + [dict(last=p + 2)]:
         assert scan(B._lib.dgc_gated_scan_forward, **bad) == B.EINVAL, bad
     for bad in both + [dict(dh=0), dict(dz=0), dict(dx=0), dict(lddh=3), dict(lddz=3), dict(lddx=3), dict(dh=p + 1), dict(dlast=p + 1),
                        dict(dh0=p + 2)]:
         assert scan(B._lib.dgc_gated_scan_backward, **bad) == B.EINVAL, bad
+
+    for call in (B._lib.dgc_gated_scan_forward, B._lib.dgc_gated_scan_backward):   # a workspace that is too small
+        assert scan(call, tokens=8192, seqs=1, work=p, size=100) == B.ECAPACITY
+    size = B._lib.dgc_gated_scan_workspace_bytes
+    pack = lambda dtype, seqs, ch, tokens: B.SCAN.pack(dtype, seqs, ch, 0, tokens, *[0] * 19)  # noqa: E731
+    assert size(pack(1, 1, 100, 8192)) == (8192 // 64 + 1) * 100 * 8
+    assert size(pack(1, 1, 100, 100)) == 0 and size(pack(1, 8, 4096, 65536)) == 0
+    assert size(pack(7, 1, 1, 1)) == B.EINVAL and size(None) == B.EINVAL
 
     def step(dtype=0, rows=2, ch=4, n=2, z=p, ldz=4, x=p, ldx=4, out=p, ldo=4, state=p, slots=0):
         return B._lib.dgc_gated_scan_step(B.SCAN_ONE.pack(dtype, rows, ch, n, z, ldz, x, ldx, out, ldo, state, slots), None)
