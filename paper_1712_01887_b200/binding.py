@@ -509,9 +509,11 @@ def _scan(call, name: str, args: bytes, tokens: int, num_seqs: int, stream, devi
     if tokens >= 2048 * num_seqs > 0:
         need = int(_lib.dgc_gated_scan_workspace_bytes(args))
         if need > 0:
-            work = torch.empty(need, dtype=torch.uint8, device=f"cuda:{device}")
-            if stream is not None:   # the allocator must not hand it out again before that stream is done
-                work.record_stream(torch.cuda.ExternalStream(_stream(stream), device=device))
+            if stream is None:
+                work = torch.empty(need, dtype=torch.uint8, device=f"cuda:{device}")
+            else:   # from the call's own stream: what was freed on another may still be written there
+                with torch.cuda.stream(torch.cuda.ExternalStream(_stream(stream), device=device)):
+                    work = torch.empty(need, dtype=torch.uint8, device=f"cuda:{device}")
             args = args[:-16] + struct.pack("@Pq", work.data_ptr(), need)
     _enqueue(call, name, args, stream, device)
 

@@ -175,6 +175,27 @@ def test_long_and_narrow_sequences_go_by_runs(lens, C, joint, packed, reverse, d
 
 
 @pytest.mark.gpu
+def test_long_sequences_on_two_streams_at_once():
+    """Calls on a given stream beside calls on the current one: each has a workspace of its own."""
+    B = _bind()
+    g = torch.Generator(device="cuda").manual_seed(5)
+    z, x = (torch.randn(40000, 96, device="cuda", generator=g) for _ in range(2))
+    want = [torch.empty_like(z) for _ in range(2)]
+    B.gated_scan_forward(z, x, want[0])
+    B.gated_scan_forward(x, z, want[1])
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = [[torch.empty_like(z) for _ in range(2)] for _ in range(6)]
+    torch.cuda.synchronize()
+    for a, b in got:
+        B.gated_scan_forward(z, x, a)
+        B.gated_scan_forward(x, z, b, stream=side)
+    torch.cuda.synchronize()
+    for a, b in got:
+        assert torch.equal(a, want[0]) and torch.equal(b, want[1])
+
+
+@pytest.mark.gpu
 def test_extreme_gates_and_neighbours_that_are_not_finite():
     """Gates of +-inf and of the type's lowest value are exactly 1 and 0; a sequence full of NaN
     and infinities leaves its neighbours in the pack untouched, bit for bit."""
