@@ -401,7 +401,8 @@ int32_t dgc_timeline_read(dgc_state* st, void* stream, uint64_t* ns_out);
  * at any alignment of the element.  All arithmetic is in 32 bits; results are rounded once.
  * Outputs must not overlap inputs unless stated.  Errors: DGC_EINVAL (a NULL struct, a size
  * out of range, a stride below the row's length, a required pointer NULL or misaligned; nothing
- * is enqueued then), DGC_ECUDA.  Asynchronous on `stream`; may be captured into a CUDA graph. */
+ * is enqueued then), DGC_ECUDA.  Asynchronous on `stream`; may be captured into a CUDA graph.
+ * They run on the calling thread's current device, which `stream` and all pointers belong to. */
 typedef struct dgc_matrix {
   void*   data;    /* device; inputs are not modified */
   int64_t ld;      /* elements from one row to the next */

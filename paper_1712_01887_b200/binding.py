@@ -463,10 +463,17 @@ SCAN_ONE = struct.Struct("@4i6P2P")              # dgc_scan_one
 TOP = struct.Struct("@4iq2P2P")                  # dgc_top
 DISTILL = struct.Struct("@4iq2P3P4f3P2P")        # dgc_distill
 _raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else None
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _enqueue(call, name: str, args: bytes, stream, device: int) -> None:
-    """Calls with the given stream, or the current one of the tensors' device."""
+    """Calls on the tensors' device (made current for the call where it is not), with the given
+    stream, or the current one of that device."""
+    if device != _current_device():
+        with torch.cuda.device(device):
+            return _enqueue(call, name, args, stream, device)
+    if isinstance(stream, torch.cuda.Stream) and stream.device_index != device:
+        raise ValueError(f"stream: it is of device {stream.device_index}, the tensors are on device {device}")
     rc = call(args, _raw_stream(device) if stream is None and _raw_stream else _stream(stream))
     if rc:
         _check(rc, name)
