@@ -7,6 +7,7 @@ pointers, `stream` arguments default to torch's current stream.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 import struct
@@ -511,16 +512,25 @@ def _vec(t: Optional[torch.Tensor], dtype, numel: int, device: int, what: str) -
     return t.data_ptr()
 
 
+def _stream_context(stream, device: int):
+    """Makes torch allocate from the call's stream.  (An external stream of handle 0 would not be
+    the default stream but one of torch's own.)"""
+    if stream is None:
+        return contextlib.nullcontext()
+    if isinstance(stream, torch.cuda.Stream):
+        return torch.cuda.stream(stream)
+    return torch.cuda.stream(torch.cuda.ExternalStream(int(stream), device=device) if int(stream)
+                             else torch.cuda.default_stream(device))
+
+
 def _scan(call, name: str, args: bytes, tokens: int, num_seqs: int, stream, device: int) -> None:
     """The scan calls, with a workspace where one is of use (asked for long sequences only)."""
     if tokens >= 2048 * num_seqs > 0:
         need = int(_lib.dgc_gated_scan_workspace_bytes(args))
         if need > 0:
-            if stream is None:
+            # from the call's own stream: what was freed on another may still be written there
+            with _stream_context(stream, device):
                 work = torch.empty(need, dtype=torch.uint8, device=f"cuda:{device}")
-            else:   # from the call's own stream: what was freed on another may still be written there
-                with torch.cuda.stream(torch.cuda.ExternalStream(_stream(stream), device=device)):
-                    work = torch.empty(need, dtype=torch.uint8, device=f"cuda:{device}")
             args = args[:-16] + struct.pack("@Pq", work.data_ptr(), need)
     _enqueue(call, name, args, stream, device)
 

@@ -93,3 +93,33 @@ def test_a_given_stream_is_of_the_tensors_device(machine):
         with pytest.raises(ValueError):
             call()
     assert len(machine.calls) == 14 and machine.current == 0
+
+
+def test_the_workspace_comes_from_the_calls_stream(machine, monkeypatch):
+    """Torch's allocator is asked on the very stream that the kernels run on, the default stream's
+    handle 0 included (an external stream of handle 0 is one of torch's own streams)."""
+    now, asked = [None], []
+
+    @contextlib.contextmanager
+    def stream(s):
+        before, now[0] = now[0], s.cuda_stream
+        try:
+            yield
+        finally:
+            now[0] = before
+
+    def empty(n, **how):
+        asked.append((n, now[0], how["device"]))
+        return Tensor((n,), torch.uint8, 1)
+    monkeypatch.setattr(torch.cuda, "stream", stream)
+    monkeypatch.setattr(torch.cuda, "ExternalStream", lambda handle, device: Stream(handle or "a stream of torch's", device))
+    monkeypatch.setattr(torch.cuda, "default_stream", lambda device: Stream(0, device))
+    monkeypatch.setattr(torch, "empty", empty)
+    m = [Tensor((8192, 40)) for _ in range(6)]
+    need = (8192 // 64 + 1) * 40 * 8
+    for given, handle in ((None, None), (Stream(77, 1), 77), (Stream(0, 1), 0), (55, 55), (0, 0)):
+        asked.clear()
+        B.gated_scan_forward(*m[:3], stream=given)
+        B.gated_scan_backward(*m, stream=given)
+        assert asked == [(need, handle, "cuda:1")] * 2 and now[0] is None
+        assert machine.calls[-2:] == [(1, 101 if given is None else handle)] * 2
