@@ -12,10 +12,10 @@
 //
 // Exponentials are 2^(s c - round(m c)), c = log2(e) / T, m the row's maximum: the rounding of m c is
 // the same factor in every term and cancels in p, and where the loss needs logarithms the same
-// expression is used.  Rows whose maximum is out of the range where m c is safe (a mask of the
-// type's lowest value in every place) or that hold no finite number are found by their sum and
-// done again as 2^((s - m) c).  Sums are 32-bit: a thread adds at most a few hundred terms, the
-// rest is a tree.
+// expression is used.  Below 2^24 that factor is within 2^-1/2 .. 2^1/2; rows whose m c or m log2(e)
+// is larger (a mask of -1e9 or of the type's lowest value in every place: the factor of 1e10 can be
+// 2^440, out of range) or that hold no finite number are done again as 2^((s - m) c).  Sums are
+// 32-bit: a thread adds at most a few hundred terms, the rest is a tree.
 
 #include <cooperative_groups.h>
 
@@ -46,7 +46,7 @@ struct DistillArgs {
   float *loss, *stats;
   int64_t ld, ld_d;
   float temperature, c, soft, hard;   // c = log2(e) / temperature
-  float lowest;                       // below it, and above its opposite, exponents are taken with care
+  float lowest;                       // maxima not above it, or not below its opposite, are taken with care
   int32_t vocab, k, cluster;
 };
 
@@ -130,7 +130,7 @@ __global__ void __launch_bounds__(NT, kBlocks<T, MODE> * 256 / NT) k_distill(con
     // sums, these as z 2^n each: p = 2^(s c - n) / z (a logarithm would cost p the bits before the
     // point).  Rows out of the ordinary have 0 there and are summed once more.
     const float x = a.stats_in[2 * r], x1 = a.stats_in[2 * r + 1];
-    walk = TWO ? !(x > kLeast && x < kMost && x1 > kLeast && x1 < kMost) : !(x1 > 0.0f);
+    walk = TWO ? !(x > kLeast && x < kMost && x1 > kLeast && x1 < kMost) : !(x1 > 0.0f && x1 < kMost);
     mc = x;
     sum = x1;
     if (TWO) {
@@ -175,7 +175,7 @@ __global__ void __launch_bounds__(NT, kBlocks<T, MODE> * 256 / NT) k_distill(con
   if (walk) {   // (the same for all threads of the row)
     Sums<TWO, false> st(a.lowest);
     Val<2> s2 = fill<2>(0.0f), s1 = fill<2>(0.0f);   // (sums of the even and the odd places)
-    Val<2> minus = fill<2>(-(st.m * a.c)), minus1 = fill<2>(-(st.m * kLog2e));
+    Val<2> minus = fill<2>(-__fmul_rn(st.m, a.c)), minus1 = fill<2>(-__fmul_rn(st.m, kLog2e));   // (rounded: see above)
     const Val<2> c = fill<2>(a.c), c1 = fill<2>(kLog2e);
     each_group<T, NT, U>(row, lo, hi, [&](const uint4 (&x)[U], int, int count) {
       uint32_t best = max_word<T, false>(x[0]);
@@ -184,7 +184,7 @@ __global__ void __launch_bounds__(NT, kBlocks<T, MODE> * 256 / NT) k_distill(con
         if (u < count) best = max_words<T, false>(best, max_word<T, false>(x[u]));
       const float top = max_of_word<T, false>(best);
       if (top > st.m) {
-        const Val<2> now = fill<2>(-(top * a.c)), now1 = fill<2>(-(top * kLog2e));
+        const Val<2> now = fill<2>(-__fmul_rn(top, a.c)), now1 = fill<2>(-__fmul_rn(top, kLog2e));
         s2 = mul_(s2, fill<2>(exp2_fast(now.v[0] - minus.v[0])));
         if (TWO) s1 = mul_(s1, fill<2>(exp2_fast(now1.v[0] - minus1.v[0])));
         st.m = top;
@@ -217,7 +217,7 @@ __global__ void __launch_bounds__(NT, kBlocks<T, MODE> * 256 / NT) k_distill(con
     sum = st.s;
     sum1 = TWO ? st.s1 : st.s;
     careful = !(sum > 0.0f && fabsf(st.m) < -a.lowest);
-    if (careful) {   // (the same for all threads of the row) out of the ordinary range, or not finite
+    if (careful) {   // (the same for all threads of the row)
       __syncthreads();
       Sums<TWO, true> ca(-FLT_MAX);
       each_group<T, NT, 1>(row, lo, hi, [&](const uint4 (&x)[1], int, int) {
@@ -409,7 +409,7 @@ int32_t distill(int mode, const dgc_distill* d, void* stream) {
   a.logits = d->logits.data; a.ld = d->logits.ld; a.idx = d->idx; a.val = d->val; a.labels = d->labels;
   a.vocab = d->vocab; a.k = d->k; a.temperature = d->temperature; a.soft = d->soft_weight; a.hard = d->hard_weight;
   a.c = (float)(1.4426950408889634 / (double)d->temperature);
-  a.lowest = -1e30f / std::max(1.0f, a.c);
+  a.lowest = -0x1p24f / std::max(kLog2e, a.c);
   a.loss = d->loss; a.stats = d->stats; a.stats_in = d->stats; a.dloss = d->dloss;
   a.dlogits = d->dlogits.data; a.ld_d = d->dlogits.ld;
   cudaStream_t s = as_stream(stream);

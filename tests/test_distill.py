@@ -386,3 +386,35 @@ def test_refusals_of_the_binding():
         B.distill_forward(s, i, v, loss, labels=torch.zeros(3, dtype=torch.int64, device="cuda"))
     with pytest.raises(B.DgcError):
         B.distill_forward(s, i, v, loss, temperature=0.0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16], ids=str)
+@pytest.mark.parametrize("T", [1.0, 2.0, 3.5, 0.25])
+def test_distill_rows_of_large_logits(dt, T):
+    """Rows whose maximum is so large that its product with log2(e) / T is off by whole numbers: masks of
+    -1e9 to -1e20 in every place, a few words far above the rest, and both sides of 2^24 / log2(e) = 1.16e7
+    and T times that.  (Tolerance as above; there (s - m) / T < 64 for every word that has a share, and a
+    word without one is off by 2^-22 of its own logarithm, which the term in |loss| covers.)"""
+    B = _bind()
+    V, K = 9001, 12
+    full = [-1e9, -1e10, -1e20, -1e29, -1e31, 1e10, 1e20, 1e29]
+    limit = 2.0 ** 24 / 1.4426950408889634
+    near = [sign * by * limit * t for t in (1.0, T) for by in (0.96, 1.04) for sign in (1, -1)]
+    R = len(full) + 3 + len(near)
+    s, idx, val, lab, w = _problem(R, V, K, dt, 91, True, std=1.0)
+    for r, v in enumerate(full):
+        s[r] = v
+    r = len(full)
+    s[r], s[r + 1], s[r + 2] = s[r].clamp(-4, 4), s[r + 1].clamp(-4, 4), -1e10
+    s[r, 77] = 1e10                                          # one word far above the rest
+    s[r + 1, [5, 6000, 9000]] = 1e11                         # three of them
+    s[r + 2, 4000:] = -1e20
+    idx[r, 0], lab[r] = 77, 77
+    idx[r + 1, :2], lab[r + 1] = torch.tensor([5, 6000]).to(torch.int32), 9000
+    idx[r + 2], lab[r + 2] = torch.arange(K).to(torch.int32), 9
+    steps = torch.randint(-8, 1, (V,), generator=torch.Generator().manual_seed(92)).float()
+    for q, v in enumerate(near):                             # (f32: whole numbers, exact at this size)
+        s[r + 3 + q] = (round(v) + steps).to(dt)
+    _check_distill(B, s, idx, val, lab, w, T, 0.5, 0.5)
+    _check_distill(B, s, idx, val, None, w, T, 1.0, 0.0)
