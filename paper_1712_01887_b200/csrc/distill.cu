@@ -114,9 +114,10 @@ __global__ void __launch_bounds__(NT, kBlocks<T, MODE> * 256 / NT) k_distill(con
   }
   if (a.labels) y = a.labels[r];
   if (MODE != kForward) w = a.dloss[r];
-  // and, after the walk, the student's logits there (the row is then in L2)
+  // and, after the walk, the student's logits there (the row is then in L2); without a soft term
+  // (0 times an infinite loss would not be 0) nothing is listed
   const auto pick = [&] {
-    if (mine < 0 || mine >= a.vocab || !(t > -INFINITY)) mine = -1;
+    if (mine < 0 || mine >= a.vocab || !(t > -INFINITY) || a.soft == 0.0f) mine = -1;
     else sk = to_float<T>(row.p[mine]);
     if (y < 0 || y >= a.vocab) y = -1;
     else sy = to_float<T>(row.p[y]);

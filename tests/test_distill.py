@@ -418,3 +418,39 @@ def test_distill_rows_of_large_logits(dt, T):
         s[r + 3 + q] = (round(v) + steps).to(dt)
     _check_distill(B, s, idx, val, lab, w, T, 0.5, 0.5)
     _check_distill(B, s, idx, val, None, w, T, 1.0, 0.0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dt", DT, ids=str)
+@pytest.mark.parametrize("T", [1.0, 2.0])
+def test_no_soft_term_where_its_weight_is_zero(dt, T):
+    """Labels alone: a list that names words masked in the student, or holds infinities, says nothing."""
+    B = _bind()
+    R, V, K = 4, 5003, 6
+    s, idx, val, lab, w = _problem(R, V, K, dt, 17, True)
+    s[0, int(idx[0, 1])] = -INF
+    s[1, idx[1].long()] = -INF
+    lab[1] = (int(idx[1].max()) + 1) % V
+    while int(lab[1]) in idx[1].tolist():
+        lab[1] = (int(lab[1]) + 1) % V
+    lab[0] = lab[1]
+    s[:2, int(lab[1])] = 0.5
+    val[2, 3] = INF
+    lab[3] = -1
+    absent = torch.full_like(idx, -1)
+    want, grad, size = plain_distill(s, absent, val, lab, T, 0.0, 0.75, w)
+    assert torch.isfinite(want).all() and float(want[3]) == 0
+    dev = [t.cuda() for t in (s, idx, val)]
+    how = dict(temperature=T, soft_weight=0.0, hard_weight=0.75, labels=lab.cuda())
+    loss, stats = torch.empty(R, device="cuda"), torch.empty(R, 2, device="cuda")
+    out, out2 = (torch.empty(R, V, dtype=dt, device="cuda") for _ in range(2))
+    B.distill_forward(*dev, loss, stats, **how)
+    B.distill_backward(*dev, stats, w.cuda(), out, **how)
+    loss2 = torch.empty_like(loss)
+    B.distill_loss_grad(*dev, w.cuda(), loss2, out2, **how)
+    for x in (loss, loss2):
+        assert ((x.double().cpu() - want).abs() <= TOL * (0.75 + want.abs())).all()
+    for x in (out, out2):
+        assert ((x.double().cpu() - grad).abs() <= TOL * size + HALF_ULP[dt] * grad.abs() + TINY[dt]).all()
+    B.distill_loss_grad(*dev, w.cuda(), loss2, out2, temperature=T, soft_weight=0.0)     # neither term
+    assert (loss2 == 0).all() and (out2 == 0).all()
