@@ -501,7 +501,9 @@ typedef struct dgc_distill {
   const float*   val;               /* [rows, k], the teacher's list (dgc_top_logits): an entry whose
                                        index is outside [0, vocab) or whose value is -infinity or
                                        NaN is absent; an index listed twice counts twice.  A row
-                                       with no entry has no soft term                             */
+                                       with no entry has no soft term.  +infinity leaves q
+                                       undefined: the row's loss and its gradient at the listed
+                                       places are NaN                                             */
   const int32_t* labels;            /* [rows] or NULL; a label outside [0, vocab) (a padding token)
                                        has no hard term                                           */
   float          temperature;       /* > 0                                                        */

@@ -249,7 +249,7 @@ __global__ void __launch_bounds__(NT, kBlocks<T, MODE> * 256 / NT) k_distill(con
   float tm = -FLT_MAX, ts = 0.0f;   // the teacher's maximum and sum
   for (int i = 0; i * 32 < a.k; ++i) tm = fmaxf(tm, sm.teacher[i].x);
   for (int i = 0; i * 32 < a.k; ++i) ts += sm.teacher[i].y * exp2_fast((sm.teacher[i].x - tm) * a.c);
-  const bool taught = ts > 0.0f, labelled = y >= 0;
+  const bool taught = !(ts <= 0.0f), labelled = y >= 0;   // (a teacher of +infinity: ts and q are NaN)
   float q = 0.0f;
   if (warp * 32 < a.k) {
     float logq = 0.0f;

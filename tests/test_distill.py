@@ -454,3 +454,37 @@ def test_no_soft_term_where_its_weight_is_zero(dt, T):
         assert ((x.double().cpu() - grad).abs() <= TOL * size + HALF_ULP[dt] * grad.abs() + TINY[dt]).all()
     B.distill_loss_grad(*dev, w.cuda(), loss2, out2, temperature=T, soft_weight=0.0)     # neither term
     assert (loss2 == 0).all() and (out2 == 0).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dt", DT, ids=str)
+@pytest.mark.parametrize("T", [1.0, 2.0])
+def test_an_infinite_teacher_is_not_passed_over(dt, T):
+    """A listed value of +infinity leaves q undefined: the row's loss and its gradient at the listed places
+    are NaN, as by the definition; the other places and rows have the formula's values."""
+    B = _bind()
+    R, V, K = 4, 3001, 6
+    s, idx, val, lab, w = _problem(R, V, K, dt, 23, True)
+    val[1, 2] = INF
+    val[2, 0], val[2, 5] = INF, INF
+    idx[2, 5] = -1                                           # (an absent entry's value does not count)
+    want, grad, size = plain_distill(s, idx, val, lab, T, 0.5, 0.5, w)
+    want[1:3] = float("nan")                                 # q log q of them
+    dev = [t.cuda() for t in (s, idx, val)]
+    how = dict(temperature=T, soft_weight=0.5, hard_weight=0.5, labels=lab.cuda())
+    loss, stats = torch.empty(R, device="cuda"), torch.empty(R, 2, device="cuda")
+    out, out2 = (torch.empty(R, V, dtype=dt, device="cuda") for _ in range(2))
+    B.distill_forward(*dev, loss, stats, **how)
+    B.distill_backward(*dev, stats, w.cuda(), out, **how)
+    loss2 = torch.empty_like(loss)
+    B.distill_loss_grad(*dev, w.cuda(), loss2, out2, **how)
+    fine, rows = ~torch.isnan(grad), ~torch.isnan(want)
+    assert int((~fine).sum()) == K + K - 1
+    for x in (loss, loss2):
+        x = x.double().cpu()
+        assert torch.equal(torch.isnan(x), torch.isnan(want))
+        assert ((x - want).abs()[rows] <= TOL * (0.5 * T * T + 0.5 + want.abs()[rows])).all()
+    for x in (out, out2):
+        x = x.double().cpu()
+        assert torch.equal(torch.isnan(x), ~fine)
+        assert ((x - grad).abs()[fine] <= (TOL * size + HALF_ULP[dt] * grad.abs() + TINY[dt])[fine]).all()
