@@ -506,7 +506,7 @@ typedef struct dgc_distill {
                                        places are NaN                                             */
   const int32_t* labels;            /* [rows] or NULL; a label outside [0, vocab) (a padding token)
                                        has no hard term                                           */
-  float          temperature;       /* > 0                                                        */
+  float          temperature;       /* 2^-60 .. 2^60                                              */
   float          soft_weight, hard_weight;   /* 0: there is no such term, whatever it would be */
   float          reserved1;         /* 0                                                          */
   float*         loss;              /* output [rows]; +infinity where a listed entry or the label

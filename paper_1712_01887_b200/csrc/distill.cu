@@ -395,7 +395,8 @@ int32_t distill(int mode, const dgc_distill* d, void* stream) {
   if (!d || bad_dtype(d->dtype) || d->rows < 0 || d->rows > INT32_MAX || d->vocab < 1 || d->vocab > INT32_MAX - 64 ||
       d->k < 1 || d->k > DGC_MAX_TOP)
     return DGC_EINVAL;
-  if (!(d->temperature > 0.0f) || !std::isfinite(d->temperature) || !std::isfinite(d->soft_weight) ||
+  // (T^2 and log2(e) / T are normal numbers then)
+  if (!(d->temperature >= 0x1p-60f && d->temperature <= 0x1p60f) || !std::isfinite(d->soft_weight) ||
       !std::isfinite(d->hard_weight))
     return DGC_EINVAL;
   const size_t es = element_size(d->dtype);

@@ -488,3 +488,21 @@ def test_an_infinite_teacher_is_not_passed_over(dt, T):
         x = x.double().cpu()
         assert torch.equal(torch.isnan(x), ~fine)
         assert ((x - grad).abs()[fine] <= (TOL * size + HALF_ULP[dt] * grad.abs() + TINY[dt])[fine]).all()
+
+
+def test_temperatures_out_of_range_are_refused():
+    """T^2 or 1 / T would not be a normal 32-bit number (the loss 0 x infinity)."""
+    from paper_1712_01887_b200 import binding as B
+    for which in ("forward", "backward", "loss_grad"):
+        for T in (1e-45, 1e-39, 1e-30, 0.99 * 2.0 ** -60, 1.01 * 2.0 ** 60, 1e30, 3e38):
+            args = B.DISTILL.pack(0, 8, 4, 0, 2, 4096, 8, 4096, 4096, 0, T, 1.0, 0.0, 0.0, 4096, 4096, 4096, 4096, 8)
+            assert getattr(B._lib, "dgc_distill_" + which)(args, None) == B.EINVAL, (which, T)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [2.0 ** -60, 2.0 ** -20, 2.0 ** 20, 2.0 ** 60])
+def test_temperatures_at_the_ends_of_the_range(T):
+    for dt in (torch.float32, torch.bfloat16):
+        s, idx, val, _, w = _problem(5, 3001, 7, dt, 41, False)
+        idx[1, 4:] = -1
+        _check_distill(_bind(), s, idx, val, None, w, T, 1.0, 0.0)
