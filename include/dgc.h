@@ -415,7 +415,7 @@ typedef struct dgc_matrix {
 typedef struct dgc_scan {
   int32_t        dtype;      /* DGC_F32, DGC_BF16, DGC_F16: of all matrices                      */
   int32_t        num_seqs;   /* >= 1                                                             */
-  int32_t        channels;   /* >= 1                                                             */
+  int32_t        channels;   /* 1 .. 2^31 - 1025                                                 */
   int32_t        reverse;    /* non-zero: every sequence is walked from its last row to its first */
   int64_t        tokens;     /* 0 .. 2^31 - 1                                                    */
   const int32_t* seq_start;  /* device [num_seqs + 1], ascending from 0 to tokens; offsets outside
@@ -462,7 +462,7 @@ int32_t dgc_gated_scan_check(void* stream);
  * in a cache: row r's state is row slots[r] of `state`, which is advanced in place; out's row r
  * is the new state. */
 typedef struct dgc_scan_one {
-  int32_t        dtype, rows, channels;
+  int32_t        dtype, rows, channels;   /* channels 1 .. 2^31 - 1025                           */
   int32_t        num_slots;  /* rows of state                                                    */
   dgc_matrix     gate, x;    /* [rows, channels] inputs                                          */
   dgc_matrix     out;        /* [rows, channels] output                                          */
@@ -478,7 +478,7 @@ int32_t dgc_gated_scan_step(const dgc_scan_one* step, void* stream);
  * (-0 equals +0, NaN counts as larger than every number).  Entries of -infinity (words masked
  * out) are never listed; a row with fewer than k others is filled up with (-1, -infinity). */
 typedef struct dgc_top {
-  int32_t    dtype, vocab;   /* vocab >= 1                                                       */
+  int32_t    dtype, vocab;   /* vocab 1 .. 2^31 - 65                                             */
   int32_t    k;              /* 1 .. DGC_MAX_TOP                                                 */
   int32_t    reserved;       /* 0                                                                */
   int64_t    rows;           /* 0 .. 2^31 - 1                                                    */

@@ -888,8 +888,8 @@ k_scan_step(const T* z, int64_t ld_z, const T* x, int64_t ld_x, float* state, co
   pdl_enter();
   const int c = (blockIdx.x * 256 + threadIdx.x) * N;
   if (c >= channels) return;
-  for (int r = blockIdx.y; r < rows; r += gridDim.y) {
-    const int slot = slots ? __ldg(slots + r) : r;
+  for (unsigned r = blockIdx.y; r < (unsigned)rows; r += gridDim.y) {
+    const int slot = slots ? __ldg(slots + r) : (int)r;
     const bool live = slot >= 0 && slot < num_slots;
     float* st = state + (int64_t)(live ? slot : 0) * channels + c;
     struct alignas(sizeof(T) * N) Pack { T v[N]; };
@@ -909,6 +909,10 @@ k_scan_step(const T* z, int64_t ld_z, const T* x, int64_t ld_x, float* state, co
     *reinterpret_cast<Pack*>(out + r * ld_out + c) = o;
   }
 }
+
+// The last tile of channels ends below 2^31 (a block of k_scan_step takes 1024).
+constexpr int32_t kMaxChannels = INT32_MAX - 1024;
+inline bool bad_channels(int32_t channels) { return channels < 1 || channels > kMaxChannels; }
 
 constexpr int kFwdL = 16, kBwdL = 8, kSms = 148;
 constexpr int kWideUnits = 16, kWideShort = 2048, kWideLong = 8192, kWideWork = 32768;
@@ -1040,7 +1044,7 @@ Lie lie_of(std::initializer_list<Matrix> ms, int32_t channels, size_t es) {
 }
 
 int32_t scan(const dgc_scan* d, bool backward, void* stream) {
-  if (!d || bad_dtype(d->dtype) || d->tokens < 0 || d->tokens > INT32_MAX || d->num_seqs < 1 || d->channels < 1 ||
+  if (!d || bad_dtype(d->dtype) || d->tokens < 0 || d->tokens > INT32_MAX || d->num_seqs < 1 || bad_channels(d->channels) ||
       (!d->seq_start && d->tokens % d->num_seqs != 0))
     return DGC_EINVAL;
   const size_t es = element_size(d->dtype);
@@ -1077,13 +1081,13 @@ int32_t dgc_gated_scan_forward(const dgc_scan* d, void* stream) { return scan(d,
 int32_t dgc_gated_scan_backward(const dgc_scan* d, void* stream) { return scan(d, true, stream); }
 
 int64_t dgc_gated_scan_workspace_bytes(const dgc_scan* d) {
-  if (!d || bad_dtype(d->dtype) || d->tokens < 0 || d->tokens > INT32_MAX || d->num_seqs < 1 || d->channels < 1)
+  if (!d || bad_dtype(d->dtype) || d->tokens < 0 || d->tokens > INT32_MAX || d->num_seqs < 1 || bad_channels(d->channels))
     return DGC_EINVAL;
   return wide_bytes(d->tokens, d->num_seqs, d->channels, element_size(d->dtype));
 }
 
 int32_t dgc_gated_scan_step(const dgc_scan_one* d, void* stream) {
-  if (!d || bad_dtype(d->dtype) || d->rows < 0 || d->channels < 1 || d->num_slots < 0) return DGC_EINVAL;
+  if (!d || bad_dtype(d->dtype) || d->rows < 0 || bad_channels(d->channels) || d->num_slots < 0) return DGC_EINVAL;
   const size_t es = element_size(d->dtype);
   if (bad_matrix(d->gate, d->rows, d->channels, es) || bad_matrix(d->x, d->rows, d->channels, es) ||
       bad_matrix(d->out, d->rows, d->channels, es) || misaligned(d->slots, 4))

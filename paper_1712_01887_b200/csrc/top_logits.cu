@@ -210,7 +210,7 @@ __device__ int top_of_part(const Row<T>& row, int lo, int hi, int k, TopShared<N
     for (int j0 = lo; j0 < hi && n < k; j0 += NT) {
       const int j = j0 + tid;
       uint32_t hit = 0;
-      const int e0 = row.first(j);
+      const int e0 = row.first(min(j, hi));
       if (j < hi) {
 #pragma unroll
         for (int i = 0; i < E; ++i) {

@@ -361,3 +361,17 @@ def test_refusals_of_the_binding():
         B.gated_scan_forward(z, z.clone(), z.clone(), h0=torch.zeros(3, 4, device="cuda"))
     with pytest.raises(B.DgcError):
         B.gated_scan_forward(z, z.clone(), z.clone(), num_seqs=3)
+
+
+def test_channels_up_to_the_last_tile_of_32_bit_indices():
+    """A tile of channels that ends past 2^31 is refused; nothing is enqueued."""
+    from paper_1712_01887_b200 import binding as B
+    p, lib = 4096, B._lib
+    for ch in (2 ** 31 - 1, 2 ** 31 - 64, 2 ** 31 - 1024):
+        scan = B.SCAN.pack(0, 1, ch, 0, 1, 0, *[p, ch] * 3, 0, 0, *[p, ch] * 3, 0, 0, 0, 0)
+        assert lib.dgc_gated_scan_forward(scan, None) == B.EINVAL
+        assert lib.dgc_gated_scan_backward(scan, None) == B.EINVAL
+        assert lib.dgc_gated_scan_workspace_bytes(scan) == B.EINVAL
+        assert lib.dgc_gated_scan_step(B.SCAN_ONE.pack(0, 1, ch, 1, *[p, ch] * 3, p, 0), None) == B.EINVAL
+    for ch in (1, 2 ** 31 - 1025):
+        assert lib.dgc_gated_scan_workspace_bytes(B.SCAN.pack(0, 1, ch, 0, 1, *[0] * 19)) == 0
