@@ -108,6 +108,17 @@ __device__ __forceinline__ int by_length(const ScanArgs& a, int place) {
 // A map y_out = P y_in + S of a lane's channels, as it lies in shared memory.
 template <int VEC> struct alignas(8 * VEC) Map { Val<VEC> p, s; };
 
+// The product of a run's coefficients, none of which is 0, held at the smallest normal number where
+// it underflows: times an infinite y_in it must be infinite, not NaN (a finite one gets at most
+// 2^-126 of itself too much).
+__device__ __forceinline__ float held(float p) { return fmaxf(p, 0x1p-126f); }
+template <int VEC>
+__device__ __forceinline__ Val<VEC> held(Val<VEC> p) {
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) p.v[i] = held(p.v[i]);
+  return p;
+}
+
 // A block's warps work in G groups that take the rounds in turn.  By group: the maps of a round's
 // runs and the states they start from; by round: the maps of the cluster's blocks and the state
 // before the round.  (Slots of `blocks`: a block sends round i + 4 after it has every block's map
@@ -172,8 +183,9 @@ __device__ __forceinline__ bool wait_arrived(uint32_t barrier, uint32_t phase) {
 // every store of results under way.
 template <int VEC, int NW, int G, int CL>
 __device__ __forceinline__ Val<VEC> join_runs(Join<VEC, NW, G, CL>& sm, int round, bool last, int ncl, int rank, int group,
-                                              int warp, int lane, const Val<VEC>& P, const Val<VEC>& S,
+                                              int warp, int lane, Val<VEC> P, const Val<VEC>& S,
                                               Val<VEC>& carry, bool& waits) {
+  P = held(P);
   sm.runs[group][warp][lane] = {P, S};
   bar_sync<NW * 32>(kGroupBarrier + group);
   if (warp == 0) {
@@ -186,6 +198,7 @@ __device__ __forceinline__ Val<VEC> join_runs(Join<VEC, NW, G, CL>& sm, int roun
         tp = mul_(m.p, tp);
         ts = fma_(m.p, ts, m.s);
       }
+      tp = held(tp);
       const uint32_t to = shared_address(&sm.blocks[slot][rank][lane]), bar = shared_address(&sm.arrived[slot]);
       if (lane == 0)
         asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(ncl * 32 * 2 * VEC * 4) : "memory");
@@ -704,7 +717,7 @@ __global__ void __launch_bounds__(kWideWarps * 32) k_wide_reduce(const WideArgs 
   float2* m = w.maps + at.slot * a.channels + at.c;
 #pragma unroll
   for (int v = 0; v < VEC; ++v)
-    if (v ? at.on1 : at.on0) m[v] = make_float2(P.v[v], S.v[v]);
+    if (v ? at.on1 : at.on0) m[v] = make_float2(held(P.v[v]), S.v[v]);
 }
 
 // The starts of a sequence's runs, in the order of the walk, and the state after the last.
@@ -728,7 +741,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32) k_wide_join(const WideArgs w,
       t = make_float2(m.x * t.x, fmaf(m.x, t.y, m.y));
     }
   }
-  parts[warp][lane] = t;
+  parts[warp][lane] = make_float2(held(t.x), t.y);
   __syncthreads();
   if (!on) return;
   const float* from = back ? a.dh_last : a.h0;

@@ -375,3 +375,52 @@ def test_channels_up_to_the_last_tile_of_32_bit_indices():
         assert lib.dgc_gated_scan_step(B.SCAN_ONE.pack(0, 1, ch, 1, *[p, ch] * 3, p, 0), None) == B.EINVAL
     for ch in (1, 2 ** 31 - 1025):
         assert lib.dgc_gated_scan_workspace_bytes(B.SCAN.pack(0, 1, ch, 0, 1, *[0] * 19)) == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dt", DT, ids=str)
+@pytest.mark.parametrize("lens,C", [([400, 3, 150], 40), ([2600, 90], 64), ([9000], 32)])
+@pytest.mark.parametrize("reverse", [False, True])
+def test_infinite_states_and_gradients_stay_infinite(lens, C, reverse, dt):
+    """A gate that forgets, f > 0, leaves an infinite state infinite, however many such steps follow: the
+    product of a run's f must not become 0 (0 x infinity).  All other values keep their tolerance: every f
+    may be taken too large by 2e-38 and no result here is larger than 1e3."""
+    B, INF = _bind(), float("inf")
+    starts, z, x, dh, h0, dl, _ = _case(lens, C, dt, 0, 31)
+    z = (z * 0.3 - 9).to(dt)                                   # f about e^-9: sixteen of them are below 2^-126
+    N, S = sum(lens), len(lens)
+    tab = torch.tensor(starts, dtype=torch.int32, device="cuda")
+    how = dict(seq_start=tab, num_seqs=S, reverse=reverse)
+    xi, hi = x.clone(), h0.clone()
+    hi[0, 1], hi[S - 1, 2] = INF, -INF
+    xi[starts[1] // 2, 3], xi[starts[1] // 2, 4] = INF, -INF
+    h, last = torch.empty(N, C, dtype=dt, device="cuda"), torch.empty(S, C, device="cuda")
+    B.gated_scan_forward(z.cuda(), xi.cuda(), h, h_last=last, h0=hi.cuda(), **how)
+    rh, rl, _ = plain(z.double(), xi.double(), hi.double(), starts, reverse)
+    assert int(torch.isinf(rh).sum()) > N // 4 and not torch.isnan(rh).any()
+
+    def same(got, want, unit, what, scale):
+        got = got.double().cpu()
+        assert torch.equal(torch.isnan(got), torch.isnan(want)), (what, int(torch.isnan(got).sum()))
+        odd = torch.isinf(want)
+        assert torch.equal(got[odd], want[odd]) and not torch.isinf(got[~odd]).any(), what
+        fine = torch.isfinite(want)
+        assert ((got - want).abs()[fine] <= unit * want.abs()[fine] + TINY[dt] + F32_TOL * scale).all(), what
+    same(h, rh, UNIT[dt], "h", 5.0)
+    same(last, rl, 0.0, "h_last", 5.0)
+
+    # backward: infinite gradients of the states, of finite states
+    B.gated_scan_forward(z.cuda(), x.cuda(), h, h0=h0.cuda(), **how)
+    gi, li = dh.clone(), dl.clone()
+    gi[starts[1] // 2, 5], li[0, 6], li[S - 1, 7] = INF, -INF, INF
+    dz, dx = (torch.empty(N, C, dtype=dt, device="cuda") for _ in range(2))
+    d0 = torch.empty(S, C, device="cuda")
+    B.gated_scan_backward(z.cuda(), x.cuda(), h, gi.cuda(), dz, dx, h0=h0.cuda(), dh_last=li.cuda(), dh0=d0, **how)
+    rz, rx, r0, g = plain_backward(z.double(), x.double(), h0.double(), starts, reverse, gi.double(), li.double())
+    assert int(torch.isinf(rx).sum()) > N // 8
+    same(dx, rx, UNIT[dt], "dx", 5.0)
+    same(d0, r0, 0.0, "dh0", 5.0)
+    # (where the stored state before a step is the step's input, dgate is 0 x infinity and may be NaN)
+    _, _, before = plain(z.double(), x.double(), h0.double(), starts, reverse)
+    some = before.to(dt) != x
+    same(dz.cpu()[some], rz[some], 2 * UNIT[dt], "dgate", 5.0)
