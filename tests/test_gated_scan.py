@@ -424,3 +424,31 @@ def test_infinite_states_and_gradients_stay_infinite(lens, C, reverse, dt):
     _, _, before = plain(z.double(), x.double(), h0.double(), starts, reverse)
     some = before.to(dt) != x
     same(dz.cpu()[some], rz[some], 2 * UNIT[dt], "dgate", 5.0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dt", DT, ids=str)
+@pytest.mark.parametrize("lens,C,joint,packed", [
+    ([16385], 33, 0, True),                # 16 blocks of a cluster, 9 rounds forward and 17 backward
+    ([30011, 0, 777], 40, 1, True),        # 8 (f32) or 16, rows at any address; a short one and an empty one
+    ([8192, 8192], 100, 4, False)])        # 8 (f32) or 16, without a table
+@pytest.mark.parametrize("reverse", [False, True])
+def test_long_sequences_by_clusters_without_a_workspace(lens, C, joint, packed, reverse, dt, monkeypatch):
+    """A C call without a workspace: the clusters' barriers are used over many rounds and phases."""
+    B = _bind()
+    monkeypatch.setattr(B, "_scan", lambda call, name, args, tokens, num_seqs, stream, device: B._enqueue(call, name, args, stream, device))
+    _check(B, lens, C, dt, joint, reverse, packed=packed, seed=C + 7)
+    B.gated_scan_check()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dt", DT, ids=str)
+def test_long_and_wide_sequences_by_clusters(dt):
+    """More tiles of channels than go by runs (18 of 32 words): twenty rounds and more of eight blocks a
+    cluster, then of four."""
+    B = _bind()
+    C = 18 * 128 // torch.tensor([], dtype=dt).element_size()
+    assert B._lib.dgc_gated_scan_workspace_bytes(B.SCAN.pack(B.DTYPES[dt], 1, C, 0, 21000, *[0] * 19)) == 0
+    _check(B, [21000], C, dt, packed=False, seed=3)
+    _check(B, [300, 20500], C, dt, reverse=True, seed=4)
+    B.gated_scan_check()
