@@ -35,7 +35,9 @@ using namespace dgc;
 namespace {
 
 constexpr int kMaxCluster = 16, kPortableCluster = 8;
-constexpr unsigned long long kWaitNs = 1000000000ull;   // bound of a wait on a peer: a second
+// Bound of a wait on a peer: a second, of which a time in which nothing of the GPU ran (another
+// process's turn, a debugger) counts as a hundredth.
+constexpr uint32_t kWaitNs = 1000000000, kPauseNs = kWaitNs / 100;
 
 // A matrix argument.  The strides that the loops add are laid out by the host: as kernel
 // parameters they cost no registers.
@@ -131,6 +133,7 @@ struct Join {
   Map<VEC> blocks[kBlockSlots][CL][32];
   Val<VEC> carry[2][32];
   unsigned long long arrived[kBlockSlots];   // mbarriers of `blocks`
+  int gone[G];                               // a wait of the group's ran out
 };
 
 // Named barriers: one of each group, two between the groups' joining warps.
@@ -141,7 +144,9 @@ __device__ __forceinline__ void bar_arrive(int id) { asm volatile("barrier.cta.a
 constexpr int kGroupBarrier = 1, kCarryBarrier = 3;
 
 // Waits that run out (they cannot, short of a fault: the blocks of a cluster run together) are
-// counted here and not waited for again; dgc_gated_scan_check reports them.
+// counted here; dgc_gated_scan_check reports them.  Their group takes no further part in the
+// exchange (a second arrival in the barrier's phase is not allowed), and stays until every block
+// is through: see join_end.
 __device__ int g_scan_waits_out;
 
 __device__ __forceinline__ uint32_t shared_address(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -149,30 +154,39 @@ __device__ __forceinline__ uint32_t shared_address(const void* p) { return (uint
 template <int VEC, int NW, int G, int CL>
 __device__ __forceinline__ void join_begin(Join<VEC, NW, G, CL>& sm, int ncl) {
   if (ncl == 1) return;
+  if (threadIdx.x < G) sm.gone[threadIdx.x] = 0;
   if (threadIdx.x < kBlockSlots)
     asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(shared_address(&sm.arrived[threadIdx.x])) : "memory");
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   cg::this_cluster().sync();   // every block runs, its barriers are there
 }
 
-__device__ __forceinline__ unsigned long long clock_ns() {
-  unsigned long long t;
-  asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
+__device__ __forceinline__ uint32_t clock_ns() {   // modulo 2^32: 4.3 seconds
+  uint32_t t;
+  asm volatile("mov.u32 %0, %%globaltimer_lo;" : "=r"(t));
   return t;
 }
 
 __device__ __forceinline__ bool wait_arrived(uint32_t barrier, uint32_t phase) {
-  unsigned long long since = 0;
-  for (;;) {
+  uint32_t last = 0, waited = 0;
+  while (waited <= kWaitNs) {
     uint32_t done;
     asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
                  : "=r"(done) : "r"(barrier), "r"(phase) : "memory");
     if (done) return true;
-    if (since == 0) since = clock_ns();
-    else if (clock_ns() - since > kWaitNs) break;
+    const uint32_t now = clock_ns();
+    if (last) waited += min(now - last, kPauseNs);
+    last = now;
   }
   atomicAdd(&g_scan_waits_out, 1);
   return false;
+}
+
+// A group of warps whose wait ran out stays until every other thread of the cluster has come here
+// or ended (all waits are bounded, so all do): its block's shared memory may still be stored to.
+template <int VEC, int NW, int G, int CL>
+__device__ __forceinline__ void join_end(const Join<VEC, NW, G, CL>& sm, int ncl, int group) {
+  if (ncl > 1 && sm.gone[group]) asm volatile("barrier.cluster.arrive.release;\nbarrier.cluster.wait.acquire;" ::: "memory");
 }
 
 // Joins the runs of a round in order: takes this warp's map (P, S), returns the state its run
@@ -184,13 +198,13 @@ __device__ __forceinline__ bool wait_arrived(uint32_t barrier, uint32_t phase) {
 template <int VEC, int NW, int G, int CL>
 __device__ __forceinline__ Val<VEC> join_runs(Join<VEC, NW, G, CL>& sm, int round, bool last, int ncl, int rank, int group,
                                               int warp, int lane, Val<VEC> P, const Val<VEC>& S,
-                                              Val<VEC>& carry, bool& waits) {
+                                              Val<VEC>& carry) {
   P = held(P);
   sm.runs[group][warp][lane] = {P, S};
   bar_sync<NW * 32>(kGroupBarrier + group);
   if (warp == 0) {
     const int slot = round % kBlockSlots;
-    if (ncl > 1) {
+    if (ncl > 1 && !sm.gone[group]) {
       Val<VEC> tp = P, ts = S;
 #pragma unroll
       for (int w = 1; w < NW; ++w) {
@@ -216,7 +230,8 @@ __device__ __forceinline__ Val<VEC> join_runs(Join<VEC, NW, G, CL>& sm, int roun
                          ::"r"(far), "f"(tp.v[0]), "f"(ts.v[0]), "r"(far_bar) : "memory");
         }
       }
-      if (waits) waits = wait_arrived(bar, (uint32_t)(round / kBlockSlots) & 1u);
+      if (!wait_arrived(bar, (uint32_t)(round / kBlockSlots) & 1u)) sm.gone[group] = 1;
+      __syncwarp();
     }
     if (G == 2 && round > 0) {
       bar_sync<64>(kCarryBarrier + (round & 1));
@@ -447,7 +462,6 @@ __global__ void __launch_bounds__(NW * G * 32, BLOCKS) k_scan_forward(const Scan
   join_begin(sm, at.ncl);
 
   char* out = row_at<T>(a.h, row0, at.c);
-  bool waits = true;
   int stage = 0;
   const int rounds = (len - 1) / (at.step / G) + 1;   // of the block
   int left = len - at.mine0;   // steps from this warp's first of the round on
@@ -474,7 +488,7 @@ __global__ void __launch_bounds__(NW * G * 32, BLOCKS) k_scan_forward(const Scan
     stage ^= 1;
     z0 += (uint32_t)a.z.stride * (uint32_t)at.step;
     x0 += (uint32_t)a.x.stride * (uint32_t)at.step;
-    Val<VEC> cur = join_runs(sm, round, round + 1 == rounds, at.ncl, at.rank, at.group, at.warp, at.lane, P, S, carry, waits);
+    Val<VEC> cur = join_runs(sm, round, round + 1 == rounds, at.ncl, at.rank, at.group, at.warp, at.lane, P, S, carry);
     auto write = [&](auto whole) {
 #pragma unroll
       for (int i = 0; i < L; ++i, out += a.h.stride) {
@@ -489,6 +503,7 @@ __global__ void __launch_bounds__(NW * G * 32, BLOCKS) k_scan_forward(const Scan
     if (a.h_last && left > 0 && left <= L) at.put(a.h_last, a.channels, cur);
   }
   wait_copies<0>();
+  join_end(sm, at.ncl, at.group);
 }
 
 // Backward, walked from the sequence's end: position u = len-1-t.  A thread's run of L steps
@@ -550,7 +565,6 @@ __global__ void __launch_bounds__(NW * G * 32, BLOCKS) k_scan_backward(const Sca
   char* gz = row_at<T>(a.dz, at.at0 + at.dir * (int64_t)(left - 1), at.c);
   char* gx = row_at<T>(a.dx, at.at0 + at.dir * (int64_t)(left - 1), at.c);
   fetch_state(left);
-  bool waits = true;
   int stage = 0;
   const int rounds = (len - 1) / (at.step / G) + 1;   // of the block
   for (int round = at.group; round < rounds; round += G, left -= at.step) {
@@ -586,7 +600,7 @@ __global__ void __launch_bounds__(NW * G * 32, BLOCKS) k_scan_backward(const Sca
     if (full) walk(std::true_type{});
     else walk(std::false_type{});
     fetch_state(left - at.step);
-    Val<VEC> cur = join_runs(sm, round, round + 1 == rounds, at.ncl, at.rank, at.group, at.warp, at.lane, P, S, carry, waits);
+    Val<VEC> cur = join_runs(sm, round, round + 1 == rounds, at.ncl, at.rank, at.group, at.warp, at.lane, P, S, carry);
     auto write = [&](auto whole) {
 #pragma unroll
       for (int j = L - 1; j >= 0; --j, gz -= a.dz.stride, gx -= a.dx.stride) {
@@ -611,6 +625,7 @@ __global__ void __launch_bounds__(NW * G * 32, BLOCKS) k_scan_backward(const Sca
     d0 -= (uint32_t)a.dh.stride * (uint32_t)at.step;
   }
   wait_copies<0>();
+  join_end(sm, at.ncl, at.group);
 }
 
 // ------------------------------------------------------------------ few and narrow sequences
