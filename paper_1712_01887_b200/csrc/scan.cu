@@ -122,18 +122,25 @@ __device__ __forceinline__ Val<VEC> held(Val<VEC> p) {
 }
 
 // A block's warps work in G groups that take the rounds in turn.  By group: the maps of a round's
-// runs and the states they start from; by round: the maps of the cluster's blocks and the state
-// before the round.  (Slots of `blocks`: a block sends round i + 4 after it has every block's map
-// of round i + 2, and the warp that sent that one has read round i by then.)
+// runs and the states they start from; by round, where there are two groups: the maps of the cluster's
+// blocks and the state before the round.  (Slots of `blocks`: a block sends round i + 4 after it has
+// every block's map of round i + 2, and the warp that sent that one has read round i by then.)  Only
+// blocks of two groups stand in clusters.
 constexpr int kBlockSlots = 4;
-template <int VEC, int NW, int G, int CL>   // CL: the most blocks of a cluster
-struct Join {
-  Map<VEC> runs[G][NW][32];
-  Val<VEC> starts[G][NW][32];
+template <int VEC, int G, int CL>   // CL: the most blocks of a cluster
+struct Exchange {
   Map<VEC> blocks[kBlockSlots][CL][32];
   Val<VEC> carry[2][32];
   unsigned long long arrived[kBlockSlots];   // mbarriers of `blocks`
   int gone[G];                               // a wait of the group's ran out
+};
+template <int VEC>
+struct Exchange<VEC, 1, 1> {};
+template <int VEC, int NW, int G, int CL>
+struct Join : Exchange<VEC, G, CL> {
+  static_assert((G == 2) == (CL > 1), "");
+  Map<VEC> runs[G][NW][32];
+  Val<VEC> starts[G][NW][32];
 };
 
 // Named barriers: one of each group, two between the groups' joining warps.
@@ -153,12 +160,14 @@ __device__ __forceinline__ uint32_t shared_address(const void* p) { return (uint
 
 template <int VEC, int NW, int G, int CL>
 __device__ __forceinline__ void join_begin(Join<VEC, NW, G, CL>& sm, int ncl) {
-  if (ncl == 1) return;
-  if (threadIdx.x < G) sm.gone[threadIdx.x] = 0;
-  if (threadIdx.x < kBlockSlots)
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(shared_address(&sm.arrived[threadIdx.x])) : "memory");
-  asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-  cg::this_cluster().sync();   // every block runs, its barriers are there
+  if constexpr (CL > 1) {
+    if (ncl == 1) return;
+    if (threadIdx.x < G) sm.gone[threadIdx.x] = 0;
+    if (threadIdx.x < kBlockSlots)
+      asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(shared_address(&sm.arrived[threadIdx.x])) : "memory");
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    cg::this_cluster().sync();   // every block runs, its barriers are there
+  }
 }
 
 __device__ __forceinline__ uint32_t clock_ns() {   // modulo 2^32: 4.3 seconds
@@ -186,7 +195,9 @@ __device__ __forceinline__ bool wait_arrived(uint32_t barrier, uint32_t phase) {
 // or ended (all waits are bounded, so all do): its block's shared memory may still be stored to.
 template <int VEC, int NW, int G, int CL>
 __device__ __forceinline__ void join_end(const Join<VEC, NW, G, CL>& sm, int ncl, int group) {
-  if (ncl > 1 && sm.gone[group]) asm volatile("barrier.cluster.arrive.release;\nbarrier.cluster.wait.acquire;" ::: "memory");
+  if constexpr (CL > 1) {
+    if (ncl > 1 && sm.gone[group]) asm volatile("barrier.cluster.arrive.release;\nbarrier.cluster.wait.acquire;" ::: "memory");
+  }
 }
 
 // Joins the runs of a round in order: takes this warp's map (P, S), returns the state its run
@@ -203,62 +214,67 @@ __device__ __forceinline__ Val<VEC> join_runs(Join<VEC, NW, G, CL>& sm, int roun
   sm.runs[group][warp][lane] = {P, S};
   bar_sync<NW * 32>(kGroupBarrier + group);
   if (warp == 0) {
-    const int slot = round % kBlockSlots;
-    if (ncl > 1 && !sm.gone[group]) {
-      Val<VEC> tp = P, ts = S;
+    if constexpr (CL > 1) {
+      const int slot = round % kBlockSlots;
+      if (ncl > 1 && !sm.gone[group]) {
+        Val<VEC> tp = P, ts = S;
 #pragma unroll
-      for (int w = 1; w < NW; ++w) {
-        const Map<VEC> m = sm.runs[group][w][lane];
-        tp = mul_(m.p, tp);
-        ts = fma_(m.p, ts, m.s);
-      }
-      tp = held(tp);
-      const uint32_t to = shared_address(&sm.blocks[slot][rank][lane]), bar = shared_address(&sm.arrived[slot]);
-      if (lane == 0)
-        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(ncl * 32 * 2 * VEC * 4) : "memory");
-#pragma unroll
-      for (int r = 0; r < CL; ++r) {
-        if (r < ncl) {
-          uint32_t far, far_bar;
-          asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(far) : "r"(to), "r"(r));
-          asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(far_bar) : "r"(bar), "r"(r));
-          if constexpr (VEC == 2)
-            asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];"
-                         ::"r"(far), "f"(tp.v[0]), "f"(tp.v[1]), "f"(ts.v[0]), "f"(ts.v[1]), "r"(far_bar) : "memory");
-          else
-            asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];"
-                         ::"r"(far), "f"(tp.v[0]), "f"(ts.v[0]), "r"(far_bar) : "memory");
+        for (int w = 1; w < NW; ++w) {
+          const Map<VEC> m = sm.runs[group][w][lane];
+          tp = mul_(m.p, tp);
+          ts = fma_(m.p, ts, m.s);
         }
-      }
-      if (!wait_arrived(bar, (uint32_t)(round / kBlockSlots) & 1u)) sm.gone[group] = 1;
-      __syncwarp();
-    }
-    if (G == 2 && round > 0) {
-      bar_sync<64>(kCarryBarrier + (round & 1));
-      carry = sm.carry[round & 1][lane];
-    }
-    Val<VEC> cur = carry;
-    if (ncl > 1) {
+        tp = held(tp);
+        const uint32_t to = shared_address(&sm.blocks[slot][rank][lane]), bar = shared_address(&sm.arrived[slot]);
+        if (lane == 0)
+          asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(ncl * 32 * 2 * VEC * 4) : "memory");
 #pragma unroll
-      for (int r0 = 0; r0 < CL; r0 += 4) {   // (four loads under way at a time)
-        if (r0 < ncl) {
-          Map<VEC> m[4];
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-            if (r0 + r < ncl) m[r] = sm.blocks[slot][r0 + r][lane];
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            if (r0 + r == rank) cur = carry;
-            if (r0 + r < ncl) carry = fma_(m[r].p, carry, m[r].s);
+        for (int r = 0; r < CL; ++r) {
+          if (r < ncl) {
+            uint32_t far, far_bar;
+            asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(far) : "r"(to), "r"(r));
+            asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(far_bar) : "r"(bar), "r"(r));
+            if constexpr (VEC == 2)
+              asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];"
+                           ::"r"(far), "f"(tp.v[0]), "f"(tp.v[1]), "f"(ts.v[0]), "f"(ts.v[1]), "r"(far_bar) : "memory");
+            else
+              asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];"
+                           ::"r"(far), "f"(tp.v[0]), "f"(ts.v[0]), "r"(far_bar) : "memory");
           }
         }
+        if (!wait_arrived(bar, (uint32_t)(round / kBlockSlots) & 1u)) sm.gone[group] = 1;
+        __syncwarp();
       }
-      if (G == 2 && !last) {
-        sm.carry[(round + 1) & 1][lane] = carry;
-        bar_arrive<64>(kCarryBarrier + ((round + 1) & 1));
+      if (round > 0) {
+        bar_sync<64>(kCarryBarrier + (round & 1));
+        carry = sm.carry[round & 1][lane];
       }
     }
-    constexpr int Q = NW < 4 ? NW : 4;
+    Val<VEC> cur = carry;
+    const bool several = CL > 1 && ncl > 1;
+    if constexpr (CL > 1) {
+      if (several) {
+#pragma unroll
+        for (int r0 = 0; r0 < CL; r0 += 4) {   // (four loads under way at a time)
+          if (r0 < ncl) {
+            Map<VEC> m[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              if (r0 + r < ncl) m[r] = sm.blocks[round % kBlockSlots][r0 + r][lane];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              if (r0 + r == rank) cur = carry;
+              if (r0 + r < ncl) carry = fma_(m[r].p, carry, m[r].s);
+            }
+          }
+        }
+        if (!last) {
+          sm.carry[(round + 1) & 1][lane] = carry;
+          bar_arrive<64>(kCarryBarrier + ((round + 1) & 1));
+        }
+      }
+    }
+    constexpr int Q = 4;
 #pragma unroll
     for (int w0 = 0; w0 < NW; w0 += Q) {
       Map<VEC> m[Q];
@@ -270,11 +286,13 @@ __device__ __forceinline__ Val<VEC> join_runs(Join<VEC, NW, G, CL>& sm, int roun
         cur = fma_(m[w].p, cur, m[w].s);
       }
     }
-    if (ncl == 1) {
+    if (!several) {
       carry = cur;
-      if (G == 2 && !last) {
-        sm.carry[(round + 1) & 1][lane] = carry;
-        bar_arrive<64>(kCarryBarrier + ((round + 1) & 1));
+      if constexpr (CL > 1) {
+        if (!last) {
+          sm.carry[(round + 1) & 1][lane] = carry;
+          bar_arrive<64>(kCarryBarrier + ((round + 1) & 1));
+        }
       }
     }
   }
@@ -397,8 +415,8 @@ struct Place {
     lane = threadIdx.x & 31;
     warp = (threadIdx.x >> 5) % NW;
     group = (threadIdx.x >> 5) / NW;
-    rank = a.cluster > 1 ? (int)(blockIdx.x % a.cluster) : 0;
-    const int unit = blockIdx.x / a.cluster;
+    rank = G > 1 && a.cluster > 1 ? (int)(blockIdx.x % a.cluster) : 0;
+    const int unit = G > 1 ? blockIdx.x / a.cluster : blockIdx.x;
     s = a.longest_first ? by_length(a, unit / a.ctiles) : unit / a.ctiles;
     c0 = (unit % a.ctiles) * 32 * VEC;
     c = c0 + lane * VEC;
@@ -410,7 +428,7 @@ struct Place {
     dir = a.reverse ? -1 : 1;
     // a short sequence is left to the cluster's first blocks
     constexpr int share = NW * L * G;
-    ncl = min(a.cluster, max(1, (len - 1) / share + 1));
+    ncl = G > 1 ? min(a.cluster, max(1, (len - 1) / share + 1)) : 1;
     mine0 = ((group * ncl + rank) * NW + warp) * L;
     step = ncl * NW * L * G;   // from one of a group's rounds to its next
   }
@@ -996,7 +1014,7 @@ int32_t enqueue(ScanArgs a, bool backward, cudaStream_t s) {
   // take 65536 x 2048 bf16 from 515 to 164 us; where the SMs have enough to do without, the
   // exchange costs (40 -> 56 us for 16 x 1024 x 1001).
   a.cluster = 1;
-  if (G == 2)
+  if (CL > 1)
     while (a.cluster < CL && units * (a.cluster + 1) <= kSms &&
            (int64_t)a.cluster * (L * NW * G) < a.tokens / a.seqs)
       ++a.cluster;
@@ -1009,12 +1027,14 @@ int32_t enqueue(ScanArgs a, bool backward, cudaStream_t s) {
     constexpr auto f = decltype(kernel)::value;
     const int32_t rc = allow_shared<f>(smem);
     if (rc != DGC_OK) return rc;
-    if (CL > kPortableCluster && !allow_cluster<f>(CL, NW * G * 32, smem)) {
-      a.cluster = std::min(a.cluster, kPortableCluster);
-      grid = units * a.cluster;
+    if constexpr (CL > kPortableCluster) {
+      if (!allow_cluster<f>(CL, NW * G * 32, smem)) {
+        a.cluster = std::min(a.cluster, kPortableCluster);
+        grid = units * a.cluster;
+      }
     }
     const dim3 blocks((unsigned)grid), threads(NW * G * 32);
-    if (a.cluster > 1) launch_cluster(f, blocks, threads, smem, s, (unsigned)a.cluster, a);
+    if (CL > 1 && a.cluster > 1) launch_cluster(f, blocks, threads, smem, s, (unsigned)a.cluster, a);
     else launch(f, blocks, threads, smem, s, a);
     return check_launch();
   };
@@ -1043,9 +1063,9 @@ int32_t enqueue(const ScanArgs& a, float2* maps, bool backward, cudaStream_t s) 
   const int64_t units = (int64_t)((a.channels + words - 1) / words) * a.seqs;
   const bool uneven = a.seq_start != nullptr;
   if (len <= 64 || (units >= 500 && len <= (uneven ? 200 : 1024)))
-    return enqueue<T, LIE, 4, 1, kPortableCluster>(a, backward, s);
+    return enqueue<T, LIE, 4, 1, 1>(a, backward, s);
   if (len < (uneven ? 400 : 640) && (len <= 128 || units >= kSms))
-    return enqueue<T, LIE, 8, 1, kPortableCluster>(a, backward, s);
+    return enqueue<T, LIE, 8, 1, 1>(a, backward, s);
   if (units <= 4 && len > 1024) return enqueue<T, LIE, 8, 2, kMaxCluster>(a, backward, s);
   return enqueue<T, LIE, 8, 2, kPortableCluster>(a, backward, s);
 }
