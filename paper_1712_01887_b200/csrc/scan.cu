@@ -55,9 +55,13 @@ struct ScanArgs {
   int32_t tokens, seqs, seq_len, channels, ctiles, cluster, reverse, longest_first;
 };
 
-// f = sigma(z) and 1 - f, each to full relative precision (1 - f is not formed by subtraction:
-// for gates near 1 it is the weight of the input).  The logit is held above -87, so that e f
-// cannot become inf * 0; f is then at most 2e-38 too large.  A NaN passes through.
+// f = sigma(z) and 1 - f, each within 4.8e-7 + 7.4e-8 |z| of itself: 1 - f is not formed by
+// subtraction, for gates near 1 it is the weight of the input.  The term in |z| is the rounding of
+// z log2(e) before the exponential (2^-24 |z| of it) and of the constant.  It is left: f and 1 - f
+// come from one exponential and move together, so that h sees f (1 - f) of it, and to take it back
+// (the product's remainder by a multiply-add, times ln(2), onto the exponential) made calls bound by
+// issue 4 to 7 % slower (65536 x 2048 bf16 forward and backward 446 -> 472 us).  The logit is held
+// above -87, so that e f cannot become inf * 0; f is then at most 2e-38 too large.  A NaN passes.
 template <int VEC>
 __device__ __forceinline__ void gate(Val<VEC> z, Val<VEC>& f, Val<VEC>& omf) {
 #pragma unroll
@@ -1046,13 +1050,13 @@ int32_t enqueue(ScanArgs a, bool backward, cudaStream_t s) {
 // Which blocks.  All have 16 warps of 128 registers an SM; they differ in how many of them work at
 // one sequence (forward / backward, bf16 unless stated):
 //   four blocks of 4 warps   where there are blocks for all slots, or runs end early:
-//                            32 x 1024 steps x 1024 channels 35 / 63 us against 44 / 70 with 8 warps,
-//                            20 x 35 x 1500 f32 5.1 / 7.4 against 9.5 / 9.1
-//   two blocks of 8 warps    in between: 16 x 512 x 1024 10 / 18 us against 11 / 22 with 4 warps and
-//                            12 / 18 with 16
+//                            32 x 1024 steps x 1024 channels 36 / 60 us against 36 / 64 with 8 warps,
+//                            20 x 35 x 1500 f32 4.6 / 7.3 against 8.5 / 9.4
+//   two blocks of 8 warps    in between: 16 x 512 x 1024 12 / 19 us against 13 / 22 with 4 warps and
+//                            16 / 23 with 16
 //   one block of 2 x 8 warps puts a whole SM behind a sequence, where they are long and few, or uneven
-//                            (the longest then decides): 20 of 500 on average x 1024 16 / 24 us against
-//                            20 / 37; clusters are for these
+//                            (the longest then decides): 20 of 500 on average x 1024 19 / 27 us against
+//                            22 / 43 with 4 warps; clusters are for these
 // More blocks of a cluster than the portable eight where next to nothing else is there to do
 // (69 against 131 us for one sequence of 60000 x 100 f16 without a workspace); beyond four clusters of sixteen not all
 // find room at once (8 of them: 19 against 14 us for 8192 x 512).

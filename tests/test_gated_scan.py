@@ -452,3 +452,47 @@ def test_long_and_wide_sequences_by_clusters(dt):
     _check(B, [21000], C, dt, packed=False, seed=3)
     _check(B, [300, 20500], C, dt, reverse=True, seed=4)
     B.gated_scan_check()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16], ids=str)
+def test_both_weights_of_a_gate_over_its_whole_range(dt):
+    """A step from state 1 with input 0 is f, from state 0 with input 1 it is 1 - f.  The logit's product with
+    log2(e) is rounded: 2^-24 |z| of the exponential, and 1.4e-8 |z| for the constant's own rounding; the
+    exponential, the sum, the reciprocal and the product add at most 2^-22 + 2^-24 + 2^-23 + 2^-24."""
+    B = _bind()
+    z = torch.cat([torch.linspace(-86, 86, 40001), torch.linspace(-8, 8, 40001)]).to(dt)[None]
+    n = z.shape[1]
+    one, none = torch.ones(1, n), torch.zeros(1, n)
+    f64 = z.double()
+    tol = f64.abs() * (2.0 ** -24 + 1.4e-8) + 2.0 ** -22 + 2.0 ** -23 + 2.0 ** -23
+    for state, x, want in ((one, none, torch.sigmoid(f64)), (none, one, torch.sigmoid(-f64))):
+        sd, out = state.cuda(), torch.empty(1, n, dtype=dt, device="cuda")
+        B.gated_scan_step(z.cuda(), x.to(dt).cuda(), sd, out)
+        off = (sd.double().cpu() - want).abs() / want
+        assert (off <= tol).all(), (float((off / tol).max()), float(f64[0, (off / tol).argmax()]))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dt", DT, ids=str)
+def test_scan_with_finite_gates_of_any_size(dt):
+    """Logits far beyond [-6, 6].  f and 1 - f come from the same exponential, so its error moves h by
+    f (1 - f) of itself: with the roundings above less than 4e-7 of the largest value a step and 1e-6 with both
+    products, and at most as many steps as the sequence has: 3e-4 for 300."""
+    B = _bind()
+    lens, C = [300, 7, 250], 96
+    starts, _, x, dh, h0, dl, _ = _case(lens, C, dt, 0, 12)
+    z = (torch.randn(sum(lens), C, generator=torch.Generator().manual_seed(13)) * 20).clamp(-80, 80).to(dt)
+    how = dict(seq_start=torch.tensor(starts, dtype=torch.int32, device="cuda"), num_seqs=3, h0=h0.cuda())
+    h, dz, dx = (torch.empty(sum(lens), C, dtype=dt, device="cuda") for _ in range(3))
+    d0 = torch.empty(3, C, device="cuda")
+    B.gated_scan_forward(z.cuda(), x.cuda(), h, **how)
+    B.gated_scan_backward(z.cuda(), x.cuda(), h, dh.cuda(), dz, dx, dh_last=dl.cuda(), dh0=d0, **how)
+    zz, xx, hh = z.double(), x.double(), h0.double()
+    rh, _, _ = plain(zz, xx, hh, starts, False)
+    rz, rx, r0, g = plain_backward(zz, xx, hh, starts, False, dh.double(), dl.double())
+    f = torch.sigmoid(zz)
+    stored = UNIT[dt] * float(rh.abs().max()) * (f * (1 - f) * g).abs()     # the stored state's rounding
+    for got, want, unit, more in ((h, rh, UNIT[dt], 0.0), (dx, rx, UNIT[dt], 0.0), (d0, r0, 0.0, 0.0), (dz, rz, UNIT[dt], stored)):
+        off = (got.double().cpu() - want).abs()
+        assert (off <= unit * want.abs() + TINY[dt] + 3e-4 * float(want.abs().max()) + more).all()
