@@ -15,7 +15,9 @@
 // expression is used.  Below 2^24 that factor is within 2^-1/2 .. 2^1/2; rows whose m c or m log2(e)
 // is larger (a mask of -1e9 or of the type's lowest value in every place: the factor of 1e10 can be
 // 2^440, out of range) or that hold no finite number are done again as 2^((s - m) c).  Sums are
-// 32-bit: a thread adds at most a few hundred terms, the rest is a tree.
+// 32-bit, two a thread (even and odd places), the rest is a tree: of a vocabulary of 262144 in one
+// block a thread adds 512 terms to each, of 2^31 - 65 four million, whose roundings (at worst 2^-24
+// of the sum each) are then no longer small.
 
 #include <cooperative_groups.h>
 
