@@ -496,3 +496,41 @@ def test_scan_with_finite_gates_of_any_size(dt):
     for got, want, unit, more in ((h, rh, UNIT[dt], 0.0), (dx, rx, UNIT[dt], 0.0), (d0, r0, 0.0, 0.0), (dz, rz, UNIT[dt], stored)):
         off = (got.double().cpu() - want).abs()
         assert (off <= unit * want.abs() + TINY[dt] + 3e-4 * float(want.abs().max()) + more).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("workspace", [True, False])
+def test_scan_of_matrices_whose_offsets_pass_32_bits(workspace, monkeypatch):
+    """Slices of a [8192, 2^19] product (its last rows start past 2^32 elements): the bits of packed copies."""
+    B = _bind()
+    if not workspace:
+        monkeypatch.setattr(B, "_scan", lambda call, name, args, tokens, num_seqs, stream, device: B._enqueue(call, name, args, stream, device))
+    N, C, dt = 8192, 64, torch.bfloat16
+    starts, z, x, dh, h0, dl, _ = _case([N - 3, 3], C, dt, 0, 6)
+    big = torch.empty(N, 1 << 19, dtype=dt, device="cuda")
+    wide = [big[:, (1 << 19) - (6 - i) * C:][:, :C] for i in range(6)]
+    flat = [torch.empty(N, C, dtype=dt, device="cuda") for _ in range(6)]
+    how = dict(seq_start=torch.tensor(starts, dtype=torch.int32, device="cuda"), num_seqs=2, h0=h0.cuda(), reverse=True)
+    for m in (wide, flat):
+        for to, t in zip(m, (z, x, dh)):
+            to.copy_(t)
+        B.gated_scan_forward(m[0], m[1], m[3], **how)
+        B.gated_scan_backward(m[0], m[1], m[3], m[2], m[4], m[5], dh_last=dl.cuda(), **how)
+    for a, b in zip(wide, flat):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.gpu
+def test_step_in_a_cache_whose_offsets_pass_32_bits():
+    B = _bind()
+    slots, C = (1 << 21) + 3, 1024                             # 8.6 GB of states
+    state = torch.empty(slots, C, device="cuda")
+    at = torch.tensor([slots - 1, 0, (1 << 21) - 1, slots], dtype=torch.int32, device="cuda")
+    z, x = torch.randn(4, C, device="cuda"), torch.randn(4, C, device="cuda")
+    before = torch.randn(3, C, device="cuda")
+    state[at[:3].long()] = before
+    out = torch.empty(4, C, device="cuda")
+    B.gated_scan_step(z, x, state, out, slots=at)
+    want, got = before.clone(), torch.empty(3, C, device="cuda")
+    B.gated_scan_step(z[:3], x[:3], want, got)                 # the same rows in a small cache
+    assert torch.equal(out[:3], got) and torch.equal(state[at[:3].long()], want) and (out[3] == 0).all()
