@@ -450,7 +450,9 @@ int32_t dgc_gated_scan_forward(const dgc_scan* scan, void* stream);
 
 /* The gradients of dgc_gated_scan_forward, with g_t the gradient that reaches h_t in all:
  *   g_t = dh_t + f_{t+1} g_{t+1}  (+ dh_last at the last step)
- *   dx_t = (1 - f_t) g_t ;  dgate_t = f_t (1 - f_t) g_t (h_{t-1} - x_t) ;  dh0 = f_first g_first */
+ *   dx_t = (1 - f_t) g_t ;  dgate_t = f_t (1 - f_t) g_t (h_{t-1} - x_t) ;  dh0 = f_first g_first
+ * h is taken as it is stored, once every few steps (those between are formed again in 32 bits): in a
+ * 16-bit call its rounding enters dgate, by half a unit in the last place of h times f (1 - f) |g|. */
 int32_t dgc_gated_scan_backward(const dgc_scan* scan, void* stream);
 
 /* Synchronises `stream` and returns DGC_ECUDA if, since the last check on the current device, a

@@ -591,7 +591,7 @@ def gated_scan_step(gate: torch.Tensor, x: torch.Tensor, state: torch.Tensor, ou
 
 
 def gated_scan_check(stream=None) -> None:
-    """Synchronises and raises DgcError if a scan kernel's bounded wait has run out."""
+    """Synchronises and raises DgcError if a scan kernel's bounded wait has run out on the current device."""
     _check(_lib.dgc_gated_scan_check(_stream(stream)), "dgc_gated_scan_check")
 
 

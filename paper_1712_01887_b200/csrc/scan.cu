@@ -531,7 +531,9 @@ __global__ void __launch_bounds__(NW * G * 32, BLOCKS) k_scan_forward(const Scan
 // Backward, walked from the sequence's end: position u = len-1-t.  A thread's run of L steps
 // needs h_{t-1} at each of them; it reads the stored h once, before the run's first step, and
 // recomputes the others in 32 bits from z and x, which it has to read anyway: 5 words moved a
-// step instead of 6, and the states inside a run carry no rounding of the output type.
+// step instead of 6, and the states inside a run carry no rounding of the output type.  The one
+// before it does: of 65536 x 2048 bf16 dgate is 1.73e-3 from its 64-bit values in the 2-norm, where
+// states of 32 bits throughout, rounded at the end as here, would give 1.66e-3.
 template <class T, Lie LIE, int L, int NW, int G, int BLOCKS, int CL>
 __global__ void __launch_bounds__(NW * G * 32, BLOCKS) k_scan_backward(const ScanArgs a) {
   pdl_enter();
