@@ -511,8 +511,8 @@ typedef struct dgc_distill {
   float          temperature;       /* 2^-60 .. 2^60                                              */
   float          soft_weight, hard_weight;   /* 0: there is no such term, whatever it would be */
   float          reserved1;         /* 0                                                          */
-  float*         loss;              /* output [rows]; +infinity where a listed entry or the label
-                                       has p = 0                                                  */
+  float*         loss;              /* output [rows]; +infinity where the logit of a listed entry or of
+                                       the label is -infinity, or where 32 bits do not hold it    */
   float*         stats;             /* [rows, 2], forward output (may be NULL) that backward takes as it
                                        is: what the walk over the row found.  The two calls agree in
                                        all arguments above                                        */

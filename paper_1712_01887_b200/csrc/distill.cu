@@ -34,6 +34,7 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kMaxCluster = 8;
+constexpr float kDown = 0x1p-20f, kUp = 0x1p20f;        // logarithms on their way to the loss
 constexpr float kLeast = 0x1p-110f, kMost = 0x1p110f;   // two sums kept from forward to backward
 enum { kForward = 0, kBackward = 1, kBoth = 2 };
 
@@ -247,6 +248,12 @@ __global__ void __launch_bounds__(NT, kBlocks<T, MODE> * 256 / NT) k_distill(con
   }
   const auto exponent = [&](float v) { return careful ? (v - m) * a.c : fmaf(v, a.c, -mc); };
   const auto exponent1 = [&](float v) { return careful ? (v - m) * kLog2e : fmaf(v, kLog2e, -mc1); };
+  // 2^-20 log p (a power of two changes no bit): a word masked with the type's lowest value has a finite log p,
+  // whose exponent of two, or which itself before the weight, is out of range
+  const auto log_of = [&](float v, float c, float minus, float total) {
+    const float e = careful ? (kDown * v - kDown * m) * c : fmaf(kDown * v, c, -kDown * minus);
+    return v == -INFINITY ? -INFINITY : e * kLn2 - kDown * logf(total);
+  };
 
   float tm = -FLT_MAX, ts = 0.0f;   // the teacher's maximum and sum
   for (int i = 0; i * 32 < a.k; ++i) tm = fmaxf(tm, sm.teacher[i].x);
@@ -263,7 +270,7 @@ __global__ void __launch_bounds__(NT, kBlocks<T, MODE> * 256 / NT) k_distill(con
     if (MODE != kForward && tid < a.k) { sm.idx[tid] = mine; sm.q[tid] = q; }
     if (MODE != kBackward && rank == 0) {
       float kl = 0.0f;
-      if (!(q <= 0.0f)) kl = q * (logq - (sk == -INFINITY ? -INFINITY : exponent(sk) * kLn2 - logf(sum)));
+      if (!(q <= 0.0f)) kl = q * (kDown * logq - log_of(sk, a.c, mc, sum));
 #pragma unroll
       for (int d = 16; d; d /= 2) kl += __shfl_xor_sync(0xFFFFFFFFu, kl, d);
       if (lane == 0) sm.loss[warp] = kl;
@@ -273,9 +280,9 @@ __global__ void __launch_bounds__(NT, kBlocks<T, MODE> * 256 / NT) k_distill(con
   if (MODE != kBackward && rank == 0 && tid == 0) {
     float soft = 0.0f;
     for (int i = 0; i * 32 < a.k; ++i) soft += sm.loss[i];
-    float loss = taught ? a.soft * a.temperature * a.temperature * soft : 0.0f;
+    float loss = taught ? a.soft * a.temperature * soft * a.temperature * kUp : 0.0f;
     if (labelled && a.hard != 0.0f)
-      loss -= a.hard * (sy == -INFINITY ? -INFINITY : exponent1(sy) * kLn2 - logf(sum1));
+      loss -= a.hard * log_of(sy, kLog2e, mc1, sum1) * kUp;
     a.loss[r] = loss;
     if (MODE == kForward && a.stats) {
       const auto total = [](float s, float e) {   // s 2^e, or 0: to be summed again

@@ -506,3 +506,19 @@ def test_temperatures_at_the_ends_of_the_range(T):
         s, idx, val, _, w = _problem(5, 3001, 7, dt, 41, False)
         idx[1, 4:] = -1
         _check_distill(_bind(), s, idx, val, None, w, T, 1.0, 0.0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dt", DT, ids=str)
+@pytest.mark.parametrize("T", [1.0, 2.0, 3.5])
+def test_listed_words_masked_with_the_lowest_value(dt, T):
+    """Their log p is finite, -3.4e38 / T in f32 and bf16, and so is the loss (weights that keep it below 3.4e38)."""
+    R, V, K = 5, 4001, 8
+    s, idx, val, lab, w = _problem(R, V, K, dt, 61, True)
+    low = torch.finfo(dt).min
+    s[0, int(idx[0, 3])] = low
+    s[1, idx[1].long()] = low
+    s[2, int(lab[2])] = low
+    s[3, 100:] = low
+    s[4], s[4, 7] = low, torch.finfo(dt).max / 8                # a row that is taken with care
+    _check_distill(_bind(), s, idx, val, lab, w, T, 1 / 32, 1 / 16)
