@@ -6,7 +6,7 @@
  * (tensors j = 0..M laid out in one fp32 arena) and compresses one gradient
  * per call.  The receive side (`dgc_decode_accumulate`, `dgc_apply_sgd`) is
  * stateless, and so are the operators of a recurrent model's step
- * (`dgc_gated_scan_*`, `dgc_top_logits`, `dgc_distill_*`).
+ * (`dgc_gated_scan_*`, `dgc_top_logits`, `dgc_distill_*`, `dgc_decay_attention_*`, `dgc_vocab_loss_*`).
  *
  * Conventions
  *  - "device" pointers are CUDA device memory of the state's device, owned by
@@ -533,6 +533,125 @@ int32_t dgc_distill_backward(const dgc_distill* d, void* stream);
 /* Loss and gradient in one call (dloss known beforehand: a token's weight over the number of
  * tokens): the same results, the logits read from memory once.  stats is not used. */
 int32_t dgc_distill_loss_grad(const dgc_distill* d, void* stream);
+
+/* ---------------------------------------------------------------- linear attention, large vocabularies
+ * The mixer of a model with a matrix for a state, and the loss such a model is trained on.  The same
+ * manner as above: structs, 32-bit arithmetic, results rounded once, DGC_EINVAL before anything
+ * is enqueued, the calling thread's current device.
+ *
+ * Linear attention with a decay for each head, over packed sequences:
+ *   S_t = decay S_{t-1} + k_t v_t^T  ([key_dim, value_dim], fp32) ;  o_t = scale S_t^T q_t
+ * The decays are the layer's constants: they get no gradient. */
+typedef struct dgc_heads {   /* [tokens, heads, dim] */
+  void*   data;    /* device; inputs are not modified */
+  int64_t ld;      /* elements from one token to the next, >= 0 */
+  int64_t head;    /* elements from one head to the next, >= 0 (an input's may be 0: heads share it);
+                      both orders of tokens and heads are accepted.  An output's elements are distinct */
+} dgc_heads;
+
+#define DGC_MAX_HEAD_DIM 128
+
+typedef struct dgc_attention {
+  int32_t        dtype;        /* of q, k, v, out and their gradients                              */
+  int32_t        num_seqs;     /* >= 1                                                             */
+  int32_t        heads;        /* 1 .. 65535                                                       */
+  int32_t        key_dim, value_dim;   /* 1 .. DGC_MAX_HEAD_DIM                                    */
+  float          scale;        /* finite                                                           */
+  int64_t        tokens;       /* 0 .. 2^31 - 129                                                  */
+  const int32_t* seq_start;    /* as in dgc_scan                                                   */
+  const float*   decay;        /* device [heads], each in [0, 1] (results are undefined for others) */
+  dgc_heads      q, k, v;      /* inputs; their values are finite: one that is not spoils its own sequence
+                                  and head, from up to 127 tokens before it on                     */
+  dgc_heads      out;          /* forward output [tokens, heads, value_dim]                        */
+  const float*   s0;           /* [num_seqs, heads, key_dim, value_dim], the states before the first
+                                  token; NULL: 0                                                   */
+  float*         s_last;       /* forward output, the states after the last token (s0's for an
+                                  empty sequence); may be NULL                                     */
+  /* backward only */
+  dgc_heads      dout;         /* gradient of out                                                  */
+  dgc_heads      dq, dk, dv;   /* outputs, for each head its own                                   */
+  const float*   ds_last;      /* gradient of s_last; NULL: 0                                      */
+  float*         ds0;          /* output (ds_last's for an empty sequence); may be NULL            */
+  /* both */
+  void*          workspace;    /* device scratch of dgc_decay_attention_workspace_bytes() bytes, 16-byte
+                                  aligned, or NULL.  With it a few long sequences are worked on in parts,
+                                  side by side                                                     */
+  int64_t        workspace_bytes;
+} dgc_attention;
+
+/* Bytes of workspace that make dgc_decay_attention_forward (backward != 0: _backward) faster for this
+ * struct's sizes (0: none would; a shorter one is DGC_ECAPACITY).  Host only. */
+int64_t dgc_decay_attention_workspace_bytes(const dgc_attention* a, int32_t backward);
+
+/* Writes out and s_last.  Results do not vary from run to run; nothing of one sequence reaches
+ * another; rows outside every sequence are not written.  In a 16-bit call the weights decay^n q.k and the
+ * states are rounded to the type where they enter a product (in DGC_F16 they are to stay within
+ * its range, 65504); sums, and the states from chunk to chunk, are in 32 bits. */
+int32_t dgc_decay_attention_forward(const dgc_attention* a, void* stream);
+
+/* The gradients.  With E_t what reaches S_t from later tokens (ds_last at the last one) and dS_t =
+ * E_t + scale q_t dout_t^T:
+ *   dq_t = scale S_t dout_t ;  dk_t = dS_t v_t ;  dv_t = dS_t^T k_t ;  E_{t-1} = decay dS_t ;  ds0 = E before the first
+ * S is formed again: out and s_last are not used. */
+int32_t dgc_decay_attention_backward(const dgc_attention* a, void* stream);
+
+/* One token for `rows` sequences at once, their states kept in a cache: row r's state is number slots[r]
+ * of `state`, which is advanced in place; out's row r is read from the new state. */
+typedef struct dgc_attention_one {
+  int32_t        dtype, rows, heads, key_dim, value_dim;   /* as above */
+  int32_t        num_slots;  /* states in the cache                                              */
+  float          scale;
+  int32_t        reserved;   /* 0                                                                */
+  const float*   decay;      /* device [heads]                                                   */
+  dgc_heads      q, k, v;    /* [rows, heads, dim] inputs                                        */
+  dgc_heads      out;        /* [rows, heads, value_dim] output                                  */
+  float*         state;      /* device [num_slots, heads, key_dim, value_dim], in and out        */
+  const int32_t* slots;      /* device [rows], no two the same; one outside [0, num_slots) marks
+                                an idle row: no state changes and out's row is 0.  NULL: row r
+                                is in slot r                                                     */
+} dgc_attention_one;
+int32_t dgc_decay_attention_step(const dgc_attention_one* step, void* stream);
+
+/* Softmax cross entropy over a large vocabulary, from the hidden rows and the output matrix; the logits
+ * are formed a piece at a time and not kept:
+ *   l = h W^T + bias ;  loss_r = log sum_j exp(l_rj) - l_{r, label_r}
+ *   G_r = dloss_r (softmax(l_r) - onehot(label_r)) ;  dh = G W ;  dweight = G^T h ;  dbias = sum_r G_r */
+typedef struct dgc_vocab_loss {
+  int32_t        dtype;       /* of all matrices and the bias                                     */
+  int32_t        vocab;       /* 1 .. 2^31 - 1024                                                 */
+  int32_t        hidden;      /* 1 .. 65536                                                       */
+  int32_t        reserved;    /* 0                                                                */
+  int64_t        rows;        /* 0 .. 2^31 - 1024                                                 */
+  dgc_matrix     h;           /* [rows, hidden]                                                   */
+  dgc_matrix     weight;      /* [vocab, hidden]                                                  */
+  const void*    bias;        /* [vocab] or NULL; -infinity masks a word out (its p is 0)         */
+  const int32_t* labels;      /* [rows]; a label outside [0, vocab) marks a padding row: its loss and its
+                                 gradient are 0, and nothing of it reaches dweight, whatever it holds */
+  float*         loss;        /* output [rows]; +infinity where the label is masked out           */
+  float*         stats;       /* [rows, 2], forward output (may be NULL) that backward takes as it is:
+                                 the row's largest logit and the sum of exponentials under it     */
+  const float*   dloss;       /* [rows], the gradient that reaches the row's loss                 */
+  dgc_matrix     dh, dweight; /* outputs, overwritten                                             */
+  void*          dbias;       /* output [vocab]; NULL: not wanted                                 */
+  void*          workspace;   /* device scratch of dgc_vocab_loss_workspace_bytes() bytes, 256-byte
+                                 aligned                                                          */
+  int64_t        workspace_bytes;   /* less than needed: DGC_ECAPACITY                            */
+} dgc_vocab_loss;
+
+/* Bytes of workspace that dgc_vocab_loss_forward (gradient = 0) or the other two (gradient != 0) need for this
+ * struct's dtype, sizes, matrices and bias.  Host only.  Bounded in rows x vocab: a gradient is formed in
+ * pieces of the vocabulary. */
+int64_t dgc_vocab_loss_workspace_bytes(const dgc_vocab_loss* d, int32_t gradient);
+
+/* Writes loss, and stats if given. */
+int32_t dgc_vocab_loss_forward(const dgc_vocab_loss* d, void* stream);
+
+/* Writes dh, dweight and, if given, dbias, from stats and dloss.  In a 16-bit call G is rounded to the type where
+ * it enters the two products.  Results do not vary from run to run. */
+int32_t dgc_vocab_loss_backward(const dgc_vocab_loss* d, void* stream);
+
+/* Loss and gradient in one call (dloss known beforehand); stats is not used. */
+int32_t dgc_vocab_loss_grad(const dgc_vocab_loss* d, void* stream);
 
 /* Number of kernels this library has launched in this process (all states). */
 uint64_t dgc_launch_count(void);

@@ -104,6 +104,11 @@ _sigs = {
         "dgc_gated_scan_forward", "dgc_gated_scan_backward", "dgc_gated_scan_step",
         "dgc_top_logits", "dgc_distill_forward", "dgc_distill_backward", "dgc_distill_loss_grad")},
     "dgc_gated_scan_check": (ctypes.c_int32, [_vp]),
+    **{name: (ctypes.c_int32, [ctypes.c_char_p, _vp]) for name in (
+        "dgc_decay_attention_forward", "dgc_decay_attention_backward", "dgc_decay_attention_step",
+        "dgc_vocab_loss_forward", "dgc_vocab_loss_backward", "dgc_vocab_loss_grad")},
+    "dgc_decay_attention_workspace_bytes": (ctypes.c_int64, [ctypes.c_char_p, ctypes.c_int32]),
+    "dgc_vocab_loss_workspace_bytes": (ctypes.c_int64, [ctypes.c_char_p, ctypes.c_int32]),
     "dgc_gated_scan_workspace_bytes": (ctypes.c_int64, [ctypes.c_char_p]),
     "dgc_launch_count": (ctypes.c_uint64, []),
     "dgc_error_string": (ctypes.c_char_p, [ctypes.c_int32]),
@@ -656,3 +661,145 @@ def distill_loss_grad(logits: torch.Tensor, idx: torch.Tensor, val: torch.Tensor
                         hard_weight, 0.0, _vec(loss, torch.float32, n, dev, "loss"), 0,
                         _vec(dloss, torch.float32, n, dev, "dloss"), dp, dl)
     _enqueue(_lib.dgc_distill_loss_grad, "dgc_distill_loss_grad", args, stream, dev)
+
+
+# ----------------------------------------------------------------- linear attention, large vocabularies
+
+MAX_HEAD_DIM = 128
+ATTENTION = struct.Struct("@5ifq2P" + "P2q" * 4 + "2P" + "P2q" * 4 + "2PPq")   # dgc_attention
+ATTENTION_ONE = struct.Struct("@6ifiP" + "P2q" * 4 + "2P")                     # dgc_attention_one
+VOCAB_LOSS = struct.Struct("@4iqPqPq5PPqPqPPq")                                # dgc_vocab_loss
+_NO_HEADS = (0, 0, 0)
+
+
+def _heads(t: torch.Tensor, dtype, shape, device: int, what: str):
+    """(pointer, strides of tokens and heads) of a [tokens, heads, dim] tensor whose last dimension is adjacent."""
+    if t.dtype is not dtype or t.get_device() != device or t.shape != shape:
+        raise ValueError(f"{what}: expected a {dtype} tensor of shape {tuple(shape)} on device {device}")
+    ld, head, one = t.stride()
+    if one != 1 and shape[2] > 1:
+        raise ValueError(f"{what}: a head's elements must be adjacent in memory")
+    return t.data_ptr(), ld, head
+
+
+def _first_heads(q: torch.Tensor, v: torch.Tensor):
+    """(type code, type, device, shapes of q and k, of v and out)."""
+    dt, shape, device = q.dtype, q.shape, q.get_device()
+    code = DTYPES.get(dt)
+    if code is None or device < 0 or len(shape) != 3:
+        raise ValueError("q: expected a CUDA float32, bfloat16 or float16 tensor [tokens, heads, key_dim]")
+    if len(v.shape) != 3 or v.shape[:2] != shape[:2]:
+        raise ValueError(f"v: expected [{shape[0]}, {shape[1]}, value_dim]")
+    return code, dt, device, shape, v.shape
+
+
+def _work(need: int, stream, device: int):
+    """Workspace from the call's own stream: what was freed on another may still be written there."""
+    with _stream_context(stream, device):
+        return torch.empty(need, dtype=torch.uint8, device=f"cuda:{device}")
+
+
+def _attend(call, name: str, args: bytes, backward: int, stream, device: int) -> None:
+    need = int(_lib.dgc_decay_attention_workspace_bytes(args, backward))
+    if need > 0:
+        work = _work(need, stream, device)
+        args = args[:-16] + struct.pack("@Pq", work.data_ptr(), need)
+    _enqueue(call, name, args, stream, device)
+
+
+def decay_attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor, decay: torch.Tensor,
+                            seq_start: Optional[torch.Tensor] = None, num_seqs: int = 1,
+                            s0: Optional[torch.Tensor] = None, s_last: Optional[torch.Tensor] = None,
+                            scale: float = 1.0, stream=None) -> None:
+    """S_t = decay S_{t-1} + k_t v_t^T, out_t = scale S_t^T q_t for each head, over packed sequences:
+    tokens seq_start[s] .. seq_start[s+1] of the [tokens, heads, dim] tensors (seq_start None: num_seqs
+    sequences of equal length).  States are fp32 [num_seqs, heads, key_dim, value_dim]."""
+    code, dt, dev, kd, vd = _first_heads(q, v)
+    n, h, dk = kd
+    dv, states = vd[2], num_seqs * h * dk * vd[2]
+    args = ATTENTION.pack(code, num_seqs, h, dk, dv, scale, n, _vec(seq_start, torch.int32, num_seqs + 1, dev, "seq_start"),
+                          _vec(decay, torch.float32, h, dev, "decay"), *_heads(q, dt, kd, dev, "q"),
+                          *_heads(k, dt, kd, dev, "k"), *_heads(v, dt, vd, dev, "v"), *_heads(out, dt, vd, dev, "out"),
+                          _vec(s0, torch.float32, states, dev, "s0"), _vec(s_last, torch.float32, states, dev, "s_last"),
+                          *_NO_HEADS, *_NO_HEADS, *_NO_HEADS, *_NO_HEADS, 0, 0, 0, 0)
+    _attend(_lib.dgc_decay_attention_forward, "dgc_decay_attention_forward", args, 0, stream, dev)
+
+
+def decay_attention_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, dout: torch.Tensor, dq: torch.Tensor,
+                             dk: torch.Tensor, dv: torch.Tensor, decay: torch.Tensor,
+                             seq_start: Optional[torch.Tensor] = None, num_seqs: int = 1,
+                             s0: Optional[torch.Tensor] = None, ds_last: Optional[torch.Tensor] = None,
+                             ds0: Optional[torch.Tensor] = None, scale: float = 1.0, stream=None) -> None:
+    """Gradients of decay_attention_forward: writes dq, dk, dv and ds0 from dout and ds_last (each head its
+    own: heads that share a tensor add theirs up)."""
+    code, dt, dev, kd, vd = _first_heads(q, v)
+    n, h, kdim = kd
+    states = num_seqs * h * kdim * vd[2]
+    args = ATTENTION.pack(code, num_seqs, h, kdim, vd[2], scale, n,
+                          _vec(seq_start, torch.int32, num_seqs + 1, dev, "seq_start"),
+                          _vec(decay, torch.float32, h, dev, "decay"), *_heads(q, dt, kd, dev, "q"),
+                          *_heads(k, dt, kd, dev, "k"), *_heads(v, dt, vd, dev, "v"), *_NO_HEADS,
+                          _vec(s0, torch.float32, states, dev, "s0"), 0, *_heads(dout, dt, vd, dev, "dout"),
+                          *_heads(dq, dt, kd, dev, "dq"), *_heads(dk, dt, kd, dev, "dk"), *_heads(dv, dt, vd, dev, "dv"),
+                          _vec(ds_last, torch.float32, states, dev, "ds_last"),
+                          _vec(ds0, torch.float32, states, dev, "ds0"), 0, 0)
+    _attend(_lib.dgc_decay_attention_backward, "dgc_decay_attention_backward", args, 1, stream, dev)
+
+
+def decay_attention_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, state: torch.Tensor, out: torch.Tensor,
+                         decay: torch.Tensor, slots: Optional[torch.Tensor] = None, scale: float = 1.0,
+                         stream=None) -> None:
+    """One token for each row: state number slots[r] of `state` (fp32 [slots, heads, key_dim, value_dim]) is
+    advanced in place, out[r] is read from it; a slot outside the cache marks an idle row."""
+    code, dt, dev, kd, vd = _first_heads(q, v)
+    n, h, dk = kd
+    rows = state.shape[0]
+    args = ATTENTION_ONE.pack(code, n, h, dk, vd[2], rows, scale, 0, _vec(decay, torch.float32, h, dev, "decay"),
+                              *_heads(q, dt, kd, dev, "q"), *_heads(k, dt, kd, dev, "k"), *_heads(v, dt, vd, dev, "v"),
+                              *_heads(out, dt, vd, dev, "out"),
+                              _vec(state, torch.float32, rows * h * dk * vd[2], dev, "state"),
+                              _vec(slots, torch.int32, n, dev, "slots"))
+    _enqueue(_lib.dgc_decay_attention_step, "dgc_decay_attention_step", args, stream, dev)
+
+
+def _vocab_loss(call, name: str, gradient: int, hidden, weight, labels, bias, loss, stats, dloss, dhidden, dweight,
+                dbias, stream) -> None:
+    code, dt, shape, dev, hp, hl = _first(hidden, "hidden")
+    n, d = shape
+    v = weight.shape[0]
+    wp, wl = _matrix(weight, dt, torch.Size((v, d)), dev, "weight")
+    dhp, dhl = _matrix(dhidden, dt, shape, dev, "dhidden") if gradient else (0, 0)
+    dwp, dwl = _matrix(dweight, dt, torch.Size((v, d)), dev, "dweight") if gradient else (0, 0)
+    args = VOCAB_LOSS.pack(code, v, d, 0, n, hp, hl, wp, wl, _vec(bias, dt, v, dev, "bias"),
+                           _vec(labels, torch.int32, n, dev, "labels"), _vec(loss, torch.float32, n, dev, "loss"),
+                           _vec(stats, torch.float32, 2 * n, dev, "stats"), _vec(dloss, torch.float32, n, dev, "dloss"),
+                           dhp, dhl, dwp, dwl, _vec(dbias, dt, v, dev, "dbias"), 0, 0)
+    need = int(_lib.dgc_vocab_loss_workspace_bytes(args, gradient))
+    if need > 0:
+        work = _work(need, stream, dev)
+        args = args[:-16] + struct.pack("@Pq", work.data_ptr(), need)
+    _enqueue(call, name, args, stream, dev)
+
+
+def vocab_loss_forward(hidden: torch.Tensor, weight: torch.Tensor, labels: torch.Tensor, loss: torch.Tensor,
+                       stats: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, stream=None) -> None:
+    """loss[r] = cross entropy of softmax(hidden[r] weight^T + bias) with labels[r] (0 for a label outside the
+    vocabulary: a padding row); the logits are not kept.  stats [rows, 2] is kept for vocab_loss_backward."""
+    _vocab_loss(_lib.dgc_vocab_loss_forward, "dgc_vocab_loss_forward", 0, hidden, weight, labels, bias, loss, stats, None,
+                None, None, None, stream)
+
+
+def vocab_loss_backward(hidden: torch.Tensor, weight: torch.Tensor, labels: torch.Tensor, stats: torch.Tensor,
+                        dloss: torch.Tensor, dhidden: torch.Tensor, dweight: torch.Tensor,
+                        bias: Optional[torch.Tensor] = None, dbias: Optional[torch.Tensor] = None, stream=None) -> None:
+    """The gradient of vocab_loss_forward's losses, dloss[r] being that of row r's."""
+    _vocab_loss(_lib.dgc_vocab_loss_backward, "dgc_vocab_loss_backward", 1, hidden, weight, labels, bias, None, stats, dloss,
+                dhidden, dweight, dbias, stream)
+
+
+def vocab_loss_grad(hidden: torch.Tensor, weight: torch.Tensor, labels: torch.Tensor, dloss: torch.Tensor,
+                    loss: torch.Tensor, dhidden: torch.Tensor, dweight: torch.Tensor,
+                    bias: Optional[torch.Tensor] = None, dbias: Optional[torch.Tensor] = None, stream=None) -> None:
+    """vocab_loss_forward and vocab_loss_backward in one call."""
+    _vocab_loss(_lib.dgc_vocab_loss_grad, "dgc_vocab_loss_grad", 1, hidden, weight, labels, bias, loss, None, dloss, dhidden,
+                dweight, dbias, stream)

@@ -1,0 +1,360 @@
+// Linear attention with a decay for each head (sm_100a): kernels and C ABI.  The mathematics stands in
+// attention.cuh.
+
+#include <algorithm>
+#include <cmath>
+
+#include "attention.cuh"
+
+using namespace dgc;
+
+namespace {
+
+// ------------------------------------------------------------------ the walk in 32-bit arithmetic
+// A block walks one item (a sequence, or a part of it) of one head and 64 of the rows' elements.  A thread
+// holds 8 x 4 elements of the state in registers.
+constexpr int kC = 32, kDy = 64, kDyPitch = kDy + 4, kThreads = 256;
+
+__host__ __device__ inline int pitch_of(int du) { return (du + 3) / 4 * 4 + 4; }
+inline size_t walk_shared(int du) {
+  return sizeof(float) * (2 * kC * pitch_of(du) + kC * kDyPitch + kC * (kC + 1) + DGC_MAX_HEAD_DIM * kDyPitch + kC + 1);
+}
+
+template <class T>
+__device__ __forceinline__ void fetch(float* to, int pitch, const Heads& from, int h, int token, int n, int d0, int d, int width) {
+  const T* p = static_cast<const T*>(from.p) + (int64_t)token * from.ld + (int64_t)h * from.head + d0;
+  for (int e = threadIdx.x; e < kC * width; e += kThreads) {
+    const int i = e / width, c = e - i * width;
+    to[i * pitch + c] = i < n && c < d ? to_float<T>(p[(int64_t)i * from.ld + c]) : 0.0f;
+  }
+}
+
+// STATES: only the states are wanted, from 0 (a part's own share).
+template <class T, bool STATES>
+__global__ void __launch_bounds__(kThreads) k_walk(const __grid_constant__ WalkArgs a) {
+  pdl_enter();
+  extern __shared__ float sm[];
+  const Walk& w = a.w[blockIdx.y];
+  const int slice = blockIdx.x % a.slices, rest = blockIdx.x / a.slices, h = rest % a.heads, item = rest / a.heads;
+  const Item it = item_of(a, item);
+  const int du = w.du, y0 = slice * kDy, dy = min(w.dy - y0, kDy);
+  if (dy <= 0 || (a.part && it.len == 0)) return;
+  const int up = pitch_of(du), du4 = up - 4;
+  float* U = sm;
+  float* X = U + kC * up;
+  float* Y = X + kC * up;
+  float* P = Y + kC * kDyPitch;
+  float* Z = P + kC * (kC + 1);
+  float* power = Z + DGC_MAX_HEAD_DIM * kDyPitch;   // g^0 .. g^C
+  const int tid = threadIdx.x, tx = tid % 16, ty = tid / 16;
+  const float lg = log_decay(a.decay, h);
+  if (tid <= kC) power[tid] = exp2f(tid * lg);
+  const int64_t at = ((int64_t)(a.part ? item : it.s) * a.heads + h) * du * w.dy;
+  float z[8][4];
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const int r = ty + 16 * i, col = tx * 4 + c;
+      z[i][c] = !STATES && w.z_in && r < du && col < dy
+                    ? w.z_in[at + (w.turned ? (int64_t)(y0 + col) * du + r : (int64_t)r * w.dy + y0 + col)] : 0.0f;
+    }
+  const int chunks = (it.len + kC - 1) / kC;
+  for (int t = 0; t < chunks; ++t) {
+    const int chunk = w.late ? chunks - 1 - t : t, token = it.first + chunk * kC, n = min(kC, it.len - chunk * kC);
+    __syncthreads();
+    if (!STATES) fetch<T>(U, up, w.u, h, token, n, 0, du, du4);
+    fetch<T>(X, up, w.x, h, token, n, 0, du, du4);
+    fetch<T>(Y, kDyPitch, w.y, h, token, n, y0, dy, kDy);
+    if (!STATES) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        *reinterpret_cast<float4*>(Z + (ty + 16 * i) * kDyPitch + tx * 4) = make_float4(z[i][0], z[i][1], z[i][2], z[i][3]);
+    }
+    __syncthreads();
+    if (!STATES) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int i = ty * 2 + e / 2, j = tx + 16 * (e % 2);
+        float s = 0.0f;
+        for (int c = 0; c < du4; c += 4) {
+          const float4 u = *reinterpret_cast<const float4*>(U + i * up + c), x = *reinterpret_cast<const float4*>(X + j * up + c);
+          s = fmaf(u.x, x.x, fmaf(u.y, x.y, fmaf(u.z, x.z, fmaf(u.w, x.w, s))));
+        }
+        const int away = w.late ? j - i : i - j;
+        P[i * (kC + 1) + j] = away >= 0 ? s * power[away] * w.w_near : 0.0f;
+      }
+      __syncthreads();
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int i = ty * 2 + e;
+        float far[4] = {}, near[4] = {};
+        for (int c = 0; c < du; ++c) {
+          const float u = U[i * up + c];
+          const float4 s = *reinterpret_cast<const float4*>(Z + c * kDyPitch + tx * 4);
+          far[0] = fmaf(u, s.x, far[0]); far[1] = fmaf(u, s.y, far[1]);
+          far[2] = fmaf(u, s.z, far[2]); far[3] = fmaf(u, s.w, far[3]);
+        }
+        for (int j = w.late ? i : 0; j < (w.late ? n : i + 1); ++j) {
+          const float p = P[i * (kC + 1) + j];
+          const float4 y = *reinterpret_cast<const float4*>(Y + j * kDyPitch + tx * 4);
+          near[0] = fmaf(p, y.x, near[0]); near[1] = fmaf(p, y.y, near[1]);
+          near[2] = fmaf(p, y.z, near[2]); near[3] = fmaf(p, y.w, near[3]);
+        }
+        if (i < n) {
+          const float by = power[w.late ? n - 1 - i : i + 1] * w.w_row;
+          T* out = static_cast<T*>(w.out) + (int64_t)(token + i) * w.out_ld + (int64_t)h * w.out_head + y0;
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+            if (tx * 4 + c < dy) out[tx * 4 + c] = from_float<T>(fmaf(by, far[c], near[c]));
+        }
+      }
+    }
+    const float keep = power[n];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) z[i][c] *= keep;
+    for (int j = 0; j < n; ++j) {
+      const float by = power[w.late ? j + 1 : n - 1 - j] * w.w_x;
+      const float4 y = *reinterpret_cast<const float4*>(Y + j * kDyPitch + tx * 4);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int r = ty + 16 * i;
+        if (r < du) {
+          const float x = X[j * up + r] * by;
+          z[i][0] = fmaf(x, y.x, z[i][0]); z[i][1] = fmaf(x, y.y, z[i][1]);
+          z[i][2] = fmaf(x, y.z, z[i][2]); z[i][3] = fmaf(x, y.w, z[i][3]);
+        }
+      }
+    }
+  }
+  if (w.z_out) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const int r = ty + 16 * i, col = tx * 4 + c;
+        if (r < du && col < dy) w.z_out[at + (int64_t)r * w.dy + y0 + col] = z[i][c];
+      }
+  }
+}
+
+// The parts' own shares, in `z` by item, become the states before each part in the walk's order; the
+// state after the last goes to z_out.
+struct JoinArgs {
+  WalkArgs a;
+  float* z[2];               // by item
+  const float* z_in[2];      // by sequence; may be NULL
+  float* z_out[2];           // by sequence; may be NULL
+  int32_t late[2], size;     // size: du dy
+};
+__global__ void __launch_bounds__(256) k_join(const __grid_constant__ JoinArgs j) {
+  pdl_enter();
+  const int e = blockIdx.x * 256 + threadIdx.x, h = blockIdx.y % j.a.heads, s = blockIdx.y / j.a.heads, which = blockIdx.z;
+  if (e >= j.size) return;
+  int first, len;
+  sequence_of(j.a, s, first, len);
+  const int parts = (len + j.a.part - 1) / j.a.part, base = first / j.a.part + s;
+  const float lg = log_decay(j.a.decay, h);
+  const int64_t step = (int64_t)j.a.heads * j.size;
+  float* z = j.z[which] + base * step + (int64_t)h * j.size + e;
+  float state = j.z_in[which] ? j.z_in[which][s * step + (int64_t)h * j.size + e] : 0.0f;
+  const float whole = exp2f(j.a.part * lg), last = exp2f((len - (parts - 1) * j.a.part) * lg);
+  for (int t = 0; t < parts; ++t) {
+    const int p = j.late[which] ? parts - 1 - t : t;
+    const float own = z[p * step];
+    z[p * step] = state;
+    state = fmaf(p == parts - 1 ? last : whole, state, own);
+  }
+  if (j.z_out[which]) j.z_out[which][s * step + (int64_t)h * j.size + e] = state;
+}
+
+// ------------------------------------------------------------------ one token
+// A block advances one state: warps take its rows in turn, a lane four (or one) of their elements.
+template <class T, int N>
+__global__ void __launch_bounds__(256) k_attention_step(const __grid_constant__ dgc_attention_one a) {
+  pdl_enter();
+  __shared__ float part[8][DGC_MAX_HEAD_DIM];
+  const int h = blockIdx.x % a.heads, tid = threadIdx.x, lane = tid % 32, warp = tid / 32;
+  const int64_t r = blockIdx.x / a.heads;
+  const int slot = a.slots ? a.slots[r] : (int)r;
+  T* out = static_cast<T*>(a.out.data) + r * a.out.ld + (int64_t)h * a.out.head;
+  if (slot < 0 || slot >= a.num_slots) {
+    for (int c = tid; c < a.value_dim; c += 256) out[c] = from_float<T>(0.0f);
+    return;
+  }
+  const T* q = static_cast<const T*>(a.q.data) + r * a.q.ld + (int64_t)h * a.q.head;
+  const T* k = static_cast<const T*>(a.k.data) + r * a.k.ld + (int64_t)h * a.k.head;
+  const T* v = static_cast<const T*>(a.v.data) + r * a.v.ld + (int64_t)h * a.v.head;
+  float* z = a.state + ((int64_t)slot * a.heads + h) * a.key_dim * a.value_dim;
+  const float g = a.decay[h];
+  for (int c0 = 0; c0 < a.value_dim; c0 += 32 * N) {
+    const int c = c0 + lane * N;
+    float vv[N], sum[N] = {};
+#pragma unroll
+    for (int i = 0; i < N; ++i) vv[i] = c + i < a.value_dim ? to_float<T>(v[c + i]) : 0.0f;
+    if (c < a.value_dim) {
+      for (int d = warp; d < a.key_dim; d += 8) {
+        const float kk = to_float<T>(k[d]), qq = to_float<T>(q[d]);
+        float* p = z + (int64_t)d * a.value_dim + c;
+        struct alignas(4 * N) Pack { float f[N]; } s = *reinterpret_cast<const Pack*>(p);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          s.f[i] = fmaf(g, s.f[i], kk * vv[i]);
+          sum[i] = fmaf(qq, s.f[i], sum[i]);
+        }
+        *reinterpret_cast<Pack*>(p) = s;
+      }
+#pragma unroll
+      for (int i = 0; i < N; ++i) part[warp][c + i] = sum[i];
+    }
+  }
+  __syncthreads();
+  for (int c = tid; c < a.value_dim; c += 256) {
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum += part[i][c];
+    out[c] = from_float<T>(a.scale * sum);
+  }
+}
+
+// ------------------------------------------------------------------ host
+constexpr int kSms = 148;
+
+inline bool bad_heads(const dgc_heads& m, int64_t tokens, size_t es) {
+  return m.ld < 0 || m.head < 0 || (tokens > 0 && (!m.data || misaligned(m.data, es)));
+}
+inline bool bad_output(const dgc_heads& m, int64_t tokens, int64_t heads, int64_t dim, size_t es) {
+  if (bad_heads(m, tokens, es)) return true;
+  const bool token_major = (heads == 1 || m.head >= dim) && (tokens <= 1 || m.ld >= (heads == 1 ? 0 : (heads - 1) * m.head) + dim);
+  const bool head_major = (tokens <= 1 || m.ld >= dim) && (heads == 1 || m.head >= (tokens <= 1 ? 0 : (tokens - 1) * m.ld) + dim);
+  return !token_major && !head_major;
+}
+inline bool bad_dims(int32_t heads, int32_t dk, int32_t dv, float scale) {
+  return heads < 1 || heads > 65535 || dk < 1 || dk > DGC_MAX_HEAD_DIM || dv < 1 || dv > DGC_MAX_HEAD_DIM || !std::isfinite(scale);
+}
+inline bool bad_sizes(const dgc_attention* d) {
+  return !d || bad_dtype(d->dtype) || d->num_seqs < 1 || d->tokens < 0 || d->tokens > INT32_MAX - 128 ||
+         (!d->seq_start && d->tokens % d->num_seqs != 0) || bad_dims(d->heads, d->key_dim, d->value_dim, d->scale);
+}
+
+// Tokens of a part, 0: sequences are walked whole.  A part costs reading x and y once more and a
+// state written and read twice, so only calls are cut that would leave SMs idle.
+int32_t part_of_call(const dgc_attention* d, bool backward) {
+  const int64_t units = (int64_t)d->num_seqs * d->heads * (backward ? 3 : 1), len = d->tokens / d->num_seqs;
+  if (units >= 2 * kSms || len < 1024) return 0;
+  const int64_t want = std::max<int64_t>(512, len * units / (4 * kSms));
+  return (int32_t)((want + 127) / 128 * 128);
+}
+inline int64_t items_of(const dgc_attention* d, int32_t part) { return part ? d->tokens / part + d->num_seqs : d->num_seqs; }
+inline int64_t states_bytes(const dgc_attention* d, int32_t part) {
+  return (items_of(d, part) * d->heads * d->key_dim * d->value_dim * 4 + 255) / 256 * 256;
+}
+
+template <class T>
+int32_t walk(WalkArgs a, int walks, int64_t items, bool states, cudaStream_t s) {
+  int du = 0, dy = 0;
+  for (int i = 0; i < walks; ++i) { du = std::max(du, a.w[i].du); dy = std::max(dy, a.w[i].dy); }
+  a.slices = (dy + kDy - 1) / kDy;
+  const int64_t grid = items * a.heads * a.slices;
+  if (grid > INT32_MAX) return DGC_EINVAL;
+  const dim3 blocks((unsigned)grid, walks);
+  const size_t smem = walk_shared(du);
+  const int32_t rc = states ? allow_shared<&k_walk<T, true>>(walk_shared(DGC_MAX_HEAD_DIM)) : allow_shared<&k_walk<T, false>>(walk_shared(DGC_MAX_HEAD_DIM));
+  if (rc != DGC_OK) return rc;
+  if (states) launch(k_walk<T, true>, blocks, kThreads, smem, s, a);
+  else launch(k_walk<T, false>, blocks, kThreads, smem, s, a);
+  return check_launch();
+}
+
+int32_t walk(const WalkArgs& a, int32_t dtype, int walks, int64_t items, bool states, cudaStream_t s) {
+  if (dtype == DGC_F32) return walk<float>(a, walks, items, states, s);
+  if (dtype == DGC_BF16) return walk<__nv_bfloat16>(a, walks, items, states, s);
+  return walk<__half>(a, walks, items, states, s);
+}
+
+Heads side(const dgc_heads& m) { return Heads{m.data, m.ld, m.head}; }
+
+int32_t attention(const dgc_attention* d, bool backward, void* stream) {
+  if (bad_sizes(d)) return DGC_EINVAL;
+  const size_t es = element_size(d->dtype);
+  if (bad_heads(d->q, d->tokens, es) || bad_heads(d->k, d->tokens, es) || bad_heads(d->v, d->tokens, es) || !d->decay ||
+      misaligned(d->decay, 4) || misaligned(d->seq_start, 4) || misaligned(d->s0, 4) || misaligned(d->workspace, 16) ||
+      d->workspace_bytes < 0)
+    return DGC_EINVAL;
+  const auto bad_out = [&](const dgc_heads& m, int32_t dim) { return bad_output(m, d->tokens, d->heads, dim, es); };
+  if (backward ? bad_heads(d->dout, d->tokens, es) || bad_out(d->dq, d->key_dim) || bad_out(d->dk, d->key_dim) ||
+                     bad_out(d->dv, d->value_dim) || misaligned(d->ds_last, 4) || misaligned(d->ds0, 4)
+               : bad_out(d->out, d->value_dim) || misaligned(d->s_last, 4))
+    return DGC_EINVAL;
+  if (d->tokens == 0 && !(backward ? d->ds0 : d->s_last)) return DGC_OK;
+  cudaStream_t s = as_stream(stream);
+  const int32_t part = d->workspace ? part_of_call(d, backward) : 0;
+  if (part && d->workspace_bytes < (backward ? 2 : 1) * states_bytes(d, part)) return DGC_ECAPACITY;
+  const int64_t items = items_of(d, part);
+  if (items * d->heads > INT32_MAX / 2) return DGC_EINVAL;
+  const int32_t dk = d->key_dim, dv = d->value_dim;
+  const float c = d->scale;
+  WalkArgs a{};
+  a.decay = d->decay; a.seq_start = d->seq_start; a.tokens = (int32_t)d->tokens; a.seqs = d->num_seqs;
+  a.seq_len = (int32_t)(d->tokens / d->num_seqs); a.heads = d->heads; a.part = part;
+  float* const early = static_cast<float*>(d->workspace);
+  float* const late = early + (part ? states_bytes(d, part) / 4 : 0);
+  if (part) {   // the parts' shares of the states, and the states before the parts
+    WalkArgs st = a;
+    st.w[0] = Walk{{}, side(d->k), side(d->v), nullptr, 0, 0, nullptr, early, dk, dv, 0, 0, 0.0f, 0.0f, 1.0f};
+    if (backward) st.w[1] = Walk{{}, side(d->q), side(d->dout), nullptr, 0, 0, nullptr, late, dk, dv, 1, 0, 0.0f, 0.0f, c};
+    int32_t rc = walk(st, d->dtype, backward ? 2 : 1, items, true, s);
+    if (rc != DGC_OK) return rc;
+    JoinArgs j{a, {early, late}, {d->s0, d->ds_last}, {backward ? nullptr : d->s_last, d->ds0}, {0, 1}, dk * dv};
+    if ((int64_t)d->num_seqs * d->heads > 65535) return DGC_EINVAL;
+    launch(k_join, dim3((dk * dv + 255) / 256, d->num_seqs * d->heads, backward ? 2 : 1), 256, 0, s, j);
+    if ((rc = check_launch()) != DGC_OK) return rc;
+  }
+  const float* const s_in = part ? early : d->s0;
+  const float* const e_in = part ? late : d->ds_last;
+  if (!backward) {
+    a.w[0] = Walk{side(d->q), side(d->k), side(d->v), d->out.data, d->out.ld, d->out.head, s_in, part ? nullptr : d->s_last, dk, dv, 0, 0, c, c, 1.0f};
+    return walk(a, d->dtype, 1, items, false, s);
+  }
+  a.w[0] = Walk{side(d->dout), side(d->v), side(d->k), d->dq.data, d->dq.ld, d->dq.head, s_in, nullptr, dv, dk, 0, 1, c, c, 1.0f};
+  a.w[1] = Walk{side(d->k), side(d->q), side(d->dout), d->dv.data, d->dv.ld, d->dv.head, e_in, part ? nullptr : d->ds0, dk, dv, 1, 0, 1.0f, c, c};
+  a.w[2] = Walk{side(d->v), side(d->dout), side(d->q), d->dk.data, d->dk.ld, d->dk.head, e_in, nullptr, dv, dk, 1, 1, 1.0f, c, c};
+  return walk(a, d->dtype, 3, items, false, s);
+}
+
+}  // namespace
+
+extern "C" {
+
+int32_t dgc_decay_attention_forward(const dgc_attention* a, void* stream) { return attention(a, false, stream); }
+int32_t dgc_decay_attention_backward(const dgc_attention* a, void* stream) { return attention(a, true, stream); }
+
+int64_t dgc_decay_attention_workspace_bytes(const dgc_attention* a, int32_t backward) {
+  if (bad_sizes(a)) return DGC_EINVAL;
+  const int32_t part = part_of_call(a, backward != 0);
+  return part ? (backward ? 2 : 1) * states_bytes(a, part) : 0;
+}
+
+int32_t dgc_decay_attention_step(const dgc_attention_one* d, void* stream) {
+  if (!d || bad_dtype(d->dtype) || d->rows < 0 || d->num_slots < 0 || bad_dims(d->heads, d->key_dim, d->value_dim, d->scale))
+    return DGC_EINVAL;
+  const size_t es = element_size(d->dtype);
+  if (bad_heads(d->q, d->rows, es) || bad_heads(d->k, d->rows, es) || bad_heads(d->v, d->rows, es) ||
+      bad_output(d->out, d->rows, d->heads, d->value_dim, es) || misaligned(d->slots, 4) || !d->decay || misaligned(d->decay, 4))
+    return DGC_EINVAL;
+  if (d->rows == 0) return DGC_OK;
+  if (!d->state || misaligned(d->state, 4) || (!d->slots && d->num_slots < d->rows) || (int64_t)d->rows * d->heads > INT32_MAX)
+    return DGC_EINVAL;
+  const unsigned grid = (unsigned)(d->rows * d->heads);
+  cudaStream_t s = as_stream(stream);
+  const bool four = d->value_dim % 4 == 0 && !misaligned(d->state, 16);
+  if (d->dtype == DGC_F32) four ? launch(k_attention_step<float, 4>, grid, 256, 0, s, *d) : launch(k_attention_step<float, 1>, grid, 256, 0, s, *d);
+  else if (d->dtype == DGC_BF16)
+    four ? launch(k_attention_step<__nv_bfloat16, 4>, grid, 256, 0, s, *d) : launch(k_attention_step<__nv_bfloat16, 1>, grid, 256, 0, s, *d);
+  else four ? launch(k_attention_step<__half, 4>, grid, 256, 0, s, *d) : launch(k_attention_step<__half, 1>, grid, 256, 0, s, *d);
+  return check_launch();
+}
+
+}  // extern "C"
