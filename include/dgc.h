@@ -653,6 +653,11 @@ int32_t dgc_vocab_loss_backward(const dgc_vocab_loss* d, void* stream);
 /* Loss and gradient in one call (dloss known beforehand); stats is not used. */
 int32_t dgc_vocab_loss_grad(const dgc_vocab_loss* d, void* stream);
 
+/* Synchronises `stream` and returns DGC_ECUDA if, since the last check on the current device, a wait inside a
+ * kernel of the dgc_decay_attention_* or dgc_vocab_loss_* calls ran out (every such wait, for a copy or a product of the
+ * same kernel, is bounded; the call's results are then wrong), else DGC_OK. */
+int32_t dgc_tensor_check(void* stream);
+
 /* Number of kernels this library has launched in this process (all states). */
 uint64_t dgc_launch_count(void);
 

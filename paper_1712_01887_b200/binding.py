@@ -107,6 +107,7 @@ _sigs = {
     **{name: (ctypes.c_int32, [ctypes.c_char_p, _vp]) for name in (
         "dgc_decay_attention_forward", "dgc_decay_attention_backward", "dgc_decay_attention_step",
         "dgc_vocab_loss_forward", "dgc_vocab_loss_backward", "dgc_vocab_loss_grad")},
+    "dgc_tensor_check": (ctypes.c_int32, [_vp]),
     "dgc_decay_attention_workspace_bytes": (ctypes.c_int64, [ctypes.c_char_p, ctypes.c_int32]),
     "dgc_vocab_loss_workspace_bytes": (ctypes.c_int64, [ctypes.c_char_p, ctypes.c_int32]),
     "dgc_gated_scan_workspace_bytes": (ctypes.c_int64, [ctypes.c_char_p]),
@@ -803,3 +804,9 @@ def vocab_loss_grad(hidden: torch.Tensor, weight: torch.Tensor, labels: torch.Te
     """vocab_loss_forward and vocab_loss_backward in one call."""
     _vocab_loss(_lib.dgc_vocab_loss_grad, "dgc_vocab_loss_grad", 1, hidden, weight, labels, bias, loss, None, dloss, dhidden,
                 dweight, dbias, stream)
+
+
+def tensor_check(stream=None) -> None:
+    """Synchronises and raises DgcError if a bounded wait of a decay_attention or vocab_loss kernel has run out on
+    the current device."""
+    _check(_lib.dgc_tensor_check(_stream(stream)), "dgc_tensor_check")
