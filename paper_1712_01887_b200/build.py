@@ -9,7 +9,8 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(_HERE)
 SRC = [os.path.join(_HERE, "csrc", f) for f in ("dgc.cu", "scan.cu", "top_logits.cu", "distill.cu",
                                                "attention.cu", "vocab_loss.cu")]
-HEADERS = [os.path.join(_HERE, "csrc", f) for f in ("common.cuh", "dgc_kernels.cuh", "rows.cuh", "attention.cuh", "tensor.cuh")]
+HEADERS = [os.path.join(_HERE, "csrc", f) for f in ("common.cuh", "dgc_kernels.cuh", "rows.cuh", "attention.cuh",
+                                                   "attention_tensor.cuh", "tensor.cuh")]
 LIB = os.path.join(_HERE, "libdgc.so")
 INCLUDE = os.path.join(ROOT, "include")
 

@@ -4,7 +4,7 @@
 #include <algorithm>
 #include <cmath>
 
-#include "attention.cuh"
+#include "attention_tensor.cuh"
 
 using namespace dgc;
 
@@ -268,7 +268,60 @@ int32_t walk(WalkArgs a, int walks, int64_t items, bool states, cudaStream_t s) 
   return check_launch();
 }
 
+// Whether tensor copies can fetch the walks' inputs: rows on 16 bytes.  (Heads that share a tensor do not
+// move along it, tokens that do are taken by the other kernel.)
+inline bool fetched(const Heads& m, int64_t tokens, int64_t heads) {
+  return !misaligned(m.p, 16) && (m.ld > 0 || tokens <= 1) && m.ld % 8 == 0 && (m.head % 8 == 0 || heads == 1);
+}
+bool on_tensor_cores(const WalkArgs& a, int walks, int32_t dtype, bool states) {
+  if (dtype == DGC_F32 || a.tokens == 0) return false;
+  for (int i = 0; i < walks; ++i) {
+    const Walk& w = a.w[i];
+    if ((!states && !fetched(w.u, a.tokens, a.heads)) || !fetched(w.x, a.tokens, a.heads) || !fetched(w.y, a.tokens, a.heads)) return false;
+  }
+  return true;
+}
+
+template <class T, int D, bool STATES>
+int32_t walk_tensor(const WalkArgs& a, int walks, int64_t items, cudaStream_t s) {
+  TensorWalkArgs g{};
+  g.a = a;
+  g.a.slices = 1;
+  for (int i = 0; i < walks; ++i) {
+    const Walk& w = a.w[i];
+    const Heads* sides[3] = {&w.u, &w.x, &w.y};
+    for (int k = STATES ? 1 : 0; k < 3; ++k) {
+      const Heads& m = *sides[k];
+      const bool one = m.head == 0 || a.heads == 1;
+      const int64_t ld = a.tokens > 1 ? m.ld : 8;
+      const int32_t rc = tensor_map(&g.map[i][k], m.p, std::is_same_v<T, __nv_bfloat16>, k == 2 ? w.dy : w.du, a.tokens, one ? 1 : a.heads, ld,
+                                    one ? 8 : m.head, kTokens);
+      if (rc != DGC_OK) return rc;
+      if (one) g.shared[i] |= 1 << k;
+    }
+    size_t bits = reinterpret_cast<uintptr_t>(w.out) | (size_t)w.out_ld * 2;
+    if (a.heads > 1) bits |= (size_t)w.out_head * 2;
+    g.align[i] = bits % 32 == 0 ? 32 : bits % 16 == 0 ? 16 : 2;
+  }
+  constexpr int smem = kTensorShared<D, STATES>;
+  const int32_t rc = allow_shared<&k_walk_tensor<T, D, STATES>>(smem);
+  if (rc != DGC_OK) return rc;
+  launch(k_walk_tensor<T, D, STATES>, dim3((unsigned)(items * a.heads), walks), kTensorThreads, smem, s, g);
+  return check_launch();
+}
+template <class T, bool STATES>
+int32_t walk_tensor(const WalkArgs& a, int walks, int64_t items, cudaStream_t s) {
+  int dim = 0;
+  for (int i = 0; i < walks; ++i) dim = std::max({dim, a.w[i].du, a.w[i].dy});
+  return dim <= 64 ? walk_tensor<T, 64, STATES>(a, walks, items, s) : walk_tensor<T, 128, STATES>(a, walks, items, s);
+}
+
 int32_t walk(const WalkArgs& a, int32_t dtype, int walks, int64_t items, bool states, cudaStream_t s) {
+  if (on_tensor_cores(a, walks, dtype, states)) {
+    if (dtype == DGC_BF16)
+      return states ? walk_tensor<__nv_bfloat16, true>(a, walks, items, s) : walk_tensor<__nv_bfloat16, false>(a, walks, items, s);
+    return states ? walk_tensor<__half, true>(a, walks, items, s) : walk_tensor<__half, false>(a, walks, items, s);
+  }
   if (dtype == DGC_F32) return walk<float>(a, walks, items, states, s);
   if (dtype == DGC_BF16) return walk<__nv_bfloat16>(a, walks, items, states, s);
   return walk<__half>(a, walks, items, states, s);
@@ -325,6 +378,8 @@ int32_t attention(const dgc_attention* d, bool backward, void* stream) {
 }
 
 }  // namespace
+
+int32_t dgc::attention_waits_out(int* count) { return take_waits_out(count); }
 
 extern "C" {
 

@@ -90,6 +90,8 @@ __device__ __forceinline__ Item item_of(const WalkArgs& a, int item) {
   return it;
 }
 
+int32_t attention_waits_out(int* count);   // of the attention's kernels, see tensor.cuh
+
 // log2 of a decay, finite: decays below 2^-1000 (0) forget everything at once, and 0^0 is 1.
 __device__ __forceinline__ float log_decay(const float* decay, int h) { return fmaxf(log2f(__ldg(decay + h)), -1000.0f); }
 

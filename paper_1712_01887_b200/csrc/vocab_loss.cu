@@ -19,6 +19,7 @@
 #include <cfloat>
 #include <cmath>
 
+#include "attention.cuh"
 #include "tensor.cuh"
 
 using namespace dgc;
@@ -46,7 +47,7 @@ enum { kStats = 0, kGrad = 1, kDh = 2, kDw = 3 };
 template <class T> constexpr int kPlanes = sizeof(T) == 4 ? 3 : 1;
 template <class T> constexpr int kPairs = sizeof(T) == 4 ? 6 : 1;
 template <class T> constexpr int kN = sizeof(T) == 4 ? 128 : 256;
-template <class T> constexpr int kInterval = sizeof(T) == 4 ? 4 : 1 << 30;
+template <class T> constexpr int kInterval = sizeof(T) == 4 ? 2 : 1 << 30;
 template <class T> using Operand = std::conditional_t<std::is_same_v<T, __half>, __half, __nv_bfloat16>;
 constexpr int kM = 256, kK = 64, kThreads = 384, kRing = 196608, kStaging = 8 * 4096;
 constexpr int kSharedBytes = 1024 + kRing + kStaging;
@@ -164,7 +165,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
           if (++stage == STAGES) { stage = 0; ++round; }
         }
       }
-      if (!ok) let_copies_end();
     }
   } else if (warp == 1 && rank == 0) {
     if (elect_one()) {
@@ -394,6 +394,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
   }
   fence_before();
   __syncthreads();
+  if (failed) let_copies_end();
   cluster_barrier();   // (the other block may still load, multiply and arrive here)
   fence_after();
   if (warp == 2) tmem_free<2>(tmem, COLUMNS);
@@ -686,9 +687,10 @@ int64_t dgc_vocab_loss_workspace_bytes(const dgc_vocab_loss* d, int32_t gradient
 }
 int32_t dgc_tensor_check(void* stream) {
   DGC_CUDA(cudaStreamSynchronize(as_stream(stream)));
-  int count = 0;
-  const int32_t rc = take_waits_out(&count);
-  return rc != DGC_OK ? rc : count ? DGC_ECUDA : DGC_OK;
+  int here = 0, there = 0;
+  int32_t rc = take_waits_out(&here);
+  if (rc == DGC_OK) rc = attention_waits_out(&there);
+  return rc != DGC_OK ? rc : here || there ? DGC_ECUDA : DGC_OK;
 }
 int32_t dgc_vocab_loss_forward(const dgc_vocab_loss* d, void* stream) { return vocab_loss(d, true, false, stream); }
 int32_t dgc_vocab_loss_backward(const dgc_vocab_loss* d, void* stream) { return vocab_loss(d, false, true, stream); }
