@@ -303,11 +303,18 @@ int32_t walk_tensor(const WalkArgs& a, int walks, int64_t items, cudaStream_t s)
     if (a.heads > 1) bits |= (size_t)w.out_head * 2;
     g.align[i] = bits % 32 == 0 ? 32 : bits % 16 == 0 ? 16 : 2;
   }
-  constexpr int smem = kTensorShared<D, STATES>;
-  const int32_t rc = allow_shared<&k_walk_tensor<T, D, STATES>>(smem);
-  if (rc != DGC_OK) return rc;
-  launch(k_walk_tensor<T, D, STATES>, dim3((unsigned)(items * a.heads), walks), kTensorThreads, smem, s, g);
-  return check_launch();
+  constexpr int smem = kTensorShared<D, STATES>, exact = std::is_same_v<T, __half> ? 2 : 3;
+  bool results = STATES;
+  for (int i = 0; i < walks; ++i) results |= a.w[i].z_out != nullptr;
+  const auto go = [&](auto parts) {
+    constexpr auto kernel = &k_walk_tensor<T, D, STATES, decltype(parts)::value>;
+    const int32_t rc = allow_shared<kernel>(smem);
+    if (rc != DGC_OK) return rc;
+    launch(kernel, dim3((unsigned)(items * a.heads), walks), kTensorThreads, smem, s, g);
+    return check_launch();
+  };
+  if constexpr (STATES) return go(std::integral_constant<int, exact>{});
+  else return results ? go(std::integral_constant<int, exact>{}) : go(std::integral_constant<int, 2>{});
 }
 template <class T, bool STATES>
 int32_t walk_tensor(const WalkArgs& a, int walks, int64_t items, cudaStream_t s) {

@@ -43,10 +43,11 @@ __device__ __forceinline__ uint32_t in_block(uint32_t local, uint32_t rank) {
 __device__ __forceinline__ void arrive_remote(uint32_t bar) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
+// Whether the phase of this parity is over; the thread is suspended meanwhile, up to 20 us.
 __device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity) {
   uint32_t done;
-  asm volatile("{.reg .pred p; mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p;}"
-               : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+  asm volatile("{.reg .pred p; mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3; selp.u32 %0, 1, 0, p;}"
+               : "=r"(done) : "r"(bar), "r"(parity), "r"(20000u) : "memory");
   return done;
 }
 // Waits until the phase of this parity is over; false once it has taken too long, or another of the
@@ -57,9 +58,7 @@ __device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity, volatile
   uint64_t last = now_ns();
   uint32_t spent = 0;
   for (;;) {
-#pragma unroll 1
-    for (int i = 0; i < 64; ++i)
-      if (try_wait(bar, parity)) return true;
+    if (try_wait(bar, parity)) return true;
     const uint64_t now = now_ns();
     spent += (uint32_t)min(now - last, (uint64_t)kLongestStepNs);
     last = now;
@@ -85,6 +84,36 @@ __device__ __forceinline__ void let_copies_end() {
 }
 __device__ __forceinline__ void cluster_barrier() {
   asm volatile("barrier.cluster.arrive.release.aligned; barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+// ------------------------------------------------------------------ pairs of 16-bit numbers, each operation rounded to the type
+template <class T>
+__device__ __forceinline__ uint32_t fma16(uint32_t a, uint32_t b, uint32_t c) {
+  uint32_t r;
+  if constexpr (std::is_same_v<T, __half>) asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
+  else asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
+  return r;
+}
+template <class T>
+__device__ __forceinline__ uint32_t mul16(uint32_t a, uint32_t b) {
+  uint32_t r;
+  if constexpr (std::is_same_v<T, __half>) asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  else asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+template <class T>
+__device__ __forceinline__ uint32_t sub16(uint32_t a, uint32_t b) {
+  uint32_t r;
+  if constexpr (std::is_same_v<T, __half>) asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  else asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+template <class T>
+__device__ __forceinline__ uint32_t add16(uint32_t a, uint32_t b) {
+  uint32_t r;
+  if constexpr (std::is_same_v<T, __half>) asm("add.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  else asm("add.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
 }
 
 // ------------------------------------------------------------------ tensor copies
@@ -139,6 +168,11 @@ __device__ __forceinline__ void tmem_ld32(uint32_t at, uint32_t (&r)[32]) {
       "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, "
       "%20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
       : DGC_R8(r, 0), DGC_R8(r, 8), DGC_R8(r, 16), DGC_R8(r, 24) : "r"(at));
+}
+__device__ __forceinline__ void tmem_ld16(uint32_t at, uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : DGC_R8(r, 0), DGC_R8(r, 8) : "r"(at));
 }
 __device__ __forceinline__ void tmem_st16(uint32_t at, const uint32_t (&r)[16]) {
   asm volatile(
