@@ -161,11 +161,19 @@ __global__ void __launch_bounds__(256) k_join(const __grid_constant__ JoinArgs j
   float* z = j.z[which] + base * step + (int64_t)h * j.size + e;
   float state = j.z_in[which] ? j.z_in[which][s * step + (int64_t)h * j.size + e] : 0.0f;
   const float whole = exp2f(j.a.part * lg), last = exp2f((len - (parts - 1) * j.a.part) * lg);
-  for (int t = 0; t < parts; ++t) {
-    const int p = j.late[which] ? parts - 1 - t : t;
-    const float own = z[p * step];
-    z[p * step] = state;
-    state = fmaf(p == parts - 1 ? last : whole, state, own);
+  constexpr int AHEAD = 8;   // (a part's share is written over: the loads of the next few go first)
+  for (int t0 = 0; t0 < parts; t0 += AHEAD) {
+    float own[AHEAD];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i)
+      if (t0 + i < parts) own[i] = z[(j.late[which] ? parts - 1 - t0 - i : t0 + i) * step];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      if (t0 + i >= parts) break;
+      const int p = j.late[which] ? parts - 1 - t0 - i : t0 + i;
+      z[p * step] = state;
+      state = fmaf(p == parts - 1 ? last : whole, state, own[i]);
+    }
   }
   if (j.z_out[which]) j.z_out[which][s * step + (int64_t)h * j.size + e] = state;
 }
@@ -239,13 +247,20 @@ inline bool bad_sizes(const dgc_attention* d) {
          (!d->seq_start && d->tokens % d->num_seqs != 0) || bad_dims(d->heads, d->key_dim, d->value_dim, d->scale);
 }
 
-// Tokens of a part, 0: sequences are walked whole.  A part costs reading x and y once more and a
-// state written and read twice, so only calls are cut that would leave SMs idle.
+// Tokens of a part, 0: sequences are walked whole.  A part costs reading x and y once more and a state written
+// and read twice, so only calls are cut that would leave SMs idle, and into as few parts as fill them: of one
+// to three parts for each SM the number that ends first.
 int32_t part_of_call(const dgc_attention* d, bool backward) {
   const int64_t units = (int64_t)d->num_seqs * d->heads * (backward ? 3 : 1), len = d->tokens / d->num_seqs;
   if (units >= 2 * kSms || len < 1024) return 0;
-  const int64_t want = std::max<int64_t>(512, len * units / (4 * kSms));
-  return (int32_t)((want + 127) / 128 * 128);
+  int64_t best = 0, ends = INT64_MAX;
+  for (int64_t waves = 1; waves <= 3; ++waves) {
+    const int64_t parts = std::max<int64_t>(1, waves * kSms / units);
+    const int64_t part = std::max<int64_t>(512, ((len + parts - 1) / parts + 127) / 128 * 128);
+    const int64_t rounds = ((len + part - 1) / part * units + kSms - 1) / kSms;
+    if (rounds * part < ends) { best = part; ends = rounds * part; }
+  }
+  return (int32_t)best;
 }
 inline int64_t items_of(const dgc_attention* d, int32_t part) { return part ? d->tokens / part + d->num_seqs : d->num_seqs; }
 inline int64_t states_bytes(const dgc_attention* d, int32_t part) {
@@ -359,6 +374,7 @@ int32_t attention(const dgc_attention* d, bool backward, void* stream) {
   WalkArgs a{};
   a.decay = d->decay; a.seq_start = d->seq_start; a.tokens = (int32_t)d->tokens; a.seqs = d->num_seqs;
   a.seq_len = (int32_t)(d->tokens / d->num_seqs); a.heads = d->heads; a.part = part;
+  a.longest_first = !part && d->seq_start && d->num_seqs > 1 && d->num_seqs <= kSorted && (int64_t)d->num_seqs * d->heads > kSms;
   float* const early = static_cast<float*>(d->workspace);
   float* const late = early + (part ? states_bytes(d, part) / 4 : 0);
   if (part) {   // the parts' shares of the states, and the states before the parts

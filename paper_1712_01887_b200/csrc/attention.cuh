@@ -42,6 +42,7 @@ struct WalkArgs {
   int32_t tokens, seqs, seq_len, heads;
   int32_t part;          // tokens of a part (a multiple of 128), or 0: whole sequences
   int32_t slices;        // blocks that share the rows' dy
+  int32_t longest_first; // whole sequences, taken in the order of their lengths
 };
 
 // Which sequence and which of its tokens an item is.  Sequences are cut into parts; part 0 of sequence s is
@@ -59,6 +60,26 @@ __device__ __forceinline__ void sequence_of(const WalkArgs& a, int s, int& first
     len = a.seq_len;
   }
 }
+// The sequence that is `place`-th in length (the longest first, the first first among equals): blocks start
+// in this order, so that the last to start have little left to do.  For a whole block.
+constexpr int kSorted = 256;
+__device__ __forceinline__ int by_length(const WalkArgs& a, int place) {
+  __shared__ int lens[kSorted];
+  __shared__ int found;
+  for (int t = threadIdx.x; t < a.seqs; t += blockDim.x) {
+    int first;
+    sequence_of(a, t, first, lens[t]);
+  }
+  __syncthreads();
+  for (int t = threadIdx.x; t < a.seqs; t += blockDim.x) {
+    const int len = lens[t];
+    int before = 0;
+    for (int j = 0; j < a.seqs; ++j) before += lens[j] > len || (lens[j] == len && j < t);
+    if (before == place) found = t;
+  }
+  __syncthreads();
+  return found;
+}
 __device__ __forceinline__ int first_item(const WalkArgs& a, int s) {
   int first, len;
   sequence_of(a, s, first, len);
@@ -67,8 +88,8 @@ __device__ __forceinline__ int first_item(const WalkArgs& a, int s) {
 __device__ __forceinline__ Item item_of(const WalkArgs& a, int item) {
   Item it{};
   if (!a.part) {
-    it.s = item;
-    sequence_of(a, item, it.seq_first, it.seq_len);
+    it.s = a.longest_first ? by_length(a, item) : item;
+    sequence_of(a, it.s, it.seq_first, it.seq_len);
     it.first = it.seq_first;
     it.len = it.seq_len;
     return it;
