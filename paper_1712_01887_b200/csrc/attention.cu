@@ -325,7 +325,7 @@ int32_t walk_tensor(const WalkArgs& a, int walks, int64_t items, cudaStream_t s)
     constexpr auto kernel = &k_walk_tensor<T, D, STATES, decltype(parts)::value>;
     const int32_t rc = allow_shared<kernel>(smem);
     if (rc != DGC_OK) return rc;
-    launch(kernel, dim3((unsigned)(items * a.heads), walks), kTensorThreads, smem, s, g);
+    launch(kernel, dim3((unsigned)(items * a.heads), walks), kTensorThreads<STATES>, smem, s, g);
     return check_launch();
   };
   if constexpr (STATES) return go(std::integral_constant<int, exact>{});

@@ -8,9 +8,9 @@
 // and by role:
 //   warp 0      brings the tiles of X, U and Y into a ring of slots
 //   warp 1      issues the products
-//   warps 2-9   keep the state in registers (a thread half a row of Z^T), put it into shared memory, add near
+//   warps 4-11  keep the state in registers (a thread half a row of Z^T), put it into shared memory, add near
 //               and far up and write the rows
-//   warps 10-13 make X' and P'
+//   from 12 on  make X' and P'
 // X' is kept in two parts of the type, in three of bf16 where the state is a result: one would put its rounding, 2^-9,
 // into the state, two of 8 bits leave 2^-18.  They are made in the type's own arithmetic: with the weight as w1 + w2 + w3,
 //   hi1 = round(x w1), lo1 = x w1 - hi1 (exact, by a multiply-add), and
@@ -27,7 +27,7 @@
 
 namespace dgc {
 
-constexpr int kTokens = 128, kTensorThreads = 14 * 32;
+constexpr int kTokens = 128;
 
 struct TensorWalkArgs {
   CUtensorMap map[kMaxWalks][3];   // u, x, y: [heads][tokens][dim]
@@ -36,9 +36,16 @@ struct TensorWalkArgs {
   int32_t align[kMaxWalks];        // bytes the output's rows are aligned to: 32, 16 or 2
 };
 
-template <int D, bool STATES> constexpr int kSlots = D == 128 ? (STATES ? 5 : 4) : 8;
+// Slots of the ring, buffers of X', warps that make it.  Shared memory is the limit: of 128 x 128 tiles there is room for four
+// slots, one X' and the state; without rows two X' are worth more than slots (the one is made while the other is
+// multiplied: 507 -> xxx us for the states of 2 x 65536 x 16 x 128).
+template <int D, bool STATES> constexpr int kSlots = D == 128 ? (STATES ? 3 : 4) : 8;
+template <int D, bool STATES> constexpr int kScaled = D == 128 && !STATES ? 1 : 2;
+template <bool STATES> constexpr int kMakers = STATES ? 8 : 4;
+template <bool STATES> constexpr int kTensorThreads = (12 + kMakers<STATES>) * 32;
 template <int D> constexpr int kSlotBytes = kTokens * D * 2;
-template <int D, bool STATES> constexpr int kTensorShared = 1024 + (kSlots<D, STATES> + 2) * kSlotBytes<D> + (STATES ? 0 : D * D * 2);
+template <int D, bool STATES>
+constexpr int kTensorShared = 1024 + (kSlots<D, STATES> + 2 * kScaled<D, STATES>) * kSlotBytes<D> + (STATES ? 0 : D * D * 2);
 
 __device__ __forceinline__ void store_shared(uint32_t at, const uint32_t (&w)[4]) {
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
@@ -51,28 +58,49 @@ __device__ __forceinline__ float exp2_here(float x) {
   return y;
 }
 
+// 32 elements of a row, of which `left` are there, at an address on `align` bytes.
+template <class T>
+__device__ __forceinline__ void write_row(T* out, int left, int align, const uint32_t (&packed)[16]) {
+  if (align == 32 && left >= 32) {
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+      asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(out + 16 * e), DGC_I8(packed, 8 * e) : "memory");
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    if (align >= 16 && left >= 8 * e + 8) {
+      *reinterpret_cast<uint4*>(out + 8 * e) = make_uint4(packed[4 * e], packed[4 * e + 1], packed[4 * e + 2], packed[4 * e + 3]);
+    } else {
+#pragma unroll
+      for (int f = 0; f < 8; ++f)
+        if (8 * e + f < left) store_word<T, 1>(out + 8 * e + f, f % 2 ? packed[4 * e + f / 2] >> 16 : packed[4 * e + f / 2] & 0xFFFFu);
+    }
+  }
+}
+
 template <class T, int D, bool STATES, int PARTS>
-__global__ void __launch_bounds__(kTensorThreads, 1) k_walk_tensor(const __grid_constant__ TensorWalkArgs g) {
-  constexpr int SLOTS = kSlots<D, STATES>, SLOT = kSlotBytes<D>, BOX = kTokens * 128, PER = STATES ? 2 : 3;
+__global__ void __launch_bounds__(kTensorThreads<STATES>, 1) k_walk_tensor(const __grid_constant__ TensorWalkArgs g) {
+  constexpr int SLOTS = kSlots<D, STATES>, NB = kScaled<D, STATES>, MAKERS = kMakers<STATES>, SLOT = kSlotBytes<D>, BOX = kTokens * 128, PER = STATES ? 2 : 3;
   constexpr bool BF16 = std::is_same_v<T, __nv_bfloat16>;
   constexpr uint32_t P_AT = 0, NEAR = 128, FAR = 128 + D, DELTA = 128 + 2 * D;
   extern __shared__ char dynamic[];
-  __shared__ __align__(8) uint64_t bars[2 * 8 + 9];
+  __shared__ __align__(8) uint64_t bars[2 * 8 + 13];
   __shared__ float power[kTokens + 1];   // g^0 .. g^128
   __shared__ uint32_t tmem_at;
   __shared__ volatile int failed;
   const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
-  const uint32_t ring = (shared_u32(dynamic) + 1023) & ~1023u, hi = ring + SLOTS * SLOT, lo = hi + SLOT, zs = lo + SLOT;
+  const uint32_t ring = (shared_u32(dynamic) + 1023) & ~1023u, scaled = ring + SLOTS * SLOT, zs = scaled + 2 * NB * SLOT;
   const auto full = [&](int i) { return shared_u32(bars + i % SLOTS); };
   const auto empty = [&](int i) { return shared_u32(bars + 8 + i % SLOTS); };
   const auto tile = [&](int i) { return ring + i % SLOTS * SLOT; };
-  const uint32_t p_full = shared_u32(bars + 16), p_ready = p_full + 8, o_full = p_full + 16, o_empty = p_full + 24, x_ready = p_full + 32,
-                 d_full = p_full + 40, z_ready = p_full + 48, z_empty = p_full + 56, d_empty = p_full + 64;
+  const uint32_t p_full = shared_u32(bars + 16), p_ready = p_full + 8, o_full = p_full + 16, o_empty = p_full + 24, x_ready = p_full + 88,
+                 d_full = p_full + 40, z_ready = p_full + 48, z_empty = p_full + 56, d_empty = p_full + 64, x_free = p_full + 72;
   if (tid == 0) {
     failed = 0;
     for (int s = 0; s < SLOTS; ++s) { barrier_init(shared_u32(bars + s), 1); barrier_init(shared_u32(bars + 8 + s), 1); }
     barrier_init(p_full, 1); barrier_init(p_ready, 4); barrier_init(o_full, 1); barrier_init(o_empty, 8);
-    barrier_init(x_ready, 4); barrier_init(d_full, 1); barrier_init(d_empty, 8); barrier_init(z_ready, 8); barrier_init(z_empty, 1);
+    barrier_init(x_ready, MAKERS); barrier_init(x_ready + 8, MAKERS); barrier_init(x_free, 1); barrier_init(x_free + 8, 1); barrier_init(d_full, 1); barrier_init(d_empty, 8); barrier_init(z_ready, 8); barrier_init(z_empty, 1);
     barrier_init_visible();
   }
   if (warp == 1) tmem_alloc<1>(shared_u32(&tmem_at), 512);
@@ -91,8 +119,9 @@ __global__ void __launch_bounds__(kTensorThreads, 1) k_walk_tensor(const __grid_
   const auto first_of = [&](int c) { return (late ? chunks - 1 - c : c) * kTokens; };
   bool ok = true;
 
-  if (warp == 0) {
-    if (elect_one()) {
+  if (warp < 4) {
+    if (!STATES) fewer_registers<88>();
+    if (warp == 0 && elect_one()) {
       for (int i = 0; i < chunks * PER && ok; ++i) {
         const int part = i % PER, side = STATES ? part + 1 : part;   // u, x, y in turn: the order in which slots come free
         if (!(ok = wait_for(empty(i), (i / SLOTS & 1) ^ 1, &failed))) break;
@@ -101,9 +130,7 @@ __global__ void __launch_bounds__(kTensorThreads, 1) k_walk_tensor(const __grid_
 #pragma unroll
         for (int b = 0; b < D / 64; ++b) load_tile<1>(tile(i) + b * BOX, &g.map[which][side], full(i), b * 64, y, z);
       }
-    }
-  } else if (warp == 1) {
-    if (elect_one()) {
+    } else if (warp == 1 && elect_one()) {
       constexpr uint32_t p_what = product_descriptor(128, 128, BF16, false, false), far_what = product_descriptor(128, D, BF16, false, false),
                          near_what = product_descriptor(128, D, BF16, false, true), d_what = product_descriptor(128, D, BF16, true, true);
       const auto there = [&](int i) { return wait_for(full(i), i / SLOTS & 1, &failed); };
@@ -131,9 +158,9 @@ __global__ void __launch_bounds__(kTensorThreads, 1) k_walk_tensor(const __grid_
           commit<1>(empty(xi - 1));
           commit<1>(z_empty);
         }
-        if (!(ok = there(yi) && wait_for(x_ready, c & 1, &failed))) break;
+        if (!(ok = there(yi) && wait_for(x_ready + c % NB * 8, c / NB & 1, &failed) && wait_for(d_empty, (c & 1) ^ 1, &failed))) break;
         fence_after();
-        const uint64_t y = tile_descriptor(tile(yi), BOX), xh = tile_descriptor(hi, BOX), xl = tile_descriptor(lo, BOX);
+        const uint64_t y = tile_descriptor(tile(yi), BOX), xh = tile_descriptor(scaled + c % NB * 2 * SLOT, BOX), xl = xh + SLOT / 16;
 #pragma unroll 1
         for (int k = 0; k < kTokens / 16; ++k) product<1>(tmem + DELTA, y + k * 128, xh + k * 128, d_what, k > 0);
 #pragma unroll 1
@@ -144,6 +171,7 @@ __global__ void __launch_bounds__(kTensorThreads, 1) k_walk_tensor(const __grid_
           for (int k = 0; k < kTokens / 16; ++k) product<1>(tmem + DELTA, y + k * 128, xr + k * 128, d_what, true);
         }
         commit<1>(d_full);
+        commit<1>(x_free + c % NB * 8);
         commit<1>(empty(xi));
         if (!STATES) {
           if (!(ok = wait_for(p_ready, c & 1, &failed))) break;
@@ -156,9 +184,10 @@ __global__ void __launch_bounds__(kTensorThreads, 1) k_walk_tensor(const __grid_
         if (!STATES && c + 1 < chunks) ok = form_p(c + 1);
       }
     }
-  } else if (warp < 10) {
+  } else if (warp < 12) {
+    if (!STATES) more_registers<160>();
     constexpr int H = D / 2;
-    const int quad = warp % 4, half = (warp - 2) / 4, r = quad * 32 + lane;
+    const int quad = warp % 4, half = (warp - 4) / 4, r = quad * 32 + lane;
     const uint32_t lanes = tmem + ((uint32_t)(quad * 32) << 16) + half * H;
     const int64_t at = ((int64_t)(g.a.part ? item : it.s) * g.a.heads + h) * w.du * w.dy;
     float z[H];
@@ -212,40 +241,24 @@ __global__ void __launch_bounds__(kTensorThreads, 1) k_walk_tensor(const __grid_
       const bool there = r < n;
       const float by = there ? power[late ? n - 1 - r : r + 1] * w.w_row : 0.0f;
       T* out = static_cast<T*>(w.out) + (int64_t)(it.first + from + r) * w.out_ld + (int64_t)h * w.out_head + half * H;
-#pragma unroll 1
-      for (int b = 0; b < H; b += 16) {
-        uint32_t x[16], y[16], packed[8];
-        tmem_ld16(lanes + FAR + b, x);
-        tmem_ld16(lanes + NEAR + b, y);
+#pragma unroll
+      for (int b = 0; b < H; b += 32) {
+        uint32_t x[32], y[32], packed[16];
+        tmem_ld32(lanes + FAR + b, x);
+        tmem_ld32(lanes + NEAR + b, y);
         tmem_wait_ld();
-        if (b + 16 == H) {
+        if (b + 32 == H) {
           fence_before();
           __syncwarp();
           if (lane == 0) arrive(o_empty);
         }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
+        for (int e = 0; e < 16; ++e) {
           const Val<2> v = fma_(Val<2>{{__uint_as_float(x[2 * e]), __uint_as_float(x[2 * e + 1])}}, fill<2>(by),
                                 Val<2>{{__uint_as_float(y[2 * e]), __uint_as_float(y[2 * e + 1])}});
           packed[e] = pack<T, 2>(v.v);
         }
-        const int left = w.dy - half * H - b;
-        if (!there) continue;
-        if (g.align[which] == 32 && left >= 16) {
-          asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(out + b), DGC_I8(packed, 0) : "memory");
-        } else {
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            if (g.align[which] >= 16 && left >= 8 * e + 8) {
-              *reinterpret_cast<uint4*>(out + b + 8 * e) = make_uint4(packed[4 * e], packed[4 * e + 1], packed[4 * e + 2], packed[4 * e + 3]);
-            } else {
-#pragma unroll
-              for (int f = 0; f < 8; ++f)
-                if (8 * e + f < left)
-                  store_word<T, 1>(out + b + 8 * e + f, f % 2 ? packed[4 * e + f / 2] >> 16 : packed[4 * e + f / 2] & 0xFFFFu);
-            }
-          }
-        }
+        if (there) write_row<T>(out + b, w.dy - half * H - b, g.align[which], packed);
       }
     }
     if (w.z_out && ok && r < w.dy && !(STATES && it.len == 0)) {
@@ -255,7 +268,8 @@ __global__ void __launch_bounds__(kTensorThreads, 1) k_walk_tensor(const __grid_
         if (half * H + d < w.du) *to = z[d];
     }
   } else {
-    const int quad = warp % 4, i = quad * 32 + lane, t = (warp - 10) * 32 + lane;
+    if (!STATES) fewer_registers<96>();
+    const int quad = warp % 4, i = quad * 32 + lane, t = (warp - 12) * 32 + lane;
     const uint32_t lanes = tmem + ((uint32_t)(quad * 32) << 16) + P_AT;
     // the weights of the tokens that this thread meets in X, in a chunk that is whole
     struct Weight { uint32_t part[PARTS]; };
@@ -272,32 +286,36 @@ __global__ void __launch_bounds__(kTensorThreads, 1) k_walk_tensor(const __grid_
       }
       return r;
     };
-    Weight token[8];
+    constexpr int STEP = MAKERS * 4, MET = kTokens / STEP;   // from one token that a thread meets to the next
+    Weight token[MET];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) token[e] = weight_of(e * 16 + t / 8, kTokens);
+    for (int e = 0; e < MET; ++e) token[e] = weight_of(e * STEP + t / 8, kTokens);
     const float twice = power[2];
     for (int c = 0; c < chunks; ++c) {
       const int xi = c * PER + PER - 2, yi = xi + 1, n = min(kTokens, it.len - first_of(c));
       ok = __all_sync(0xFFFFFFFFu, wait_for(full(xi), xi / SLOTS & 1, &failed));
       if (ok && n < kTokens) ok = __all_sync(0xFFFFFFFFu, wait_for(full(yi), yi / SLOTS & 1, &failed));
       if (ok && PARTS == 3 && !STATES) ok = __all_sync(0xFFFFFFFFu, wait_for(p_full, c & 1, &failed));   // (X is read no more)
-      if (ok && c) ok = __all_sync(0xFFFFFFFFu, wait_for(d_full, (c & 1) ^ 1, &failed));                 // (nor is X' of the chunk before)
+      const uint32_t hi = scaled + c % NB * 2 * SLOT, lo = hi + SLOT;
+      if (ok) ok = __all_sync(0xFFFFFFFFu, wait_for(x_free + c % NB * 8, (c / NB & 1) ^ 1, &failed));
       if (!ok) break;
       const auto scale = [&](auto whole) {
         constexpr bool WHOLE = decltype(whole)::value;
+        constexpr int BATCH = 4;
 #pragma unroll
-        for (int i0 = 0; i0 < SLOT / 16 / 128; i0 += 4) {
-          uint32_t x[4][4];
+        for (int i0 = 0; i0 < SLOT / 16 / (MAKERS * 32); i0 += BATCH) {
+          constexpr int STRIDE = MAKERS * 32 * 16;
+          uint32_t x[BATCH][4];
 #pragma unroll
-          for (int k = 0; k < 4; ++k)
+          for (int k = 0; k < BATCH; ++k)
             asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(x[k][0]), "=r"(x[k][1]), "=r"(x[k][2]), "=r"(x[k][3])
-                         : "r"(tile(xi) + ((i0 + k) * 128 + t) * 16));
+                         : "r"(tile(xi) + (i0 + k) * STRIDE + t * 16));
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const uint32_t off = ((i0 + k) * 128 + t) * 16;
-            const int j = (i0 + k) % 8 * 16 + t / 8;
+          for (int k = 0; k < BATCH; ++k) {
+            const uint32_t off = (i0 + k) * STRIDE + t * 16;
+            const int j = (i0 + k) % MET * STEP + t / 8;
             const bool there = WHOLE || j < n;   // (what lies behind the sequence may be anything)
-            Weight by = token[(i0 + k) % 8];
+            Weight by = token[(i0 + k) % MET];
             if (!WHOLE) by = weight_of(j, there ? n : kTokens);
             uint32_t part[3][4];
 #pragma unroll
@@ -326,69 +344,67 @@ __global__ void __launch_bounds__(kTensorThreads, 1) k_walk_tensor(const __grid_
       } else {
         scale(std::false_type{});
         const uint32_t none[4] = {};
-        for (int e = n * 8 + t; e < kTokens * 8; e += 128)
+        for (int e = n * 8 + t; e < kTokens * 8; e += MAKERS * 32)
 #pragma unroll
           for (int b = 0; b < D / 64; ++b) store_shared(tile(yi) + b * BOX + e * 16, none);
       }
-      // (the sums of the chunk before have to be out of the tensor memory before the next are formed)
-      if (c && !(ok = __all_sync(0xFFFFFFFFu, wait_for(d_empty, (c & 1) ^ 1, &failed)))) break;
       shared_to_async();
       __syncwarp();
-      if (lane == 0) arrive(x_ready);
+      if (lane == 0) arrive(x_ready + c % NB * 8);
       if (STATES) continue;
       if (!(ok = __all_sync(0xFFFFFFFFu, wait_for(p_full, c & 1, &failed)))) break;
       fence_after();
       const int j_first = late ? i : 0, j_span = (late ? n - 1 : i) - j_first;   // the columns that count
       // P' takes the place of columns of P that have been read; the next are on their way meanwhile
-      const auto weigh = [&](int b, const uint32_t (&v)[32]) {
-        uint32_t packed[16] = {};
-        if (late ? b >= quad && b * 32 < n : b <= quad) {
-          if (late ? b > quad && b * 32 + 32 <= n : b < quad) {
+      const auto weigh = [&](int j0, const uint32_t (&v)[16]) {
+        uint32_t packed[8] = {};
+        if (late ? j0 + 15 >= quad * 32 && j0 < n : j0 <= quad * 32 + 31) {
+          if (late ? j0 >= quad * 32 + 31 && j0 + 16 <= n : j0 + 15 <= quad * 32) {
             // all count: a column's weight is its neighbour's times the decay, from the nearest on
-            const float near1 = power[late ? b * 32 - i : i - 31 - b * 32] * w.w_near, near2 = near1 * power[1];
+            const float near1 = power[late ? j0 - i : i - 15 - j0] * w.w_near, near2 = near1 * power[1];
             Val<2> by = late ? Val<2>{{near1, near2}} : Val<2>{{near2, near1}};
             if (late) {
 #pragma unroll
-              for (int e = 0; e < 16; ++e) {
+              for (int e = 0; e < 8; ++e) {
                 const Val<2> p = mul_(Val<2>{{__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1])}}, by);
                 packed[e] = pack<T, 2>(p.v);
                 by = mul_(by, fill<2>(twice));
               }
             } else {
 #pragma unroll
-              for (int e = 15; e >= 0; --e) {
+              for (int e = 7; e >= 0; --e) {
                 const Val<2> p = mul_(Val<2>{{__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1])}}, by);
                 packed[e] = pack<T, 2>(p.v);
                 by = mul_(by, fill<2>(twice));
               }
             }
           } else {
-            const float step = late ? lg : -lg, start = (late ? b * 32 - i : i - b * 32) * lg;
+            const float step = late ? lg : -lg, start = (late ? j0 - i : i - j0) * lg;
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
+            for (int e = 0; e < 8; ++e) {
               float p[2];
 #pragma unroll
               for (int f = 0; f < 2; ++f) {
                 const int j = 2 * e + f;
                 const float q = __uint_as_float(v[j]) * w.w_near * exp2_here(fmaf(j, step, start));
-                p[f] = (unsigned)(b * 32 + j - j_first) <= (unsigned)j_span && j_span >= 0 ? q : 0.0f;
+                p[f] = (unsigned)(j0 + j - j_first) <= (unsigned)j_span && j_span >= 0 ? q : 0.0f;
               }
               packed[e] = pack<T, 2>(p);
             }
           }
         }
-        tmem_st16(lanes + b * 16, packed);
+        tmem_st8(lanes + j0 / 2, packed);
       };
-      uint32_t even[32], odd[32];
-      tmem_ld32(lanes, even);
+      uint32_t even[16], odd[16];
+      tmem_ld16(lanes, even);
 #pragma unroll 1
-      for (int b = 0; b < 4; b += 2) {
+      for (int j0 = 0; j0 < kTokens; j0 += 32) {
         tmem_wait_ld();
-        tmem_ld32(lanes + b * 32 + 32, odd);
-        weigh(b, even);
+        tmem_ld16(lanes + j0 + 16, odd);
+        weigh(j0, even);
         tmem_wait_ld();
-        if (b < 2) tmem_ld32(lanes + b * 32 + 64, even);
-        weigh(b + 1, odd);
+        if (j0 + 32 < kTokens) tmem_ld16(lanes + j0 + 32, even);
+        weigh(j0 + 16, odd);
       }
       tmem_wait_st();
       fence_before();

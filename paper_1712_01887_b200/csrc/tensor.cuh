@@ -86,6 +86,10 @@ __device__ __forceinline__ void cluster_barrier() {
   asm volatile("barrier.cluster.arrive.release.aligned; barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
+// A warpgroup's registers a thread from here on.  (All of a block's groups together have what it was launched with.)
+template <int N> __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N> __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+
 // ------------------------------------------------------------------ pairs of 16-bit numbers, each operation rounded to the type
 template <class T>
 __device__ __forceinline__ uint32_t fma16(uint32_t a, uint32_t b, uint32_t c) {
@@ -173,6 +177,9 @@ __device__ __forceinline__ void tmem_ld16(uint32_t at, uint32_t (&r)[16]) {
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
       : DGC_R8(r, 0), DGC_R8(r, 8) : "r"(at));
+}
+__device__ __forceinline__ void tmem_st8(uint32_t at, const uint32_t (&r)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(at), DGC_I8(r, 0) : "memory");
 }
 __device__ __forceinline__ void tmem_st16(uint32_t at, const uint32_t (&r)[16]) {
   asm volatile(
