@@ -53,22 +53,22 @@ __device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity) {
 // Waits until the phase of this parity is over; false once it has taken too long, or another of the
 // block's waits has (`failed`, in shared memory): the caller then leaves its loop.
 static __device__ int g_waits_out;
+struct Patience { uint64_t last; uint32_t spent; };
+static __device__ __noinline__ bool too_long(Patience* p, volatile int* failed) {
+  const uint64_t now = now_ns();
+  if (p->last) p->spent += (uint32_t)min(now - p->last, (uint64_t)kLongestStepNs);
+  p->last = now;
+  if (*failed) return true;
+  if (p->spent <= kLongestWaitNs) return false;
+  *failed = 1;
+  atomicAdd(&g_waits_out, 1);
+  return true;
+}
 __device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity, volatile int* failed) {
-  if (try_wait(bar, parity)) return true;
-  uint64_t last = now_ns();
-  uint32_t spent = 0;
-  for (;;) {
-    if (try_wait(bar, parity)) return true;
-    const uint64_t now = now_ns();
-    spent += (uint32_t)min(now - last, (uint64_t)kLongestStepNs);
-    last = now;
-    if (*failed) return false;
-    if (spent > kLongestWaitNs) {
-      *failed = 1;
-      atomicAdd(&g_waits_out, 1);
-      return false;
-    }
-  }
+  Patience p{0, 0};
+  while (!try_wait(bar, parity))
+    if (too_long(&p, failed)) return false;
+  return true;
 }
 // The waits of this file's kernels that have run out since the last look, on the current device.
 static inline int32_t take_waits_out(int* count) {
@@ -240,17 +240,17 @@ inline EncodeTiled encode_tiled() {
   }();
   return f;
 }
-// A map of [z][y][x] 16-bit elements (strides in elements, multiples of 8; 16-byte aligned), tiles of 64 x `box_y`;
-// what lies outside is read as 0 and not written.
+// A map of [z][y][x] 16-bit elements (strides in elements, multiples of 8; 16-byte aligned), tiles of box_x (64, or 32 in
+// the 64-byte swizzle) x box_y; what lies outside is read as 0 and not written.
 inline int32_t tensor_map(CUtensorMap* m, const void* p, bool bf16, int64_t x, int64_t y, int64_t z, int64_t stride_y, int64_t stride_z,
-                          int box_y) {
+                          int box_y, int box_x = 64) {
   const EncodeTiled f = encode_tiled();
   if (!f) return DGC_ECUDA;
   const cuuint64_t dims[3] = {(cuuint64_t)x, (cuuint64_t)y, (cuuint64_t)z};
   const cuuint64_t strides[2] = {(cuuint64_t)stride_y * 2, (cuuint64_t)stride_z * 2};
-  const cuuint32_t box[3] = {64, (cuuint32_t)box_y, 1}, one[3] = {1, 1, 1};
+  const cuuint32_t box[3] = {(cuuint32_t)box_x, (cuuint32_t)box_y, 1}, one[3] = {1, 1, 1};
   return f(m, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void*>(p), dims, strides, box, one,
-           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+           CU_TENSOR_MAP_INTERLEAVE_NONE, box_x == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS ? DGC_OK : DGC_ECUDA;
 }
 
