@@ -317,18 +317,13 @@ int32_t walk_tensor(const WalkArgs& a, int walks, int64_t items, cudaStream_t s)
     size_t bits = reinterpret_cast<uintptr_t>(w.out) | (a.tokens > 1 ? (size_t)w.out_ld * 2 : 0);
     if (a.heads > 1) bits |= (size_t)w.out_head * 2;
     g.align[i] = bits % 32 == 0 ? 32 : bits % 16 == 0 ? 16 : 2;
-    if (!STATES && g.align[i] >= 16) {
-      const int32_t rc = tensor_map(&g.map[i][3], w.out, std::is_same_v<T, __nv_bfloat16>, w.dy, a.tokens, a.heads, a.tokens > 1 ? w.out_ld : 8,
-                                    a.heads > 1 ? w.out_head : 8, 32, D / 2);
-      if (rc != DGC_OK) return rc;
-    }
   }
   constexpr int exact = std::is_same_v<T, __half> ? 2 : 3;
   bool results = STATES;
   for (int i = 0; i < walks; ++i) results |= a.w[i].z_out != nullptr;
   const auto go = [&](auto parts) {
     constexpr auto kernel = &k_walk_tensor<T, D, STATES, decltype(parts)::value>;
-    using L = Layout<D, STATES, decltype(parts)::value>;
+    using L = Layout<D, STATES>;
     const int32_t rc = allow_shared<kernel>(L::shared);
     if (rc != DGC_OK) return rc;
     launch(kernel, dim3((unsigned)(items * a.heads), walks), L::threads, L::shared, s, g);

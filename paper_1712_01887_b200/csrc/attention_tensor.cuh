@@ -8,15 +8,16 @@
 // and by role:
 //   warp 0      brings the tiles of X, U and Y into a ring of slots
 //   warp 1      issues the products
-//   warps 4-11  keep the state in registers (a thread half a row of Z^T), put it into shared memory, add near
+//   warps 2-9   keep the state in registers (a thread half a row of Z^T), put it into shared memory, add near
 //               and far up and write the rows
-//   from 12 on  make X' and P'
+//   warps 10-13 make X' and P'
 // X' is kept in two parts of the type, in three of bf16 where the state is a result: one would put its rounding, 2^-9,
 // into the state, two of 8 bits leave 2^-18.  They are made in the type's own arithmetic: with the weight as w1 + w2 + w3,
 //   hi1 = round(x w1), lo1 = x w1 - hi1 (exact, by a multiply-add), and
 //   two parts:    hi1, round(x w2 + lo1)
 //   three parts:  hi1, s = round(lo1 + hi2), round(x w3 + (what s has lost + lo2))     with hi2 + lo2 = x w2
-// which is a third of the instructions that 32-bit products take, taken apart by conversions.  
+// which is a third of the instructions that 32-bit products take, taken apart by conversions.  The third part takes the
+// place of X, whose product has then been formed.
 // The state's sums over a chunk are the tensor core's, over the chunks they are the registers': a tensor core cuts off
 // where an addition would round, which over 16 steps does not show and over a long sequence would.
 #pragma once
@@ -29,76 +30,56 @@ namespace dgc {
 constexpr int kTokens = 128;
 
 struct TensorWalkArgs {
-  CUtensorMap map[kMaxWalks][4];   // u, x, y and the rows: [heads][tokens][dim]
+  CUtensorMap map[kMaxWalks][3];   // u, x, y: [heads][tokens][dim]
   WalkArgs a;
   int32_t shared[kMaxWalks];       // bit i: the heads share u, x or y
   int32_t align[kMaxWalks];        // bytes the output's rows are aligned to: 32, 16 or 2
 };
 
-// How a block's shared memory is dealt out.  128 x 128 tiles leave room for seven of them: the state, X' (its last part in the
-// place of X) and four or five slots.  Narrower tiles, and walks that write no rows, have two X', the one made while the other
-// is multiplied.
-template <int D, bool STATES, int PARTS> struct Layout {
-  static constexpr bool tight = D == 128 && !STATES;
-  static constexpr int slot_bytes = kTokens * D * 2;
-  static constexpr int buffers = tight ? PARTS - 1 : 2;            // of an X'; a part beyond them is where X was
-  static constexpr int sets = tight ? 1 : 2;                       // X'
-  static constexpr int slots = D == 128 ? (STATES ? 3 : 6 - buffers) : STATES ? 8 : 7;
-  static constexpr int state_bytes = STATES ? 0 : D * D * 2, rows_bytes = D == 64 && !STATES ? slot_bytes : 0;
-  static constexpr int makers = STATES ? 8 : 4, threads = (12 + makers) * 32;   // warps that make X' and P'
-  static constexpr int shared = 1024 + (slots + sets * buffers) * slot_bytes + state_bytes + rows_bytes;
+// How a block's shared memory and warps are dealt out.  Of 128 x 128 tiles there is room for seven: X' in two parts (a third
+// takes the place of X, whose product has then been formed), the state and four slots.  Walks that write no rows have
+// two X', the one made while the other is multiplied, and twice the warps that make it (states of 2 x 65536 x 16 x 128: 508 -> 394 us).
+template <int D, bool STATES> struct Layout {
+  static constexpr int slot_bytes = kTokens * D * 2, sets = STATES ? 2 : 1, slots = D == 64 ? 8 : STATES ? 3 : 4;
+  static constexpr int makers = STATES ? 8 : 4, threads = (10 + makers) * 32;
+  static constexpr int shared = 1024 + (slots + sets * 2) * slot_bytes + (STATES ? 0 : D * D * 2);
 };
 
 __device__ __forceinline__ void store_shared(uint32_t at, const uint32_t (&w)[4]) {
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
 }
 
-// 32 elements of a row, of which `left` are there, at an address on `align` bytes.
-template <class T>
-__device__ __forceinline__ void write_row(T* out, int left, int align, const uint32_t (&packed)[16]) {
-  if (align == 32 && left >= 32) {
-#pragma unroll
-    for (int e = 0; e < 2; ++e)
-      asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(out + 16 * e), DGC_I8(packed, 8 * e) : "memory");
-    return;
-  }
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    if (align >= 16 && left >= 8 * e + 8) {
-      *reinterpret_cast<uint4*>(out + 8 * e) = make_uint4(packed[4 * e], packed[4 * e + 1], packed[4 * e + 2], packed[4 * e + 3]);
-    } else {
-#pragma unroll
-      for (int f = 0; f < 8; ++f)
-        if (8 * e + f < left) store_word<T, 1>(out + 8 * e + f, f % 2 ? packed[4 * e + f / 2] >> 16 : packed[4 * e + f / 2] & 0xFFFFu);
-    }
-  }
+// 2^x where it stands: kept from chunk to chunk, the values would not fit the registers.
+__device__ __forceinline__ float exp2_here(float x) {
+  float y;
+  asm volatile("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
 }
 
 template <class T, int D, bool STATES, int PARTS>
-__global__ void __launch_bounds__(Layout<D, STATES, PARTS>::threads, 1) k_walk_tensor(const __grid_constant__ TensorWalkArgs g) {
-  using L = Layout<D, STATES, PARTS>;
-  constexpr int SLOTS = L::slots, NB = L::sets, BUFFERS = L::buffers, MAKERS = L::makers, SLOT = L::slot_bytes;
-  constexpr int BOX = kTokens * 128, PER = STATES ? 2 : 3;
+__global__ void __launch_bounds__(Layout<D, STATES>::threads, 1) k_walk_tensor(const __grid_constant__ TensorWalkArgs g) {
+  using L = Layout<D, STATES>;
+  constexpr int SLOTS = L::slots, SLOT = L::slot_bytes, NB = L::sets, MAKERS = L::makers, BOX = kTokens * 128, PER = STATES ? 2 : 3;
   constexpr bool BF16 = std::is_same_v<T, __nv_bfloat16>;
   constexpr uint32_t P_AT = 0, NEAR = 128, FAR = 128 + D, DELTA = 128 + 2 * D;
   extern __shared__ char dynamic[];
-  __shared__ __align__(8) uint64_t bars[2 * 8 + 15];
+  __shared__ __align__(8) uint64_t bars[2 * 8 + 12];
   __shared__ float power[kTokens + 1];   // g^0 .. g^128
-  __shared__ __align__(16) float column[32];
   __shared__ uint32_t tmem_at;
   __shared__ volatile int failed;
   const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
-  const uint32_t ring = (shared_u32(dynamic) + 1023) & ~1023u, scaled = ring + SLOTS * SLOT, zs = scaled + NB * BUFFERS * SLOT, rows = zs + D * D * 2;
+  const uint32_t ring = (shared_u32(dynamic) + 1023) & ~1023u, scaled = ring + SLOTS * SLOT, zs = scaled + NB * 2 * SLOT;
   const auto full = [&](int i) { return shared_u32(bars + i % SLOTS); };
   const auto empty = [&](int i) { return shared_u32(bars + 8 + i % SLOTS); };
   const auto tile = [&](int i) { return ring + i % SLOTS * SLOT; };
-  const uint32_t p_full = shared_u32(bars + 16), p_ready = p_full + 8, o_full = p_full + 16, o_empty = p_full + 24, x_ready = p_full + 88,
-                 d_full = p_full + 40, z_ready = p_full + 48, z_empty = p_full + 56, d_empty = p_full + 64, x_free = p_full + 72, o_stored = p_full + 104;
+  const uint32_t p_full = shared_u32(bars + 16), p_ready = p_full + 8, o_full = p_full + 16, o_empty = p_full + 24, x_ready = p_full + 80,
+                 d_full = p_full + 40, z_ready = p_full + 48, z_empty = p_full + 56, d_empty = p_full + 32, x_free = p_full + 64;
   if (tid == 0) {
     failed = 0;
     for (int s = 0; s < SLOTS; ++s) { barrier_init(shared_u32(bars + s), 1); barrier_init(shared_u32(bars + 8 + s), 1); }
-    barrier_init(p_full, 1); barrier_init(p_ready, MAKERS); barrier_init(o_full, 1); barrier_init(o_empty, 8);
-    barrier_init(o_stored, 8); barrier_init(o_stored + 8, 8); barrier_init(x_ready, MAKERS); barrier_init(x_ready + 8, MAKERS); barrier_init(x_free, 1); barrier_init(x_free + 8, 1); barrier_init(d_full, 1); barrier_init(d_empty, 8); barrier_init(z_ready, 8); barrier_init(z_empty, 1);
+    barrier_init(p_full, 1); barrier_init(p_ready, 4); barrier_init(o_full, 1); barrier_init(o_empty, 8);
+    for (int b = 0; b < 2; ++b) { barrier_init(x_ready + b * 8, MAKERS); barrier_init(x_free + b * 8, 1); }
+    barrier_init(d_full, 1); barrier_init(d_empty, 8); barrier_init(z_ready, 8); barrier_init(z_empty, 1);
     barrier_init_visible();
   }
   if (warp == 1) tmem_alloc<1>(shared_u32(&tmem_at), 512);
@@ -108,7 +89,6 @@ __global__ void __launch_bounds__(Layout<D, STATES, PARTS>::threads, 1) k_walk_t
   const Item it = item_of(g.a, item);
   const float lg = log_decay(g.a.decay, h);
   if (tid <= kTokens) power[tid] = exp2f(tid * lg);
-  if (tid < 32) column[tid] = exp2f((w.late ? tid : 31 - tid) * lg);   // see weigh
   fence_before();
   __syncthreads();
   fence_after();
@@ -118,21 +98,19 @@ __global__ void __launch_bounds__(Layout<D, STATES, PARTS>::threads, 1) k_walk_t
   const auto first_of = [&](int c) { return (late ? chunks - 1 - c : c) * kTokens; };
   bool ok = true;
 
-  if (warp < 4) {
-    if (!STATES) fewer_registers<88>();
-    if (warp == 0 && elect_one()) {
+  if (warp == 0) {
+    if (elect_one()) {
       for (int i = 0; i < chunks * PER && ok; ++i) {
         const int part = i % PER, side = STATES ? part + 1 : part;   // u, x, y in turn: the order in which slots come free
         if (!(ok = wait_for(empty(i), (i / SLOTS & 1) ^ 1, &failed))) break;
-        // (the slot of an X may be the one through which its chunk's rows leave)
-        const int before = i - SLOTS, chunk = before / 3;
-        if (L::tight && before >= 0 && before % 3 == 1 && !(ok = wait_for(o_stored + chunk % 2 * 8, chunk / 2 & 1, &failed))) break;
         arrive_expect(full(i), SLOT);
         const int z = g.shared[which] >> side & 1 ? 0 : h, y = it.first + first_of(i / PER);
 #pragma unroll
         for (int b = 0; b < D / 64; ++b) load_tile<1>(tile(i) + b * BOX, &g.map[which][side], full(i), b * 64, y, z);
       }
-    } else if (warp == 1 && elect_one()) {
+    }
+  } else if (warp == 1) {
+    if (elect_one()) {
       constexpr uint32_t p_what = product_descriptor(128, 128, BF16, false, false), far_what = product_descriptor(128, D, BF16, false, false),
                          near_what = product_descriptor(128, D, BF16, false, true), d_what = product_descriptor(128, D, BF16, true, true);
       const auto there = [&](int i) { return wait_for(full(i), i / SLOTS & 1, &failed); };
@@ -162,12 +140,15 @@ __global__ void __launch_bounds__(Layout<D, STATES, PARTS>::threads, 1) k_walk_t
         }
         if (!(ok = there(yi) && wait_for(x_ready + c % NB * 8, c / NB & 1, &failed) && wait_for(d_empty, (c & 1) ^ 1, &failed))) break;
         fence_after();
-        const uint64_t y = tile_descriptor(tile(yi), BOX);
+        const uint64_t y = tile_descriptor(tile(yi), BOX), xh = tile_descriptor(scaled + c % NB * 2 * SLOT, BOX), xl = xh + SLOT / 16;
 #pragma unroll 1
-        for (int p = 0; p < PARTS; ++p) {
-          const uint64_t x = tile_descriptor(p < BUFFERS ? scaled + (c % NB * BUFFERS + p) * SLOT : tile(xi), BOX);
+        for (int k = 0; k < kTokens / 16; ++k) product<1>(tmem + DELTA, y + k * 128, xh + k * 128, d_what, k > 0);
 #pragma unroll 1
-          for (int k = 0; k < kTokens / 16; ++k) product<1>(tmem + DELTA, y + k * 128, x + k * 128, d_what, p + k > 0);
+        for (int k = 0; k < kTokens / 16; ++k) product<1>(tmem + DELTA, y + k * 128, xl + k * 128, d_what, true);
+        if (PARTS == 3) {
+          const uint64_t xr = tile_descriptor(tile(xi), BOX);
+#pragma unroll 1
+          for (int k = 0; k < kTokens / 16; ++k) product<1>(tmem + DELTA, y + k * 128, xr + k * 128, d_what, true);
         }
         commit<1>(d_full);
         commit<1>(x_free + c % NB * 8);
@@ -183,10 +164,9 @@ __global__ void __launch_bounds__(Layout<D, STATES, PARTS>::threads, 1) k_walk_t
         if (!STATES && c + 1 < chunks) ok = form_p(c + 1);
       }
     }
-  } else if (warp < 12) {
-    if (!STATES) more_registers<152>();
+  } else if (warp < 10) {
     constexpr int H = D / 2;
-    const int quad = warp % 4, half = (warp - 4) / 4, r = quad * 32 + lane;
+    const int quad = warp % 4, half = (warp - 2) / 4, r = quad * 32 + lane;
     const uint32_t lanes = tmem + ((uint32_t)(quad * 32) << 16) + half * H;
     const int64_t at = ((int64_t)(g.a.part ? item : it.s) * g.a.heads + h) * w.du * w.dy;
     float z[H];
@@ -195,104 +175,87 @@ __global__ void __launch_bounds__(Layout<D, STATES, PARTS>::threads, 1) k_walk_t
       const int u = half * H + d;
       z[d] = !STATES && w.z_in && r < w.dy && u < w.du ? w.z_in[at + (w.turned ? r * w.du + u : u * w.dy + r)] : 0.0f;
     }
-#pragma unroll 1
-    for (int c = 0; c <= chunks; ++c) {   // take in chunk c - 1, show the state before chunk c, write the rows of chunk c - 1
-      const int from = c ? first_of(c - 1) : 0, n = min(kTokens, it.len - from);
-      if (c) {
-        if (!(ok = __all_sync(0xFFFFFFFFu, wait_for(d_full, (c & 1) ^ 1, &failed)))) break;
-        fence_after();
-        const float keep = power[n];
+    const auto show = [&] {   // the state, as the product takes it
+      if (r < D) {
 #pragma unroll
-        for (int b = 0; b < H; b += 16) {
-          uint32_t v[16];
-          tmem_ld16(lanes + DELTA + b, v);
-          tmem_wait_ld();
+        for (int d = 0; d < H; d += 8) {
+          const int u = half * H + d;
+          uint32_t p[4];
 #pragma unroll
-          for (int e = 0; e < 16; ++e) z[b + e] = fmaf(keep, z[b + e], __uint_as_float(v[e]));
-        }
-        fence_before();
-        __syncwarp();
-        if (lane == 0) arrive(d_empty);
-      }
-      if (STATES) continue;
-      if (c < chunks) {   // as the product takes it
-        if (!(ok = __all_sync(0xFFFFFFFFu, wait_for(z_empty, (c & 1) ^ 1, &failed)))) break;
-        if (r < D) {
-#pragma unroll
-          for (int d = 0; d < H; d += 8) {
-            const int u = half * H + d;
-            uint32_t p[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float two[2] = {z[d + 2 * e], z[d + 2 * e + 1]};
-              p[e] = pack<T, 2>(two);
-            }
-            store_shared(zs + u / 64 * (D * 128) + r * 128 + (((u % 64 / 8) ^ (r & 7)) << 4), p);
+          for (int e = 0; e < 4; ++e) {
+            const float two[2] = {z[d + 2 * e], z[d + 2 * e + 1]};
+            p[e] = pack<T, 2>(two);
           }
+          store_shared(zs + u / 64 * (D * 128) + r * 128 + (((u % 64 / 8) ^ (r & 7)) << 4), p);
         }
-        shared_to_async();
-        __syncwarp();
-        if (lane == 0) arrive(z_ready);
       }
-      if (c == 0) continue;
-      if (!(ok = __all_sync(0xFFFFFFFFu, wait_for(o_full, (c & 1) ^ 1, &failed)))) break;
+      shared_to_async();
+      __syncwarp();
+      if (lane == 0) arrive(z_ready);
+    };
+    if (!STATES && chunks > 0) show();
+    for (int c = 0; c < chunks; ++c) {
+      const int from = first_of(c), n = min(kTokens, it.len - from);
+      if (!(ok = __all_sync(0xFFFFFFFFu, wait_for(d_full, c & 1, &failed)))) break;
+      fence_after();
+      const float keep = power[n];
+#pragma unroll
+      for (int b = 0; b < H; b += 16) {
+        uint32_t v[16];
+        tmem_ld16(lanes + DELTA + b, v);
+        tmem_wait_ld();
+#pragma unroll
+        for (int e = 0; e < 16; ++e) z[b + e] = fmaf(keep, z[b + e], __uint_as_float(v[e]));
+      }
+      fence_before();
+      __syncwarp();
+      if (lane == 0) arrive(d_empty);
+      if (STATES) continue;
+      if (c + 1 < chunks) {
+        if (!(ok = __all_sync(0xFFFFFFFFu, wait_for(z_empty, c & 1, &failed)))) break;
+        show();
+      }
+      if (!(ok = __all_sync(0xFFFFFFFFu, wait_for(o_full, c & 1, &failed)))) break;
       fence_after();
       const bool there = r < n;
       const float by = there ? power[late ? n - 1 - r : r + 1] * w.w_row : 0.0f;
       T* out = static_cast<T*>(w.out) + (int64_t)(it.first + from + r) * w.out_ld + (int64_t)h * w.out_head + half * H;
-      // the rows of a whole chunk leave by tensor copies, 32 of H elements a warp (a store of 32 bytes for each of 32 rows took
-      // 3000 cycles a chunk); in wider tiles through the slot of X, which is done with
-      const bool copied = n == kTokens && g.align[which] >= 16;
-      const uint32_t stage = (D == 128 ? tile((c - 1) * PER + 1) : rows) + (half * 4 + quad) * 32 * H * 2;
-      if (D == 64) {
-        if (lane == 0) store_wait_read();
-        __syncwarp();
-      }
 #pragma unroll 1
-      for (int b = 0; b < H; b += 32) {
-        uint32_t x[32], y[32], packed[16];
-        tmem_ld32(lanes + FAR + b, x);
-        tmem_ld32(lanes + NEAR + b, y);
+      for (int b = 0; b < H; b += 16) {
+        uint32_t x[16], y[16], packed[8];
+        tmem_ld16(lanes + FAR + b, x);
+        tmem_ld16(lanes + NEAR + b, y);
         tmem_wait_ld();
-        if (b + 32 == H) {
+        if (b + 16 == H) {
           fence_before();
           __syncwarp();
           if (lane == 0) arrive(o_empty);
         }
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
+        for (int e = 0; e < 8; ++e) {
           const Val<2> v = fma_(Val<2>{{__uint_as_float(x[2 * e]), __uint_as_float(x[2 * e + 1])}}, fill<2>(by),
                                 Val<2>{{__uint_as_float(y[2 * e]), __uint_as_float(y[2 * e + 1])}});
           packed[e] = pack<T, 2>(v.v);
         }
-        if (copied) {
+        const int left = w.dy - half * H - b;
+        if (!there) continue;
+        if (g.align[which] == 32 && left >= 16) {
+          asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(out + b), DGC_I8(packed, 0) : "memory");
+        } else {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const uint32_t p[4] = {packed[4 * e], packed[4 * e + 1], packed[4 * e + 2], packed[4 * e + 3]};
-            const int chunk = b / 8 + e, at = D == 128 ? chunk ^ (lane & 7) : chunk ^ (lane >> 1 & 3);   // (swizzled)
-            store_shared(stage + lane * H * 2 + at * 16, p);
+          for (int e = 0; e < 2; ++e) {
+            if (g.align[which] >= 16 && left >= 8 * e + 8) {
+              *reinterpret_cast<uint4*>(out + b + 8 * e) = make_uint4(packed[4 * e], packed[4 * e + 1], packed[4 * e + 2], packed[4 * e + 3]);
+            } else {
+#pragma unroll
+              for (int f = 0; f < 8; ++f)
+                if (8 * e + f < left)
+                  store_word<T, 1>(out + b + 8 * e + f, f % 2 ? packed[4 * e + f / 2] >> 16 : packed[4 * e + f / 2] & 0xFFFFu);
+            }
           }
-        } else if (there) {
-          write_row<T>(out + b, w.dy - half * H - b, g.align[which], packed);
         }
-      }
-      if (copied) {
-        shared_to_async();
-        __syncwarp();
-        if (lane == 0 && half * H < w.dy) {
-          store_tile(&g.map[which][3], stage, half * H, it.first + from + quad * 32, h);
-          store_commit();
-        }
-      }
-      if (D == 128) {
-        if (lane == 0) {
-          store_wait_read();
-          arrive(o_stored + (c - 1) % 2 * 8);
-        }
-        __syncwarp();
       }
     }
-    if (!STATES && lane == 0) store_wait_all();
     if (w.z_out && ok && r < w.dy && !(STATES && it.len == 0)) {
       float* to = w.z_out + at + (int64_t)half * H * w.dy + r;
 #pragma unroll
@@ -300,8 +263,7 @@ __global__ void __launch_bounds__(Layout<D, STATES, PARTS>::threads, 1) k_walk_t
         if (half * H + d < w.du) *to = z[d];
     }
   } else {
-    if (!STATES) fewer_registers<120>();
-    const int quad = warp % 4, row = quad * 32 + lane, t = (warp - 12) * 32 + lane;
+    const int quad = warp % 4, i = quad * 32 + lane, t = (warp - 10) * 32 + lane;
     const uint32_t lanes = tmem + ((uint32_t)(quad * 32) << 16) + P_AT;
     // the weights of the tokens that this thread meets in X, in a chunk that is whole
     struct Weight { uint32_t part[PARTS]; };
@@ -322,27 +284,27 @@ __global__ void __launch_bounds__(Layout<D, STATES, PARTS>::threads, 1) k_walk_t
     Weight token[MET];
 #pragma unroll
     for (int e = 0; e < MET; ++e) token[e] = weight_of(e * STEP + t / 8, kTokens);
+    const float twice = power[2];
     for (int c = 0; c < chunks; ++c) {
       const int xi = c * PER + PER - 2, yi = xi + 1, n = min(kTokens, it.len - first_of(c));
       ok = __all_sync(0xFFFFFFFFu, wait_for(full(xi), xi / SLOTS & 1, &failed));
       if (ok && n < kTokens) ok = __all_sync(0xFFFFFFFFu, wait_for(full(yi), yi / SLOTS & 1, &failed));
-      if (ok && PARTS > BUFFERS && !STATES) ok = __all_sync(0xFFFFFFFFu, wait_for(p_full, c & 1, &failed));   // (X is read no more)
-      const uint32_t hi = scaled + c % NB * BUFFERS * SLOT;
+      if (ok && PARTS == 3 && !STATES) ok = __all_sync(0xFFFFFFFFu, wait_for(p_full, c & 1, &failed));   // (X is read no more)
+      const uint32_t hi = scaled + c % NB * 2 * SLOT, lo = hi + SLOT;
       if (ok) ok = __all_sync(0xFFFFFFFFu, wait_for(x_free + c % NB * 8, (c / NB & 1) ^ 1, &failed));
       if (!ok) break;
       const auto scale = [&](auto whole) {
         constexpr bool WHOLE = decltype(whole)::value;
-        constexpr int BATCH = WHOLE ? MET : 1;
-#pragma unroll 1
-        for (int i0 = 0; i0 < SLOT / 16 / (MAKERS * 32); i0 += BATCH) {
-          constexpr int STRIDE = MAKERS * 32 * 16;
-          uint32_t x[BATCH][4];
 #pragma unroll
-          for (int k = 0; k < BATCH; ++k)
+        for (int i0 = 0; i0 < SLOT / 16 / (MAKERS * 32); i0 += 4) {
+          constexpr int STRIDE = MAKERS * 32 * 16;
+          uint32_t x[4][4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
             asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(x[k][0]), "=r"(x[k][1]), "=r"(x[k][2]), "=r"(x[k][3])
                          : "r"(tile(xi) + (i0 + k) * STRIDE + t * 16));
 #pragma unroll
-          for (int k = 0; k < BATCH; ++k) {
+          for (int k = 0; k < 4; ++k) {
             const uint32_t off = (i0 + k) * STRIDE + t * 16;
             const int j = (i0 + k) % MET * STEP + t / 8;
             const bool there = WHOLE || j < n;   // (what lies behind the sequence may be anything)
@@ -364,8 +326,9 @@ __global__ void __launch_bounds__(Layout<D, STATES, PARTS>::threads, 1) k_walk_t
                 part[2][e] = fma16<T>(v, by.part[2], add16<T>(lost, lo2));
               }
             }
-#pragma unroll
-            for (int p = 0; p < PARTS; ++p) store_shared((p < BUFFERS ? hi + p * SLOT : tile(xi)) + off, part[p]);
+            store_shared(hi + off, part[0]);
+            store_shared(lo + off, part[1]);
+            if (PARTS == 3) store_shared(tile(xi) + off, part[2]);
           }
         }
       };
@@ -384,53 +347,57 @@ __global__ void __launch_bounds__(Layout<D, STATES, PARTS>::threads, 1) k_walk_t
       if (STATES) continue;
       if (!(ok = __all_sync(0xFFFFFFFFu, wait_for(p_full, c & 1, &failed)))) break;
       fence_after();
-      // (what follows from these is formed anew in every chunk: kept, it would not fit the registers)
-      int i = row;
-      float rate = lg;
-      asm volatile("" : "+r"(i), "+f"(rate));
-      const int j_first = late ? i : 0, j_span = (late ? n - 1 : i) - j_first;   // the columns that count, from the first on (rows behind the sequence are not written)
+      const int j_first = late ? i : 0, j_span = (late ? n - 1 : i) - j_first;   // the columns that count
       // P' takes the place of columns of P that have been read; the next are on their way meanwhile
-      const auto weigh = [&](int j0, const uint32_t (&v)[32]) {
+      const auto weigh = [&](int b, const uint32_t (&v)[32]) {
         uint32_t packed[16] = {};
-        if (late ? j0 >= quad * 32 && j0 < n : j0 <= quad * 32) {
-          if (late ? j0 > quad * 32 && j0 + 32 <= n : j0 < quad * 32) {
-            // all count: g^|i - j| is a power for the row times one for the column
-            const Val<2> by = fill<2>(power[late ? j0 - i : i - 31 - j0] * w.w_near);
+        if (late ? b >= quad && b * 32 < n : b <= quad) {
+          if (late ? b > quad && b * 32 + 32 <= n : b < quad) {
+            // all count: a column's weight is its neighbour's times the decay, from the nearest on
+            const float near1 = power[late ? b * 32 - i : i - 31 - b * 32] * w.w_near, near2 = near1 * power[1];
+            Val<2> by = late ? Val<2>{{near1, near2}} : Val<2>{{near2, near1}};
+            if (late) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const float4 col = *reinterpret_cast<const float4*>(column + 4 * e);
-              const Val<2> p = mul_(Val<2>{{__uint_as_float(v[4 * e]), __uint_as_float(v[4 * e + 1])}}, mul_(by, Val<2>{{col.x, col.y}}));
-              const Val<2> q = mul_(Val<2>{{__uint_as_float(v[4 * e + 2]), __uint_as_float(v[4 * e + 3])}}, mul_(by, Val<2>{{col.z, col.w}}));
-              packed[2 * e] = pack<T, 2>(p.v);
-              packed[2 * e + 1] = pack<T, 2>(q.v);
+              for (int e = 0; e < 16; ++e) {
+                const Val<2> p = mul_(Val<2>{{__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1])}}, by);
+                packed[e] = pack<T, 2>(p.v);
+                by = mul_(by, fill<2>(twice));
+              }
+            } else {
+#pragma unroll
+              for (int e = 15; e >= 0; --e) {
+                const Val<2> p = mul_(Val<2>{{__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1])}}, by);
+                packed[e] = pack<T, 2>(p.v);
+                by = mul_(by, fill<2>(twice));
+              }
             }
           } else {
-            const float step = late ? rate : -rate, start = (late ? j0 - i : i - j0) * rate;
-            const uint32_t before = (uint32_t)(j0 - j_first), span = (uint32_t)j_span;
+            const float step = late ? lg : -lg, start = (late ? b * 32 - i : i - b * 32) * lg;
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
               float p[2];
 #pragma unroll
               for (int f = 0; f < 2; ++f) {
-                const float q = __uint_as_float(v[2 * e + f]) * w.w_near * exp2_fast(fmaf(2 * e + f, step, start));
-                p[f] = before + 2 * e + f <= span ? q : 0.0f;
+                const int j = 2 * e + f;
+                const float q = __uint_as_float(v[j]) * w.w_near * exp2_here(fmaf(j, step, start));
+                p[f] = (unsigned)(b * 32 + j - j_first) <= (unsigned)j_span && j_span >= 0 ? q : 0.0f;
               }
               packed[e] = pack<T, 2>(p);
             }
           }
         }
-        tmem_st16(lanes + j0 / 2, packed);
+        tmem_st16(lanes + b * 16, packed);
       };
       uint32_t even[32], odd[32];
       tmem_ld32(lanes, even);
 #pragma unroll 1
-      for (int j0 = 0; j0 < kTokens; j0 += 64) {
+      for (int b = 0; b < 4; b += 2) {
         tmem_wait_ld();
-        tmem_ld32(lanes + j0 + 32, odd);
-        weigh(j0, even);
+        tmem_ld32(lanes + b * 32 + 32, odd);
+        weigh(b, even);
         tmem_wait_ld();
-        if (j0 == 0) tmem_ld32(lanes + 64, even);
-        weigh(j0 + 32, odd);
+        if (b < 2) tmem_ld32(lanes + b * 32 + 64, even);
+        weigh(b + 1, odd);
       }
       tmem_wait_st();
       fence_before();

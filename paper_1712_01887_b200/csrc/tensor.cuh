@@ -86,10 +86,6 @@ __device__ __forceinline__ void cluster_barrier() {
   asm volatile("barrier.cluster.arrive.release.aligned; barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-// A warpgroup's registers a thread from here on.  (All of a block's groups together have what it was launched with.)
-template <int N> __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
-template <int N> __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
-
 // ------------------------------------------------------------------ pairs of 16-bit numbers, each operation rounded to the type
 template <class T>
 __device__ __forceinline__ uint32_t fma16(uint32_t a, uint32_t b, uint32_t c) {
@@ -240,17 +236,16 @@ inline EncodeTiled encode_tiled() {
   }();
   return f;
 }
-// A map of [z][y][x] 16-bit elements (strides in elements, multiples of 8; 16-byte aligned), tiles of box_x (64, or 32 in
-// the 64-byte swizzle) x box_y; what lies outside is read as 0 and not written.
+// A map of [z][y][x] 16-bit elements (strides in elements, multiples of 8; 16-byte aligned), tiles of 64 x box_y; what lies outside is read as 0 and not written.
 inline int32_t tensor_map(CUtensorMap* m, const void* p, bool bf16, int64_t x, int64_t y, int64_t z, int64_t stride_y, int64_t stride_z,
-                          int box_y, int box_x = 64) {
+                          int box_y) {
   const EncodeTiled f = encode_tiled();
   if (!f) return DGC_ECUDA;
   const cuuint64_t dims[3] = {(cuuint64_t)x, (cuuint64_t)y, (cuuint64_t)z};
   const cuuint64_t strides[2] = {(cuuint64_t)stride_y * 2, (cuuint64_t)stride_z * 2};
-  const cuuint32_t box[3] = {(cuuint32_t)box_x, (cuuint32_t)box_y, 1}, one[3] = {1, 1, 1};
+  const cuuint32_t box[3] = {64, (cuuint32_t)box_y, 1}, one[3] = {1, 1, 1};
   return f(m, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void*>(p), dims, strides, box, one,
-           CU_TENSOR_MAP_INTERLEAVE_NONE, box_x == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS ? DGC_OK : DGC_ECUDA;
 }
 
