@@ -575,12 +575,13 @@ typedef struct dgc_attention {
   /* both */
   void*          workspace;    /* device scratch of dgc_decay_attention_workspace_bytes() bytes, 16-byte
                                   aligned, or NULL.  With it a few long sequences are worked on in parts,
-                                  side by side                                                     */
+                                  side by side, and 16-bit rows that do not lie on 16 bytes are laid
+                                  out anew                                                         */
   int64_t        workspace_bytes;
 } dgc_attention;
 
 /* Bytes of workspace that make dgc_decay_attention_forward (backward != 0: _backward) faster for this
- * struct's sizes (0: none would; a shorter one is DGC_ECAPACITY).  Host only. */
+ * struct's sizes and tensors (0: none would; a shorter one is DGC_ECAPACITY).  Host only. */
 int64_t dgc_decay_attention_workspace_bytes(const dgc_attention* a, int32_t backward);
 
 /* Writes out and s_last.  Results do not vary from run to run; nothing of one sequence reaches

@@ -11,29 +11,55 @@ using namespace dgc;
 namespace {
 
 // ------------------------------------------------------------------ the walk in 32-bit arithmetic
-// A block walks one item (a sequence, or a part of it) of one head and 64 of the rows' elements.  A thread
-// holds 8 x 4 elements of the state in registers.
-constexpr int kC = 32, kDy = 64, kDyPitch = kDy + 4, kThreads = 256;
+// For 32-bit tensors and rows that tensor copies cannot fetch.  A block walks one item (a sequence, or a part of it) of one head and 64
+// of the rows' elements, in chunks of 32 tokens.  A thread holds 8 x 4 elements of the state in registers, and forms 2 x 2
+// of P and 2 x 4 of the rows; factors come from shared memory four at a time.  All loads of a chunk are under way at
+// once (fetched one after the other they were three quarters of the time: 379 -> FIG us for 20 x 35 x 12 x 125 f32).
+constexpr int kC = 32, kDy = 64, kDyPitch = kDy + 4, kThreads = 256, kPPitch = kC + 4;
 
 __host__ __device__ inline int pitch_of(int du) { return (du + 3) / 4 * 4 + 4; }
 inline size_t walk_shared(int du) {
-  return sizeof(float) * (2 * kC * pitch_of(du) + kC * kDyPitch + kC * (kC + 1) + DGC_MAX_HEAD_DIM * kDyPitch + kC + 1);
+  return sizeof(float) * (2 * kC * pitch_of(du) + kC * kDyPitch + kC * kPPitch + DGC_MAX_HEAD_DIM * kDyPitch + kC + 1);
 }
 
-template <class T>
-__device__ __forceinline__ void fetch(float* to, int pitch, const Heads& from, int h, int token, int n, int d0, int d, int width) {
-  const T* p = static_cast<const T*>(from.p) + (int64_t)token * from.ld + (int64_t)h * from.head + d0;
-  for (int e = threadIdx.x; e < kC * width; e += kThreads) {
-    const int i = e / width, c = e - i * width;
-    to[i * pitch + c] = i < n && c < d ? to_float<T>(p[(int64_t)i * from.ld + c]) : 0.0f;
+// 32 rows, a warp each fourth part of eight; WIDE: 128 columns, else 64.
+template <class T, bool WIDE>
+struct Fetched {
+  static constexpr int N = WIDE ? 4 : 2;
+  T v[4][N];
+  __device__ __forceinline__ void load(const Heads& from, int h, int token, int n, int d0, int d) {
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const T* p = static_cast<const T*>(from.p) + (int64_t)token * from.ld + (int64_t)h * from.head + d0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int c = 0; c < N; ++c) {
+        const int row = warp + 8 * i, col = lane + 32 * c;
+        v[i][c] = row < n && col < d ? p[(int64_t)row * from.ld + col] : from_float<T>(0.0f);
+      }
   }
+  __device__ __forceinline__ void store(float* to, int pitch, int width) const {
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int c = 0; c < N; ++c)
+        if (lane + 32 * c < width) to[(warp + 8 * i) * pitch + lane + 32 * c] = to_float<T>(v[i][c]);
+  }
+};
+
+__device__ __forceinline__ void add4(float (&to)[4], float by, const float4& v) {
+  to[0] = fmaf(by, v.x, to[0]);
+  to[1] = fmaf(by, v.y, to[1]);
+  to[2] = fmaf(by, v.z, to[2]);
+  to[3] = fmaf(by, v.w, to[3]);
 }
 
 // STATES: only the states are wanted, from 0 (a part's own share).
 template <class T, bool STATES>
-__global__ void __launch_bounds__(kThreads) k_walk(const __grid_constant__ WalkArgs a) {
+__global__ void __launch_bounds__(kThreads, 2) k_walk(const __grid_constant__ WalkArgs a) {
   pdl_enter();
-  extern __shared__ float sm[];
+  extern __shared__ __align__(16) float sm[];
   const Walk& w = a.w[blockIdx.y];
   const int slice = blockIdx.x % a.slices, rest = blockIdx.x / a.slices, h = rest % a.heads, item = rest / a.heads;
   const Item it = item_of(a, item);
@@ -44,89 +70,112 @@ __global__ void __launch_bounds__(kThreads) k_walk(const __grid_constant__ WalkA
   float* X = U + kC * up;
   float* Y = X + kC * up;
   float* P = Y + kC * kDyPitch;
-  float* Z = P + kC * (kC + 1);
+  float* Z = P + kC * kPPitch;
   float* power = Z + DGC_MAX_HEAD_DIM * kDyPitch;   // g^0 .. g^C
   const int tid = threadIdx.x, tx = tid % 16, ty = tid / 16;
   const float lg = log_decay(a.decay, h);
   if (tid <= kC) power[tid] = exp2f(tid * lg);
   const int64_t at = ((int64_t)(a.part ? item : it.s) * a.heads + h) * du * w.dy;
+  const auto row_of = [&](int i) { return i / 4 * 64 + ty * 4 + i % 4; };   // of the state's, the thread's i-th
   float z[8][4];
 #pragma unroll
   for (int i = 0; i < 8; ++i)
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
-      const int r = ty + 16 * i, col = tx * 4 + c;
+      const int r = row_of(i), col = tx * 4 + c;
       z[i][c] = !STATES && w.z_in && r < du && col < dy
                     ? w.z_in[at + (w.turned ? (int64_t)(y0 + col) * du + r : (int64_t)r * w.dy + y0 + col)] : 0.0f;
     }
   const int chunks = (it.len + kC - 1) / kC;
   for (int t = 0; t < chunks; ++t) {
     const int chunk = w.late ? chunks - 1 - t : t, token = it.first + chunk * kC, n = min(kC, it.len - chunk * kC);
+    Fetched<T, true> u, x;
+    Fetched<T, false> y;
+    if (!STATES) u.load(w.u, h, token, n, 0, du);
+    x.load(w.x, h, token, n, 0, du);
+    y.load(w.y, h, token, n, y0, dy);
     __syncthreads();
-    if (!STATES) fetch<T>(U, up, w.u, h, token, n, 0, du, du4);
-    fetch<T>(X, up, w.x, h, token, n, 0, du, du4);
-    fetch<T>(Y, kDyPitch, w.y, h, token, n, y0, dy, kDy);
+    if (!STATES) u.store(U, up, du4);
+    x.store(X, up, du4);
+    y.store(Y, kDyPitch, kDy);
     if (!STATES) {
 #pragma unroll
       for (int i = 0; i < 8; ++i)
-        *reinterpret_cast<float4*>(Z + (ty + 16 * i) * kDyPitch + tx * 4) = make_float4(z[i][0], z[i][1], z[i][2], z[i][3]);
+        if (row_of(i) < du4) *reinterpret_cast<float4*>(Z + row_of(i) * kDyPitch + tx * 4) = make_float4(z[i][0], z[i][1], z[i][2], z[i][3]);
     }
     __syncthreads();
     if (!STATES) {
+      const int i0 = ty * 2;
+      float p[2][2] = {};
+#pragma unroll 2
+      for (int c = 0; c < du4; c += 4) {
+        const float4 ua = *reinterpret_cast<const float4*>(U + i0 * up + c), ub = *reinterpret_cast<const float4*>(U + (i0 + 1) * up + c);
+        const float4 xa = *reinterpret_cast<const float4*>(X + tx * up + c), xb = *reinterpret_cast<const float4*>(X + (tx + 16) * up + c);
+        p[0][0] = fmaf(ua.x, xa.x, fmaf(ua.y, xa.y, fmaf(ua.z, xa.z, fmaf(ua.w, xa.w, p[0][0]))));
+        p[0][1] = fmaf(ua.x, xb.x, fmaf(ua.y, xb.y, fmaf(ua.z, xb.z, fmaf(ua.w, xb.w, p[0][1]))));
+        p[1][0] = fmaf(ub.x, xa.x, fmaf(ub.y, xa.y, fmaf(ub.z, xa.z, fmaf(ub.w, xa.w, p[1][0]))));
+        p[1][1] = fmaf(ub.x, xb.x, fmaf(ub.y, xb.y, fmaf(ub.z, xb.z, fmaf(ub.w, xb.w, p[1][1]))));
+      }
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int i = ty * 2 + e / 2, j = tx + 16 * (e % 2);
-        float s = 0.0f;
-        for (int c = 0; c < du4; c += 4) {
-          const float4 u = *reinterpret_cast<const float4*>(U + i * up + c), x = *reinterpret_cast<const float4*>(X + j * up + c);
-          s = fmaf(u.x, x.x, fmaf(u.y, x.y, fmaf(u.z, x.z, fmaf(u.w, x.w, s))));
-        }
-        const int away = w.late ? j - i : i - j;
-        P[i * (kC + 1) + j] = away >= 0 ? s * power[away] * w.w_near : 0.0f;
+        const int i = i0 + e / 2, j = tx + 16 * (e % 2), away = w.late ? j - i : i - j;
+        P[i * kPPitch + j] = away >= 0 ? p[e / 2][e % 2] * power[away] * w.w_near : 0.0f;
       }
       __syncthreads();
+      float far[2][4] = {}, near[2][4] = {};
+#pragma unroll 2
+      for (int c = 0; c < du4; c += 4) {
+        const float4 ua = *reinterpret_cast<const float4*>(U + i0 * up + c), ub = *reinterpret_cast<const float4*>(U + (i0 + 1) * up + c);
+        const float as[4] = {ua.x, ua.y, ua.z, ua.w}, bs[4] = {ub.x, ub.y, ub.z, ub.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float4 s = *reinterpret_cast<const float4*>(Z + (c + e) * kDyPitch + tx * 4);
+          add4(far[0], as[e], s);
+          add4(far[1], bs[e], s);
+        }
+      }
+#pragma unroll 2
+      for (int j = 0; j < n; j += 4) {
+        const float4 pa = *reinterpret_cast<const float4*>(P + i0 * kPPitch + j), pb = *reinterpret_cast<const float4*>(P + (i0 + 1) * kPPitch + j);
+        const float as[4] = {pa.x, pa.y, pa.z, pa.w}, bs[4] = {pb.x, pb.y, pb.z, pb.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float4 v = *reinterpret_cast<const float4*>(Y + (j + e) * kDyPitch + tx * 4);
+          add4(near[0], as[e], v);
+          add4(near[1], bs[e], v);
+        }
+      }
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        const int i = ty * 2 + e;
-        float far[4] = {}, near[4] = {};
-        for (int c = 0; c < du; ++c) {
-          const float u = U[i * up + c];
-          const float4 s = *reinterpret_cast<const float4*>(Z + c * kDyPitch + tx * 4);
-          far[0] = fmaf(u, s.x, far[0]); far[1] = fmaf(u, s.y, far[1]);
-          far[2] = fmaf(u, s.z, far[2]); far[3] = fmaf(u, s.w, far[3]);
-        }
-        for (int j = w.late ? i : 0; j < (w.late ? n : i + 1); ++j) {
-          const float p = P[i * (kC + 1) + j];
-          const float4 y = *reinterpret_cast<const float4*>(Y + j * kDyPitch + tx * 4);
-          near[0] = fmaf(p, y.x, near[0]); near[1] = fmaf(p, y.y, near[1]);
-          near[2] = fmaf(p, y.z, near[2]); near[3] = fmaf(p, y.w, near[3]);
-        }
-        if (i < n) {
-          const float by = power[w.late ? n - 1 - i : i + 1] * w.w_row;
-          T* out = static_cast<T*>(w.out) + (int64_t)(token + i) * w.out_ld + (int64_t)h * w.out_head + y0;
+        const int i = i0 + e;
+        if (i >= n) continue;
+        const float by = power[w.late ? n - 1 - i : i + 1] * w.w_row;
+        T* out = static_cast<T*>(w.out) + (int64_t)(token + i) * w.out_ld + (int64_t)h * w.out_head + y0;
 #pragma unroll
-          for (int c = 0; c < 4; ++c)
-            if (tx * 4 + c < dy) out[tx * 4 + c] = from_float<T>(fmaf(by, far[c], near[c]));
-        }
+        for (int c = 0; c < 4; ++c)
+          if (tx * 4 + c < dy) out[tx * 4 + c] = from_float<T>(fmaf(by, far[e][c], near[e][c]));
       }
     }
+    // the chunk's own sums first: added one by one to a state of many thousand tokens, terms would lose their last bits
     const float keep = power[n];
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-#pragma unroll
-      for (int c = 0; c < 4; ++c) z[i][c] *= keep;
-    for (int j = 0; j < n; ++j) {
-      const float by = power[w.late ? j + 1 : n - 1 - j] * w.w_x;
-      const float4 y = *reinterpret_cast<const float4*>(Y + j * kDyPitch + tx * 4);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int r = ty + 16 * i;
-        if (r < du) {
-          const float x = X[j * up + r] * by;
-          z[i][0] = fmaf(x, y.x, z[i][0]); z[i][1] = fmaf(x, y.y, z[i][1]);
-          z[i][2] = fmaf(x, y.z, z[i][2]); z[i][3] = fmaf(x, y.w, z[i][3]);
-        }
+    for (int k = 0; k < 2; ++k) {
+      if (k * 64 + ty * 4 >= du4) continue;
+      float own[4][4] = {};
+#pragma unroll 2
+      for (int j = 0; j < n; ++j) {
+        const float by = power[w.late ? j + 1 : n - 1 - j] * w.w_x;
+        const float4 v = *reinterpret_cast<const float4*>(Y + j * kDyPitch + tx * 4);
+        const float4 s = *reinterpret_cast<const float4*>(X + j * up + k * 64 + ty * 4);
+        add4(own[0], s.x * by, v);
+        add4(own[1], s.y * by, v);
+        add4(own[2], s.z * by, v);
+        add4(own[3], s.w * by, v);
       }
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) z[k * 4 + i][c] = fmaf(keep, z[k * 4 + i][c], own[i][c]);
     }
   }
   if (w.z_out) {
@@ -134,7 +183,7 @@ __global__ void __launch_bounds__(kThreads) k_walk(const __grid_constant__ WalkA
     for (int i = 0; i < 8; ++i)
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
-        const int r = ty + 16 * i, col = tx * 4 + c;
+        const int r = row_of(i), col = tx * 4 + c;
         if (r < du && col < dy) w.z_out[at + (int64_t)r * w.dy + y0 + col] = z[i][c];
       }
   }
@@ -176,6 +225,43 @@ __global__ void __launch_bounds__(256) k_join(const __grid_constant__ JoinArgs j
     }
   }
   if (j.z_out[which]) j.z_out[which][s * step + (int64_t)h * j.size + e] = state;
+}
+
+// Rows that do not lie on 16 bytes, laid out so that they do, [tokens][heads][dim up to 8], or taken back from there.  A thread moves
+// eight elements.
+struct PackArgs {
+  Heads far[4];
+  uint16_t* near[4];
+  int32_t dim[4], tokens, heads, seqs;
+  const int32_t* seq_start;   // when taken back: rows of no sequence are left as they were
+};
+template <bool BACK>
+__global__ void __launch_bounds__(256) k_pack_heads(const __grid_constant__ PackArgs a) {
+  pdl_enter();
+  const int which = blockIdx.y, groups = (a.dim[which] + 7) / 8;
+  const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x, row = e / groups;
+  if (row >= (int64_t)a.tokens * a.heads) return;
+  const int g = (int)(e - row * groups), h = (int)(row % a.heads);
+  const int64_t token = row / a.heads;
+  uint16_t* far = static_cast<uint16_t*>(const_cast<void*>(a.far[which].p)) + token * a.far[which].ld + h * a.far[which].head + g * 8;
+  uint4* near = reinterpret_cast<uint4*>(a.near[which] + (row * groups + g) * 8);
+  const int left = a.dim[which] - g * 8;
+  uint32_t w[4];
+  if (BACK) {
+    if (a.seq_start && (token < a.seq_start[0] || token >= a.seq_start[a.seqs])) return;
+    const uint4 v = *near;
+    w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < left) far[i] = (uint16_t)(i % 2 ? w[i / 2] >> 16 : w[i / 2]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t lo = 2 * i < left ? far[2 * i] : 0u, hi = 2 * i + 1 < left ? far[2 * i + 1] : 0u;
+      w[i] = lo | hi << 16;
+    }
+    *near = make_uint4(w[0], w[1], w[2], w[3]);
+  }
 }
 
 // ------------------------------------------------------------------ one token
@@ -247,6 +333,31 @@ inline bool bad_sizes(const dgc_attention* d) {
          (!d->seq_start && d->tokens % d->num_seqs != 0) || bad_dims(d->heads, d->key_dim, d->value_dim, d->scale);
 }
 
+// Whether tensor copies can fetch the walks' inputs: rows on 16 bytes.  (Heads that share a tensor do not
+// move along it, tokens that do are taken by the other kernel.)
+inline bool fetched(const Heads& m, int64_t tokens, int64_t heads) {
+  return !misaligned(m.p, 16) && (m.ld > 0 || tokens <= 1) && m.ld % 8 == 0 && (m.head % 8 == 0 || heads == 1);
+}
+inline Heads side(const dgc_heads& m) { return Heads{m.data, m.ld, m.head}; }
+// The tensors that are laid out anew in the workspace (q, k, v, dout; out, or dq, dk, dv), and their bytes.  Worth it from half
+// a chunk on: PACK_FIGURES.
+struct Laid { int64_t bytes; bool anew[8]; };
+inline int dim_of(const dgc_attention* d, int i, bool backward) {
+  return i < 2 || (backward && (i == 4 || i == 5)) ? d->key_dim : d->value_dim;
+}
+inline int64_t laid_bytes(const dgc_attention* d, int dim) { return (d->tokens * d->heads * ((dim + 7) / 8 * 16) + 255) / 256 * 256; }
+Laid laid_out(const dgc_attention* d, bool backward) {
+  Laid l{};
+  if (d->dtype == DGC_F32 || d->tokens < 64 * (int64_t)d->num_seqs) return l;
+  const dgc_heads* all[8] = {&d->q, &d->k, &d->v, &d->dout, backward ? &d->dq : &d->out, &d->dk, &d->dv, nullptr};
+  for (int i = 0; i < (backward ? 7 : 5); ++i) {
+    if (i == 3 && !backward) continue;
+    l.anew[i] = !fetched(side(*all[i]), d->tokens, d->heads);
+    if (l.anew[i]) l.bytes += laid_bytes(d, dim_of(d, i, backward));
+  }
+  return l;
+}
+
 // Tokens of a part, 0: sequences are walked whole.  A part costs reading x and y once more and a state written
 // and read twice, so only calls are cut that would leave SMs idle, and into as few parts as fill them: of one
 // to three parts for each SM the number that ends first.
@@ -283,11 +394,6 @@ int32_t walk(WalkArgs a, int walks, int64_t items, bool states, cudaStream_t s) 
   return check_launch();
 }
 
-// Whether tensor copies can fetch the walks' inputs: rows on 16 bytes.  (Heads that share a tensor do not
-// move along it, tokens that do are taken by the other kernel.)
-inline bool fetched(const Heads& m, int64_t tokens, int64_t heads) {
-  return !misaligned(m.p, 16) && (m.ld > 0 || tokens <= 1) && m.ld % 8 == 0 && (m.head % 8 == 0 || heads == 1);
-}
 bool on_tensor_cores(const WalkArgs& a, int walks, int32_t dtype, bool states) {
   if (dtype == DGC_F32 || a.tokens == 0) return false;
   for (int i = 0; i < walks; ++i) {
@@ -350,7 +456,6 @@ int32_t walk(const WalkArgs& a, int32_t dtype, int walks, int64_t items, bool st
   return walk<__half>(a, walks, items, states, s);
 }
 
-Heads side(const dgc_heads& m) { return Heads{m.data, m.ld, m.head}; }
 
 int32_t attention(const dgc_attention* d, bool backward, void* stream) {
   if (bad_sizes(d)) return DGC_EINVAL;
@@ -367,11 +472,47 @@ int32_t attention(const dgc_attention* d, bool backward, void* stream) {
   if (d->tokens == 0 && !(backward ? d->ds0 : d->s_last)) return DGC_OK;
   cudaStream_t s = as_stream(stream);
   const int32_t part = d->workspace ? part_of_call(d, backward) : 0;
-  if (part && d->workspace_bytes < (backward ? 2 : 1) * states_bytes(d, part)) return DGC_ECAPACITY;
+  const Laid laid = d->workspace ? laid_out(d, backward) : Laid{};
+  const int64_t states = part ? (backward ? 2 : 1) * states_bytes(d, part) : 0;
+  if (d->workspace_bytes < states + laid.bytes) return DGC_ECAPACITY;
   const int64_t items = items_of(d, part);
   if (items * d->heads > INT32_MAX / 2) return DGC_EINVAL;
   const int32_t dk = d->key_dim, dv = d->value_dim;
   const float c = d->scale;
+  // q, k, v, dout, and out or dq, dk, dv
+  Heads t[7] = {side(d->q), side(d->k), side(d->v), side(d->dout), side(backward ? d->dq : d->out), side(d->dk), side(d->dv)};
+  const Heads &q = t[0], &k = t[1], &v = t[2], &dout = t[3];
+  PackArgs in{}, back{};
+  int ins = 0, backs = 0;
+  in.tokens = back.tokens = (int32_t)d->tokens;
+  in.heads = back.heads = d->heads;
+  back.seqs = d->num_seqs;
+  back.seq_start = d->seq_start;
+  char* to = static_cast<char*>(d->workspace) + states;
+  for (int i = 0; i < 7; ++i) {
+    if (!laid.anew[i]) continue;
+    const int dim = dim_of(d, i, backward), dim8 = (dim + 7) / 8 * 8;
+    PackArgs& p = i < 4 ? in : back;
+    int& n = i < 4 ? ins : backs;
+    p.far[n] = t[i];
+    p.near[n] = reinterpret_cast<uint16_t*>(to);
+    p.dim[n++] = dim;
+    t[i] = Heads{to, (int64_t)d->heads * dim8, dim8};
+    to += laid_bytes(d, dim);
+  }
+  const int64_t blocks = (d->tokens * d->heads * ((std::max(dk, dv) + 7) / 8) + 255) / 256;
+  if ((ins || backs) && blocks > INT32_MAX) return DGC_EINVAL;
+  if (ins) {
+    launch(k_pack_heads<false>, dim3((unsigned)blocks, ins), 256, 0, s, in);
+    const int32_t rc = check_launch();
+    if (rc != DGC_OK) return rc;
+  }
+  const auto finish = [&](int32_t rc) {
+    if (rc != DGC_OK || !backs) return rc;
+    launch(k_pack_heads<true>, dim3((unsigned)blocks, backs), 256, 0, s, back);
+    return check_launch();
+  };
+  const auto at = [](const Heads& m) { return const_cast<void*>(m.p); };
   WalkArgs a{};
   a.decay = d->decay; a.seq_start = d->seq_start; a.tokens = (int32_t)d->tokens; a.seqs = d->num_seqs;
   a.seq_len = (int32_t)(d->tokens / d->num_seqs); a.heads = d->heads; a.part = part;
@@ -380,8 +521,8 @@ int32_t attention(const dgc_attention* d, bool backward, void* stream) {
   float* const late = early + (part ? states_bytes(d, part) / 4 : 0);
   if (part) {   // the parts' shares of the states, and the states before the parts
     WalkArgs st = a;
-    st.w[0] = Walk{{}, side(d->k), side(d->v), nullptr, 0, 0, nullptr, early, dk, dv, 0, 0, 0.0f, 0.0f, 1.0f};
-    if (backward) st.w[1] = Walk{{}, side(d->q), side(d->dout), nullptr, 0, 0, nullptr, late, dk, dv, 1, 0, 0.0f, 0.0f, c};
+    st.w[0] = Walk{{}, k, v, nullptr, 0, 0, nullptr, early, dk, dv, 0, 0, 0.0f, 0.0f, 1.0f};
+    if (backward) st.w[1] = Walk{{}, q, dout, nullptr, 0, 0, nullptr, late, dk, dv, 1, 0, 0.0f, 0.0f, c};
     int32_t rc = walk(st, d->dtype, backward ? 2 : 1, items, true, s);
     if (rc != DGC_OK) return rc;
     JoinArgs j{a, {early, late}, {d->s0, d->ds_last}, {backward ? nullptr : d->s_last, d->ds0}, {0, 1}, dk * dv};
@@ -392,13 +533,13 @@ int32_t attention(const dgc_attention* d, bool backward, void* stream) {
   const float* const s_in = part ? early : d->s0;
   const float* const e_in = part ? late : d->ds_last;
   if (!backward) {
-    a.w[0] = Walk{side(d->q), side(d->k), side(d->v), d->out.data, d->out.ld, d->out.head, s_in, part ? nullptr : d->s_last, dk, dv, 0, 0, c, c, 1.0f};
-    return walk(a, d->dtype, 1, items, false, s);
+    a.w[0] = Walk{q, k, v, at(t[4]), t[4].ld, t[4].head, s_in, part ? nullptr : d->s_last, dk, dv, 0, 0, c, c, 1.0f};
+    return finish(walk(a, d->dtype, 1, items, false, s));
   }
-  a.w[0] = Walk{side(d->dout), side(d->v), side(d->k), d->dq.data, d->dq.ld, d->dq.head, s_in, nullptr, dv, dk, 0, 1, c, c, 1.0f};
-  a.w[1] = Walk{side(d->k), side(d->q), side(d->dout), d->dv.data, d->dv.ld, d->dv.head, e_in, part ? nullptr : d->ds0, dk, dv, 1, 0, 1.0f, c, c};
-  a.w[2] = Walk{side(d->v), side(d->dout), side(d->q), d->dk.data, d->dk.ld, d->dk.head, e_in, nullptr, dv, dk, 1, 1, 1.0f, c, c};
-  return walk(a, d->dtype, 3, items, false, s);
+  a.w[0] = Walk{dout, v, k, at(t[4]), t[4].ld, t[4].head, s_in, nullptr, dv, dk, 0, 1, c, c, 1.0f};
+  a.w[1] = Walk{k, q, dout, at(t[6]), t[6].ld, t[6].head, e_in, part ? nullptr : d->ds0, dk, dv, 1, 0, 1.0f, c, c};
+  a.w[2] = Walk{v, dout, q, at(t[5]), t[5].ld, t[5].head, e_in, nullptr, dv, dk, 1, 1, 1.0f, c, c};
+  return finish(walk(a, d->dtype, 3, items, false, s));
 }
 
 }  // namespace
@@ -413,7 +554,7 @@ int32_t dgc_decay_attention_backward(const dgc_attention* a, void* stream) { ret
 int64_t dgc_decay_attention_workspace_bytes(const dgc_attention* a, int32_t backward) {
   if (bad_sizes(a)) return DGC_EINVAL;
   const int32_t part = part_of_call(a, backward != 0);
-  return part ? (backward ? 2 : 1) * states_bytes(a, part) : 0;
+  return (part ? (backward ? 2 : 1) * states_bytes(a, part) : 0) + laid_out(a, backward != 0).bytes;
 }
 
 int32_t dgc_decay_attention_step(const dgc_attention_one* d, void* stream) {
