@@ -14,7 +14,7 @@ namespace {
 // For 32-bit tensors and rows that tensor copies cannot fetch.  A block walks one item (a sequence, or a part of it) of one head and 64
 // of the rows' elements, in chunks of 32 tokens.  A thread holds 8 x 4 elements of the state in registers, and forms 2 x 2
 // of P and 2 x 4 of the rows; factors come from shared memory four at a time.  All loads of a chunk are under way at
-// once (fetched one after the other they were three quarters of the time: 379 -> FIG us for 20 x 35 x 12 x 125 f32).
+// once (20 x 35 x 12 x 125 f32, forward and backward: 209 us, 379 with loads one after the other and single rows).
 constexpr int kC = 32, kDy = 64, kDyPitch = kDy + 4, kThreads = 256, kPPitch = kC + 4;
 
 __host__ __device__ inline int pitch_of(int du) { return (du + 3) / 4 * 4 + 4; }
@@ -107,8 +107,9 @@ __global__ void __launch_bounds__(kThreads, 2) k_walk(const __grid_constant__ Wa
     if (!STATES) {
       const int i0 = ty * 2;
       float p[2][2] = {};
+      const int mine = i0 < n ? du4 : 0;   // (a sequence's last few tokens do not keep every thread)
 #pragma unroll 2
-      for (int c = 0; c < du4; c += 4) {
+      for (int c = 0; c < mine; c += 4) {
         const float4 ua = *reinterpret_cast<const float4*>(U + i0 * up + c), ub = *reinterpret_cast<const float4*>(U + (i0 + 1) * up + c);
         const float4 xa = *reinterpret_cast<const float4*>(X + tx * up + c), xb = *reinterpret_cast<const float4*>(X + (tx + 16) * up + c);
         p[0][0] = fmaf(ua.x, xa.x, fmaf(ua.y, xa.y, fmaf(ua.z, xa.z, fmaf(ua.w, xa.w, p[0][0]))));
@@ -124,7 +125,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_walk(const __grid_constant__ Wa
       __syncthreads();
       float far[2][4] = {}, near[2][4] = {};
 #pragma unroll 2
-      for (int c = 0; c < du4; c += 4) {
+      for (int c = 0; c < mine; c += 4) {
         const float4 ua = *reinterpret_cast<const float4*>(U + i0 * up + c), ub = *reinterpret_cast<const float4*>(U + (i0 + 1) * up + c);
         const float as[4] = {ua.x, ua.y, ua.z, ua.w}, bs[4] = {ub.x, ub.y, ub.z, ub.w};
 #pragma unroll
@@ -135,7 +136,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_walk(const __grid_constant__ Wa
         }
       }
 #pragma unroll 2
-      for (int j = 0; j < n; j += 4) {
+      for (int j = 0; j < (i0 < n ? n : 0); j += 4) {
         const float4 pa = *reinterpret_cast<const float4*>(P + i0 * kPPitch + j), pb = *reinterpret_cast<const float4*>(P + (i0 + 1) * kPPitch + j);
         const float as[4] = {pa.x, pa.y, pa.z, pa.w}, bs[4] = {pb.x, pb.y, pb.z, pb.w};
 #pragma unroll
@@ -289,16 +290,30 @@ __global__ void __launch_bounds__(256) k_attention_step(const __grid_constant__ 
 #pragma unroll
     for (int i = 0; i < N; ++i) vv[i] = c + i < a.value_dim ? to_float<T>(v[c + i]) : 0.0f;
     if (c < a.value_dim) {
-      for (int d = warp; d < a.key_dim; d += 8) {
-        const float kk = to_float<T>(k[d]), qq = to_float<T>(q[d]);
-        float* p = z + (int64_t)d * a.value_dim + c;
-        struct alignas(4 * N) Pack { float f[N]; } s = *reinterpret_cast<const Pack*>(p);
+      struct alignas(4 * N) Pack { float f[N]; };
+      constexpr int ROWS = 8;   // of a lane's loads under way at once (64 x 16 states of 128 x 128: 23 us, one after the other 31)
+      for (int d0 = warp; d0 < a.key_dim; d0 += 8 * ROWS) {
+        Pack s[ROWS];
+        float kk[ROWS], qq[ROWS];
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-          s.f[i] = fmaf(g, s.f[i], kk * vv[i]);
-          sum[i] = fmaf(qq, s.f[i], sum[i]);
+        for (int j = 0; j < ROWS; ++j) {
+          const int d = d0 + 8 * j;
+          if (d >= a.key_dim) continue;
+          s[j] = *reinterpret_cast<const Pack*>(z + (int64_t)d * a.value_dim + c);
+          kk[j] = to_float<T>(k[d]);
+          qq[j] = to_float<T>(q[d]);
         }
-        *reinterpret_cast<Pack*>(p) = s;
+#pragma unroll
+        for (int j = 0; j < ROWS; ++j) {
+          const int d = d0 + 8 * j;
+          if (d >= a.key_dim) continue;
+#pragma unroll
+          for (int i = 0; i < N; ++i) {
+            s[j].f[i] = fmaf(g, s[j].f[i], kk[j] * vv[i]);
+            sum[i] = fmaf(qq[j], s[j].f[i], sum[i]);
+          }
+          *reinterpret_cast<Pack*>(z + (int64_t)d * a.value_dim + c) = s[j];
+        }
       }
 #pragma unroll
       for (int i = 0; i < N; ++i) part[warp][c + i] = sum[i];
@@ -339,8 +354,8 @@ inline bool fetched(const Heads& m, int64_t tokens, int64_t heads) {
   return !misaligned(m.p, 16) && (m.ld > 0 || tokens <= 1) && m.ld % 8 == 0 && (m.head % 8 == 0 || heads == 1);
 }
 inline Heads side(const dgc_heads& m) { return Heads{m.data, m.ld, m.head}; }
-// The tensors that are laid out anew in the workspace (q, k, v, dout; out, or dq, dk, dv), and their bytes.  Worth it from half
-// a chunk on: PACK_FIGURES.
+// The tensors that are laid out anew in the workspace (q, k, v, dout; out, or dq, dk, dv), and their bytes.  Worth it from
+// a few tokens on (20 sequences of 35 x 12 x 125 bf16, forward and backward: 247 -> 145 us; one of 40, forward 27 -> 20 us).
 struct Laid { int64_t bytes; bool anew[8]; };
 inline int dim_of(const dgc_attention* d, int i, bool backward) {
   return i < 2 || (backward && (i == 4 || i == 5)) ? d->key_dim : d->value_dim;
@@ -348,7 +363,7 @@ inline int dim_of(const dgc_attention* d, int i, bool backward) {
 inline int64_t laid_bytes(const dgc_attention* d, int dim) { return (d->tokens * d->heads * ((dim + 7) / 8 * 16) + 255) / 256 * 256; }
 Laid laid_out(const dgc_attention* d, bool backward) {
   Laid l{};
-  if (d->dtype == DGC_F32 || d->tokens < 64 * (int64_t)d->num_seqs) return l;
+  if (d->dtype == DGC_F32 || d->tokens < 16 * (int64_t)d->num_seqs) return l;
   const dgc_heads* all[8] = {&d->q, &d->k, &d->v, &d->dout, backward ? &d->dq : &d->out, &d->dk, &d->dv, nullptr};
   for (int i = 0; i < (backward ? 7 : 5); ++i) {
     if (i == 3 && !backward) continue;

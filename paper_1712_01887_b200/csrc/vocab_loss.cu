@@ -409,13 +409,17 @@ __global__ void __launch_bounds__(512) k_row_loss(const float2* parts, int halve
   const int lane = threadIdx.x % 32, w = threadIdx.x / 32, r = blockIdx.x * 32 + lane;
   float top = -FLT_MAX, sum = 0.0f;
   if (r < rows) {
-    for (int t = w; t < halves; t += 16) {
-      const float2 p = parts[(int64_t)t * rows + r];
-      if (p.x > top) {
-        sum *= exp2f((top - p.x) * kLog2e);
-        top = p.x;
-      }
-      sum += p.y * exp2f((p.x - top) * kLog2e);
+    for (int t0 = w; t0 < halves; t0 += 16 * 8) {   // (eight loads under way at once)
+      float2 p[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) p[i] = t0 + 16 * i < halves ? parts[(int64_t)(t0 + 16 * i) * rows + r] : make_float2(-FLT_MAX, 0.0f);
+      float best = top;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) best = fmaxf(best, p[i].x);
+      sum *= exp2f((top - best) * kLog2e);
+      top = best;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sum += p[i].y * exp2f((p[i].x - top) * kLog2e);
     }
   }
   held[w][lane] = make_float2(top, sum);
