@@ -640,8 +640,9 @@ typedef struct dgc_vocab_loss {
 } dgc_vocab_loss;
 
 /* Bytes of workspace that dgc_vocab_loss_forward (gradient = 0) or the other two (gradient != 0) need for this
- * struct's dtype, sizes, matrices and bias.  Host only.  Bounded in rows x vocab: a gradient is formed in
- * pieces of the vocabulary. */
+ * struct's dtype, sizes and matrices.  Host only.  A gradient is formed in pieces of the vocabulary of at most 128 MB
+ * (or 256 words); the forward pass keeps 8 bytes for 128 logits (64 in DGC_F32); copies of h, and of weight where it is
+ * DGC_F32 (6 bytes an element) or its rows do not lie on 16 bytes, come to that. */
 int64_t dgc_vocab_loss_workspace_bytes(const dgc_vocab_loss* d, int32_t gradient);
 
 /* Writes loss, and stats if given. */

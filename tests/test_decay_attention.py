@@ -348,6 +348,37 @@ def test_a_captured_call_follows_its_inputs():
             assert torch.equal(a, b)
 
 
+@pytest.mark.gpu
+def test_offsets_beyond_32_bits():
+    """A cache of states and rows that lie further than 2^31 elements on."""
+    B = _bind()
+    H, d = 32, 128
+    slots = 2 ** 31 // (H * d * d) + 3
+    cache = torch.empty(slots, H, d, d, device="cuda")
+    q, k, v = (torch.randn(2, H, d, device="cuda") for _ in range(3))
+    at, out, g = torch.tensor([slots - 1, 1], dtype=torch.int32, device="cuda"), torch.empty(2, H, d, device="cuda"), torch.ones(H, device="cuda")
+    few = torch.randn(2, H, d, d, device="cuda")
+    cache[at.long()] = few
+    B.decay_attention_step(q, k, v, cache, out, g, slots=at)
+    same, ref = few.clone(), torch.empty_like(out)
+    B.decay_attention_step(q, k, v, same, ref, g)
+    assert torch.equal(out, ref) and torch.equal(cache[at.long()], same)
+    del cache
+    N, ld = 70000, 32768                                   # 2^31 elements are passed at token 65536
+    for dt, dim in ((torch.bfloat16, 64), (torch.bfloat16, 63), (torch.float32, 32)):
+        wide = torch.empty(N, ld, dtype=dt, device="cuda")
+        parts = [wide[:, i * 64:i * 64 + dim].unflatten(1, (1, dim)) for i in range(4)]
+        small = [torch.randn(N, 1, dim, device="cuda").to(dt) for _ in range(3)]
+        for p, s in zip(parts, small):
+            p.copy_(s)
+        decay, ref = torch.full((1,), 0.9, device="cuda"), torch.empty_like(small[2])
+        starts = torch.tensor([0, 65000, N], dtype=torch.int32, device="cuda")
+        B.decay_attention_forward(*parts, decay, seq_start=starts, num_seqs=2)
+        B.decay_attention_forward(*small, ref, decay, seq_start=starts, num_seqs=2)
+        assert torch.equal(parts[3].reshape(ref.shape), ref)
+        del wide, parts
+
+
 # ----------------------------------------------------------------- refusals, device and stream
 
 def _packed(B, **change):

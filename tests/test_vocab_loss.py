@@ -204,6 +204,28 @@ def test_small_weights_of_rows(dt):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dt", DT, ids=str)
+def test_offsets_beyond_32_bits(dt):
+    """An output matrix and its gradient whose rows lie further than 2^31 elements on."""
+    B = _bind()
+    V, D, ld = 70000, 64, 32768
+    h, w, b, y, d = _inputs(20, V, D, dt, True)
+    wide = torch.empty(V, ld, dtype=dt, device="cuda")
+    far, dfar = wide[:, :D], wide[:, 1024:1024 + D]
+    far.copy_(w)
+    ref = _run(B, h, w, b, y, d, dt)[1]
+    loss, dh, db = torch.empty(20, device="cuda"), torch.empty_like(h), torch.empty_like(b)
+    B.vocab_loss_grad(h, far, y, d, loss, dh, dfar, bias=b, dbias=db)
+    for got, want in zip((loss, dh, dfar, db), ref):
+        assert torch.equal(got, want)
+
+
+@pytest.mark.gpu
+def test_waits_do_not_run_out():
+    _bind().tensor_check()
+
+
+@pytest.mark.gpu
 def test_no_rows():
     B = _bind()
     for dt in DT:
