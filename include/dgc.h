@@ -587,7 +587,8 @@ int64_t dgc_decay_attention_workspace_bytes(const dgc_attention* a, int32_t back
 /* Writes out and s_last.  Results do not vary from run to run; nothing of one sequence reaches
  * another; rows outside every sequence are not written.  In a 16-bit call the weights decay^n q.k and the
  * states are rounded to the type where they enter a product (in DGC_F16 they are to stay within
- * its range, 65504); sums, and the states from chunk to chunk, are in 32 bits. */
+ * its range, 65504); sums, and the states from chunk to chunk, are in 32 bits.  (In DGC_F16 a term of a
+ * state, k times its decay, is held to 2^-25 at the least.) */
 int32_t dgc_decay_attention_forward(const dgc_attention* a, void* stream);
 
 /* The gradients.  With E_t what reaches S_t from later tokens (ds_last at the last one) and dS_t =
