@@ -211,12 +211,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
       const bool there = row < g.m;
       // what the row needs beside its sums
       float top = -FLT_MAX, sum = 0.0f, coef = 0.0f, weight = 0.0f;
-      uint32_t y = 0xC0000000u;   // the label's column; of padding rows none
+      bool labelled = false;
+      uint32_t y = 0xC0000000u;   // the label's column (a label in another piece has one outside this); of padding rows none
       if (MODE <= kGrad && there) {
         const int label = g.labels[row];
-        if (label >= 0 && label < g.vocab) y = (uint32_t)(label - g.n0);
+        labelled = label >= 0 && label < g.vocab;
+        if (labelled) y = (uint32_t)(label - g.n0);
       }
-      if (MODE == kGrad && y != 0xC0000000u) {
+      if (MODE == kGrad && labelled) {
         top = g.stats[2 * (int64_t)row];
         sum = g.stats[2 * (int64_t)row + 1];
         weight = g.dloss[row] * factor;
