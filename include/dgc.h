@@ -575,8 +575,8 @@ typedef struct dgc_attention {
   /* both */
   void*          workspace;    /* device scratch of dgc_decay_attention_workspace_bytes() bytes, 16-byte
                                   aligned, or NULL.  With it a few long sequences are worked on in parts,
-                                  side by side, and 16-bit rows that do not lie on 16 bytes are laid
-                                  out anew                                                         */
+                                  side by side, 16-bit rows that do not lie on 16 bytes are laid out
+                                  anew, and DGC_F16 gradients are formed on the tensor cores       */
   int64_t        workspace_bytes;
 } dgc_attention;
 
@@ -585,16 +585,19 @@ typedef struct dgc_attention {
 int64_t dgc_decay_attention_workspace_bytes(const dgc_attention* a, int32_t backward);
 
 /* Writes out and s_last.  Results do not vary from run to run; nothing of one sequence reaches
- * another; rows outside every sequence are not written.  In a 16-bit call the weights decay^n q.k and the
- * states are rounded to the type where they enter a product (in DGC_F16 they are to stay within
- * its range, 65504); sums, and the states from chunk to chunk, are in 32 bits.  (In DGC_F16 a term of a
- * state, k times its decay, is held to 2^-25 at the least.) */
+ * another; rows outside every sequence are not written.  In a 16-bit call the weights scale decay^n q.k
+ * and the states are rounded to the type where they enter a product (in DGC_F16 they are to stay within
+ * its range, 65504; of a scale outside 2^-12 .. 2^15 only what the nearest of these would do counts);
+ * sums, and the states from chunk to chunk, are in 32 bits.  (In DGC_F16 a term of a state, k times its
+ * decay, is held to 2^-25 at the least.) */
 int32_t dgc_decay_attention_forward(const dgc_attention* a, void* stream);
 
 /* The gradients.  With E_t what reaches S_t from later tokens (ds_last at the last one) and dS_t =
  * E_t + scale q_t dout_t^T:
  *   dq_t = scale S_t dout_t ;  dk_t = dS_t v_t ;  dv_t = dS_t^T k_t ;  E_{t-1} = decay dS_t ;  ds0 = E before the first
- * S is formed again: out and s_last are not used. */
+ * S is formed again: out and s_last are not used.  Roundings are the forward call's, of S, E, scale decay^n q.k and
+ * scale decay^n dout.v.  In DGC_F16 neither E nor what dout makes small is bound to the type's range: dout.v is
+ * held to 2^-22 value_dim times the largest finite |dout| of the sequence's head, at the least. */
 int32_t dgc_decay_attention_backward(const dgc_attention* a, void* stream);
 
 /* One token for `rows` sequences at once, their states kept in a cache: row r's state is number slots[r]

@@ -265,6 +265,45 @@ __global__ void __launch_bounds__(256) k_pack_heads(const __grid_constant__ Pack
   }
 }
 
+// The exponent of the largest finite |dout| of each token and head, in f16, for rows on 16 bytes.  WIDTH threads share a row, as many as
+// it has pieces of 16 bytes, or more; a thread has a piece of four rows.
+template <int WIDTH>
+__global__ void __launch_bounds__(256) k_exponents(const Heads dout, int dim, int32_t tokens, uint8_t* tops) {
+  pdl_enter();
+  constexpr int STEP = 256 / WIDTH, ROWS = 4;
+  const int c = threadIdx.x % WIDTH * 8, left = dim - c, h = blockIdx.y;
+  const int64_t first = (int64_t)blockIdx.x * (STEP * ROWS) + threadIdx.x / WIDTH;
+  const uint16_t* p = static_cast<const uint16_t*>(dout.p) + first * dout.ld + (int64_t)h * dout.head + c;
+  uint32_t w[ROWS][4] = {};
+#pragma unroll
+  for (int i = 0; i < ROWS; ++i, p += STEP * dout.ld) {
+    if (first + i * STEP >= tokens) continue;
+    if (left >= 8) {
+      const uint4 v = *reinterpret_cast<const uint4*>(p);
+      w[i][0] = v.x; w[i][1] = v.y; w[i][2] = v.z; w[i][3] = v.w;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 7; ++e)
+        if (e < left) w[i][e / 2] |= (uint32_t)p[e] << (e % 2 * 16);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < ROWS; ++i) {
+    // (without the sign the bits are in the order of the numbers; those of an infinity or a NaN are above all others)
+    const auto most = [&](auto&& of) { return __vmaxu2(__vmaxu2(of(w[i][0]), of(w[i][1])), __vmaxu2(of(w[i][2]), of(w[i][3]))); };
+    uint32_t two = most([](uint32_t v) { return v & 0x7FFF7FFFu; });
+    if (max(two >> 16, two & 0xFFFFu) >= 0x7C00u)
+      two = most([](uint32_t v) {
+        v &= 0x7FFF7FFFu;
+        return ((v & 0x7C000000u) == 0x7C000000u ? 0u : v & 0xFFFF0000u) | ((v & 0x7C00u) == 0x7C00u ? 0u : v & 0xFFFFu);
+      });
+#pragma unroll
+    for (int d = WIDTH / 2; d; d /= 2) two = __vmaxu2(two, __shfl_xor_sync(0xFFFFFFFFu, two, d));
+    const int64_t row = first + i * STEP;
+    if (threadIdx.x % WIDTH == 0 && row < tokens) tops[(int64_t)h * tokens + row] = (uint8_t)max(max(two >> 16, two & 0xFFFFu) >> 10, 1u);
+  }
+}
+
 // ------------------------------------------------------------------ one token
 // A block advances one state: warps take its rows in turn, a lane four (or one) of their elements.
 template <class T, int N>
@@ -393,6 +432,10 @@ inline int64_t items_of(const dgc_attention* d, int32_t part) { return part ? d-
 inline int64_t states_bytes(const dgc_attention* d, int32_t part) {
   return (items_of(d, part) * d->heads * d->key_dim * d->value_dim * 4 + 255) / 256 * 256;
 }
+// The exponents of dout, which the tensor cores' walk goes by in f16.
+inline int64_t tops_bytes(const dgc_attention* d, bool backward) {
+  return backward && d->dtype == DGC_F16 && d->tokens > 0 ? (d->tokens * d->heads + 255) / 256 * 256 : 0;
+}
 
 template <class T>
 int32_t walk(WalkArgs a, int walks, int64_t items, bool states, cudaStream_t s) {
@@ -414,6 +457,7 @@ bool on_tensor_cores(const WalkArgs& a, int walks, int32_t dtype, bool states) {
   if (dtype == DGC_F32 || a.tokens == 0) return false;
   for (int i = 0; i < walks; ++i) {
     const Walk& w = a.w[i];
+    if (dtype == DGC_F16 && w.dout && !a.dout_tops) return false;
     if ((!states && !fetched(w.u, a.tokens, a.heads)) || !fetched(w.x, a.tokens, a.heads) || !fetched(w.y, a.tokens, a.heads)) return false;
   }
   return true;
@@ -490,7 +534,8 @@ int32_t attention(const dgc_attention* d, bool backward, void* stream) {
   const int32_t part = d->workspace ? part_of_call(d, backward) : 0;
   const Laid laid = d->workspace ? laid_out(d, backward) : Laid{};
   const int64_t states = part ? (backward ? 2 : 1) * states_bytes(d, part) : 0;
-  if (d->workspace_bytes < states + laid.bytes) return DGC_ECAPACITY;
+  const int64_t tops = d->workspace ? tops_bytes(d, backward) : 0;
+  if (d->workspace_bytes < states + tops + laid.bytes) return DGC_ECAPACITY;
   const int64_t items = items_of(d, part);
   if (items * d->heads > INT32_MAX / 2) return DGC_EINVAL;
   const int32_t dk = d->key_dim, dv = d->value_dim;
@@ -504,7 +549,7 @@ int32_t attention(const dgc_attention* d, bool backward, void* stream) {
   in.heads = back.heads = d->heads;
   back.seqs = d->num_seqs;
   back.seq_start = d->seq_start;
-  char* to = static_cast<char*>(d->workspace) + states;
+  char* to = static_cast<char*>(d->workspace) + states + tops;
   for (int i = 0; i < 7; ++i) {
     if (!laid.anew[i]) continue;
     const int dim = dim_of(d, i, backward), dim8 = (dim + 7) / 8 * 8;
@@ -535,10 +580,22 @@ int32_t attention(const dgc_attention* d, bool backward, void* stream) {
   a.longest_first = !part && d->seq_start && d->num_seqs > 1 && d->num_seqs <= kSorted && (int64_t)d->num_seqs * d->heads > kSms;
   float* const early = static_cast<float*>(d->workspace);
   float* const late = early + (part ? states_bytes(d, part) / 4 : 0);
+  if (tops) {
+    uint8_t* const to = static_cast<uint8_t*>(d->workspace) + states;
+    a.dout_tops = to;
+    if (fetched(dout, d->tokens, d->heads)) {   // (others are walked in 32 bits)
+      const int rows = dv <= 64 ? 128 : 64;   // of a block
+      const dim3 grid((unsigned)((d->tokens + rows - 1) / rows), (unsigned)d->heads);
+      if (dv <= 64) launch(k_exponents<8>, grid, 256, 0, s, dout, dv, a.tokens, to);
+      else launch(k_exponents<16>, grid, 256, 0, s, dout, dv, a.tokens, to);
+      const int32_t rc = check_launch();
+      if (rc != DGC_OK) return rc;
+    }
+  }
   if (part) {   // the parts' shares of the states, and the states before the parts
     WalkArgs st = a;
-    st.w[0] = Walk{{}, k, v, nullptr, 0, 0, nullptr, early, dk, dv, 0, 0, 0.0f, 0.0f, 1.0f};
-    if (backward) st.w[1] = Walk{{}, q, dout, nullptr, 0, 0, nullptr, late, dk, dv, 1, 0, 0.0f, 0.0f, c};
+    st.w[0] = Walk{{}, k, v, nullptr, 0, 0, nullptr, early, dk, dv, 0, 0, 0.0f, 0.0f, 1.0f, 0};
+    if (backward) st.w[1] = Walk{{}, q, dout, nullptr, 0, 0, nullptr, late, dk, dv, 1, 0, 0.0f, 0.0f, c, 0};
     int32_t rc = walk(st, d->dtype, backward ? 2 : 1, items, true, s);
     if (rc != DGC_OK) return rc;
     JoinArgs j{a, {early, late}, {d->s0, d->ds_last}, {backward ? nullptr : d->s_last, d->ds0}, {0, 1}, dk * dv};
@@ -549,12 +606,12 @@ int32_t attention(const dgc_attention* d, bool backward, void* stream) {
   const float* const s_in = part ? early : d->s0;
   const float* const e_in = part ? late : d->ds_last;
   if (!backward) {
-    a.w[0] = Walk{q, k, v, at(t[4]), t[4].ld, t[4].head, s_in, part ? nullptr : d->s_last, dk, dv, 0, 0, c, c, 1.0f};
+    a.w[0] = Walk{q, k, v, at(t[4]), t[4].ld, t[4].head, s_in, part ? nullptr : d->s_last, dk, dv, 0, 0, c, c, 1.0f, 0};
     return finish(walk(a, d->dtype, 1, items, false, s));
   }
-  a.w[0] = Walk{dout, v, k, at(t[4]), t[4].ld, t[4].head, s_in, nullptr, dv, dk, 0, 1, c, c, 1.0f};
-  a.w[1] = Walk{k, q, dout, at(t[6]), t[6].ld, t[6].head, e_in, part ? nullptr : d->ds0, dk, dv, 1, 0, 1.0f, c, c};
-  a.w[2] = Walk{v, dout, q, at(t[5]), t[5].ld, t[5].head, e_in, nullptr, dv, dk, 1, 1, 1.0f, c, c};
+  a.w[0] = Walk{dout, v, k, at(t[4]), t[4].ld, t[4].head, s_in, nullptr, dv, dk, 0, 1, c, c, 1.0f, 1};
+  a.w[1] = Walk{k, q, dout, at(t[6]), t[6].ld, t[6].head, e_in, part ? nullptr : d->ds0, dk, dv, 1, 0, 1.0f, c, c, 0};
+  a.w[2] = Walk{v, dout, q, at(t[5]), t[5].ld, t[5].head, e_in, nullptr, dv, dk, 1, 1, 1.0f, c, c, 2};
   return finish(walk(a, d->dtype, 3, items, false, s));
 }
 
@@ -570,7 +627,8 @@ int32_t dgc_decay_attention_backward(const dgc_attention* a, void* stream) { ret
 int64_t dgc_decay_attention_workspace_bytes(const dgc_attention* a, int32_t backward) {
   if (bad_sizes(a)) return DGC_EINVAL;
   const int32_t part = part_of_call(a, backward != 0);
-  return (part ? (backward ? 2 : 1) * states_bytes(a, part) : 0) + laid_out(a, backward != 0).bytes;
+  return (part ? (backward ? 2 : 1) * states_bytes(a, part) : 0) + tops_bytes(a, backward != 0) +
+         laid_out(a, backward != 0).bytes;
 }
 
 int32_t dgc_decay_attention_step(const dgc_attention_one* d, void* stream) {

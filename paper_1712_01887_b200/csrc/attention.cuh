@@ -32,6 +32,7 @@ struct Walk {
   int32_t du, dy;        // lengths of u (and x) and of y (and the rows)
   int32_t late, turned;  // turned: z_in is kept as [dy][du], else [du][dy]
   float w_row, w_near, w_x;   // factors of Z^T u, of the sum over the chunk, of x on its way to Z
+  int32_t dout;               // 1: u is the gradient of the output, 2: x is
 };
 
 constexpr int kMaxWalks = 3;
@@ -42,6 +43,7 @@ struct WalkArgs {
   int32_t tokens, seqs, seq_len, heads;
   int32_t part;          // tokens of a part (a multiple of 128), or 0: whole sequences
   int32_t slices;        // blocks that share the rows' dy
+  const uint8_t* dout_tops;   // [heads][tokens], in DGC_F16: the biased exponent of the largest finite |dout|, 1 at the least; NULL: not known
   int32_t longest_first; // whole sequences, taken in the order of their lengths
 };
 

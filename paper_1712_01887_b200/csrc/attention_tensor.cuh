@@ -18,9 +18,17 @@
 //   three parts:  hi1, s = round(lo1 + hi2), round(x w3 + (what s has lost + lo2))     with hi2 + lo2 = x w2
 // which is a third of the instructions that 32-bit products take, taken apart by conversions.  The third part takes the
 // place of X, whose product has then been formed.
+// f16 has a narrow range.  There a factor (the scale) enters an operand by its significand and a power of two, the rest of it
+// the sums, in 32 bits.  And gradients may be far below 1 (a mean loss's are some 1e-5), so that what is as small as they
+// are is raised: P and X by a power of two that goes by the largest |dout| of the block's item, which a small kernel has
+// looked for, and the gradient's state, as the product takes it, by its own largest element.  (32 sequences of 25000 x 16 x 64,
+// backward: 219 -> 259 us, of which the small kernel 12, its results' reading 7, the state's largest 10.  With the largest of
+// each chunk's X and U, from their tiles, instead: 278 us, and 103 where 88 are taken forward.)
 // The state's sums over a chunk are the tensor core's, over the chunks they are the registers': a tensor core cuts off
 // where an addition would round, which over 16 steps does not show and over a long sequence would.
 #pragma once
+
+#include <cfloat>
 
 #include "attention.cuh"
 #include "tensor.cuh"
@@ -48,6 +56,9 @@ template <int D, bool STATES> struct Layout {
 __device__ __forceinline__ void store_shared(uint32_t at, const uint32_t (&w)[4]) {
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
 }
+__device__ __forceinline__ void load_shared(uint32_t at, uint32_t (&w)[4]) {
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at));
+}
 
 // 2^x where it stands: kept from chunk to chunk, the values would not fit the registers.
 __device__ __forceinline__ float exp2_here(float x) {
@@ -56,14 +67,43 @@ __device__ __forceinline__ float exp2_here(float x) {
   return y;
 }
 
+__device__ __forceinline__ float power_of_two(int k) { return __uint_as_float((uint32_t)(127 + k) << 23); }   // -126 .. 127
+// 2^to over the power of two in `bits`, a 32-bit number >= 0, and its inverse; both normal numbers.
+struct Raise { float up, down; };
+__device__ __forceinline__ Raise raise_to(int to, uint32_t bits) {
+  const int k = max(min(to + 127 - (int)(bits >> 23), 126), -126);
+  return Raise{power_of_two(k), power_of_two(-k)};
+}
+// A factor w of an operand as it enters the product, and what is left of it for the sums, in 32 bits.
+struct Factor { float by, back; };
+__device__ __forceinline__ float kept_finite(float v) { return fminf(fmaxf(v, -FLT_MAX), FLT_MAX); }
+// w's significand, in [1, 2) (less below 2^-126), times 2^up.
+__device__ __forceinline__ float power_in(float w) { return __uint_as_float(max(__float_as_uint(w) & 0x7F800000u, 0x00800000u)); }
+__device__ __forceinline__ Factor factor_of(float w, int up) {
+  return Factor{w / power_in(w) * power_of_two(up), kept_finite(power_in(w) * power_of_two(-up))};
+}
+template <int ID, int THREADS>
+__device__ __forceinline__ void meet() { asm volatile("bar.sync %0, %1;" ::"n"(ID), "n"(THREADS) : "memory"); }
+// The largest |v|, four at a time; a NaN is passed over.
+template <int N>
+__device__ __forceinline__ float largest(const float (&v)[N]) {
+  float top[4] = {};
+#pragma unroll
+  for (int i = 0; i < N; i += 8)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) top[k] = fmaxf(fmaxf(top[k], fabsf(v[i + k])), fabsf(v[i + 4 + k]));
+  return fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+}
+
 template <class T, int D, bool STATES, int PARTS>
 __global__ void __launch_bounds__(Layout<D, STATES>::threads, 1) k_walk_tensor(const __grid_constant__ TensorWalkArgs g) {
+  constexpr bool BF16 = std::is_same_v<T, __nv_bfloat16>, RAISED = !BF16;   // RAISED: powers of two keep the operands in range
   using L = Layout<D, STATES>;
   constexpr int SLOTS = L::slots, SLOT = L::slot_bytes, NB = L::sets, MAKERS = L::makers, BOX = kTokens * 128, PER = STATES ? 2 : 3;
-  constexpr bool BF16 = std::is_same_v<T, __nv_bfloat16>;
   constexpr uint32_t P_AT = 0, NEAR = 128, FAR = 128 + D, DELTA = 128 + 2 * D;
   extern __shared__ char dynamic[];
   __shared__ __align__(8) uint64_t bars[2 * 8 + 12];
+  __shared__ __align__(16) uint32_t z_tops[2][8], warp_tops[L::threads / 32];   // what each warp has seen: of the state (two chunks'), of dout
   __shared__ float power[kTokens + 1];   // g^0 .. g^128
   __shared__ uint32_t tmem_at;
   __shared__ volatile int failed;
@@ -89,12 +129,34 @@ __global__ void __launch_bounds__(Layout<D, STATES>::threads, 1) k_walk_tensor(c
   const Item it = item_of(g.a, item);
   const float lg = log_decay(g.a.decay, h);
   if (tid <= kTokens) power[tid] = exp2f(tid * lg);
+  if (RAISED && w.dout) {   // the exponent of the item's largest dout
+    const uint8_t* from = g.a.dout_tops + (int64_t)h * g.a.tokens + it.first;
+    uint32_t top = 1;
+#pragma unroll 4
+    for (int i = tid; i < it.len; i += L::threads) top = max(top, (uint32_t)from[i]);
+    top = __reduce_max_sync(0xFFFFFFFFu, top);
+    if (lane == 0) warp_tops[warp] = top;
+  }
   fence_before();
   __syncthreads();
   fence_after();
   const uint32_t tmem = tmem_at;
   const int chunks = (it.len + kTokens - 1) / kTokens;
   const bool late = w.late;
+  Factor x_is{w.w_x, 1.0f}, near_is{w.w_near, 1.0f};
+  if constexpr (RAISED) {
+    // without a gradient: X by less than 1, and P by w_near, of a scale within 2^-12 .. 2^15
+    int x_up = fabsf(w.w_x) > power_in(w.w_x) ? -1 : 0, near_up = min(max((int)(__float_as_uint(w.w_near) >> 23 & 255) - 127, -12), 14);
+    if (w.dout) {
+      uint32_t top = 0;
+      for (int i = 0; i < L::threads / 32; ++i) top = max(top, warp_tops[i]);
+      const int e = (int)top - 15;
+      near_up = max(near_up, -2 - e - (32 - __clz(w.du - 1)));   // |P| < du 2^(e + 1) 2^16, and its factor's significand 2
+      if (w.dout == 2) x_up = min(13 - e, 14);                   // X' < 2^15
+    }
+    x_is = factor_of(w.w_x, x_up);
+    near_is = factor_of(w.w_near, near_up);
+  }
   const auto first_of = [&](int c) { return (late ? chunks - 1 - c : c) * kTokens; };
   bool ok = true;
 
@@ -175,7 +237,22 @@ __global__ void __launch_bounds__(Layout<D, STATES>::threads, 1) k_walk_tensor(c
       const int u = half * H + d;
       z[d] = !STATES && w.z_in && r < w.dy && u < w.du ? w.z_in[at + (w.turned ? r * w.du + u : u * w.dy + r)] : 0.0f;
     }
-    const auto show = [&] {   // the state, as the product takes it
+    float z_back = 1.0f;
+    // The state before chunk c, as the product takes it.  (All of these warps come here for every chunk, those that have given
+    // up, too: they meet at a barrier that does not count time.)
+    const auto show = [&](int c) {
+      float up = 1.0f;
+      if (RAISED && late) {   // (the gradient's state is as small as dout is)
+        uint32_t bits = __reduce_max_sync(0xFFFFFFFFu, r < w.dy ? __float_as_uint(largest(z)) : 0u);
+        if (lane == 0) z_tops[c & 1][warp - 2] = bits;
+        meet<2, 256>();
+        const uint4 a = *reinterpret_cast<const uint4*>(z_tops[c & 1]), b = *reinterpret_cast<const uint4*>(z_tops[c & 1] + 4);
+        bits = max(max(max(a.x, a.y), max(a.z, a.w)), max(max(b.x, b.y), max(b.z, b.w)));
+        const Raise raise = raise_to(14, bits);
+        up = raise.up;
+        z_back = raise.down;
+      }
+      if (!ok) return;
       if (r < D) {
 #pragma unroll
         for (int d = 0; d < H; d += 8) {
@@ -183,8 +260,9 @@ __global__ void __launch_bounds__(Layout<D, STATES>::threads, 1) k_walk_tensor(c
           uint32_t p[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const float two[2] = {z[d + 2 * e], z[d + 2 * e + 1]};
-            p[e] = pack<T, 2>(two);
+            Val<2> two{{z[d + 2 * e], z[d + 2 * e + 1]}};
+            if (RAISED) two = mul_(two, fill<2>(up));
+            p[e] = pack<T, 2>(two.v);
           }
           store_shared(zs + u / 64 * (D * 128) + r * 128 + (((u % 64 / 8) ^ (r & 7)) << 4), p);
         }
@@ -193,32 +271,43 @@ __global__ void __launch_bounds__(Layout<D, STATES>::threads, 1) k_walk_tensor(c
       __syncwarp();
       if (lane == 0) arrive(z_ready);
     };
-    if (!STATES && chunks > 0) show();
+    if (!STATES && chunks > 0) show(0);
     for (int c = 0; c < chunks; ++c) {
       const int from = first_of(c), n = min(kTokens, it.len - from);
-      if (!(ok = __all_sync(0xFFFFFFFFu, wait_for(d_full, c & 1, &failed)))) break;
-      fence_after();
-      const float keep = power[n];
+      if (ok) ok = __all_sync(0xFFFFFFFFu, wait_for(d_full, c & 1, &failed));
+      if (ok) {
+        fence_after();
+        const float keep = power[n], back = RAISED && late ? x_is.back * power[1] : x_is.back;
 #pragma unroll
-      for (int b = 0; b < H; b += 16) {
-        uint32_t v[16];
-        tmem_ld16(lanes + DELTA + b, v);
-        tmem_wait_ld();
+        for (int b = 0; b < H; b += 16) {
+          uint32_t v[16];
+          tmem_ld16(lanes + DELTA + b, v);
+          tmem_wait_ld();
 #pragma unroll
-        for (int e = 0; e < 16; ++e) z[b + e] = fmaf(keep, z[b + e], __uint_as_float(v[e]));
+          for (int e = 0; e < 16; e += 2) {
+            Val<2> own{{__uint_as_float(v[e]), __uint_as_float(v[e + 1])}};
+            if (RAISED) own = mul_(own, fill<2>(back));
+            const Val<2> now = fma_(fill<2>(keep), Val<2>{{z[b + e], z[b + e + 1]}}, own);
+            z[b + e] = now.v[0];
+            z[b + e + 1] = now.v[1];
+          }
+        }
+        fence_before();
+        __syncwarp();
+        if (lane == 0) arrive(d_empty);
       }
-      fence_before();
-      __syncwarp();
-      if (lane == 0) arrive(d_empty);
       if (STATES) continue;
+      const float far_back = z_back;
       if (c + 1 < chunks) {
-        if (!(ok = __all_sync(0xFFFFFFFFu, wait_for(z_empty, c & 1, &failed)))) break;
-        show();
+        if (ok) ok = __all_sync(0xFFFFFFFFu, wait_for(z_empty, c & 1, &failed));
+        show(c + 1);
       }
-      if (!(ok = __all_sync(0xFFFFFFFFu, wait_for(o_full, c & 1, &failed)))) break;
+      if (ok) ok = __all_sync(0xFFFFFFFFu, wait_for(o_full, c & 1, &failed));
+      if (!ok) continue;
       fence_after();
       const bool there = r < n;
-      const float by = there ? power[late ? n - 1 - r : r + 1] * w.w_row : 0.0f;
+      float by = there ? power[late ? n - 1 - r : r + 1] * w.w_row : 0.0f;
+      if (RAISED) by = kept_finite(by * far_back);
       T* out = static_cast<T*>(w.out) + (int64_t)(it.first + from + r) * w.out_ld + (int64_t)h * w.out_head + half * H;
 #pragma unroll 1
       for (int b = 0; b < H; b += 16) {
@@ -233,8 +322,9 @@ __global__ void __launch_bounds__(Layout<D, STATES>::threads, 1) k_walk_tensor(c
         }
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const Val<2> v = fma_(Val<2>{{__uint_as_float(x[2 * e]), __uint_as_float(x[2 * e + 1])}}, fill<2>(by),
-                                Val<2>{{__uint_as_float(y[2 * e]), __uint_as_float(y[2 * e + 1])}});
+          Val<2> near{{__uint_as_float(y[2 * e]), __uint_as_float(y[2 * e + 1])}};
+          if (RAISED) near = mul_(near, fill<2>(near_is.back));
+          const Val<2> v = fma_(Val<2>{{__uint_as_float(x[2 * e]), __uint_as_float(x[2 * e + 1])}}, fill<2>(by), near);
           packed[e] = pack<T, 2>(v.v);
         }
         const int left = w.dy - half * H - b;
@@ -268,7 +358,7 @@ __global__ void __launch_bounds__(Layout<D, STATES>::threads, 1) k_walk_tensor(c
     // the weights of the tokens that this thread meets in X, in a chunk that is whole
     struct Weight { uint32_t part[PARTS]; };
     const auto weight_of = [&](int j, int n) {
-      float v = power[late ? j + 1 : n - 1 - j] * w.w_x;
+      float v = power[late ? RAISED ? j : j + 1 : n - 1 - j] * x_is.by;   // (RAISED: the decay that all of a late walk's have enters in 32 bits)
       Weight r;
 #pragma unroll
       for (int p = 0; p < PARTS; ++p) {
@@ -287,7 +377,7 @@ __global__ void __launch_bounds__(Layout<D, STATES>::threads, 1) k_walk_tensor(c
     const float twice = power[2];
     for (int c = 0; c < chunks; ++c) {
       const int xi = c * PER + PER - 2, yi = xi + 1, n = min(kTokens, it.len - first_of(c));
-      ok = __all_sync(0xFFFFFFFFu, wait_for(full(xi), xi / SLOTS & 1, &failed));
+      if (ok) ok = __all_sync(0xFFFFFFFFu, wait_for(full(xi), xi / SLOTS & 1, &failed));
       if (ok && n < kTokens) ok = __all_sync(0xFFFFFFFFu, wait_for(full(yi), yi / SLOTS & 1, &failed));
       if (ok && PARTS == 3 && !STATES) ok = __all_sync(0xFFFFFFFFu, wait_for(p_full, c & 1, &failed));   // (X is read no more)
       const uint32_t hi = scaled + c % NB * 2 * SLOT, lo = hi + SLOT;
@@ -300,9 +390,7 @@ __global__ void __launch_bounds__(Layout<D, STATES>::threads, 1) k_walk_tensor(c
           constexpr int STRIDE = MAKERS * 32 * 16;
           uint32_t x[4][4];
 #pragma unroll
-          for (int k = 0; k < 4; ++k)
-            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(x[k][0]), "=r"(x[k][1]), "=r"(x[k][2]), "=r"(x[k][3])
-                         : "r"(tile(xi) + (i0 + k) * STRIDE + t * 16));
+          for (int k = 0; k < 4; ++k) load_shared(tile(xi) + (i0 + k) * STRIDE + t * 16, x[k]);
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
             const uint32_t off = (i0 + k) * STRIDE + t * 16;
@@ -354,7 +442,7 @@ __global__ void __launch_bounds__(Layout<D, STATES>::threads, 1) k_walk_tensor(c
         if (late ? b >= quad && b * 32 < n : b <= quad) {
           if (late ? b > quad && b * 32 + 32 <= n : b < quad) {
             // all count: a column's weight is its neighbour's times the decay, from the nearest on
-            const float near1 = power[late ? b * 32 - i : i - 31 - b * 32] * w.w_near, near2 = near1 * power[1];
+            const float near1 = power[late ? b * 32 - i : i - 31 - b * 32] * near_is.by, near2 = near1 * power[1];
             Val<2> by = late ? Val<2>{{near1, near2}} : Val<2>{{near2, near1}};
             if (late) {
 #pragma unroll
@@ -379,7 +467,7 @@ __global__ void __launch_bounds__(Layout<D, STATES>::threads, 1) k_walk_tensor(c
 #pragma unroll
               for (int f = 0; f < 2; ++f) {
                 const int j = 2 * e + f;
-                const float q = __uint_as_float(v[j]) * w.w_near * exp2_here(fmaf(j, step, start));
+                const float q = __uint_as_float(v[j]) * near_is.by * exp2_here(fmaf(j, step, start));
                 p[f] = (unsigned)(b * 32 + j - j_first) <= (unsigned)j_span && j_span >= 0 ? q : 0.0f;
               }
               packed[e] = pack<T, 2>(p);
