@@ -412,19 +412,28 @@ Laid laid_out(const dgc_attention* d, bool backward) {
   return l;
 }
 
-// Tokens of a part, 0: sequences are walked whole.  A part costs reading x and y once more and a state written
-// and read twice, so only calls are cut that would leave SMs idle, and into as few parts as fill them: of one
-// to three parts for each SM the number that ends first.  One sequence of 1500 x 8 x 64 f16: 25 us in parts of 512, 17 of 128;
-// 3000 x 2 x 64 f32 152 and 47; 16000 x 16 x 64 f16 (parts of 1792 either way) 63.
+// Tokens of a part, 0: sequences are walked whole.  Parts fill SMs that whole sequences would leave idle, but their states come
+// first: a walk that takes `states` percent of the rows' time a token (X' in three parts and two of them in heads above 64, 135; 64-wide
+// heads 30; 32 bits 90), and two launches (of 16-bit calls the time of 512 tokens); a block's start is counted as `start` tokens.  Of
+// one to three parts for each SM the number that ends first, if it ends before whole sequences do.  Of a pack's lengths only the
+// mean is known here: its longest is taken to be three times that.
+// Whole and in parts, us: 8 x 16 sequences x heads of 4096 x 64 bf16 118, 149 (of one part each); 24 of 4096 110, 48; 8 of 768 30, 23;
+// 36 of 4096 x 128 159, 103 (gradient 175, 261); 2 of 1000 x 128 53, 30; f32, 50 of 1024 x 64 235, 132; 8 of 256 65, 54.
 int32_t part_of_call(const dgc_attention* d, bool backward) {
-  const int64_t units = (int64_t)d->num_seqs * d->heads * (backward ? 3 : 1), len = d->tokens / d->num_seqs;
-  if (units >= 2 * kSms || len < (d->dtype == DGC_F32 ? 256 : 1024)) return 0;
-  int64_t best = 0, ends = INT64_MAX;
+  const int64_t sequences = (int64_t)d->num_seqs * d->heads, units = sequences * (backward ? 3 : 1), len = d->tokens / d->num_seqs;
+  if (units >= 2 * kSms) return 0;
+  const bool uneven = d->seq_start && d->num_seqs > 1;
+  const int64_t states = d->dtype == DGC_F32 ? 90 : std::max(d->key_dim, d->value_dim) > 64 ? 135 : 30;
+  const int64_t start = d->dtype == DGC_F32 ? 8 : 64;
+  const auto rounds = [](int64_t blocks) { return (blocks + kSms - 1) / kSms; };
+  int64_t best = 0, ends = rounds(units) * (len * (uneven ? 3 : 1) + start) * 100;
   for (int64_t waves = 1; waves <= 3; ++waves) {
-    const int64_t parts = std::max<int64_t>(1, waves * kSms / units);
-    const int64_t part = std::max<int64_t>(128, ((len + parts - 1) / parts + 127) / 128 * 128);
-    const int64_t rounds = ((len + part - 1) / part * units + kSms - 1) / kSms;
-    if (rounds * part < ends) { best = part; ends = rounds * part; }
+    const int64_t parts = waves * kSms / units;
+    if (parts < (uneven ? 1 : 2)) continue;
+    const int64_t part = std::max<int64_t>(128, ((len + parts - 1) / parts + 127) / 128 * 128), cut = (len + part - 1) / part;
+    const int64_t end = rounds(cut * units) * (part + start) * 100 + rounds(cut * sequences * (backward ? 2 : 1)) * (part * states + start * 100) +
+                        (d->dtype == DGC_F32 ? 0 : 51200);
+    if (end < ends) { best = part; ends = end; }
   }
   return (int32_t)best;
 }
@@ -599,7 +608,6 @@ int32_t attention(const dgc_attention* d, bool backward, void* stream) {
     int32_t rc = walk(st, d->dtype, backward ? 2 : 1, items, true, s);
     if (rc != DGC_OK) return rc;
     JoinArgs j{a, {early, late}, {d->s0, d->ds_last}, {backward ? nullptr : d->s_last, d->ds0}, {0, 1}, dk * dv};
-    if ((int64_t)d->num_seqs * d->heads > 65535) return DGC_EINVAL;
     launch(k_join, dim3((dk * dv + 255) / 256, d->num_seqs * d->heads, backward ? 2 : 1), 256, 0, s, j);
     if ((rc = check_launch()) != DGC_OK) return rc;
   }

@@ -75,3 +75,20 @@ def test_rows_outside_the_sequences_stay_where_rows_are_laid_anew(dt):
     for t in (out, dq, dk, dv):
         assert bool((t[:20] == 7).all()) and bool((t[270:] == 7).all()) and not bool((t[20:270] == 7).all(2).any())
     B.tensor_check()
+
+
+@pytest.mark.parametrize("dt", DT, ids=str)
+def test_only_calls_that_gain_are_cut(dt):
+    """A call of equal sequences that fill the GPU is not cut; a few long sequences are.  (Host only.)"""
+    from paper_1712_01887_b200 import binding as B
+    for seqs, heads in ((8, 16), (16, 8), (4, 32), (9, 16), (16, 16), (14, 8), (1, 296), (2, 148)):
+        assert _need(B, dt, seqs, heads, 128, 128, seqs * 4096, 0) == 0, (seqs, heads)
+    for seqs, heads in ((5, 16), (3, 16), (1, 48), (1, 40), (7, 7)):
+        assert _need(B, dt, seqs, heads, 128, 128, seqs * 4096, 1) == 0, (seqs, heads)
+    for seqs, heads, backward in ((1, 8, 0), (1, 8, 1), (1, 1, 1), (2, 16, 0), (1, 16, 1)):
+        assert _need(B, dt, seqs, heads, 128, 128, seqs * 4096, backward) > 0, (seqs, heads)
+    # whatever is cut is cut into two parts at least: one part of a sequence that is no multiple of 128 takes one state a head
+    for units in range(1, 296):
+        for tokens in (1025, 1500, 4097, 65537):
+            need = _need(B, dt, 1, units, 64, 64, tokens, 0)
+            assert need == 0 or need >= 2 * units * 64 * 64 * 4, (units, tokens)
