@@ -645,15 +645,20 @@ typedef struct dgc_vocab_loss {
 
 /* Bytes of workspace that dgc_vocab_loss_forward (gradient = 0) or the other two (gradient != 0) need for this
  * struct's dtype, sizes and matrices.  Host only.  A gradient is formed in pieces of the vocabulary of at most 128 MB
- * (or 256 words); the forward pass keeps 8 bytes for 128 logits (64 in DGC_F32); copies of h, and of weight where it is
- * DGC_F32 (6 bytes an element) or its rows do not lie on 16 bytes, come to that. */
+ * (or 256 words); both keep, before that and in the same place, 8 bytes for 128 logits (64 in DGC_F32): of very many rows and
+ * words that is the more.  Copies of h, and of weight where it is DGC_F32 (6 bytes an element) or its rows do not lie on 16 bytes, come to
+ * that, 12 bytes a row, and for a gradient dh's sums in 32 bits (once, or of few rows up to 20 MB of them). */
 int64_t dgc_vocab_loss_workspace_bytes(const dgc_vocab_loss* d, int32_t gradient);
 
-/* Writes loss, and stats if given. */
+/* Writes loss, and stats if given.  A logit is a sum of 32 bits that the tensor cores form, which cut off where an addition
+ * would round: by up to 2^-23 of the sum so far for 16 of its terms.  (In DGC_F32 the sums of 128 terms are added up with rounding; of
+ * the nine products of numbers taken as three bf16 planes the three below 2^-26 are left out.) */
 int32_t dgc_vocab_loss_forward(const dgc_vocab_loss* d, void* stream);
 
 /* Writes dh, dweight and, if given, dbias, from stats and dloss.  In a 16-bit call G is rounded to the type where
- * it enters the two products.  Results do not vary from run to run. */
+ * it enters the two products, in DGC_F16 times one power of two for all rows: it is held to 2^-35 of the largest |dloss| of
+ * a labelled row at the least, so that a row whose dloss is far below that loses small probabilities.  Results do not vary from run to
+ * run. */
 int32_t dgc_vocab_loss_backward(const dgc_vocab_loss* d, void* stream);
 
 /* Loss and gradient in one call (dloss known beforehand); stats is not used. */

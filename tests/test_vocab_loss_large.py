@@ -2,7 +2,7 @@
 import pytest
 import torch
 
-from test_vocab_loss import _bind
+from test_vocab_loss import DT, _bind, _check
 
 
 @pytest.mark.gpu
@@ -29,3 +29,30 @@ def test_a_label_2_to_the_30_before_a_piece_is_a_label():
         assert got[:2].tolist() == [-1.0, -0.5] and not bool(got[2:-4].any())
     assert bool(((loss.double() - (58 + 1.3862943611198906)).abs() <= 64 * 2.0 ** -22).all())
     B.tensor_check()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dt", DT, ids=str)
+@pytest.mark.parametrize("R,V,D", [(40, 500, 8200), (3, 270, 65536)])
+def test_long_hidden_rows(R, V, D, dt):
+    """Sums of many terms: the bounds count 2^-23 for each (a tensor core's additions cut off), to the longest row there is."""
+    _check(R, V, D, dt, bias=True)
+
+
+def test_the_workspace_is_what_the_header_says():
+    """Host only.  8 bytes for 128 logits (64 in 32 bits) or a piece of the gradient, whichever is more; the rows' copy, the
+    matrix's where it is in 32 bits or off 16 bytes; dh's sums; 12 bytes a row; each on 256 bytes."""
+    from paper_1712_01887_b200 import binding as B
+    for dtype, rows, vocab, hidden, ld in ((1, 16384, 262144, 1024, 1024), (0, 16384, 262144, 1024, 1024), (2, 1, 131072, 1024, 1024),
+                                           (0, 700, 10000, 1500, 1500), (1, 33, 50021, 2048, 2048), (1, 100, 5000, 129, 130),
+                                           (0, 1, 1, 1, 1), (2, 8192, 1000, 64, 64), (1, 70000, 140000, 96, 96)):
+        wide, up = 6 if dtype == 0 else 2, (hidden + 7) // 8 * 8
+        copies = rows * up * wide + (vocab * up * wide if dtype == 0 or ld % 8 else 0)
+        logits = 8 * rows * -(-vocab // (64 if dtype == 0 else 128))
+        piece = max(128 << 20, 256 * rows * wide) + 256 * rows * wide
+        sums = max(4 * rows * up, 20 << 20)
+        args = B.VOCAB_LOSS.pack(dtype, vocab, hidden, 0, rows, 4096, ld, 4096, ld, 0, 4096, 4096, 4096, 4096, 4096, ld, 4096, ld, 0, 0, 0)
+        forward, gradient = (B._lib.dgc_vocab_loss_workspace_bytes(args, g) for g in (0, 1))
+        least = logits + copies + 12 * rows
+        assert least <= forward <= least + 8 * 256, (dtype, rows, vocab)
+        assert least <= gradient <= max(logits, piece) + copies + sums + 12 * rows + 8 * 256, (dtype, rows, vocab)
