@@ -96,7 +96,7 @@ def _run(lens, x, s, decay, scale):
 NAMES = ("out", "s_last", "dq", "dk", "dv", "ds0")
 
 
-def _verify(got, x, s, decay, scale, lens, elements=True):
+def _verify(got, x, s, decay, scale, lens, only=range(6)):
     """By element against `size` and, for rows, by 2-norm as `small` says."""
     dt, c = x[0].dtype, float(torch.tensor(scale))
     x, s, g = [t.double() for t in x], [t.double() for t in s], decay.double()
@@ -106,13 +106,12 @@ def _verify(got, x, s, decay, scale, lens, elements=True):
     if dt == torch.float16:
         y = [torch.stack([p.abs().sum(0) for p in t.split(lens)])[:, :, None, :] for t in (x[2], x[3])]     # [seqs, heads, 1, dv]
         floor[1], floor[5] = 2.0 ** -24 * y[0], 2.0 ** -24 * abs(c) * y[1]
-    for name, a, w, z, low in zip(NAMES, got, want, size, floor):
+    for name, a, w, z, low in [r for i, r in enumerate(zip(NAMES, got, want, size, floor)) if i in only]:
         assert bool(a.isfinite().all()), name
         err, is_state = (a.double() - w).abs(), name in ("s_last", "ds0")
         unit = 0.0 if is_state else UNIT[dt]
         tol = (F32 + (PARTS if is_state and UNIT[dt] else 0.0)) * z + unit * (z + w.abs()) + (low if is_state else TINY[dt])
-        if elements:
-            assert bool((err <= tol + 1e-30).all()), (name, float(err.max()), float((err / (tol + 1e-30)).max()))
+        assert bool((err <= tol + 1e-30).all()), (name, float(err.max()), float((err / (tol + 1e-30)).max()))
         if unit:
             bound = 3 * unit * w.norm() + TINY[dt] * w.numel() ** 0.5 + F32 * z.norm()
             assert float(err.norm()) <= float(bound), (name, float(err.norm() / w.norm()), float(bound / w.norm()))
@@ -184,3 +183,44 @@ def test_decays_near_0(g, dt):
     lens = [200]
     x, s, decay = _data(lens, 2, 64, 64, dt, states=(0.0, 0.0), decays=(g, g * 1.37))
     _verify(_run(lens, x, s, decay, 0.3), x, s, decay, 0.3, lens)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dt", DT, ids=str)
+def test_captured_calls_and_two_streams(dt):
+    """A captured backward call follows its inputs (dout a thousand times smaller than at the capture), and calls on two streams at
+    once give what they give alone."""
+    B = _bind()
+    lens = [400, 0, 90]
+    x, s, decay = _data(lens, 3, 64, 64, dt)
+    scale = 0.125
+    q, k, v, do = x
+    starts = torch.tensor([0, 400, 400, 490], dtype=torch.int32, device="cuda")
+    sets = [[torch.empty_like(t) for t in (q, k, v)] + [torch.empty_like(s[0])] for _ in range(3)]
+
+    def call(to, stream=None):
+        B.decay_attention_backward(q, k, v, do, *to[:3], decay, seq_start=starts, num_seqs=3, s0=s[0], ds_last=s[1], ds0=to[3], scale=scale,
+                                   stream=stream)
+    side = [torch.cuda.Stream(), torch.cuda.Stream()]
+    side[0].wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side[0]):
+        call(sets[0])
+    torch.cuda.current_stream().wait_stream(side[0])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(sets[0])
+    do.mul_(1e-3)
+    s[1].mul_(1e-3)
+    graph.replay()
+    call(sets[1])
+    for a, b in zip(sets[0], sets[1]):
+        assert torch.equal(a, b)
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for stream, to in zip(side, (sets[0], sets[2])):
+            call(to, stream)
+    torch.cuda.synchronize()
+    for to in (sets[0], sets[2]):
+        for a, b in zip(to, sets[1]):
+            assert torch.equal(a, b)
+    _verify([torch.zeros_like(v), s[0]] + sets[1], x, s, decay, scale, lens, only=(2, 3, 4, 5))
