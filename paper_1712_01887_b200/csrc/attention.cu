@@ -393,8 +393,11 @@ inline bool fetched(const Heads& m, int64_t tokens, int64_t heads) {
   return !misaligned(m.p, 16) && (m.ld > 0 || tokens <= 1) && m.ld % 8 == 0 && (m.head % 8 == 0 || heads == 1);
 }
 inline Heads side(const dgc_heads& m) { return Heads{m.data, m.ld, m.head}; }
-// The tensors that are laid out anew in the workspace (q, k, v, dout; out, or dq, dk, dv), and their bytes.  Worth it from
-// a few tokens on (20 sequences of 35 x 12 x 125 bf16, forward and backward: 247 -> 145 us; one of 40, forward 27 -> 20 us).
+// The tensors that are laid out anew in the workspace (q, k, v, dout; out, or dq, dk, dv), and their bytes.  Worth it where the walk in
+// 32-bit arithmetic would take a second chunk, and forward in wide heads a little before.  Laid anew and in 32 bits, us, bf16:
+//   20 sequences x 12 heads x 125   16 tokens 42, 41 (gradient 114, 82)   24 44, 49 (120, 101)   32 45, 57 (122, 121)   35 46, 72 (124, 154)
+//   64 x 16 x 61                    16 69, 49 (171, 107)                  32 75, 64 (181, 150)   40 79, 82 (189, 205)
+//   one x 12 x 125                  24 24, 20 (32, 21)                    36 24, 29 (30, 27)     64 24, 33 (30, 33)
 struct Laid { int64_t bytes; bool anew[8]; };
 inline int dim_of(const dgc_attention* d, int i, bool backward) {
   return i < 2 || (backward && (i == 4 || i == 5)) ? d->key_dim : d->value_dim;
@@ -402,7 +405,8 @@ inline int dim_of(const dgc_attention* d, int i, bool backward) {
 inline int64_t laid_bytes(const dgc_attention* d, int dim) { return (d->tokens * d->heads * ((dim + 7) / 8 * 16) + 255) / 256 * 256; }
 Laid laid_out(const dgc_attention* d, bool backward) {
   Laid l{};
-  if (d->dtype == DGC_F32 || d->tokens < 16 * (int64_t)d->num_seqs) return l;
+  const int64_t least = !backward && std::max(d->key_dim, d->value_dim) > 64 ? 20 : 33;   // tokens of a sequence
+  if (d->dtype == DGC_F32 || d->tokens < least * d->num_seqs) return l;
   const dgc_heads* all[8] = {&d->q, &d->k, &d->v, &d->dout, backward ? &d->dq : &d->out, &d->dk, &d->dv, nullptr};
   for (int i = 0; i < (backward ? 7 : 5); ++i) {
     if (i == 3 && !backward) continue;

@@ -92,3 +92,20 @@ def test_only_calls_that_gain_are_cut(dt):
         for tokens in (1025, 1500, 4097, 65537):
             need = _need(B, dt, 1, units, 64, 64, tokens, 0)
             assert need == 0 or need >= 2 * units * 64 * 64 * 4, (units, tokens)
+
+
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float16], ids=str)
+def test_rows_are_laid_anew_where_it_gains(dt):
+    """Rows off 16 bytes: taken in 32-bit arithmetic as they are where a sequence is hardly more than one chunk of that.  (Host only.)"""
+    from paper_1712_01887_b200 import binding as B
+
+    def need(seqs, heads, dim, tokens, backward):
+        t, n = (ALIGNED + 2, heads * dim, dim), seqs * tokens
+        args = B.ATTENTION.pack(B.DTYPES[dt], seqs, heads, dim, dim, 1.0, n, 0, ALIGNED, *t * 4, 0, 0, *t * 4, 0, 0, 0, 0)
+        kept = (n * heads + 255) // 256 * 256 if backward and dt == torch.float16 else 0
+        return int(B._lib.dgc_decay_attention_workspace_bytes(args, backward)) - kept
+    for seqs, heads, dim, tokens, backward in ((20, 12, 125, 24, 1), (200, 4, 61, 32, 0), (200, 4, 61, 32, 1), (64, 16, 61, 16, 0), (1, 12, 125, 16, 0)):
+        assert need(seqs, heads, dim, tokens, backward) == 0, (seqs, heads, dim, tokens)
+    for seqs, heads, dim, tokens, backward in ((20, 12, 125, 24, 0), (20, 12, 125, 35, 1), (64, 16, 61, 40, 0), (64, 16, 61, 40, 1)):
+        rows = (7 if backward else 4) * seqs * tokens * heads * ((dim + 7) // 8 * 16)
+        assert need(seqs, heads, dim, tokens, backward) >= rows, (seqs, heads, dim, tokens)
