@@ -561,7 +561,7 @@ typedef struct dgc_attention {
   const int32_t* seq_start;    /* as in dgc_scan                                                   */
   const float*   decay;        /* device [heads], each in [0, 1] (results are undefined for others) */
   dgc_heads      q, k, v;      /* inputs; their values are finite: one that is not spoils its own sequence
-                                  and head, from up to 127 tokens before it on                     */
+                                  and head, from up to 127 tokens before it on (all of its gradients) */
   dgc_heads      out;          /* forward output [tokens, heads, value_dim]                        */
   const float*   s0;           /* [num_seqs, heads, key_dim, value_dim], the states before the first
                                   token; NULL: 0                                                   */

@@ -24,6 +24,7 @@
 // looked for, and the gradient's state, as the product takes it, by its own largest element.  (32 sequences of 25000 x 16 x 64,
 // backward: 219 -> 259 us, of which the small kernel 12, its results' reading 7, the state's largest 10.  With the largest of
 // each chunk's X and U, from their tiles, instead: 278 us, and 103 where 88 are taken forward.)
+// dk with a dout of 1e-5 is 4.1e-4 off, where rounding it costs 3.6e-4; 2.8e-3 without.
 // The state's sums over a chunk are the tensor core's, over the chunks they are the registers': a tensor core cuts off
 // where an addition would round, which over 16 steps does not show and over a long sequence would.
 #pragma once
