@@ -420,21 +420,23 @@ Laid laid_out(const dgc_attention* d, bool backward) {
 // first: a walk that takes `states` percent of the rows' time a token (X' in three parts and two of them in heads above 64, 135; 64-wide
 // heads 30; 32 bits 90), and two launches (of 16-bit calls the time of 512 tokens); a block's start is counted as `start` tokens.  Of
 // one to three parts for each SM the number that ends first, if it ends before whole sequences do.  Of a pack's lengths only the
-// mean is known here: its longest is taken to be three times that.
+// mean is known here: its longest is taken to be three times that, and packs of shorter sequences are not cut, since equal ones would
+// lose more than uneven ones gain (32 x 4 of 512 on the average x 64 bf16, the longest 4.9 times that: 72, 58 in parts; equal 25, 53).
 // Whole and in parts, us: 8 x 16 sequences x heads of 4096 x 64 bf16 118, 149 (of one part each); 24 of 4096 110, 48; 8 of 768 30, 23;
 // 36 of 4096 x 128 159, 103 (gradient 175, 261); 2 of 1000 x 128 53, 30; f32, 50 of 1024 x 64 235, 132; 8 of 256 65, 54.
 int32_t part_of_call(const dgc_attention* d, bool backward) {
   const int64_t sequences = (int64_t)d->num_seqs * d->heads, units = sequences * (backward ? 3 : 1), len = d->tokens / d->num_seqs;
-  if (units >= 2 * kSms) return 0;
   const bool uneven = d->seq_start && d->num_seqs > 1;
+  if (units >= 2 * kSms || (uneven && len < (d->dtype == DGC_F32 ? 256 : 1024))) return 0;
   const int64_t states = d->dtype == DGC_F32 ? 90 : std::max(d->key_dim, d->value_dim) > 64 ? 135 : 30;
   const int64_t start = d->dtype == DGC_F32 ? 8 : 64;
   const auto rounds = [](int64_t blocks) { return (blocks + kSms - 1) / kSms; };
   int64_t best = 0, ends = rounds(units) * (len * (uneven ? 3 : 1) + start) * 100;
   for (int64_t waves = 1; waves <= 3; ++waves) {
     const int64_t parts = waves * kSms / units;
-    if (parts < (uneven ? 1 : 2)) continue;
+    if (parts < 1) continue;
     const int64_t part = std::max<int64_t>(128, ((len + parts - 1) / parts + 127) / 128 * 128), cut = (len + part - 1) / part;
+    if (cut < (uneven ? 1 : 2)) continue;
     const int64_t end = rounds(cut * units) * (part + start) * 100 + rounds(cut * sequences * (backward ? 2 : 1)) * (part * states + start * 100) +
                         (d->dtype == DGC_F32 ? 0 : 51200);
     if (end < ends) { best = part; ends = end; }

@@ -92,6 +92,14 @@ def test_only_calls_that_gain_are_cut(dt):
         for tokens in (1025, 1500, 4097, 65537):
             need = _need(B, dt, 1, units, 64, 64, tokens, 0)
             assert need == 0 or need >= 2 * units * 64 * 64 * 4, (units, tokens)
+    # packs, of which only the mean length is known, from a mean of 1024 (256 in 32 bits) on; nothing to cut, nothing cut
+    mean = 256 if dt == torch.float32 else 1024
+    for seqs, heads in ((8, 4), (4, 2), (32, 4)):
+        assert _need(B, dt, seqs, heads, 64, 64, seqs * mean - 1, 0, True) == 0 < _need(B, dt, seqs, heads, 64, 64, seqs * mean, 0, True)
+    for seqs, tokens in ((1, 0), (1, 1), (2, 0), (3, 2), (2, 100)):
+        for backward in (0, 1):
+            assert _need(B, dt, seqs, 4, 64, 64, tokens, backward, True) == 0
+            assert tokens % seqs or _need(B, dt, seqs, 4, 64, 64, tokens, backward) == 0
 
 
 @pytest.mark.parametrize("dt", [torch.bfloat16, torch.float16], ids=str)
